@@ -368,6 +368,60 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
                                   int max_blocks_per_seq, const int32_t *seq_lens, float scale, float *scores,
                                   int64_t max_len, void *stream);
 
+/*
+ * isoq_kv_attn -- attention of new tokens over a paged cache of quantized keys
+ * and values written by isoq_kv_append, without decompressing either: decoding
+ * steps (one new token a sequence), drafted tokens and chunks of a prompt
+ * (several, causal).  For token i of a sequence's n new tokens, query head hq
+ * and key head h = hq / (n_q_heads / n_kv_heads):
+ *     s_t = scale * <q, k_hat(t)>,  out = sum_t softmax(s)_t v_hat(t),
+ *     lse = ln sum_t exp(s_t)
+ * over the positions t < seq_lens[s] - (n - 1 - i): the new tokens are the
+ * sequence's last positions (append them first), and each attends to those up
+ * to its own.  Positions past max_len or max_blocks_per_seq * block_size, and
+ * positions whose block id lies outside [0, n_blocks), are left out, whatever
+ * the cache holds there.  A token with no position left: out = 0, lse = -inf.
+ *
+ *   pk, pv      the K and V quantizers, of one variant, d and bits (any d in
+ *               1..1024); n_sets 1 or n_kv_heads each.
+ *   dtype       ISOQ_F16 or ISOQ_F32: the element type of q and out.
+ *   q, out      device, [n_tokens][n_q_heads][d] (16-byte aligned).
+ *   q_start     device, int32 [n_seqs + 1], ascending: sequence s has the tokens
+ *               q_start[s] .. q_start[s+1] - 1.  max_q_len: the most tokens that a
+ *               sequence has (known to the host).  Rows of no sequence are left
+ *               as they were, in out and lse; so are a sequence's tokens from
+ *               max_q_len on.  NULL: one token a sequence, n_tokens == n_seqs and
+ *               max_q_len == 1.
+ *   k_idx, k_rho, v_idx, v_rho, n_blocks, block_size, block_table,
+ *   max_blocks_per_seq, seq_lens  as in isoq_kv_scores (the records 16-byte
+ *               aligned).
+ *   max_len     positions of the longest sequence at most, as far as the host
+ *               knows (max_blocks_per_seq * block_size if it does not): a closer
+ *               bound cuts long caches into better splits.
+ *   lse         device, fp32 [n_tokens][n_q_heads], or NULL.
+ *   workspace   device, at least isoq_kv_attn_workspace(...) bytes for the same
+ *               arguments (16-byte aligned; may be NULL where that is 0).  Its
+ *               contents matter only while the call runs on its stream: calls
+ *               on different streams, or captured graphs that may run at the
+ *               same time, need one each.  A smaller one is ISOQ_E_INVALID.
+ * Limits: n_seqs <= 65535, n_tokens * n_q_heads < 2^31, max_q_len * n_q_heads <=
+ * 2^23, max_blocks_per_seq * block_size < 2^31.
+ * Arithmetic: logits, softmax statistics and sums in fp32 or in integers of 32
+ * bits (see the kernels for what is rounded).  A query with an infinity or NaN
+ * gives NaN in its row of out and lse.  The result does not depend on the order in which
+ * workgroups run.
+ */
+isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
+                         const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
+                         int n_kv_heads, const uint8_t *k_idx, const float *k_rho, const uint8_t *v_idx,
+                         const float *v_rho, int64_t n_blocks, int block_size, const int32_t *block_table,
+                         int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len, float scale, void *out,
+                         float *lse, void *workspace, size_t workspace_bytes, void *stream);
+/* Bytes of workspace for isoq_kv_attn with these arguments (0 for invalid ones). */
+size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int dtype, int64_t n_tokens, int max_q_len,
+                              int n_seqs, int n_q_heads, int n_kv_heads, int block_size, int max_blocks_per_seq,
+                              int64_t max_len);
+
 /* Sizes: bytes of one packed index record, ceil(pw * bits / 8) with the
  * padded width pw = 4 g4 (Full, Fast) or 2 g2 (2-D); isoq_packed_bytes is
  * ceil(d * bits / 8), the same number whenever d is a multiple of 4.  Raw

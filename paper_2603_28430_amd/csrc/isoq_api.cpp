@@ -9,55 +9,62 @@
 #include <new>
 #include <vector>
 
+#include "isoq_handles.h"
 #include "isoq_internal.h"
 #include "isoq_scores_generic.h"
 #include "isoquant.h"
 
-struct isoq_params {
-    int variant, d, bits, n_sets;
-    int device;
-    float *dparams;                 // device, [n_sets][slots_per_set][params_per_slot], then the LUT
-    size_t lut_offset;              // floats from dparams to the magnitude LUT (0: none)
-    size_t mfma_offset;             // floats from dparams to the matrix-core parameters (0: none)
-    int lut_cells;
-    float lut_inv_h;
-    std::vector<float> exported;    // unit parameters as used (Table 1 layout)
-    float levels[16], thresholds[15];
-    isoq::LevelDigits lv;             // levels as digits (the first set)
-    size_t lv_offset;               // floats from dparams to the further sets
-    int n_pass;                     // sets in all
-    bool wide;                      // the logits need all sets and digit products
-};
-
-struct isoq_sketch {
-    int variant, d, n_sets, m;
-    int device;
-    uint16_t *dfrag;                // device, [n_sets][m/16][d/32][64][8] fp16 of S' = S T^{-1}
-    float *dS;                      // device, [m][d] fp32 of S (query side)
-    std::vector<float> S;           // host copy of S as used
-};
-
-namespace {
-
-using namespace isoq;
+namespace isoq {
 
 // Text of the last HIP error seen by a call on this thread.
-thread_local char g_last_hip_error[160] = "";
+static thread_local char g_last_hip_error[160] = "";
 
-isoq_status hip_fail(hipError_t e, const char *where, isoq_status st = ISOQ_E_HIP)
+isoq_status hip_fail(hipError_t e, const char *where, isoq_status st)
 {
     std::snprintf(g_last_hip_error, sizeof g_last_hip_error, "%s: %s (%d)", where,
                   hipGetErrorString(e), (int)e);
     return st;
 }
 
-bool valid_variant(int v) { return v == ISOQ_FULL || v == ISOQ_FAST || v == ISOQ_PLANAR2D || v == ISOQ_BLOCK8; }
 // Widths of the tuned kernels (every entry point); other widths up to
 // kGenericMaxD have quantize, dequantize and round trip only.
-bool tuned_d(int d) { return d == 64 || d == 128 || d == 256 || d == 512; }
+static bool tuned_d(int d) { return d == 64 || d == 128 || d == 256 || d == 512; }
 // widths of the decoding calls (append, logits): the tuned ones and three
 // common attention head widths
 bool decode_d(int d) { return tuned_d(d) || d == 80 || d == 96 || d == 160 || d == 192; }
+
+isoq_status check_device(const isoq_params *p)
+{
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess)
+        return hip_fail(e, "hipGetDevice");
+    return dev == p->device ? ISOQ_OK : ISOQ_E_DEVICE;
+}
+
+size_t record_bytes(int variant, int d, int bits)
+{
+    return ((size_t)padded_width(variant, d) * bits + 7) / 8;
+}
+
+isoq_status launch_lds(const void *fn, dim3 grid, int threads, void **args, size_t lds, void *stream)
+{
+    hipError_t e = hipLaunchKernel(fn, grid, dim3(threads), args, lds, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess)
+        return hip_fail(e, "hipLaunchKernel");
+    e = hipGetLastError();
+    if (e != hipSuccess)
+        return hip_fail(e, "after hipLaunchKernel");
+    return ISOQ_OK;
+}
+
+}  // namespace isoq
+
+namespace {
+
+using namespace isoq;
+
+bool valid_variant(int v) { return v == ISOQ_FULL || v == ISOQ_FAST || v == ISOQ_PLANAR2D || v == ISOQ_BLOCK8; }
 // (d, m) of the stage-2 sketch: m = 64 or 128 sign bits at the decoding
 // widths up to 192, m = 64 at 256 and 512 (the staged projection, m d fp16,
 // has to fit the LDS next to the error tiles)
@@ -74,7 +81,6 @@ bool packed_decode(int d, int bits, bool f16)
 }
 bool supported_d(int d) { return d >= 1 && d <= kGenericMaxD; }
 bool supported_bits(int b) { return b >= 2 && b <= 4; }
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 isoq_status check_common(const isoq_params *p, int dtype, int64_t n, int64_t rows_per_set)
 {
@@ -87,24 +93,10 @@ isoq_status check_common(const isoq_params *p, int dtype, int64_t n, int64_t row
     return ISOQ_OK;
 }
 
-isoq_status check_device(const isoq_params *p)
-{
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess)
-        return hip_fail(e, "hipGetDevice");
-    return dev == p->device ? ISOQ_OK : ISOQ_E_DEVICE;
-}
-
 // Rows of one block of the tuned stage-1 kernels (a wave holds 512/d rows).
 int64_t rows_per_block(const isoq_params *p)
 {
     return (int64_t)(64 / (p->d / kCoordsPerLane)) * (kBlockThreads / 64) * kTileGroups;
-}
-
-size_t record_bytes(int variant, int d, int bits)
-{
-    return ((size_t)padded_width(variant, d) * bits + 7) / 8;
 }
 
 // Per-handle kernel arguments: codebook halves, parameters, lookup table.
@@ -127,13 +119,7 @@ void fill_args(const isoq_params *p, KArgs &a)
 
 isoq_status launch(const void *fn, dim3 grid, void **args, void *stream, int threads = kBlockThreads)
 {
-    hipError_t e = hipLaunchKernel(fn, grid, dim3(threads), args, 0, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess)
-        return hip_fail(e, "hipLaunchKernel");
-    e = hipGetLastError();
-    if (e != hipSuccess)
-        return hip_fail(e, "after hipLaunchKernel");
-    return ISOQ_OK;
+    return launch_lds(fn, grid, threads, args, 0, stream);
 }
 
 const void *packed_kernel(int variant, int bits, int mode, int chunks, int cache_lp = -1)
@@ -423,6 +409,8 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             while (layout.size() % 4)
                 layout.push_back(0.f);
             p->lv = lv[0];
+            build_value_digits(bits, p->levels, 2, p->vd[0]);
+            build_value_digits(bits, p->levels, 3, p->vd[1]);
             p->n_pass = (int)lv.size();
             p->lv_offset = layout.size();
             const float *f = reinterpret_cast<const float *>(lv.data() + 1);

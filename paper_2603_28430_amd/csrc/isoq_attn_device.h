@@ -1,0 +1,62 @@
+// Device helpers shared by the attention kernels: which rows a sequence has,
+// and the last step of a row.
+#pragma once
+
+#include "isoq_attn.h"
+#include "isoq_device.h"
+#include "isoq_generic.h"
+
+namespace isoq {
+namespace {
+
+// The new tokens of sequence s: rows first .. first + n - 1 of q, of which
+// `rows` are computed (max_q_len at most), and its length.
+struct AttnSeq {
+    int first, n, rows, len;
+    // Positions that token i attends to: those up to its own, the newest token
+    // being the last position.
+    __device__ __forceinline__ int limit(int i, int cap) const
+    {
+        const int64_t l = (int64_t)len - (n - 1 - i);
+        return (int)(l < 0 ? 0 : l < cap ? l : cap);
+    }
+};
+
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
+{
+    AttnSeq q{s, 1, 1, a.seq_lens[s]};
+    if (a.q_start) {   // (clamped: no row outside q is touched, whatever q_start holds)
+        q.first = min(max(a.q_start[s], 0), a.n_tokens);
+        q.n = min(max(a.q_start[s + 1], q.first), a.n_tokens) - q.first;
+        q.rows = min(q.n, a.max_q_len);
+    }
+    return q;
+}
+
+// Slot j (SW coordinates) of row `row` (head hq of its token): the sum of
+// values y, rotated, rotated back and stored.
+template <int VAR, int SW>
+__device__ __forceinline__ void attn_emit(const AttnArgs &a, int64_t row, int h, int j, const float y[SW])
+{
+    constexpr int PS = SW == 8 ? 64 : kSlotParams<VAR>;
+    float P[PS], o[SW];
+    load_params<PS>(a.v_params + (a.v_sets == 1 ? 0 : h) * a.set_stride + (int64_t)j * PS, P);
+    if constexpr (SW == 8)
+        rotate_inverse<VAR>(P, y, o);
+    else
+        rotate4_inverse<VAR>(P, y, o);
+    const bool vec = a.d % SW == 0;
+    if (a.q_f16)
+        gen_store<true, SW>(static_cast<char *>(a.out) + row * a.d * 2, j, a.d, vec, o);
+    else
+        gen_store<false, SW>(static_cast<char *>(a.out) + row * a.d * 4, j, a.d, vec, o);
+}
+
+// lse from m (in units of ln 2) and l.
+__device__ __forceinline__ float attn_lse(float m, float l)
+{
+    return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+}  // namespace
+}  // namespace isoq

@@ -550,6 +550,44 @@ bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> 
     }
 }
 
+void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out)
+{
+    const int K = 1 << bits;
+    out = ValueDigits{};
+    // in units of a power of two that brings the largest level to 0.5 .. 1
+    int exp = 0;
+    const double big = std::frexp((double)levels[K - 1], &exp);
+    if (!(big > 0))
+        return;   // every level is zero as a float
+    const double top = digits == 2 ? 32639.0 : 8355711.0;   // 127 in every digit
+    const int tries = 4096;
+    double best = INFINITY, scale = big / top;
+    for (int i = 0; i < tries; i++) {
+        const double q = big / top * (1.0 + (double)i / tries);
+        double sum = 0;
+        for (int k = K / 2; k < K; k++) {
+            const double u = std::ldexp((double)levels[k], -exp) / q, e = (u - std::nearbyint(u)) * q;
+            sum += e * e;
+        }
+        if (sum < best) {
+            best = sum;
+            scale = q;
+        }
+    }
+    uint8_t bytes[3][16] = {};
+    for (int k = 0; k < K; k++) {
+        long v = std::lrint(std::ldexp((double)levels[k], -exp) / scale);
+        for (int t = 0; t < digits; t++) {
+            const long d = ((v + 128) & 255) - 128;
+            bytes[t][k] = (uint8_t)(d & 255);
+            v = (v - d) / 256;
+        }
+    }
+    for (int t = 0; t < digits; t++)
+        std::memcpy(out.tab[t], bytes[t], 16);
+    out.scale = (float)std::ldexp(scale, exp);
+}
+
 bool build_magnitude_lut(int H, const double *tau, const double *lev, double *inv_h,
                          std::vector<LutEntry> &lut)
 {

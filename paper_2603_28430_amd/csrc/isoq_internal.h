@@ -122,6 +122,14 @@ struct LevelDigits {
     int32_t exp;
 };
 
+// The codebook as 8-bit digits for the weighted sums of attention (isoq_attn_m.h):
+// byte k of tab[t] is digit t (least significant first) of level k's integer,
+// n_k = d_0 + 256 d_1 (+ 65536 d_2), and scale n_k the level.
+struct ValueDigits {
+    uint32_t tab[3][4];
+    float scale;
+};
+
 // Attention logits against a paged cache of quantized keys (isoq_scores.h,
 // isoq_scores_generic.hip).
 struct SArgs {
@@ -354,6 +362,10 @@ bool build_magnitude_lut(int H, const double *tau, const double *lev, double *in
 // square, come to 2^-24 of those that it has (a rotated query whose largest
 // coordinate is four times its root mean square).
 bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> &out);
+// The levels as integers of `digits` (2 or 3) balanced 8-bit digits.  The scale
+// is searched for the least sum of squared errors over the levels; the largest
+// level's integer is at least half of what the digits hold.
+void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out);
 // Lloyd-Max levels for N(0, sigma^2) (ascending, symmetrised).
 bool lloyd_levels(int bits, double sigma, int iters, double *levels);
 // Seeded raw draws (Philox4x32-10 + Box-Muller), layout of the public header.

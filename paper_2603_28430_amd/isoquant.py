@@ -63,6 +63,10 @@ def _load():
     L.isoq_kv_scores_filled.argtypes = L.isoq_kv_scores_qjl.argtypes
     L.isoq_kv_scores.argtypes = [vp, c_int, vp, c_int, c_int, c_int, vp, vp, i64, c_int, vp, c_int, vp,
                                  ctypes.c_float, vp, i64, vp]
+    L.isoq_kv_attn.argtypes = [vp, vp, c_int, vp, vp, i64, c_int, c_int, c_int, c_int, vp, vp, vp, vp, i64, c_int, vp,
+                               c_int, vp, i64, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
+    L.isoq_kv_attn_workspace.argtypes = [vp, vp, c_int, i64, c_int, c_int, c_int, c_int, c_int, c_int, i64]
+    L.isoq_kv_attn_workspace.restype = ctypes.c_size_t
     L.isoq_packed_bytes.argtypes = [c_int, c_int]
     L.isoq_packed_bytes.restype = ctypes.c_size_t
     L.isoq_record_bytes.argtypes = [c_int, c_int, c_int]
@@ -80,7 +84,7 @@ def _load():
     for f in ("isoq_params_init", "isoq_params_destroy", "isoq_params_export", "isoq_params_info",
               "isoq_quantize", "isoq_dequantize", "isoq_roundtrip", "isoq_kv_append", "isoq_kv_scores", "isoq_sketch_init",
               "isoq_sketch_destroy", "isoq_sketch_export", "isoq_quantize_qjl", "isoq_kv_append_qjl",
-              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_codebook_lloyd",
+              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn", "isoq_codebook_lloyd",
               "isoq_rotation_draws"):
         getattr(L, f).restype = c_int
     return L
@@ -438,6 +442,83 @@ def isoq_kv_scores_qjl(pk: Params, sketch, q, k_idx, k_rho, k_signs, k_gamma, bl
     """isoq_kv_scores with the stage-2 residual correction (see include/isoquant.h)."""
     return isoq_kv_scores(pk, q, k_idx, k_rho, block_table, seq_lens, scale, max_len, scores, stream,
                           sketch=sketch, k_signs=k_signs, k_gamma=k_gamma)
+
+
+def isoq_kv_attn_workspace(pk: Params, pv: Params, dtype, n_tokens: int, max_q_len: int, n_seqs: int, n_q_heads: int,
+                           n_kv_heads: int, block_size: int, max_blocks_per_seq: int, max_len: int) -> int:
+    """Bytes of workspace that isoq_kv_attn takes for these sizes (see include/isoquant.h)."""
+    return int(lib.isoq_kv_attn_workspace(pk.handle, pv.handle, _dtype_code(dtype), int(n_tokens), int(max_q_len),
+                                          int(n_seqs), int(n_q_heads), int(n_kv_heads), int(block_size),
+                                          int(max_blocks_per_seq), int(max_len)))
+
+
+def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, scale: float = 1.0,
+                 q_start=None, max_q_len: int = 1, max_len=None, out=None, lse=None, workspace=None, stream=None):
+    """Attention of new tokens' queries q [n_tokens, n_q_heads, d] over the paged
+    caches k_idx, v_idx [n_blocks, n_kv_heads, block_size, R] / k_rho, v_rho
+    [n_blocks, n_kv_heads, block_size] with block_table int32 [n_seqs,
+    max_blocks] and seq_lens int32 [n_seqs].  One token a sequence, or with
+    q_start int32 [n_seqs + 1] the tokens q_start[s] .. q_start[s + 1] - 1 of
+    sequence s, at most max_q_len, which are its last positions (causal).
+    Returns (out like q, lse fp32 [n_tokens, n_q_heads]); rows of no sequence
+    are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
+    least isoq_kv_attn_workspace(...) bytes; by default one is allocated from
+    torch's pool on torch's current stream, so pass one where `stream` is
+    another."""
+    torch = _torch()
+    if q.dim() != 3 or k_idx.dim() != 4 or k_rho.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q [n_tokens, n_q_heads, d], k_idx [n_blocks, n_kv_heads, block_size, R], "
+                         "k_rho [n_blocks, n_kv_heads, block_size], block_table [n_seqs, max_blocks]")
+    shape, cache = q.shape, k_idx.shape
+    n_tokens, n_q_heads, d = shape
+    n_blocks, n_kv_heads, block_size, rb = cache
+    n_seqs, max_blocks = block_table.shape
+    if (d != pk.d or rb != pk.record_bytes or v_idx.shape != cache or k_rho.shape != cache[:3]
+            or v_rho.shape != cache[:3]):
+        raise ValueError("cache shapes do not match the queries and the handle")
+    if seq_lens.shape != (n_seqs,):
+        raise ValueError("block_table and seq_lens need one row per sequence")
+    if k_idx.dtype != torch.uint8 or v_idx.dtype != torch.uint8 or k_rho.dtype != torch.float32 \
+            or v_rho.dtype != torch.float32:
+        raise TypeError("k_idx and v_idx uint8, k_rho and v_rho float32")
+    if block_table.dtype != torch.int32 or seq_lens.dtype != torch.int32:
+        raise TypeError("block_table and seq_lens must be int32")
+    code = _dtype_code(q.dtype)
+    if q_start is None:
+        if n_tokens != n_seqs or max_q_len != 1:
+            raise ValueError("without q_start there is one token a sequence")
+    elif q_start.shape != (n_seqs + 1,) or q_start.dtype != torch.int32:
+        raise ValueError("q_start must be int32 [n_seqs + 1]")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and dtype")
+    if lse is None:
+        lse = torch.empty((n_tokens, n_q_heads), dtype=torch.float32, device=q.device)
+    elif lse.shape != shape[:2] or lse.dtype != torch.float32:
+        raise ValueError("lse must be fp32 [n_tokens, n_q_heads]")
+    if max_len is None:
+        max_len = max_blocks * block_size
+    need = lib.isoq_kv_attn_workspace(pk.handle, pv.handle, code, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
+                                      block_size, max_blocks, max_len)
+    tensors = (q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens, out, lse)
+    if q_start is not None:
+        tensors += (q_start,)
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or workspace.numel() < need:
+            raise ValueError(f"workspace must be uint8 of at least {need} bytes")
+        tensors += (workspace,)
+    _placed(q, tensors)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = lib.isoq_kv_attn(pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs,
+                          n_q_heads, n_kv_heads, k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(),
+                          v_rho.data_ptr(), n_blocks, block_size, block_table.data_ptr(), max_blocks,
+                          seq_lens.data_ptr(), max_len, scale, out.data_ptr(), lse.data_ptr(), _ptr(workspace),
+                          0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if st:
+        _check(st, "isoq_kv_attn")
+    return out, lse
 
 
 class Sketch:

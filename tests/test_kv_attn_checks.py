@@ -1,0 +1,75 @@
+"""CPU checks of the arguments of isoq_kv_attn in the binding and of null
+handles in the library: a bad argument is refused before anything is launched
+(the stand-ins are those of test_binding_checks.py)."""
+import pytest
+import torch
+
+import paper_2603_28430_amd as iq
+from paper_2603_28430_amd import isoquant as binding
+from test_binding_checks import _params, _raises
+
+
+class _NoLaunch:
+    def __init__(self, real):
+        self._real = real
+
+    def __getattr__(self, name):
+        if name == "isoq_kv_attn":
+            raise AssertionError("the library was reached with a bad argument")
+        return getattr(self._real, name)
+
+
+@pytest.fixture
+def cpu_as_device(monkeypatch):
+    monkeypatch.setattr(binding, "_is_gpu", lambda t: t.device.type == "cpu")
+    monkeypatch.setattr(binding, "lib", _NoLaunch(binding.lib))
+
+
+def good():
+    p = _params()
+    cache = torch.zeros((2, 2, 16, p.record_bytes), dtype=torch.uint8)
+    rho = torch.zeros((2, 2, 16))
+    return dict(pk=p, pv=p, q=torch.zeros((3, 4, 128), dtype=torch.float16), k_idx=cache, k_rho=rho,
+                v_idx=cache.clone(), v_rho=rho.clone(), block_table=torch.zeros((3, 2), dtype=torch.int32),
+                seq_lens=torch.zeros(3, dtype=torch.int32))
+
+
+def test_attn_tensor_checks(cpu_as_device):
+    ok = good()
+    q, cache, rho, table, lens = ok["q"], ok["k_idx"], ok["k_rho"], ok["block_table"], ok["seq_lens"]
+    bad = [("q", q.to("meta")), ("q", q[..., :64]), ("q", q.to(torch.bfloat16)), ("q", q[:2]), ("q", q[0]),
+           ("q", torch.zeros((4, 3, 128), dtype=torch.float16).transpose(0, 1)),
+           ("block_table", table.to("meta")), ("block_table", table.long()), ("block_table", table[:2]),
+           ("block_table", torch.zeros((2, 3), dtype=torch.int32).t()),
+           ("seq_lens", lens.to("meta")), ("seq_lens", lens.long()), ("seq_lens", lens[:2]), ("seq_lens", lens[None])]
+    for k in ("k", "v"):
+        bad += [(k + "_idx", cache.to("meta")), (k + "_idx", cache[..., :40]), (k + "_idx", cache[:1]),
+                (k + "_idx", cache.to(torch.int8)), (k + "_idx", cache[:, :, ::2]),
+                (k + "_rho", rho.to("meta")), (k + "_rho", rho[:, :, :8]), (k + "_rho", rho.double()),
+                (k + "_rho", torch.zeros((2, 16, 2)).transpose(1, 2))]
+    for name, t in bad:
+        _raises(lambda: iq.isoq_kv_attn(**dict(ok, **{name: t})))
+
+
+def test_attn_token_checks(cpu_as_device):
+    ok = good()
+    start = torch.tensor([0, 1, 2, 3], dtype=torch.int32)
+    for more in (dict(max_q_len=2), dict(q_start=start[:3]), dict(q_start=start.long()), dict(q_start=start[None]),
+                 dict(q_start=start.to("meta")), dict(q_start=torch.zeros(8, dtype=torch.int32)[::2])):
+        _raises(lambda: iq.isoq_kv_attn(**ok, **more))
+
+
+def test_attn_output_checks(cpu_as_device):
+    ok = good()
+    out, lse = torch.zeros_like(ok["q"]), torch.zeros((3, 4))
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for more in (dict(out=out.float()), dict(out=out[:2]), dict(out=out.to("meta")), dict(lse=lse.half()),
+                 dict(lse=lse[:, :3]), dict(lse=lse.to("meta")), dict(lse=torch.zeros((4, 3)).t()),
+                 dict(workspace=ws.float()), dict(workspace=ws.to("meta")), dict(workspace=ws[::2])):
+        _raises(lambda: iq.isoq_kv_attn(**ok, **more))
+
+
+def test_attn_null_handles():
+    assert binding.lib.isoq_kv_attn(None, None, 1, None, None, 1, 1, 1, 1, 1, None, None, None, None, 1, 16, None, 1,
+                                    None, 16, 1.0, None, None, None, 0, None) == 3
+    assert binding.lib.isoq_kv_attn_workspace(None, None, 1, 1, 1, 1, 1, 1, 16, 1, 16) == 0
