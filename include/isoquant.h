@@ -405,7 +405,7 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  *               on different streams, or captured graphs that may run at the
  *               same time, need one each.  A smaller one is ISOQ_E_INVALID.
  * Limits: n_seqs <= 65535, n_tokens * n_q_heads < 2^31, max_q_len * n_q_heads <=
- * 2^23, max_blocks_per_seq * block_size < 2^31.
+ * 2^23, max_blocks_per_seq * block_size <= 2^31 - 1024.
  * Arithmetic: logits, softmax statistics and sums in fp32 or in integers of 32
  * bits (see the kernels for what is rounded).  A query with an infinity or NaN
  * gives NaN in its row of out and lse.  The result does not depend on the order in which

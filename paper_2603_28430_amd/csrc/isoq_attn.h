@@ -53,6 +53,18 @@ constexpr int kAttnJoinRows = 4;   // rows per workgroup of the join
 // token, split, sequence).
 const void *attn_generic_kernel_for(int variant, int bits);
 size_t attn_generic_lds(int slots, int variant);
+// Matrix-core kernel (isoq_attn_m.h; widths of the tuned decoding kernels) for
+// `rows` rows per sequence and key head: its entry, its dynamic LDS, and the
+// rows that a workgroup takes.  Grid (key head + n_kv_heads row tile, split,
+// sequence).
+struct AttnKernel {
+    const void *fn;
+    size_t lds;
+    int rows;
+};
+AttnKernel attn_m_kernel_b2(int d, int rows, bool f16);
+AttnKernel attn_m_kernel_b3(int d, int rows, bool f16);
+AttnKernel attn_m_kernel_b4(int d, int rows, bool f16);
 // Join of the splits: grid (rows of a sequence / kAttnJoinRows, sequence).
 const void *attn_join_kernel_for(int variant);
 

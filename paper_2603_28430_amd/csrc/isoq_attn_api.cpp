@@ -16,25 +16,40 @@ using namespace isoq;
 // Rows (query heads of a sequence's tokens): a grid of one workgroup of 256 a row
 // stays below 2^32 threads.
 constexpr int kAttnMaxRows = 1 << 23;
+// Positions: a workgroup's first one past them still fits 31 bits.
+constexpr int64_t kAttnMaxPos = 0x7FFFFFFF - 1023;
 
 // How a call is cut up; from its sizes alone, so that isoq_kv_attn_workspace
 // answers for the call that follows.
 struct AttnPlan {
+    AttnKernel kern;   // fn null: the width-generic kernel, a row per workgroup
     int64_t max_pos;   // positions a sequence has at most
+    int64_t groups;    // workgroups per sequence and split
     int width, slots;  // rotated coordinates per row (a multiple of the slot), slots
     int chunk, n_splits;
 };
 
-AttnPlan attn_plan(const isoq_params *pk, int n_seqs, int max_q_len, int n_q_heads, int n_kv_heads, int block_size,
-                   int max_blocks_per_seq, int64_t max_len)
+AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int n_seqs, int max_q_len, int n_q_heads,
+                   int n_kv_heads, int block_size, int max_blocks_per_seq, int64_t max_len)
 {
     AttnPlan p{};
     const int sw = pk->variant == VAR_BLOCK8 ? 8 : 4;
     p.slots = (padded_width(pk->variant, pk->d) + sw - 1) / sw;
     p.width = p.slots * sw;
     p.max_pos = std::min<int64_t>(max_len, (int64_t)max_blocks_per_seq * block_size);
-    const int64_t want = 1024, blocks = (int64_t)n_q_heads * max_q_len * n_seqs;
-    int64_t splits = std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
+    const bool f16 = dtype == ISOQ_F16;
+    const int64_t rows = (int64_t)(n_q_heads / n_kv_heads) * max_q_len;
+    p.groups = (int64_t)n_q_heads * max_q_len;
+    // (wide codebooks: levels that one set of digits does not hold)
+    if (decode_d(pk->d) && !pk->wide && !pv->wide) {
+        const int r = (int)std::min<int64_t>(rows, 1 << 20);
+        p.kern = pk->bits == 2   ? attn_m_kernel_b2(pk->d, r, f16)
+                 : pk->bits == 3 ? attn_m_kernel_b3(pk->d, r, f16)
+                                 : attn_m_kernel_b4(pk->d, r, f16);
+        p.groups = n_kv_heads * ((rows + p.kern.rows - 1) / p.kern.rows);
+    }
+    const int64_t want = 2048, blocks = p.groups * n_seqs;
+    const int64_t splits = std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
     p.chunk = (int)std::min<int64_t>(chunk, 0x7FFFFF00);
@@ -63,7 +78,7 @@ isoq_status check_attn(const isoq_params *pk, const isoq_params *pv, int dtype, 
         return ISOQ_E_INVALID;
     if ((pk->n_sets != 1 && pk->n_sets != n_kv_heads) || (pv->n_sets != 1 && pv->n_sets != n_kv_heads))
         return ISOQ_E_INVALID;
-    if (n_seqs > 65535 || (int64_t)max_blocks_per_seq * block_size > 0x7FFFFFFF ||
+    if (n_seqs > 65535 || (int64_t)max_blocks_per_seq * block_size > kAttnMaxPos ||
         n_tokens > 0x7FFFFFFF / n_q_heads || max_q_len > kAttnMaxRows / n_q_heads)
         return ISOQ_E_UNSUPPORTED;
     return ISOQ_OK;
@@ -81,7 +96,7 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
                    max_len) != ISOQ_OK ||
         n_tokens == 0 || n_seqs == 0)
         return 0;
-    return plan_bytes(attn_plan(pk, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len),
+    return plan_bytes(attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len),
                       n_tokens, n_q_heads);
 }
 
@@ -108,7 +123,7 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
         !aligned(lse, 4) || !aligned(workspace, 16))
         return ISOQ_E_ALIGN;
     const AttnPlan plan =
-        attn_plan(pk, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len);
+        attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len);
     const size_t need = plan_bytes(plan, n_tokens, n_q_heads);
     if (need > 0 && !workspace)
         return ISOQ_E_NULL;
@@ -160,12 +175,19 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
         a.k_lev[k] = pk->levels[k];
         a.v_lev[k] = pv->levels[k];
     }
+    a.k_dig = pk->lv;
+    a.v_dig = pv->vd[dtype == ISOQ_F16 ? 0 : 1];
     void *args[] = {&a};
-    const void *fn = attn_generic_kernel_for(pk->variant, pk->bits);
+    const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(pk->variant, pk->bits);
+    const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, pk->variant);
     if (!fn)
         return ISOQ_E_UNSUPPORTED;
-    st = launch_lds(fn, dim3((unsigned)n_q_heads * (unsigned)max_q_len, (unsigned)plan.n_splits, (unsigned)n_seqs), 256,
-                    args, attn_generic_lds(plan.slots, pk->variant), stream);
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess)
+            return hip_fail(e, "hipFuncSetAttribute");
+    }
+    st = launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)plan.n_splits, (unsigned)n_seqs), 256, args, lds, stream);
     if (st != ISOQ_OK || plan.n_splits == 1)
         return st;
     const unsigned rows = (unsigned)n_q_heads * (unsigned)max_q_len;

@@ -1,0 +1,689 @@
+// Attention over the paged quantized cache on the integer matrix cores (widths
+// of the tuned decoding kernels).
+//
+// The logits are those of isoq_scores_m.h: rotated query and codebook as 8-bit
+// digits, products of digits summed exactly in int32 by v_mfma_i32_16x16x64_i8,
+// the level digits picked four at a time by v_perm_b32.  The sum of values is
+// the same product the other way round: with w_t = p_t rho_vt,
+//     sum_t w_t c[idx_tj],
+// w as a 31-bit integer cut into four digits (in units of 2^-30 of the largest
+// norm of the tile, p <= 1) and the levels as two digits (fp16 queries: a level
+// within 2^-16 of the largest) or three (fp32: 2^-24).
+//
+// Lane layout.  A tile is 64 positions of a wave and four rows (query heads of
+// new tokens that share the key head).  The logits' instruction has the rows'
+// digits as A's rows (4 per row) and keys as columns, so lane 16 r + i ends up
+// with row r's logits of the positions i, 16 + i, 32 + i, 48 + i.  It turns them
+// into w, whose 4 x 4 (position, digit) bytes are transposed in registers and
+// go through 1 KB of LDS to become A of the second product: rows again (row,
+// digit), k = the tile's 64 positions, lane 16 g + m holding row m's digit for
+// the positions 16 i + 4 g + c (word c, byte i).  B's columns are coordinates:
+// lane 16 g + n has the coordinates n D/16 .. (n + 1) D/16 - 1 of the same 16
+// positions, read from the records (staged in LDS as they are): the index bits
+// of four positions are transposed bytewise (v_perm) and then masked, which
+// gives selector bytes of four positions without spreading each row's bits.
+// Its result has row r's four digit sums in lane 16 r + n: the digits are
+// combined by shifts and adds and enter an fp32 sum, one register per
+// coordinate and row, which the running maximum of the row rescales.
+#pragma once
+
+#include "isoq_attn_device.h"
+#include "isoq_scores_m.h"
+
+namespace isoq {
+namespace {
+
+// Bytes of a 16-lane row's maximum: every lane of the row gets it.
+__device__ __forceinline__ float row_max16(float v)
+{
+    v = fmaxf(v, dpp_f<DPP_QUAD_1032>(v));
+    v = fmaxf(v, dpp_f<DPP_QUAD_2301>(v));
+    v = fmaxf(v, dpp_f<DPP_ROW_HALF_MIRROR>(v));
+    return fmaxf(v, dpp_f<DPP_ROW_MIRROR>(v));
+}
+
+// The value of lane 16 c + i in x[c] of every lane 16 r + i.
+__device__ __forceinline__ void spread_rows(uint32_t v, uint32_t x[4])
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
+    x[0] = b[0];
+    x[1] = b[1];
+    x[2] = c[0];
+    x[3] = c[1];
+}
+
+// Rotate the rows r0 .. r0 + n - 1 of a sequence's key head h (scale folded
+// in) into qt[n][D]; the largest magnitude of each to mx[8 r], an infinity or
+// NaN among them.
+template <int VAR, int D>
+__device__ __forceinline__ void attn_rotate(const AttnArgs &a, const AttnSeq &sq, int h, int r0, int n, float *qt,
+                                            uint32_t *mx)
+{
+    constexpr int LPQ = D / kCoordsPerLane, PL = kLanePL<VAR>;
+    const int set = a.k_sets == 1 ? 0 : h;
+    for (int e = threadIdx.x; e < n * LPQ; e += 256) {
+        const int r = e / LPQ, l = e - r * LPQ;
+        const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
+        const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
+        float x[8], y[8], P[VAR == VAR_BLOCK8 ? 8 : PL];
+        if (a.q_f16) {
+            Raw<true> raw;
+            load_row_chunk<true>(static_cast<const char *>(a.q) + row * D * 2 + l * 16, raw);
+            unpack<true>(raw, x);
+        } else {
+            Raw<false> raw;
+            load_row_chunk<false>(static_cast<const char *>(a.q) + row * D * 4 + l * 32, raw);
+            unpack<false>(raw, x);
+        }
+        const float *par = a.k_params + ((int64_t)set * LPQ + l) * PL;
+        if constexpr (VAR == VAR_BLOCK8) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) {   // row by row: all 64 parameters at once would set the kernel's registers
+                load_params<8>(par + 8 * q, P);
+                y[q] = P[0] * x[0];
+#pragma unroll
+                for (int c = 1; c < 8; c++)
+                    y[q] = fmaf(P[c], x[c], y[q]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            load_params<PL>(par, P);
+            rotate_forward<VAR>(P, x, y);
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const float v = y[k] * a.scale;
+            qt[r * D + 8 * l + k] = v;
+            m = max(m, __float_as_uint(fabsf(v)));   // ordered as the magnitudes; NaN above all
+        }
+        atomicMax(mx + 8 * r, m);
+    }
+}
+
+// Write one row's chunk of 8 coordinates of the sum of values, rotated back.
+template <int VAR, int D>
+__device__ __forceinline__ void attn_emit8(const AttnArgs &a, int64_t row, int h, int l, const float y[8])
+{
+    constexpr int LPQ = D / kCoordsPerLane, PL = kLanePL<VAR>;
+    const float *par = a.v_params + ((int64_t)(a.v_sets == 1 ? 0 : h) * LPQ + l) * PL;
+    float o[8];
+    if constexpr (VAR == VAR_BLOCK8) {
+#pragma unroll
+        for (int c = 0; c < 8; c++)
+            o[c] = 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; r++) {
+            float P[8];
+            load_params<8>(par + 8 * r, P);
+#pragma unroll
+            for (int c = 0; c < 8; c++)
+                o[c] = fmaf(P[c], y[r], o[c]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+        float P[PL];
+        load_params<PL>(par, P);
+        rotate_inverse<VAR>(P, y, o);
+    }
+    if (a.q_f16)
+        store_row_chunk<true>(static_cast<char *>(a.out) + row * D * 2 + l * 16, o);
+    else
+        store_row_chunk<false>(static_cast<char *>(a.out) + row * D * 4 + l * 32, o);
+}
+
+template <int D, int BITS, int NT>
+struct AttnMShape {
+    using S = ScoreMShape<D, BITS, 0>;
+    static constexpr int ROWS = 4 * NT;              // rows per workgroup
+    static constexpr int CL = D / 16;                // coordinates per lane of the second product
+    static constexpr int REC = 4 * S::RW;            // bytes of a staged record
+    // LDS words: per row of the workgroup its digit rows, digit sums (8), then
+    // the rotated queries; per wave the staged records (+ 4 bytes read past
+    // the last) and w's digits
+    static constexpr int row_words() { return 4 * S::ROWW + 8; }
+    static constexpr int wave_words() { return 64 * S::RW + 4 + NT * 256; }
+    static constexpr int lds_words()
+    {
+        // the rotated queries are gone when the waves' parts are written, and
+        // everything when the waves' sums are merged (4 x rows x D, m and l)
+        const int loop = ROWS * row_words() + (ROWS * D > 4 * wave_words() ? ROWS * D : 4 * wave_words());
+        const int merge = 4 * ROWS * D + 8 * ROWS;
+        return loop > merge ? loop : merge;
+    }
+};
+
+// Selector bytes of the four positions x[0..3] for the coordinates of a group:
+// `n` coordinates whose bits start at bit 0 of x; sel[c] byte i = index of
+// coordinate c at position i.
+template <int BITS, int N>
+__device__ __forceinline__ void position_selectors(const uint32_t x[4], uint32_t sel[N])
+{
+    constexpr int PLANES = (N * BITS + 7) / 8;
+    uint32_t b[4];   // byte k of the four positions
+    {
+        const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), hi = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u);
+        b[0] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+        if constexpr (PLANES > 1)
+            b[1] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+    }
+    if constexpr (PLANES > 2) {
+        const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u), hi = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+        b[2] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+        if constexpr (PLANES > 3)
+            b[3] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+    }
+    constexpr uint32_t mask = BITS == 2 ? 0x03030303u : BITS == 3 ? 0x07070707u : 0x0F0F0F0Fu;
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+        const int bit = c * BITS, k = bit >> 3, sh = bit & 7;
+        if (sh + BITS <= 8)
+            sel[c] = (sh ? b[k] >> sh : b[k]) & mask;
+        else   // (3 bits) across two bytes
+            sel[c] = bit_select(vector_const(sh == 6 ? 0x03030303u : 0x01010101u), b[k] >> sh, b[k + 1] << (8 - sh)) & mask;
+    }
+}
+
+// Level digits of four selector bytes: tab holds 8 levels (2 and 3 bits) or 16.
+template <int BITS>
+__device__ __forceinline__ uint32_t level_bytes(const uint32_t tab[4], uint32_t sel, uint32_t upper)
+{
+    if constexpr (BITS < 4)
+        return __builtin_amdgcn_perm(tab[1], tab[0], sel);
+    // sel: index mod 8; upper: 0xFF where the index is 8 or more
+    return bit_select(upper, __builtin_amdgcn_perm(tab[3], tab[2], sel), __builtin_amdgcn_perm(tab[1], tab[0], sel));
+}
+
+template <int D, int BITS, int NT, int VD>
+__global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
+{
+    using H = AttnMShape<D, BITS, NT>;
+    using S = typename H::S;
+    constexpr int64_t RB = (int64_t)D * BITS / 8;
+    constexpr int QP = BITS == 4 ? 29 : 30;   // query integers below 2^QP (4 bits: digits of twice them)
+    constexpr int CL = H::CL, ROWS = H::ROWS;
+    extern __shared__ __align__(16) uint32_t smem[];
+
+    const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads), rt = (int)(blockIdx.x / (uint32_t)a.n_kv_heads);
+    const int h = (int)xcd_head((uint32_t)hx, (uint32_t)a.n_kv_heads, a.block_size * RB % 128 != 0);
+    const int s = blockIdx.z;
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnSeq sq = attn_seq(a, s);
+    const int r0 = rt * ROWS, total = sq.rows * a.group;   // rows of the sequence's key head
+    if (r0 >= total)   // (block-uniform, as every early return here)
+        return;
+    const int n = min(ROWS, total - r0);
+    // rows come in the tokens' order, so the last one attends to the most positions
+    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap), lim_min = sq.limit(r0 / a.group, a.cap);
+    const int64_t t0l = (int64_t)blockIdx.y * a.chunk;
+    if (t0l >= lim_all && blockIdx.y > 0)
+        return;   // the join looks at the splits below a row's limit only
+    const int t0 = (int)t0l, tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+
+    uint32_t *dig = smem;                                            // [ROWS][4][ROWW]
+    int *sums = reinterpret_cast<int *>(dig + ROWS * 4 * S::ROWW);   // [ROWS][8]: 4 digit sums, largest magnitude
+    uint32_t *mx = reinterpret_cast<uint32_t *>(sums) + 4;
+    float *qt = reinterpret_cast<float *>(sums + ROWS * 8);          // [ROWS][D], before the waves' parts
+    uint32_t *mine = reinterpret_cast<uint32_t *>(qt) + w * H::wave_words();
+    uint32_t *wdig = mine + 64 * S::RW + 4;
+
+    // 0. places, records and norms of the wave's positions, as in
+    //    isoq_scores_m.h: the block-table entry two batches ahead, records one
+    const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
+    struct Place {
+        int32_t blk, pos;
+        bool ok;
+    };
+    struct Batch {
+        uint32_t w[S::RW];
+        float rho;
+    };
+    const int tw = t0 + 64 * w + lane;
+    const uint64_t rstride = (uint64_t)a.n_kv_heads * a.block_size, row0 = (uint64_t)h * a.block_size;
+    const uint64_t bstride = rstride * RB;
+    auto times = [](uint32_t blk, uint64_t stride, uint32_t add) {   // one multiply unless the stride needs 33 bits
+        uint64_t o = (uint64_t)blk * (uint32_t)stride + add;
+        if (stride >> 32)
+            o += (uint64_t)(blk * (uint32_t)(stride >> 32)) << 32;
+        return o;
+    };
+    auto place = [&](int b) {
+        const int64_t tl = (int64_t)tw + 256 * (int64_t)b;
+        const uint32_t tt = (uint32_t)min(tl, (int64_t)tend - 1);
+        const uint32_t bi = fast_div(tt, a.div_block);
+        const int32_t blk = table[bi];
+        const bool ok = tl < tend && blk >= 0 && blk < a.n_blocks;
+        // an invalid position reads position 0 of the head in block 0 (always
+        // present) and gets no weight
+        return Place{ok ? blk : 0, ok ? (int)(tt - bi * a.block_size) : 0, ok};
+    };
+    auto issue = [&](const Place &pl, const uint8_t *idx, const float *rho, Batch &k) {
+        const uint32_t blk = (uint32_t)pl.blk, pos = (uint32_t)pl.pos;
+        const uint8_t *pc0 = idx + row0 * RB + times(blk, bstride, 0) + (uint64_t)pos * S::CP;
+        const int64_t pstep = (int64_t)a.block_size * S::CP;
+        const uint64_t row = row0 + times(blk, rstride, pos);
+        if constexpr (S::LW == 4) {
+#pragma unroll
+            for (int v = 0; v < S::RW / 4; v++) {
+                const u32x4 q4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(pc0 + v * pstep));
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const uint32_t e = q4[c];
+                    k.w[4 * v + c] = e;
+                }
+            }
+        } else if constexpr (S::LW == 2) {
+            static_assert(S::LW != 2 || S::CP == 8, "one load per piece");
+#pragma unroll
+            for (int v = 0; v < S::RW / 2; v++) {
+                const u32x2 q2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(pc0 + v * pstep));
+                const uint32_t e0 = q2[0], e1 = q2[1];
+                k.w[2 * v] = e0;
+                k.w[2 * v + 1] = e1;
+            }
+        } else if constexpr (S::LW == 1) {
+#pragma unroll
+            for (int v = 0; v < S::RW; v++)
+                k.w[v] = reinterpret_cast<const uint32_t *>(pc0)[v];
+        } else {
+            // an odd number of half-words, stored whole (isoq_scores_m.h)
+            const bool odd = row & 1;
+            const uint32_t *al = reinterpret_cast<const uint32_t *>(pc0 + (odd ? 2 : 0));
+            const uint32_t half = *reinterpret_cast<const uint16_t *>(pc0 + (odd ? 0 : RB - 2));
+            uint32_t r[S::RW - 1];
+#pragma unroll
+            for (int v = 0; v < S::RW - 1; v++)
+                r[v] = al[v];
+            k.w[0] = odd ? (r[0] << 16) | half : r[0];
+#pragma unroll
+            for (int v = 1; v < S::RW - 1; v++)
+                k.w[v] = odd ? __builtin_amdgcn_alignbit(r[v], r[v - 1], 16) : r[v];
+            k.w[S::RW - 1] = odd ? r[S::RW - 2] >> 16 : half;
+        }
+        k.rho = rho[row];
+    };
+    const int nb = (tend - t0 + 255) / 256;   // (0 where no position is left)
+    Batch k{}, v{};
+    Place here{}, next{};
+    if (nb > 0) {
+        here = place(0);
+        issue(here, a.k_idx, a.k_rho, k);
+        issue(here, a.v_idx, a.v_rho, v);
+        next = place(1);
+    }
+
+    // 1. rotated queries, 2. their digits, as in isoq_scores_m.h
+    for (int i = threadIdx.x; i < ROWS * 8; i += 256)
+        sums[i] = 0;
+    __syncthreads();
+    switch (a.variant) {
+    case VAR_FULL: attn_rotate<VAR_FULL, D>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_FAST: attn_rotate<VAR_FAST, D>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D>(a, sq, h, r0, n, qt, mx); break;
+    default: attn_rotate<VAR_BLOCK8, D>(a, sq, h, r0, n, qt, mx); break;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * 4 * S::NQ; i += 256) {
+        const int g = i / (4 * S::NQ), cq = i - g * (4 * S::NQ);
+        const int c = cq / S::NQ, q = cq - c * S::NQ;
+        const int e = head_exponent(__uint_as_float(mx[8 * g]), QP);
+        uint32_t word[4] = {0u, 0u, 0u, 0u};
+        int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            const bool full = BITS == 2 && 4 * (q / 4) + 4 <= S::CC / 4;
+            const int ci = full ? 16 * (q / 4) + 4 * b + q % 4 : 8 * (q / 2) + 2 * b + q % 2;
+            const int x = ci < S::CC ? to_fixed(qt[g * D + c * S::CC + ci], e) : 0;
+            int d[4];
+            if constexpr (BITS == 4) {
+                digits4(x, d);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    sum[j] += d[j];
+            }
+            digits4(BITS == 4 ? 2 * x : x, d);
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                word[j] |= (uint32_t)(d[j] & 255) << (8 * b);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            dig[(g * 4 + j) * S::ROWW + cq] = word[j];
+            if constexpr (BITS == 4)
+                atomicAdd(sums + 8 * g + j, sum[j]);
+        }
+    }
+    __syncthreads();   // (the waves' parts take the rotated queries' place from here on)
+
+    const int col = lane & 15, kq = lane >> 4;
+    uint32_t A[NT][S::NQ];
+    i32x4 asum[NT];
+    float f1[NT], f2[NT];   // 2^-e (with the quantum) of the digits, in two factors
+    float m[NT], l[NT];     // running maximum and (the lane's part of the) sum of row 4 nt + kq
+    int lim[NT];
+    float acc[NT][CL];
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int ga = 4 * nt + (col >> 2), gr = 4 * nt + kq;
+        const uint32_t *row = dig + ((ga < n ? ga : 0) * 4 + (col & 3)) * S::ROWW + kq * S::NQ;
+#pragma unroll
+        for (int q = 0; q < S::NQ; q += 2) {
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(row + q);
+            const uint32_t x0 = x[0], x1 = x[1];
+            A[nt][q] = ga < n ? x0 : 0u;
+            A[nt][q + 1] = ga < n ? x1 : 0u;
+        }
+        const int gi = gr < n ? gr : 0;
+        const int e = head_exponent(__uint_as_float(mx[8 * gi]), QP) - a.k_dig.exp;
+        f1[nt] = __builtin_amdgcn_ldexpf(a.k_dig.quantum, -(e / 2));
+        f2[nt] = __builtin_amdgcn_ldexpf(1.f, e / 2 - e);
+        asum[nt] = i32x4{0, 0, 0, 0};
+        if constexpr (BITS == 4)
+            asum[nt] = *reinterpret_cast<const i32x4 *>(sums + 8 * gi);
+        lim[nt] = gr < n ? sq.limit((r0 + gr) / a.group, a.cap) : 0;
+        m[nt] = -INFINITY;
+        l[nt] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CL; c++)
+            acc[nt][c] = 0.f;
+    }
+
+    for (int b = 0; b < nb; b++) {
+        const int tb = t0 + 256 * b + 64 * w;   // the wave's first position
+        const uint64_t ok_mask = __builtin_amdgcn_ballot_w64(here.ok);
+        // 3. the keys' records, chunk kq of key 16 r + col in y[r]
+        uint32_t y[4][S::WC];
+#pragma unroll
+        for (int i = 0; i < S::WC; i++) {
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                const int o = c * S::CB + 32 * i, at = o >> 5, sh = o & 31;
+                if (at >= S::RW)
+                    y[c][i] = 0u;
+                else if (sh == 0)
+                    y[c][i] = k.w[at];
+                else
+                    y[c][i] = __builtin_amdgcn_alignbit(at + 1 < S::RW ? k.w[at + 1] : 0u, k.w[at], sh);
+            }
+            transpose_rows(y[0][i], y[1][i], y[2][i], y[3][i]);
+        }
+        uint32_t krho[4], vrho[4];
+        spread_rows(__float_as_uint(k.rho), krho);
+        // the values' records as they are, for the second product
+#pragma unroll
+        for (int i = 0; i < S::RW; i++)
+            mine[lane * S::RW + i] = v.w[i];
+        // their norms, and the unit of w: 2^-30 of the tile's largest norm
+        const float vr = here.ok ? fabsf(v.rho) : 0.f;
+        float vmax = row_max16(vr);
+        {
+            uint32_t x[4];
+            spread_rows(__float_as_uint(vmax), x);
+            vmax = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
+                         fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
+        }
+        const int ve = __builtin_amdgcn_readfirstlane(head_exponent(vmax, 30));
+        spread_rows(__float_as_uint(here.ok ? __builtin_amdgcn_ldexpf(v.rho, ve) : 0.f), vrho);
+        // what the digit sums count: 2^-ve, the levels' scale, 256 (the
+        // lowest digit products are left out)
+        const float vunit = __builtin_amdgcn_ldexpf(a.v_dig.scale, -ve);
+        __builtin_amdgcn_sched_barrier(0);
+        if (b + 1 < nb) {
+            here = next;
+            issue(here, a.k_idx, a.k_rho, k);
+            issue(here, a.v_idx, a.v_rho, v);
+            next = place(b + 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (ok_mask == 0)
+            continue;
+
+        // 4. logits (in units of ln 2) of the lane's row and its four positions
+        float val[NT][4];
+#pragma unroll
+        for (int st = 0; st < 4; st++) {
+            i32x4 d[NT][3];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int t = 0; t < 3; t++)
+                    d[nt][t] = asum[nt];
+            auto step = [&](auto nsc, int q0) {
+                constexpr int NS = decltype(nsc)::value;
+                uint32_t sel[NS], inv[NS], p[NS];
+                selectors<S, BITS, NS>(y[st], q0, sel);
+                if constexpr (BITS == 4) {
+#pragma unroll
+                    for (int j = 0; j < NS; j++) {
+                        const uint32_t neg = 0x0D0D0D0Du - ((sel[j] >> 3) & 0x01010101u);
+                        inv[j] = __builtin_amdgcn_perm(0u, 0u, neg);
+                        sel[j] = (sel[j] ^ inv[j]) & 0x07070707u;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 3; t++) {
+#pragma unroll
+                    for (int j = 0; j < NS; j++) {
+                        p[j] = __builtin_amdgcn_perm(a.k_dig.tab[t][1], a.k_dig.tab[t][0], sel[j]);
+                        if constexpr (BITS == 4)
+                            p[j] ^= inv[j];
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+                        d[nt][t] = digit_mfma<NS>(A[nt] + q0, p, d[nt][t]);
+                }
+            };
+#pragma unroll
+            for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
+                step(std::integral_constant<int, 4>{}, q0);
+            if constexpr (S::NQ % 4 != 0)
+                step(std::integral_constant<int, 2>{}, S::NQ - 2);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                const i32x4 *x = d[nt];
+                const int w01 = (x[0][0] << 8) + x[0][1] + x[1][0];
+                const int w2 = x[0][2] + x[1][1] + x[2][0];
+                const int w3 = x[0][3] + x[1][2] + x[2][1];
+                const float f = fmaf((float)w01, 65536.f, fmaf((float)w2, 256.f, (float)w3));
+                val[nt][st] = (f * f1[nt]) * (__uint_as_float(krho[st]) * f2[nt]);
+            }
+        }
+        const bool whole = ok_mask == ~0ull && tb + 64 <= lim_min && n == ROWS;   // (uniform)
+        if (!whole) {
+#pragma unroll
+            for (int st = 0; st < 4; st++) {
+                const int kk = 16 * st + col;
+                const bool ok = (ok_mask >> kk) & 1;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+                    val[nt][st] = ok && tb + kk < lim[nt] ? val[nt][st] : -INFINITY;
+            }
+        }
+        // 5. running maximum, weights, and their digits to LDS
+        float alpha[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            float top = fmaxf(fmaxf(val[nt][0], val[nt][1]), fmaxf(val[nt][2], val[nt][3]));
+            top = fmaxf(m[nt], row_max16(top));
+            const float ref = top == -INFINITY ? 0.f : top;
+            alpha[nt] = __builtin_amdgcn_exp2f(m[nt] - ref);
+            m[nt] = top;
+            uint32_t u[4];
+            float sum = 0.f;
+#pragma unroll
+            for (int st = 0; st < 4; st++) {
+                const float p = __builtin_amdgcn_exp2f(val[nt][st] - ref);
+                sum += p;
+                // balanced digits: each byte of x + 128 (in the three lower
+                // places), less 128
+                const int x = (int)__builtin_rintf(p * __uint_as_float(vrho[st]));
+                u[st] = ((uint32_t)x + 0x00808080u) ^ 0x00808080u;
+            }
+            l[nt] = fmaf(l[nt], alpha[nt], sum);
+            const uint32_t a01 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), a23 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+            const uint32_t b01 = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), b23 = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
+            uint32_t *dst = wdig + nt * 256 + lane;   // [digit][row][position mod 16]
+            dst[0] = __builtin_amdgcn_perm(a23, a01, 0x05040100u);
+            dst[64] = __builtin_amdgcn_perm(a23, a01, 0x07060302u);
+            dst[128] = __builtin_amdgcn_perm(b23, b01, 0x05040100u);
+            dst[192] = __builtin_amdgcn_perm(b23, b01, 0x07060302u);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        uint32_t W[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            // A's row col: row col / 4, digit col mod 4 (lowest first); word c: positions 16 i + 4 kq + c
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(wdig + nt * 256 + (col & 3) * 64 + (col >> 2) * 16 + 4 * kq);
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                const uint32_t e = x[c];
+                W[nt][c] = e;
+            }
+        }
+        // 6. sums of values, up to 8 of the lane's coordinates at a time
+        auto group = [&](auto nc, int c0) {
+            constexpr int N = decltype(nc)::value;
+            uint32_t sel[4][N];
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t x[4];
+                const int bit0 = col * CL * BITS + c0 * BITS;   // of the record
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const uint8_t *src = reinterpret_cast<const uint8_t *>(mine) + (16 * i + 4 * kq + c) * H::REC + (bit0 >> 3);
+                    uint32_t e;
+                    __builtin_memcpy(&e, src, 4);
+                    x[i] = (CL * BITS) % 8 == 0 && (8 * BITS) % 8 == 0 ? e : e >> (bit0 & 7);
+                }
+                position_selectors<BITS, N>(x, sel[c]);
+            }
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                uint32_t up[4];
+                if constexpr (BITS == 4) {
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        up[c] = __builtin_amdgcn_perm(0u, 0u, 0x0C0C0C0Cu + ((sel[c][j] >> 3) & 0x01010101u));
+                        sel[c][j] &= 0x07070707u;
+                    }
+                }
+                i32x4 d[NT][VD];
+#pragma unroll
+                for (int t = 0; t < VD; t++) {
+                    uint32_t p[4];
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        p[c] = level_bytes<BITS>(a.v_dig.tab[t], sel[c][j], BITS == 4 ? up[c] : 0u);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+                        d[nt][t] = digit_mfma<4>(W[nt], p, i32x4{0, 0, 0, 0});
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    // d[t][r]: level digit t, weight digit r, both lowest first
+                    const i32x4 *x = d[nt];
+                    float f;
+                    if constexpr (VD == 2) {
+                        const int hi = (x[1][3] << 8) + x[1][2] + x[0][3];
+                        const int lo = ((x[1][1] + x[0][2]) << 8) + x[1][0] + x[0][1];
+                        f = fmaf((float)hi, 65536.f * 256.f, (float)lo * 256.f);
+                    } else {
+                        const int hi = (x[2][3] << 8) + x[2][2] + x[1][3];
+                        const int lo = ((x[2][1] + x[1][2] + x[0][3]) << 8) + x[2][0] + x[1][1] + x[0][2];
+                        f = fmaf((float)hi, 65536.f * 65536.f, (float)lo * 65536.f);
+                    }
+                    acc[nt][c0 + j] = fmaf(f, vunit, acc[nt][c0 + j] * alpha[nt]);
+                }
+            }
+        };
+#pragma unroll
+        for (int c0 = 0; c0 + 8 <= CL; c0 += 8)
+            group(std::integral_constant<int, 8>{}, c0);
+        if constexpr (CL % 8 != 0)
+            group(std::integral_constant<int, CL % 8>{}, CL / 8 * 8);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();   // (the next batch's records and digits take this one's place)
+    }
+
+    // 7. the four waves' m, l and sums, merged through LDS
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        float x = l[nt];
+        x += dpp_f<DPP_QUAD_1032>(x);
+        x += dpp_f<DPP_QUAD_2301>(x);
+        x += dpp_f<DPP_ROW_HALF_MIRROR>(x);
+        l[nt] = x + dpp_f<DPP_ROW_MIRROR>(x);
+        if (nonfinite(mx[8 * (4 * nt + kq)]) && lim[nt] > 0)
+            l[nt] = NAN;   // an infinity or NaN in the rotated query: no digits hold it
+    }
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(smem);          // [4 waves][ROWS][D]
+    float *ml = part + 4 * ROWS * D;                        // [4 waves][ROWS][2]
+#pragma unroll
+    for (int nt = 0; nt < NT; nt++) {
+        const int r = 4 * nt + kq;
+#pragma unroll
+        for (int c = 0; c < CL; c++)
+            part[(w * ROWS + r) * D + col * CL + c] = acc[nt][c];
+        if (col == 0) {
+            ml[(w * ROWS + r) * 2] = m[nt];
+            ml[(w * ROWS + r) * 2 + 1] = l[nt];
+        }
+    }
+    __syncthreads();
+    constexpr int LPQ = D / 8;
+    for (int e = threadIdx.x; e < n * LPQ; e += 256) {
+        const int r = e / LPQ, j = e - r * LPQ;
+        const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
+        const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
+        float top = -INFINITY, sum = 0.f, f[4], y[8];
+#pragma unroll
+        for (int x = 0; x < 4; x++)
+            top = fmaxf(top, ml[(x * ROWS + r) * 2]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int x = 0; x < 4; x++) {
+            f[x] = __builtin_amdgcn_exp2f(ml[(x * ROWS + r) * 2] - ref);
+            sum = fmaf(f[x], ml[(x * ROWS + r) * 2 + 1], sum);
+        }
+#pragma unroll
+        for (int c = 0; c < 8; c++) {
+            y[c] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                y[c] = fmaf(f[x], part[(x * ROWS + r) * D + 8 * j + c], y[c]);
+        }
+        if (a.n_splits > 1) {
+            float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 8 * j;
+#pragma unroll
+            for (int c = 0; c < 8; c++)
+                dst[c] = y[c];
+            if (j == 0) {
+                float *to = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+                to[0] = top;
+                to[1] = sum;
+            }
+            continue;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int c = 0; c < 8; c++)
+            y[c] *= inv;
+        switch (a.variant) {
+        case VAR_FULL: attn_emit8<VAR_FULL, D>(a, row, h, j, y); break;
+        case VAR_FAST: attn_emit8<VAR_FAST, D>(a, row, h, j, y); break;
+        case VAR_PLANAR2D: attn_emit8<VAR_PLANAR2D, D>(a, row, h, j, y); break;
+        default: attn_emit8<VAR_BLOCK8, D>(a, row, h, j, y); break;
+        }
+        if (j == 0 && a.lse)
+            a.lse[row] = attn_lse(top, sum);
+    }
+}
+
+}  // namespace
+}  // namespace isoq

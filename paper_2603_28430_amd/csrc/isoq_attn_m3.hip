@@ -1,0 +1,9 @@
+// Matrix-core attention kernels of 3-bit caches (the kernel template is in
+// isoq_attn_m.h).
+#include "isoq_attn_m_pick.h"
+
+namespace isoq {
+
+AttnKernel attn_m_kernel_b3(int d, int rows, bool f16) { return attn_m_d<3>(d, rows, f16); }
+
+}  // namespace isoq
