@@ -422,6 +422,57 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
                               int n_seqs, int n_q_heads, int n_kv_heads, int block_size, int max_blocks_per_seq,
                               int64_t max_len);
 
+/*
+ * isoq_kv_copy_blocks -- copy whole cache blocks inside a paged cache (forking
+ * a sequence whose last block is shared, copy on write; moving blocks): for
+ * every pair (source, destination) of block_pairs, the records and norms of
+ * all heads, and with sk the signs and gammas, of block `source` go to block
+ * `destination`, in one launch.
+ *
+ *   pk          the K quantizer, whose record size V shares (v_idx and v_rho, or
+ *               both NULL: keys only).
+ *   sk, k_signs, k_gamma  the keys' sketch and its arrays, or all NULL.
+ *   block_pairs device, int32 [n_pairs][2].  A pair with a block outside [0,
+ *               n_blocks), or of equal blocks, is skipped.  A destination must
+ *               not be a source or destination of another pair (its contents are
+ *               then unspecified; nothing else is touched).
+ *   k_idx .. k_gamma, n_blocks, block_size  the cache, laid out as in
+ *               isoq_kv_append (records 16-byte aligned).
+ * Limits: n_pairs < 2^24, n_blocks * block_size < 2^31.  n_pairs = 0 is a no-op.
+ */
+isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, const int32_t *block_pairs,
+                                int64_t n_pairs, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,
+                                float *v_rho, uint8_t *k_signs, float *k_gamma, int64_t n_blocks, int block_size,
+                                void *stream);
+
+/*
+ * isoq_kv_compact -- keep some positions of sequences and drop the others, in
+ * place: afterwards position i < n_keep[s] of sequence s holds, for head h,
+ * what position keep[s][h][i] held (records, norms, signs, gammas), in one
+ * launch.  n_keep is then the sequences' lengths, and a sequence's blocks from
+ * ceil(n_keep / block_size) on are free.
+ *
+ *   keep        device, int32 [n_seqs][keep_heads][max_keep], each list strictly
+ *               ascending; keep_heads is n_heads, or 1: one list for all heads.
+ *   n_keep      device, int32 [n_seqs], entries of each list that count (cut to
+ *               [0, max_keep]).
+ *   block_table, max_blocks_per_seq  as in isoq_kv_scores.  The blocks of a
+ *               sequence that is compacted must not be another's too (copy a
+ *               shared block first).  An entry whose source or destination has no
+ *               block in [0, n_blocks), or lies outside the table, is skipped.
+ *   pk, sk, k_idx .. k_gamma, n_heads, n_blocks, block_size  as in
+ *               isoq_kv_copy_blocks.
+ * Positions from n_keep[s] on keep their contents.  A list that does not ascend
+ * strictly leaves the positions below its n_keep unspecified and touches nothing
+ * else.  Limits: n_seqs <= 65535, n_heads < 2^22, max_keep <= 2^31 - 8192,
+ * max_blocks_per_seq * block_size < 2^31.
+ */
+isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const int32_t *keep, int keep_heads,
+                            int max_keep, const int32_t *n_keep, int n_seqs, const int32_t *block_table,
+                            int max_blocks_per_seq, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,
+                            float *v_rho, uint8_t *k_signs, float *k_gamma, int64_t n_blocks, int block_size,
+                            void *stream);
+
 /* Sizes: bytes of one packed index record, ceil(pw * bits / 8) with the
  * padded width pw = 4 g4 (Full, Fast) or 2 g2 (2-D); isoq_packed_bytes is
  * ceil(d * bits / 8), the same number whenever d is a multiple of 4.  Raw

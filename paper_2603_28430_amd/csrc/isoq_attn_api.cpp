@@ -8,6 +8,7 @@
 
 #include "isoq_attn.h"
 #include "isoq_handles.h"
+#include "isoq_pages.h"
 
 namespace {
 
@@ -18,6 +19,9 @@ using namespace isoq;
 constexpr int kAttnMaxRows = 1 << 23;
 // Positions: a workgroup's first one past them still fits 31 bits.
 constexpr int64_t kAttnMaxPos = 0x7FFFFFFF - 1023;
+
+// Kept positions: a workgroup's first one past them still fits 31 bits.
+constexpr int kCompactMaxKeep = 0x7FFFFFFF - 8191;
 
 // How a call is cut up; from its sizes alone, so that isoq_kv_attn_workspace
 // answers for the call that follows.
@@ -81,6 +85,45 @@ isoq_status check_attn(const isoq_params *pk, const isoq_params *pv, int dtype, 
     if (n_seqs > 65535 || (int64_t)max_blocks_per_seq * block_size > kAttnMaxPos ||
         n_tokens > 0x7FFFFFFF / n_q_heads || max_q_len > kAttnMaxRows / n_q_heads)
         return ISOQ_E_UNSUPPORTED;
+    return ISOQ_OK;
+}
+
+// The planes of a cache that a page call was given: records and norms of K, of
+// V (or null), signs and gamma of a sketch (or null).
+struct Planes {
+    uint8_t *base[kCachePlanes];
+    int64_t row[kCachePlanes];   // bytes of a position of a head
+    bool record[kCachePlanes];   // stored in the cache's pieces
+    int n;
+};
+
+isoq_status cache_planes(const isoq_params *pk, const isoq_sketch *sk, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,
+                         float *v_rho, uint8_t *k_signs, float *k_gamma, Planes &p)
+{
+    if (!k_idx || !k_rho || !v_idx != !v_rho)
+        return ISOQ_E_NULL;
+    if (sk ? !k_signs || !k_gamma : k_signs || k_gamma)
+        return ISOQ_E_NULL;
+    if (sk && (sk->variant != pk->variant || sk->d != pk->d || sk->device != pk->device))
+        return ISOQ_E_INVALID;
+    if (!aligned(k_idx, 16) || !aligned(v_idx, 16) || !aligned(k_rho, 4) || !aligned(v_rho, 4) ||
+        !aligned(k_signs, 4) || !aligned(k_gamma, 4))
+        return ISOQ_E_ALIGN;
+    p.n = 0;
+    auto add = [&](void *base, int64_t row, bool record) {
+        if (base) {
+            p.base[p.n] = static_cast<uint8_t *>(base);
+            p.row[p.n] = row;
+            p.record[p.n++] = record;
+        }
+    };
+    const int64_t rec = (int64_t)record_bytes(pk->variant, pk->d, pk->bits);
+    add(k_idx, rec, true);
+    add(v_idx, rec, true);
+    add(k_rho, 4, false);
+    add(v_rho, 4, false);
+    add(k_signs, sk ? sk->m / 8 : 0, false);
+    add(k_gamma, 4, false);
     return ISOQ_OK;
 }
 
@@ -194,6 +237,110 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
     return launch_lds(attn_join_kernel_for(pk->variant),
                       dim3((rows + kAttnJoinRows - 1) / kAttnJoinRows, (unsigned)n_seqs), 64 * kAttnJoinRows, args, 0,
                       stream);
+}
+
+isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, const int32_t *block_pairs,
+                                int64_t n_pairs, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,
+                                float *v_rho, uint8_t *k_signs, float *k_gamma, int64_t n_blocks, int block_size,
+                                void *stream)
+{
+    if (!pk)
+        return ISOQ_E_NULL;
+    if (n_pairs < 0 || n_heads < 1 || block_size < 1 || n_blocks < 0)
+        return ISOQ_E_INVALID;
+    if (n_pairs > 0xFFFFFF || n_blocks > 0x7FFFFFFF / block_size)
+        return ISOQ_E_UNSUPPORTED;
+    if (n_pairs == 0 || n_blocks == 0)
+        return ISOQ_OK;
+    if (!block_pairs)
+        return ISOQ_E_NULL;
+    Planes pl;
+    isoq_status st = cache_planes(pk, sk, k_idx, k_rho, v_idx, v_rho, k_signs, k_gamma, pl);
+    if (st != ISOQ_OK)
+        return st;
+    if (!aligned(block_pairs, 4))
+        return ISOQ_E_ALIGN;
+    CopyArgs a{};
+    int64_t most = 0;
+    for (int c = 0; c < pl.n; c++) {
+        a.plane[c] = pl.base[c];
+        a.stride[c] = pl.row[c] * n_heads * block_size;
+        a.unit[c] = a.stride[c] % 16 == 0 && aligned(pl.base[c], 16) ? 16 : a.stride[c] % 4 == 0 ? 4 : 1;
+        most = std::max(most, (a.stride[c] / a.unit[c] + kCopyUnits - 1) / kCopyUnits);
+    }
+    if (most > 65535)
+        return ISOQ_E_UNSUPPORTED;
+    a.pairs = block_pairs;
+    a.n_blocks = n_blocks;
+    st = check_device(pk);
+    if (st != ISOQ_OK)
+        return st;
+    void *args[] = {&a};
+    return launch_lds(copy_blocks_kernel(), dim3((unsigned)n_pairs, (unsigned)pl.n, (unsigned)most), 256, args, 0,
+                      stream);
+}
+
+isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const int32_t *keep, int keep_heads,
+                            int max_keep, const int32_t *n_keep, int n_seqs, const int32_t *block_table,
+                            int max_blocks_per_seq, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,
+                            float *v_rho, uint8_t *k_signs, float *k_gamma, int64_t n_blocks, int block_size,
+                            void *stream)
+{
+    if (!pk)
+        return ISOQ_E_NULL;
+    if (n_seqs < 0 || max_keep < 0 || n_heads < 1 || block_size < 1 || n_blocks < 0 || max_blocks_per_seq < 0 ||
+        (keep_heads != 1 && keep_heads != n_heads))
+        return ISOQ_E_INVALID;
+    if (n_seqs > 65535 || n_heads > 0x3FFFFF || (int64_t)max_blocks_per_seq * block_size > 0x7FFFFFFF ||
+        n_blocks > 0x7FFFFFFF / block_size || max_keep > kCompactMaxKeep)
+        return ISOQ_E_UNSUPPORTED;
+    if (n_seqs == 0 || max_keep == 0 || n_blocks == 0 || max_blocks_per_seq == 0)
+        return ISOQ_OK;
+    if (!keep || !n_keep || !block_table)
+        return ISOQ_E_NULL;
+    Planes pl;
+    isoq_status st = cache_planes(pk, sk, k_idx, k_rho, v_idx, v_rho, k_signs, k_gamma, pl);
+    if (st != ISOQ_OK)
+        return st;
+    if (!aligned(keep, 4) || !aligned(n_keep, 4) || !aligned(block_table, 4))
+        return ISOQ_E_ALIGN;
+    CompactArgs a{};
+    for (int c = 0; c < pl.n; c++) {
+        const int64_t row = pl.row[c];
+        a.base[c] = pl.base[c];
+        a.head_stride[c] = row * block_size;
+        a.block_stride[c] = a.head_stride[c] * n_heads;
+        const int piece = pl.record[c] ? cache_piece(row) : (int)row;
+        if (piece != row) {   // pieces of 16 or 8 bytes, those of one position block_size of them apart
+            a.width[c] = a.pos_stride[c] = piece;
+            a.step[c] = (int64_t)piece * block_size;
+        } else {   // records stored whole
+            int w = 16;
+            while (row % w != 0 || !aligned(pl.base[c], (size_t)w))
+                w /= 2;
+            a.width[c] = w;
+            a.pos_stride[c] = (int32_t)row;
+            a.step[c] = w;
+        }
+        a.first[c + 1] = a.first[c] + (int32_t)(row / a.width[c]);
+    }
+    for (int c = pl.n; c < kCachePlanes; c++)
+        a.first[c + 1] = a.first[c];
+    a.keep = keep;
+    a.n_keep = n_keep;
+    a.block_table = block_table;
+    a.n_blocks = n_blocks;
+    a.keep_heads = keep_heads;
+    a.max_keep = max_keep;
+    a.max_blocks = max_blocks_per_seq;
+    a.block_size = block_size;
+    a.div_block = make_fastdiv((uint32_t)block_size);
+    st = check_device(pk);
+    if (st != ISOQ_OK)
+        return st;
+    void *args[] = {&a};
+    return launch_lds(compact_kernel(), dim3((unsigned)n_heads, (unsigned)n_seqs, (unsigned)a.first[pl.n]),
+                      kCompactThreads, args, 0, stream);
 }
 
 }  // extern "C"

@@ -67,6 +67,9 @@ def _load():
                                c_int, vp, i64, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     L.isoq_kv_attn_workspace.argtypes = [vp, vp, c_int, i64, c_int, c_int, c_int, c_int, c_int, c_int, i64]
     L.isoq_kv_attn_workspace.restype = ctypes.c_size_t
+    L.isoq_kv_copy_blocks.argtypes = [vp, vp, vp, i64, c_int, vp, vp, vp, vp, vp, vp, i64, c_int, vp]
+    L.isoq_kv_compact.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, vp, c_int, c_int, vp, vp, vp, vp, vp, vp, i64,
+                                  c_int, vp]
     L.isoq_packed_bytes.argtypes = [c_int, c_int]
     L.isoq_packed_bytes.restype = ctypes.c_size_t
     L.isoq_record_bytes.argtypes = [c_int, c_int, c_int]
@@ -84,7 +87,8 @@ def _load():
     for f in ("isoq_params_init", "isoq_params_destroy", "isoq_params_export", "isoq_params_info",
               "isoq_quantize", "isoq_dequantize", "isoq_roundtrip", "isoq_kv_append", "isoq_kv_scores", "isoq_sketch_init",
               "isoq_sketch_destroy", "isoq_sketch_export", "isoq_quantize_qjl", "isoq_kv_append_qjl",
-              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn", "isoq_codebook_lloyd",
+              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn",
+              "isoq_kv_copy_blocks", "isoq_kv_compact", "isoq_codebook_lloyd",
               "isoq_rotation_draws"):
         getattr(L, f).restype = c_int
     return L
@@ -621,3 +625,76 @@ def isoq_kv_append_qjl(pk: Params, sk: Sketch, k_new, slot_mapping, k_idx, k_rho
                                 k_signs.data_ptr(), k_gamma.data_ptr(), n_blocks, block_size, _stream_ptr(stream))
     if st:
         _check(st, "isoq_kv_append_qjl")
+
+
+def _cache_planes(pk: Params, k_idx, k_rho, v_idx, v_rho, sketch, k_signs, k_gamma):
+    """Checks of the cache that a page call moves; the tensors that are there."""
+    torch = _torch()
+    if k_idx.dim() != 4 or k_rho.dim() != 3:
+        raise ValueError("k_idx [n_blocks, n_heads, block_size, R], k_rho [n_blocks, n_heads, block_size]")
+    cache = k_idx.shape
+    if cache[3] != pk.record_bytes or k_rho.shape != cache[:3]:
+        raise ValueError("cache shapes do not match the handle")
+    tensors = (k_idx, k_rho)
+    if (v_idx is None) != (v_rho is None):
+        raise ValueError("v_idx and v_rho come together")
+    if v_idx is not None:
+        if v_idx.shape != cache or v_rho.shape != cache[:3]:
+            raise ValueError("V tensors must have the shapes of the K tensors")
+        tensors += (v_idx, v_rho)
+    if sketch is None:
+        if k_signs is not None or k_gamma is not None:
+            raise ValueError("k_signs and k_gamma need their sketch")
+    else:
+        if k_signs is None or k_gamma is None:
+            raise ValueError("a sketch needs k_signs and k_gamma")
+        if k_signs.shape != cache[:3] + (sketch.m // 8,) or k_gamma.shape != cache[:3]:
+            raise ValueError("k_signs [n_blocks, n_heads, block_size, m/8], k_gamma like k_rho")
+        tensors += (k_signs, k_gamma)
+    for i, t in enumerate(tensors):   # records (or signs) and norms in turn
+        if t.dtype != (torch.float32 if i % 2 else torch.uint8):
+            raise TypeError("records and signs must be uint8, norms and gammas float32")
+    return tensors
+
+
+def isoq_kv_copy_blocks(pk: Params, block_pairs, k_idx, k_rho, v_idx=None, v_rho=None, sketch=None, k_signs=None,
+                        k_gamma=None, stream=None):
+    """Copy whole cache blocks: block_pairs int32 [n_pairs, 2], (source,
+    destination) each, over all heads of the K (and V) records and norms and
+    of the sketch's arrays (see include/isoquant.h)."""
+    torch = _torch()
+    tensors = _cache_planes(pk, k_idx, k_rho, v_idx, v_rho, sketch, k_signs, k_gamma)
+    if block_pairs.dim() != 2 or block_pairs.shape[1] != 2 or block_pairs.dtype != torch.int32:
+        raise ValueError("block_pairs must be int32 [n_pairs, 2]")
+    _placed(k_idx, tensors + (block_pairs,))
+    n_blocks, n_heads, block_size, _ = k_idx.shape
+    st = lib.isoq_kv_copy_blocks(pk.handle, None if sketch is None else sketch.handle, block_pairs.data_ptr(),
+                                 block_pairs.shape[0], n_heads, k_idx.data_ptr(), k_rho.data_ptr(), _ptr(v_idx),
+                                 _ptr(v_rho), _ptr(k_signs), _ptr(k_gamma), n_blocks, block_size, _stream_ptr(stream))
+    if st:
+        _check(st, "isoq_kv_copy_blocks")
+
+
+def isoq_kv_compact(pk: Params, keep, n_keep, block_table, k_idx, k_rho, v_idx=None, v_rho=None, sketch=None,
+                    k_signs=None, k_gamma=None, stream=None):
+    """Compact sequences in place to the positions that stay: keep int32
+    [n_seqs, n_heads or 1, max_keep], strictly ascending, of which n_keep int32
+    [n_seqs] count; block_table int32 [n_seqs, max_blocks].  Afterwards n_keep is
+    the sequences' lengths (see include/isoquant.h)."""
+    torch = _torch()
+    tensors = _cache_planes(pk, k_idx, k_rho, v_idx, v_rho, sketch, k_signs, k_gamma)
+    n_blocks, n_heads, block_size, _ = k_idx.shape
+    if keep.dim() != 3 or keep.shape[1] not in (1, n_heads):
+        raise ValueError("keep must be [n_seqs, n_heads or 1, max_keep]")
+    n_seqs, keep_heads, max_keep = keep.shape
+    if n_keep.shape != (n_seqs,) or block_table.dim() != 2 or block_table.shape[0] != n_seqs:
+        raise ValueError("n_keep [n_seqs] and block_table [n_seqs, max_blocks] need one row per sequence")
+    if keep.dtype != torch.int32 or n_keep.dtype != torch.int32 or block_table.dtype != torch.int32:
+        raise TypeError("keep, n_keep and block_table must be int32")
+    _placed(k_idx, tensors + (keep, n_keep, block_table))
+    st = lib.isoq_kv_compact(pk.handle, None if sketch is None else sketch.handle, keep.data_ptr(), keep_heads,
+                             max_keep, n_keep.data_ptr(), n_seqs, block_table.data_ptr(), block_table.shape[1],
+                             n_heads, k_idx.data_ptr(), k_rho.data_ptr(), _ptr(v_idx), _ptr(v_rho), _ptr(k_signs),
+                             _ptr(k_gamma), n_blocks, block_size, _stream_ptr(stream))
+    if st:
+        _check(st, "isoq_kv_compact")

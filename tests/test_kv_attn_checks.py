@@ -73,3 +73,46 @@ def test_attn_null_handles():
     assert binding.lib.isoq_kv_attn(None, None, 1, None, None, 1, 1, 1, 1, 1, None, None, None, None, 1, 16, None, 1,
                                     None, 16, 1.0, None, None, None, 0, None) == 3
     assert binding.lib.isoq_kv_attn_workspace(None, None, 1, 1, 1, 1, 1, 1, 16, 1, 16) == 0
+
+
+class _NoPages(_NoLaunch):
+    def __getattr__(self, name):
+        if name in ("isoq_kv_copy_blocks", "isoq_kv_compact"):
+            raise AssertionError("the library was reached with a bad argument")
+        return getattr(self._real, name)
+
+
+def test_page_call_checks(monkeypatch):
+    monkeypatch.setattr(binding, "_is_gpu", lambda t: t.device.type == "cpu")
+    monkeypatch.setattr(binding, "lib", _NoPages(binding.lib))
+    ok = good()
+    sk = iq.Sketch(0, ok["pk"], 64)
+    planes = {k: ok[k] for k in ("k_idx", "k_rho", "v_idx", "v_rho")}
+    signs, gamma = torch.zeros((2, 2, 16, 8), dtype=torch.uint8), torch.zeros((2, 2, 16))
+    pairs = torch.zeros((3, 2), dtype=torch.int32)
+    keep, n_keep = torch.zeros((3, 1, 5), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    table = ok["block_table"]
+    cache, rho = planes["k_idx"], planes["k_rho"]
+    bad = [dict(v_idx=None), dict(v_rho=None), dict(sketch=sk), dict(sketch=sk, k_signs=signs), dict(k_signs=signs),
+           dict(sketch=sk, k_signs=signs[..., :4], k_gamma=gamma), dict(sketch=sk, k_signs=signs.int(), k_gamma=gamma),
+           dict(sketch=sk, k_signs=signs, k_gamma=gamma.half()), dict(sketch=sk, k_signs=signs, k_gamma=gamma[:1])]
+    for k in ("k", "v"):
+        bad += [{k + "_idx": x} for x in (cache.to("meta"), cache[..., :40], cache[:1], cache.to(torch.int8), cache[:, :, ::2])]
+        bad += [{k + "_rho": x} for x in (rho.to("meta"), rho[:, :, :8], rho.double(), torch.zeros((2, 16, 2)).transpose(1, 2))]
+    for kw in bad:
+        _raises(lambda: iq.isoq_kv_copy_blocks(ok["pk"], pairs, **dict(planes, **kw)))
+        _raises(lambda: iq.isoq_kv_compact(ok["pk"], keep, n_keep, table, **dict(planes, **kw)))
+    for x in (pairs.long(), pairs[:, :1], pairs.to("meta"), pairs.t().contiguous().t(), pairs[0]):
+        _raises(lambda: iq.isoq_kv_copy_blocks(ok["pk"], x, **planes))
+    three = torch.zeros((3, 3, 5), dtype=torch.int32)
+    for args in ((keep.long(), n_keep, table), (keep[0], n_keep, table), (three, n_keep, table), (keep[:2], n_keep, table),
+                 (keep[:, :, ::2], n_keep, table), (keep.to("meta"), n_keep, table), (keep, n_keep.long(), table),
+                 (keep, n_keep[:2], table), (keep, n_keep.to("meta"), table), (keep, n_keep, table.long()),
+                 (keep, n_keep, table[:2]), (keep, n_keep, table.to("meta"))):
+        _raises(lambda: iq.isoq_kv_compact(ok["pk"], *args, **planes))
+
+
+def test_page_calls_null_handles():
+    assert binding.lib.isoq_kv_copy_blocks(None, None, None, 1, 1, None, None, None, None, None, None, 1, 16, None) == 3
+    assert binding.lib.isoq_kv_compact(None, None, None, 1, 1, None, 1, None, 1, 1, None, None, None, None, None, None, 1,
+                                       16, None) == 3
