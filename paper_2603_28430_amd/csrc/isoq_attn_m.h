@@ -139,12 +139,39 @@ struct AttnMShape {
     using S = ScoreMShape<D, BITS, 0>;
     static constexpr int ROWS = 4 * NT;              // rows per workgroup
     static constexpr int CL = D / 16;                // coordinates per lane of the second product
-    static constexpr int REC = 4 * S::RW;            // bytes of a staged record
+    // A record as staged in LDS: a lane's coordinates in groups of up to 8,
+    // [group][lane] (one aligned read each: reads that are not aligned to
+    // their size took 60 cycles here, aligned ones 10).  Groups of exactly 32
+    // or 16 bits that start on whole ones are the record itself; others get a
+    // word each.  A row's words + 4: the rows 4 apart that a read's quarters
+    // touch lie 16 banks apart.
+    static constexpr int NG = (CL + 7) / 8;
+    static constexpr int GB = (CL < 8 ? CL : 8) * BITS;   // bits of a full group
+    static constexpr bool HALF = GB == 16 && CL % 8 == 0;
+    static constexpr int SW = HALF ? 8 * NG : 16 * NG;    // words of a staged record
+    static constexpr int RS = SW + 4;
+    // word i of a staged record from the record's words
+    static __device__ __forceinline__ uint32_t staged(const uint32_t *w, int i)
+    {
+        if (HALF) {   // groups 2 i and 2 i + 1 (lanes 2 j, 2 j + 1)
+            const int g = i / 8, j = i - 8 * g, lo = half(2 * j, g), hi = half(2 * j + 1, g);
+            if (hi == lo + 1 && lo % 2 == 0)
+                return w[lo / 2];
+            return __builtin_amdgcn_perm(w[hi / 2], w[lo / 2], (lo % 2 ? 0x0302u : 0x0100u) | (hi % 2 ? 0x07060000u : 0x05040000u));
+        }
+        const int g = i / 16, n = i - 16 * g, bit = (n * CL + 8 * g) * BITS, at = bit >> 5, sh = bit & 31;
+        const int bits = (CL - 8 * g < 8 ? CL - 8 * g : 8) * BITS;
+        if (sh == 0)
+            return w[at];
+        if (sh + bits <= 32)
+            return w[at] >> sh;
+        return __builtin_amdgcn_alignbit(w[at + 1], w[at], sh);
+    }
+    static constexpr int half(int n, int g) { return n * (CL / 8) + g; }   // half-word of lane n's group g
     // LDS words: per row of the workgroup its digit rows, digit sums (8), then
-    // the rotated queries; per wave the staged records (+ 4 bytes read past
-    // the last) and w's digits
+    // the rotated queries; per wave the staged records and w's digits
     static constexpr int row_words() { return 4 * S::ROWW + 8; }
-    static constexpr int wave_words() { return 64 * S::RW + 4 + NT * 256; }
+    static constexpr int wave_words() { return 64 * RS + NT * 256; }
     static constexpr int lds_words()
     {
         // the rotated queries are gone when the waves' parts are written, and
@@ -228,7 +255,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     uint32_t *mx = reinterpret_cast<uint32_t *>(sums) + 4;
     float *qt = reinterpret_cast<float *>(sums + ROWS * 8);          // [ROWS][D], before the waves' parts
     uint32_t *mine = reinterpret_cast<uint32_t *>(qt) + w * H::wave_words();
-    uint32_t *wdig = mine + 64 * S::RW + 4;
+    uint32_t *wdig = mine + 64 * H::RS;
 
     // 0. places, records and norms of the wave's positions, as in
     //    isoq_scores_m.h: the block-table entry two batches ahead, records one
@@ -414,8 +441,9 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         spread_rows(__float_as_uint(k.rho), krho);
         // the values' records as they are, for the second product
 #pragma unroll
-        for (int i = 0; i < S::RW; i++)
-            mine[lane * S::RW + i] = v.w[i];
+        for (int i = 0; i < H::SW; i += 4)
+            *reinterpret_cast<u32x4 *>(mine + lane * H::RS + i) =
+                u32x4{H::staged(v.w, i), H::staged(v.w, i + 1), H::staged(v.w, i + 2), H::staged(v.w, i + 3)};
         // their norms, and the unit of w: 2^-30 of the tile's largest norm
         const float vr = here.ok ? fabsf(v.rho) : 0.f;
         float vmax = row_max16(vr);
@@ -552,13 +580,13 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 #pragma unroll
             for (int c = 0; c < 4; c++) {
                 uint32_t x[4];
-                const int bit0 = col * CL * BITS + c0 * BITS;   // of the record
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const uint8_t *src = reinterpret_cast<const uint8_t *>(mine) + (16 * i + 4 * kq + c) * H::REC + (bit0 >> 3);
-                    uint32_t e;
-                    __builtin_memcpy(&e, src, 4);
-                    x[i] = (CL * BITS) % 8 == 0 && (8 * BITS) % 8 == 0 ? e : e >> (bit0 & 7);
+                    const int at = (16 * i + 4 * kq + c) * H::RS;   // position 16 i + 4 kq + c
+                    if constexpr (H::HALF)
+                        x[i] = reinterpret_cast<const uint16_t *>(mine + at)[2 * c0 + col];
+                    else
+                        x[i] = mine[at + 2 * c0 + col];
                 }
                 position_selectors<BITS, N>(x, sel[c]);
             }
