@@ -411,6 +411,8 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             p->lv = lv[0];
             build_value_digits(bits, p->levels, 2, p->vd[0]);
             build_value_digits(bits, p->levels, 3, p->vd[1]);
+            build_half_levels(bits, p->levels, true, p->kh);
+            build_half_levels(bits, p->levels, false, p->vh);
             p->n_pass = (int)lv.size();
             p->lv_offset = layout.size();
             const float *f = reinterpret_cast<const float *>(lv.data() + 1);

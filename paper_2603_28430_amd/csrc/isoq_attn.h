@@ -44,10 +44,10 @@ struct AttnArgs {
     float k_lev[16], v_lev[16];  // codebooks (width-generic kernel)
     LevelDigits k_dig;           // the same as digits (matrix-core kernel)
     ValueDigits v_dig;
+    HalfLevels k_half, v_half;   // and in fp16 (kernel of many rows)
 };
 
 constexpr int kAttnMaxSplits = 256;
-constexpr int kAttnJoinRows = 4;   // rows per workgroup of the join
 
 // Width-generic kernel: one row per workgroup, grid (query head + n_q_heads
 // token, split, sequence).
@@ -61,11 +61,17 @@ struct AttnKernel {
     const void *fn;
     size_t lds;
     int rows;
+    bool parts;   // leaves parts for the join even with one split
 };
 AttnKernel attn_m_kernel_b2(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b3(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b4(int d, int rows, bool f16);
-// Join of the splits: grid (rows of a sequence / kAttnJoinRows, sequence).
-const void *attn_join_kernel_for(int variant);
+// Kernel of many rows (isoq_attn_c.h; fp16 queries, widths up to 128), or {}.
+AttnKernel attn_c_kernel_for(int d, int bits);
+// Join of the splits, 256 threads: up to kAttnJoinFew splits (few) grid (rows of
+// a sequence / (256 / slots), sequence), more (row, sequence); a row being query
+// head + n_q_heads token.
+constexpr int kAttnJoinFew = 8;
+const void *attn_join_kernel_for(int variant, bool few);
 
 }  // namespace isoq

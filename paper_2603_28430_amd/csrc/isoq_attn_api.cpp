@@ -50,10 +50,28 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         p.kern = pk->bits == 2   ? attn_m_kernel_b2(pk->d, r, f16)
                  : pk->bits == 3 ? attn_m_kernel_b3(pk->d, r, f16)
                                  : attn_m_kernel_b4(pk->d, r, f16);
+        // Many rows: where decoding a tile for 128 rows at once pays for what
+        // fewer leave idle (16 x 8 heads, 4,096 positions, d = 128, 3 bits: 24
+        // rows 74 us by digits, 80 us in fp16; 32: 82, 73; 64: 138, 87; 256: 464,
+        // 177.  4 x 4 heads, 8,192, d = 64, 4 bits: 24 rows 27, 24; 64: 44, 27.)
+        if (f16 && rows >= 32) {
+            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits);
+            if (many.fn)
+                p.kern = many;
+        }
         p.groups = n_kv_heads * ((rows + p.kern.rows - 1) / p.kern.rows);
     }
-    const int64_t want = 2048, blocks = p.groups * n_seqs;
-    const int64_t splits = std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
+    // Splits: as many as give so many workgroups (a compute unit holds 2 to 5 at
+    // once; what is over evens out sequences of different lengths, and is not
+    // wanted where there is one sequence, or where a split leaves its part of
+    // 128 rows in memory); none up to 1,024 positions, where a second launch
+    // takes longer than the four tiles a wave then has (one sequence of 700, 8 x 4
+    // heads: 12.1 us, with three splits 15.6).
+    // (1 x 8 x 8 heads, 131,071 positions, 64 / 96 / 128 / 256 splits: 48 / 50 / 49 /
+    // 53 us; 16 ragged sequences x 8 heads of up to 4,096, 3 / 4 / 6 splits: 52 / 45 /
+    // 37 us; 8 x 32 heads, 32,768, 2 / 4 / 8 splits: 227 / 204 / 201 us.)
+    const int64_t want = p.kern.parts ? 1024 : n_seqs == 1 ? 768 : 2048, blocks = p.groups * n_seqs;
+    const int64_t splits = p.max_pos <= 1024 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
     p.chunk = (int)std::min<int64_t>(chunk, 0x7FFFFF00);
@@ -63,7 +81,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
 
 size_t plan_bytes(const AttnPlan &p, int64_t n_tokens, int n_q_heads)
 {
-    return p.n_splits == 1 ? 0 : sizeof(float) * (size_t)n_tokens * n_q_heads * p.n_splits * (p.width + 2);
+    return p.n_splits == 1 && !p.kern.parts ? 0 : sizeof(float) * (size_t)n_tokens * n_q_heads * p.n_splits * (p.width + 2);
 }
 
 // Argument values of isoq_kv_attn that do not need its pointers.
@@ -220,6 +238,8 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
     }
     a.k_dig = pk->lv;
     a.v_dig = pv->vd[dtype == ISOQ_F16 ? 0 : 1];
+    a.k_half = pk->kh;
+    a.v_half = pv->vh;
     void *args[] = {&a};
     const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(pk->variant, pk->bits);
     const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, pk->variant);
@@ -231,11 +251,11 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
             return hip_fail(e, "hipFuncSetAttribute");
     }
     st = launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)plan.n_splits, (unsigned)n_seqs), 256, args, lds, stream);
-    if (st != ISOQ_OK || plan.n_splits == 1)
+    if (st != ISOQ_OK || need == 0)
         return st;
-    const unsigned rows = (unsigned)n_q_heads * (unsigned)max_q_len;
-    return launch_lds(attn_join_kernel_for(pk->variant),
-                      dim3((rows + kAttnJoinRows - 1) / kAttnJoinRows, (unsigned)n_seqs), 64 * kAttnJoinRows, args, 0,
+    const bool few = plan.n_splits <= kAttnJoinFew;
+    const unsigned rows = (unsigned)n_q_heads * (unsigned)max_q_len, per = few ? 256 / plan.slots : 1;
+    return launch_lds(attn_join_kernel_for(pk->variant, few), dim3((rows + per - 1) / per, (unsigned)n_seqs), 256, args, 0,
                       stream);
 }
 

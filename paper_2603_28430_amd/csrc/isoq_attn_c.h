@@ -1,0 +1,516 @@
+// Attention of many rows (chunks of new tokens) over the paged quantized cache:
+// fp16 queries, widths up to 128, on the fp16 matrix cores.
+//
+// isoq_attn_m.h decodes a tile of 64 positions for 4 or 8 rows; with hundreds of
+// rows per key head that decoding is what it spends its time on.  Here a
+// workgroup has 128 rows, decodes each tile once into LDS, and multiplies in
+// fp16 with fp32 sums:
+//   logits   both factors in two parts, x = hi + lo with hi = fp16(x) and lo =
+//            fp16(x - hi), three products (lo lo is left out): the rotated query
+//            row in units of a power of two that brings its largest coordinate
+//            to 8 .. 16, the codebook in units that bring its largest level to
+//            0.5 .. 1; what is left out is 2^-22 of a product, so that logits and
+//            lse keep fp32's accuracy;
+//   values   one product: w = p rho (p <= 1, in units of a power of two next to the
+//            tile's largest norm, up to 2^14) and the levels rounded to fp16 once,
+//            the levels in units for which they lie closest to fp16 numbers.  w's
+//            rounding, 2^-12 at most and of random sign from position to
+//            position, is like the output's own (fp16) rounding, not a sum of
+//            them; l sums the p before rounding, in fp32.
+//
+// Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
+// lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
+// 32: a row's maximum and sum are in-lane but for one exchange of halves, and
+// the fp16 weights are B of O^T = V^T P^T as they stand, if V^T's positions
+// are in the same order: [16 s][h][b][i].  K rows and V^T rows lie in LDS with
+// 16 bytes of padding (reads of 16 bytes by 16 rows touch every bank once).
+//
+// Decoding.  Wave c spreads chunk c (a quarter of the coordinates) of 64 keys;
+// values are decoded four positions at a time (position_selectors), which
+// gives V^T's rows directly.  A level's two bytes are two v_perm_b32 for four
+// coordinates, two more put them together.  Waves 0 and 1 fetch the records of
+// the next tile (K, V) while all compute.
+#pragma once
+
+#include "isoq_attn_m.h"
+
+namespace isoq {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int D, int BITS>
+struct AttnCShape {
+    using S = ScoreMShape<D, BITS, 0>;
+    using H = AttnMShape<D, BITS, 1>;
+    static constexpr int ROWS = 128;
+    static constexpr int KS = S::NQ;                 // 16-coordinate steps of the logits' product (4 chunks of 4 NQ)
+    static constexpr int KROW = 32 * KS + 16;        // bytes of a decoded key part
+    static constexpr int CT = (D + 31) / 32;         // 32-coordinate tiles of the values
+    static constexpr int VROW = 2 * 64 + 16;         // bytes of a coordinate's 64 positions
+    static constexpr int RK = 4 * S::WC + 1;         // words of a key's raw record (odd: lanes are keys)
+    static constexpr int RV = H::SW + 1;             // words of a value's raw record
+    // LDS bytes: keys hi, lo; values; raw records; per tile parity the norms
+    // (K, V), the valid positions and the values' unit
+    static constexpr int kHi = 0, kLo = 64 * KROW, kV = 2 * 64 * KROW, kRawK = kV + 32 * CT * VROW,
+                         kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV, kTile = kNorm + 2 * 512;
+    static constexpr int loop_bytes() { return kTile + 2 * 16; }
+    // before the loop the rotated queries and their largest magnitudes
+    static constexpr int QS = D + 1;
+    static constexpr int query_bytes() { return 4 * ROWS * (QS + 8); }
+    static constexpr int lds_bytes() { return loop_bytes() > query_bytes() ? loop_bytes() : query_bytes(); }
+    static_assert(kV % 16 == 0 && kRawK % 16 == 0 && kNorm % 16 == 0, "aligned parts");
+};
+
+// Four levels' fp16 values for four selector bytes: tables of the values' low
+// and high bytes.
+template <int BITS>
+__device__ __forceinline__ void level_halves(const uint32_t lo[4], const uint32_t hi[4], uint32_t sel, uint32_t upper,
+                                             uint32_t out[2])
+{
+    const uint32_t l = level_bytes<BITS>(lo, sel, upper), h = level_bytes<BITS>(hi, sel, upper);
+    out[0] = __builtin_amdgcn_perm(h, l, 0x05010400u);
+    out[1] = __builtin_amdgcn_perm(h, l, 0x07030602u);
+}
+
+// (4 bits) 0xFF where the index is 8 or more; the index mod 8.
+template <int BITS>
+__device__ __forceinline__ uint32_t split_index(uint32_t &sel)
+{
+    if constexpr (BITS < 4)
+        return 0u;
+    const uint32_t up = __builtin_amdgcn_perm(0u, 0u, 0x0C0C0C0Cu + ((sel >> 3) & 0x01010101u));
+    sel &= 0x07070707u;
+    return up;
+}
+
+__device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
+
+template <int D, int BITS>
+__global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
+{
+    using C = AttnCShape<D, BITS>;
+    using S = typename C::S;
+    using H = typename C::H;
+    constexpr int64_t RB = (int64_t)D * BITS / 8;
+    extern __shared__ __align__(16) uint32_t smem[];
+    uint8_t *const lds = reinterpret_cast<uint8_t *>(smem);
+
+    const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads), rt = (int)(blockIdx.x / (uint32_t)a.n_kv_heads);
+    const int h = (int)xcd_head((uint32_t)hx, (uint32_t)a.n_kv_heads, a.block_size * RB % 128 != 0);
+    const int s = blockIdx.z;
+    const int lane = threadIdx.x & 63, n32 = lane & 31, half = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnSeq sq = attn_seq(a, s);
+    const int r0 = rt * C::ROWS, total = sq.rows * a.group;
+    if (r0 >= total)   // (block-uniform, as every early return here)
+        return;
+    const int n = min(C::ROWS, total - r0);
+    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap);
+    const int64_t t0l = (int64_t)blockIdx.y * a.chunk;
+    if (t0l >= lim_all && blockIdx.y > 0)
+        return;   // the join looks at the splits below a row's limit only
+    const int t0 = (int)t0l, tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+    const int nt = (tend - t0 + 63) / 64;
+
+    // the wave's rows: one per lane of each half
+    const int r = 32 * w + n32;
+    const bool on = r < n;
+    const int tok = (r0 + (on ? r : 0)) / a.group;
+    const int lim = on ? sq.limit(tok, a.cap) : 0;
+    const int64_t row = (int64_t)(sq.first + tok) * a.n_q_heads + h * a.group + (r0 + (on ? r : 0) - tok * a.group);
+    // (rows in the tokens' order) the least of the wave's limits
+    const int lim_min = 32 * w + 32 <= n ? sq.limit((r0 + 32 * w) / a.group, a.cap) : 0;
+    const int lim_max = 32 * w < n ? sq.limit((r0 + min(32 * w + 31, n - 1)) / a.group, a.cap) : 0;
+
+    // 0. records of the next tile: waves 0 (K) and 1 (V), a position per lane
+    const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
+    const uint64_t rstride = (uint64_t)a.n_kv_heads * a.block_size, row0 = (uint64_t)h * a.block_size;
+    const uint64_t bstride = rstride * RB;
+    const uint8_t *const idx = (w == 0 ? a.k_idx : a.v_idx) + row0 * RB;
+    const float *const rhos = (w == 0 ? a.k_rho : a.v_rho) + row0;
+    const int64_t pstep = (int64_t)a.block_size * S::CP;
+    struct Batch {
+        uint32_t w[S::RW];
+        float rho;
+        bool ok;
+    } rec{};
+    auto block_of = [&](int t) {   // the block-table entry of the lane's position of tile t
+        const uint32_t tt = (uint32_t)min((int64_t)t0 + 64 * (int64_t)t + lane, (int64_t)tend - 1);
+        return table[fast_div(tt, a.div_block)];
+    };
+    auto fetch = [&](int t, int32_t blk) {
+        const int64_t tl = (int64_t)t0 + 64 * (int64_t)t + lane;
+        const uint32_t tt = (uint32_t)min(tl, (int64_t)tend - 1);
+        rec.ok = tl < tend && blk >= 0 && blk < a.n_blocks;
+        // (an invalid position reads position 0 of the head in block 0, which is always present)
+        const uint64_t b = rec.ok ? (uint32_t)blk : 0u;
+        const uint32_t pos = rec.ok ? tt - fast_div(tt, a.div_block) * a.block_size : 0u;
+        const uint8_t *src = idx + b * bstride + (uint64_t)pos * S::CP;
+        const uint64_t crow = b * rstride + pos;
+        if constexpr (S::LW == 4) {
+#pragma unroll
+            for (int v = 0; v < S::RW / 4; v++) {
+                const u32x4 q4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src + v * pstep));
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const uint32_t e = q4[c];
+                    rec.w[4 * v + c] = e;
+                }
+            }
+        } else if constexpr (S::LW == 2) {
+#pragma unroll
+            for (int v = 0; v < S::RW / 2; v++) {
+                const u32x2 q2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(src + v * pstep));
+                const uint32_t e0 = q2[0], e1 = q2[1];
+                rec.w[2 * v] = e0;
+                rec.w[2 * v + 1] = e1;
+            }
+        } else if constexpr (S::LW == 1) {
+#pragma unroll
+            for (int v = 0; v < S::RW; v++)
+                rec.w[v] = reinterpret_cast<const uint32_t *>(src)[v];
+        } else {
+            // an odd number of half-words, stored whole (isoq_scores_m.h)
+            const bool odd = (row0 + crow) & 1;
+            const uint32_t *al = reinterpret_cast<const uint32_t *>(src + (odd ? 2 : 0));
+            const uint32_t hw = *reinterpret_cast<const uint16_t *>(src + (odd ? 0 : RB - 2));
+            uint32_t x[S::RW - 1];
+#pragma unroll
+            for (int v = 0; v < S::RW - 1; v++)
+                x[v] = al[v];
+            rec.w[0] = odd ? (x[0] << 16) | hw : x[0];
+#pragma unroll
+            for (int v = 1; v < S::RW - 1; v++)
+                rec.w[v] = odd ? __builtin_amdgcn_alignbit(x[v], x[v - 1], 16) : x[v];
+            rec.w[S::RW - 1] = odd ? x[S::RW - 2] >> 16 : hw;
+        }
+        rec.rho = rhos[crow];
+    };
+    // the values' unit: norms below 2^unit; kept while the tile's largest norm
+    // is above 2^(unit - 4)
+    int unit = 0;
+    auto store_raw = [&](int t) {   // (waves 0 and 1) into tile t's places
+        float *norm = reinterpret_cast<float *>(lds + C::kNorm + 512 * (t & 1));
+        uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 16 * (t & 1));
+        if (w == 0) {
+            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawK) + lane * C::RK;
+#pragma unroll
+            for (int c = 0; c < 4; c++)
+#pragma unroll
+                for (int i = 0; i < S::WC; i++) {
+                    const int o = c * S::CB + 32 * i, at = o >> 5, sh = o & 31;
+                    dst[c * S::WC + i] = at >= S::RW ? 0u
+                                         : sh == 0   ? rec.w[at]
+                                                     : __builtin_amdgcn_alignbit(at + 1 < S::RW ? rec.w[at + 1] : 0u, rec.w[at], sh);
+                }
+            norm[lane] = rec.ok ? rec.rho : 0.f;
+            const uint64_t ok = __builtin_amdgcn_ballot_w64(rec.ok);
+            if (lane == 0) {
+                tile[0] = (uint32_t)ok;
+                tile[1] = (uint32_t)(ok >> 32);
+            }
+        } else {
+            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawV) + lane * C::RV;
+#pragma unroll
+            for (int i = 0; i < H::SW; i++)
+                dst[i] = H::staged(rec.w, i);
+            float top = row_max16(rec.ok ? fabsf(rec.rho) : 0.f);
+#pragma unroll
+            for (int o = 16; o < 64; o *= 2)
+                top = fmaxf(top, __shfl_xor(top, o));
+            const int e = __builtin_amdgcn_readfirstlane(top > 0.f ? __builtin_amdgcn_frexp_expf(top) : unit);
+            if (t == 0 || e > unit || e < unit - 4)
+                unit = e;
+            norm[64 + lane] = rec.ok ? __builtin_amdgcn_ldexpf(rec.rho, 14 - unit) : 0.f;
+            if (lane == 0)
+                tile[2] = (uint32_t)unit;
+        }
+    };
+    int32_t next = 0;
+    if (nt > 0 && w < 2) {
+        fetch(0, block_of(0));
+        next = block_of(1);
+    }
+
+    // 1. rotated queries, and the wave's rows of them as fp16 pairs in registers
+    float *qt = reinterpret_cast<float *>(smem);
+    uint32_t *mx = smem + C::ROWS * C::QS;   // [ROWS][8], as attn_rotate has them
+    for (int i = threadIdx.x; i < 8 * C::ROWS; i += 256)
+        mx[i] = 0;
+    __syncthreads();
+    switch (a.variant) {
+    case VAR_FULL: attn_rotate<VAR_FULL, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_FAST: attn_rotate<VAR_FAST, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
+    default: attn_rotate<VAR_BLOCK8, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
+    }
+    __syncthreads();
+    const uint32_t qmax = on ? mx[8 * r] : 0u;
+    const int qe = head_exponent(__uint_as_float(qmax), 4);
+    u32x4 qh[C::KS], ql[C::KS];
+#pragma unroll
+    for (int st = 0; st < C::KS; st++) {
+        // places 16 st + 8 half + 0 .. 7 of the keys' order: quads 4 st + 2 half + 0, 1 of all chunks in turn
+        f16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const int quad = 4 * st + 2 * half + e / 4, c = quad / S::NQ, q = quad - c * S::NQ;
+            const int ci = attn_coord<S, BITS>(q, e % 4);
+            const float x = on && ci < S::CC ? __builtin_amdgcn_ldexpf(qt[r * C::QS + c * S::CC + ci], qe) : 0.f;
+            const float v = nonfinite(qmax) ? 0.f : x;
+            hi[e] = (_Float16)v;
+            lo[e] = (_Float16)(v - (float)hi[e]);
+        }
+        qh[st] = __builtin_bit_cast(u32x4, hi);
+        ql[st] = __builtin_bit_cast(u32x4, lo);
+    }
+    // a logit (in units of ln 2) is f1 times sum and norm
+    const float f1 = fmaxf(__builtin_amdgcn_ldexpf(a.k_half.scale, -qe), 0x1p-126f);
+    __syncthreads();   // (the loop's parts take the queries' place)
+
+    f32x16 acc[C::CT];
+#pragma unroll
+    for (int c = 0; c < C::CT; c++)
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            acc[c][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    int now = 0;   // the unit of acc
+    if (D % 32 != 0) {   // coordinates past D: rows of zeros
+        for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW / 4; i += 256)
+            reinterpret_cast<uint32_t *>(lds + C::kV + D * C::VROW)[i] = 0u;
+    }
+    if (nt > 0 && w < 2)
+        store_raw(0);
+    __syncthreads();
+
+    for (int t = 0; t < nt; t++) {
+        // 2. decode the tile; the next one's records are asked for
+        {
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(lds + C::kRawK) + lane * C::RK + w * S::WC;
+            uint32_t y[S::WC];
+#pragma unroll
+            for (int i = 0; i < S::WC; i++)
+                y[i] = src[i];
+            uint8_t *dst = lds + lane * C::KROW + w * 8 * S::NQ;
+            auto part = [&](auto nsc, int q0) {
+                constexpr int NS = decltype(nsc)::value;
+                uint32_t sel[NS];
+                attn_selectors<S, BITS, NS>(y, q0, sel);
+#pragma unroll
+                for (int j = 0; j < NS; j += 2) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int k = 0; k < 2; k++) {
+                        const uint32_t up = split_index<BITS>(sel[j + k]);
+                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], up, hi + 2 * k);
+                        level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], up, lo + 2 * k);
+                    }
+                    *reinterpret_cast<u32x4 *>(dst + C::kHi + 8 * (q0 + j)) = u32x4{hi[0], hi[1], hi[2], hi[3]};
+                    *reinterpret_cast<u32x4 *>(dst + C::kLo + 8 * (q0 + j)) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+                }
+            };
+#pragma unroll
+            for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
+                part(std::integral_constant<int, 4>{}, q0);
+            if constexpr (S::NQ % 4 != 0)
+                part(std::integral_constant<int, 2>{}, S::NQ - 2);
+        }
+        {
+            // lane word 4 w + lane / 16 of the positions 4 p .. 4 p + 3, p = lane mod 16
+            const int p = lane & 15, v = 4 * w + (lane >> 4);
+            const uint32_t *raw = reinterpret_cast<const uint32_t *>(lds + C::kRawV) + 4 * p * C::RV;
+            // place of the positions 16 s + 8 b + 4 h in a row: [16 s][h][b]
+            uint8_t *dst = lds + C::kV + v * H::CL * C::VROW + 2 * (16 * (p >> 2) + 8 * (p & 1) + 4 * ((p >> 1) & 1));
+            auto part = [&](auto nc, int c0) {
+                constexpr int N = decltype(nc)::value;
+                uint32_t x[4], sel[N];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if constexpr (H::HALF)
+                        x[i] = reinterpret_cast<const uint16_t *>(raw + i * C::RV)[2 * c0 + v];
+                    else
+                        x[i] = raw[i * C::RV + 2 * c0 + v];
+                }
+                position_selectors<BITS, N>(x, sel);
+#pragma unroll
+                for (int c = 0; c < N; c++) {
+                    const uint32_t up = split_index<BITS>(sel[c]);
+                    uint32_t o[2];
+                    level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], up, o);
+                    *reinterpret_cast<u32x2 *>(dst + (c0 + c) * C::VROW) = u32x2{o[0], o[1]};
+                }
+            };
+#pragma unroll
+            for (int c0 = 0; c0 + 8 <= H::CL; c0 += 8)
+                part(std::integral_constant<int, 8>{}, c0);
+            if constexpr (H::CL % 8 != 0)
+                part(std::integral_constant<int, H::CL % 8>{}, H::CL / 8 * 8);
+        }
+        if (t + 1 < nt && w < 2) {
+            fetch(t + 1, next);
+            next = block_of(t + 2);
+        }
+        __syncthreads();
+
+        const int tb = t0 + 64 * t;
+        const uint32_t *tile = reinterpret_cast<const uint32_t *>(lds + C::kTile + 16 * (t & 1));
+        if (tb < lim_max) {   // (wave-uniform)
+            // 3. S^T of the wave's rows and the tile's positions; a step's keys
+            //    are read while the one before multiplies
+            f32x16 st[2];
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    st[k][e] = 0.f;
+            const uint8_t *key = lds + n32 * C::KROW + 16 * half;
+            u32x4 kh[2][2], kl[2][2];
+            auto read_keys = [&](int ks) {
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    kh[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kHi + 32 * k * C::KROW + 32 * ks);
+                    kl[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kLo + 32 * k * C::KROW + 32 * ks);
+                }
+            };
+            read_keys(0);
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ks++) {
+                if (ks + 1 < C::KS)
+                    read_keys(ks + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(ql[ks]), st[k], 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kl[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // 4. running maximum (in units of 1 / f1) and weights
+            const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
+            const uint32_t ok0 = tile[0], ok1 = tile[1];
+            const bool whole = (ok0 & ok1) == ~0u && tb + 64 <= lim_min;
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(norm + 32 * k + 8 * b);
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        st[k][4 * b + i] *= x[i];
+                }
+            if (!whole) {
+                // the lane's positions are 32 k + 8 b + i, 4 half further
+                const int left = lim - tb - 4 * half;
+                const uint32_t mask[2] = {ok0 >> (4 * half), ok1 >> (4 * half)};
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        const int pos = 8 * (e / 4) + e % 4;
+                        if (!(mask[k] & (1u << pos)) || left <= 32 * k + pos)
+                            st[k][e] = -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    top = fmaxf(top, st[k][e]);
+            {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                top = fmaxf(m, fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])));
+            }
+            const float ref = (top == -INFINITY ? 0.f : top) * f1;
+            const int u = __builtin_amdgcn_readfirstlane((int)tile[2]);
+            const float alpha = __builtin_amdgcn_exp2f(fmaf(m, f1, -ref));
+            const float scale = __builtin_amdgcn_ldexpf(alpha, now - u);
+            m = top;
+            now = u;
+            if (__builtin_amdgcn_ballot_w64(scale != 1.f) != 0) {
+#pragma unroll
+                for (int c = 0; c < C::CT; c++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        acc[c][e] *= scale;
+            }
+            float sum = 0.f;
+            u32x4 p[4];   // positions 16 s .. 16 s + 15: B's order
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(norm + 64 + 32 * k + 8 * b);
+                    float y[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(st[k][4 * b + i], f1, -ref));
+                        sum += e;
+                        y[i] = e * x[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        uint32_t o;
+                        asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(o) : "v"(y[2 * i]), "v"(y[2 * i + 1]));
+                        p[2 * k + b / 2][2 * (b % 2) + i] = o;
+                    }
+                }
+            l = fmaf(l, alpha, sum);
+            // 5. O^T += V^T P^T, likewise
+            const uint8_t *val = lds + C::kV + n32 * C::VROW + 16 * half;
+            u32x4 vv[2][C::CT];
+            auto read_values = [&](int k) {
+#pragma unroll
+                for (int c = 0; c < C::CT; c++)
+                    vv[k & 1][c] = *reinterpret_cast<const u32x4 *>(val + 32 * c * C::VROW + 32 * k);
+            };
+            read_values(0);
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (k + 1 < 4)
+                    read_values(k + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < C::CT; c++)
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(vv[k & 1][c]), as_halves(p[k]), acc[c], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (t + 1 < nt && w < 2)
+            store_raw(t + 1);
+        __syncthreads();
+    }
+
+    // 6. the row's part, for the join
+    {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    if (nonfinite(qmax) && lim > 0)
+        l = NAN;   // an infinity or NaN in the rotated query
+    if (!on)
+        return;
+    const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, now - 14);
+    float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 4 * half;
+#pragma unroll
+    for (int c = 0; c < C::CT; c++)
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+            if (D % 32 == 0 || 32 * c + 8 * b < D)
+                *reinterpret_cast<f32x4 *>(dst + 32 * c + 8 * b) =
+                    f32x4{acc[c][4 * b] * vs, acc[c][4 * b + 1] * vs, acc[c][4 * b + 2] * vs, acc[c][4 * b + 3] * vs};
+    if (half == 0) {
+        float *ml = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+        ml[0] = m == -INFINITY ? m : m * f1;
+        ml[1] = l;
+    }
+}
+
+}  // namespace
+}  // namespace isoq

@@ -42,22 +42,10 @@ __device__ __forceinline__ float row_max16(float v)
     return fmaxf(v, dpp_f<DPP_ROW_MIRROR>(v));
 }
 
-// The value of lane 16 c + i in x[c] of every lane 16 r + i.
-__device__ __forceinline__ void spread_rows(uint32_t v, uint32_t x[4])
-{
-    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    const auto b = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false);
-    const auto c = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
-    x[0] = b[0];
-    x[1] = b[1];
-    x[2] = c[0];
-    x[3] = c[1];
-}
-
 // Rotate the rows r0 .. r0 + n - 1 of a sequence's key head h (scale folded
-// in) into qt[n][D]; the largest magnitude of each to mx[8 r], an infinity or
+// in) into qt[n][QS]; the largest magnitude of each to mx[8 r], an infinity or
 // NaN among them.
-template <int VAR, int D>
+template <int VAR, int D, int QS = D>
 __device__ __forceinline__ void attn_rotate(const AttnArgs &a, const AttnSeq &sq, int h, int r0, int n, float *qt,
                                             uint32_t *mx)
 {
@@ -96,7 +84,7 @@ __device__ __forceinline__ void attn_rotate(const AttnArgs &a, const AttnSeq &sq
 #pragma unroll
         for (int k = 0; k < 8; k++) {
             const float v = y[k] * a.scale;
-            qt[r * D + 8 * l + k] = v;
+            qt[r * QS + 8 * l + k] = v;
             m = max(m, __float_as_uint(fabsf(v)));   // ordered as the magnitudes; NaN above all
         }
         atomicMax(mx + 8 * r, m);
@@ -169,9 +157,9 @@ struct AttnMShape {
     }
     static constexpr int half(int n, int g) { return n * (CL / 8) + g; }   // half-word of lane n's group g
     // LDS words: per row of the workgroup its digit rows, digit sums (8), then
-    // the rotated queries; per wave the staged records and w's digits
+    // the rotated queries; per wave the staged records w's digits and the norms
     static constexpr int row_words() { return 4 * S::ROWW + 8; }
-    static constexpr int wave_words() { return 64 * RS + NT * 256; }
+    static constexpr int wave_words() { return 64 * RS + NT * 256 + 128; }
     static constexpr int lds_words()
     {
         // the rotated queries are gone when the waves' parts are written, and
@@ -181,6 +169,62 @@ struct AttnMShape {
         return loop > merge ? loop : merge;
     }
 };
+
+// Selector words of the coordinates 0 .. n - 1 from byte planes: byte i of b[k]
+// is byte k of record part i (n * BITS bits each), byte i of sel[c] the index of
+// part i's coordinate c.
+template <int BITS, int N>
+__device__ __forceinline__ void plane_selectors(const uint32_t *b, uint32_t *sel)
+{
+    constexpr uint32_t mask = BITS == 2 ? 0x03030303u : BITS == 3 ? 0x07070707u : 0x0F0F0F0Fu;
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+        const int bit = c * BITS, k = bit >> 3, sh = bit & 7;
+        if (sh + BITS <= 8)
+            sel[c] = (sh ? b[k] >> sh : b[k]) & mask;
+        else   // (3 bits) across two bytes
+            sel[c] = bit_select(vector_const(sh == 6 ? 0x03030303u : 0x01010101u), b[k] >> sh, b[k + 1] << (8 - sh)) & mask;
+    }
+}
+
+// A chunk's 3-bit indices, 32 coordinates (three words of the chunk) at a time:
+// the four octets' bytes gathered into planes give eight selector words for 25
+// instructions, spreading an octet's bits over its own words 8 or 9 for two.
+// Word j of a block of 32: coordinates j, 8 + j, 16 + j, 24 + j.
+template <int BITS>
+constexpr bool attn_by_planes(int chunk, int quad) { return BITS == 3 && 4 * (quad / 8 * 8 + 8) <= chunk; }
+
+template <class S, int BITS, int NS>
+__device__ __forceinline__ void attn_selectors(const uint32_t *y, int q0, uint32_t *sel)
+{
+    if constexpr (BITS == 3) {
+        if (attn_by_planes<BITS>(S::CC, q0)) {
+            const uint32_t *w = y + q0 / 8 * 3;
+            const uint32_t b[3] = {
+                __builtin_amdgcn_perm(w[2], __builtin_amdgcn_perm(w[1], w[0], 0x0C060300u), 0x05020100u),
+                __builtin_amdgcn_perm(w[2], __builtin_amdgcn_perm(w[1], w[0], 0x0C070401u), 0x06020100u),
+                __builtin_amdgcn_perm(w[2], __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0502u), 0x07040100u)};
+            uint32_t all[8];
+            plane_selectors<3, 8>(b, all);
+#pragma unroll
+            for (int j = 0; j < NS; j++)
+                sel[j] = all[q0 % 8 + j];
+            return;
+        }
+    }
+    selectors<S, BITS, NS>(y, q0, sel);
+}
+
+// Chunk coordinate of byte b of quad q.
+template <class S, int BITS>
+__device__ __forceinline__ int attn_coord(int q, int b)
+{
+    if (attn_by_planes<BITS>(S::CC, q))
+        return q / 8 * 32 + 8 * b + q % 8;
+    if (BITS == 2 && 4 * (q / 4) + 4 <= S::CC / 4)
+        return 16 * (q / 4) + 4 * b + q % 4;
+    return 8 * (q / 2) + 2 * b + q % 2;
+}
 
 // Selector bytes of the four positions x[0..3] for the coordinates of a group:
 // `n` coordinates whose bits start at bit 0 of x; sel[c] byte i = index of
@@ -202,15 +246,7 @@ __device__ __forceinline__ void position_selectors(const uint32_t x[4], uint32_t
         if constexpr (PLANES > 3)
             b[3] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
     }
-    constexpr uint32_t mask = BITS == 2 ? 0x03030303u : BITS == 3 ? 0x07070707u : 0x0F0F0F0Fu;
-#pragma unroll
-    for (int c = 0; c < N; c++) {
-        const int bit = c * BITS, k = bit >> 3, sh = bit & 7;
-        if (sh + BITS <= 8)
-            sel[c] = (sh ? b[k] >> sh : b[k]) & mask;
-        else   // (3 bits) across two bytes
-            sel[c] = bit_select(vector_const(sh == 6 ? 0x03030303u : 0x01010101u), b[k] >> sh, b[k + 1] << (8 - sh)) & mask;
-    }
+    plane_selectors<BITS, N>(b, sel);
 }
 
 // Level digits of four selector bytes: tab holds 8 levels (2 and 3 bits) or 16.
@@ -256,6 +292,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     float *qt = reinterpret_cast<float *>(sums + ROWS * 8);          // [ROWS][D], before the waves' parts
     uint32_t *mine = reinterpret_cast<uint32_t *>(qt) + w * H::wave_words();
     uint32_t *wdig = mine + 64 * H::RS;
+    float *norms = reinterpret_cast<float *>(wdig + NT * 256);
 
     // 0. places, records and norms of the wave's positions, as in
     //    isoq_scores_m.h: the block-table entry two batches ahead, records one
@@ -287,15 +324,14 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         // present) and gets no weight
         return Place{ok ? blk : 0, ok ? (int)(tt - bi * a.block_size) : 0, ok};
     };
-    auto issue = [&](const Place &pl, const uint8_t *idx, const float *rho, Batch &k) {
-        const uint32_t blk = (uint32_t)pl.blk, pos = (uint32_t)pl.pos;
-        const uint8_t *pc0 = idx + row0 * RB + times(blk, bstride, 0) + (uint64_t)pos * S::CP;
-        const int64_t pstep = (int64_t)a.block_size * S::CP;
-        const uint64_t row = row0 + times(blk, rstride, pos);
+    const int64_t pstep = (int64_t)a.block_size * S::CP;
+    const uint8_t *const k_idx = a.k_idx + row0 * RB, *const v_idx = a.v_idx + row0 * RB;
+    const float *const k_rho = a.k_rho + row0, *const v_rho = a.v_rho + row0;
+    auto issue = [&](uint64_t at, uint64_t row, const uint8_t *idx, const float *rho, Batch &k) {
         if constexpr (S::LW == 4) {
 #pragma unroll
             for (int v = 0; v < S::RW / 4; v++) {
-                const u32x4 q4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(pc0 + v * pstep));
+                const u32x4 q4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(idx + v * pstep + at));
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
                     const uint32_t e = q4[c];
@@ -306,7 +342,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             static_assert(S::LW != 2 || S::CP == 8, "one load per piece");
 #pragma unroll
             for (int v = 0; v < S::RW / 2; v++) {
-                const u32x2 q2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(pc0 + v * pstep));
+                const u32x2 q2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(idx + v * pstep + at));
                 const uint32_t e0 = q2[0], e1 = q2[1];
                 k.w[2 * v] = e0;
                 k.w[2 * v + 1] = e1;
@@ -314,10 +350,11 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         } else if constexpr (S::LW == 1) {
 #pragma unroll
             for (int v = 0; v < S::RW; v++)
-                k.w[v] = reinterpret_cast<const uint32_t *>(pc0)[v];
+                k.w[v] = reinterpret_cast<const uint32_t *>(idx + at)[v];
         } else {
             // an odd number of half-words, stored whole (isoq_scores_m.h)
-            const bool odd = row & 1;
+            const bool odd = (row0 + row) & 1;
+            const uint8_t *pc0 = idx + at;
             const uint32_t *al = reinterpret_cast<const uint32_t *>(pc0 + (odd ? 2 : 0));
             const uint32_t half = *reinterpret_cast<const uint16_t *>(pc0 + (odd ? 0 : RB - 2));
             uint32_t r[S::RW - 1];
@@ -335,10 +372,15 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     const int nb = (tend - t0 + 255) / 256;   // (0 where no position is left)
     Batch k{}, v{};
     Place here{}, next{};
+    auto fetch = [&](const Place &pl) {
+        const uint64_t at = times(pl.blk, bstride, 0) + (uint64_t)((uint32_t)pl.pos * S::CP);
+        const uint64_t row = times(pl.blk, rstride, pl.pos);
+        issue(at, row, k_idx, k_rho, k);
+        issue(at, row, v_idx, v_rho, v);
+    };
     if (nb > 0) {
         here = place(0);
-        issue(here, a.k_idx, a.k_rho, k);
-        issue(here, a.v_idx, a.v_rho, v);
+        fetch(here);
         next = place(1);
     }
 
@@ -361,8 +403,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         int sum[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int b = 0; b < 4; b++) {
-            const bool full = BITS == 2 && 4 * (q / 4) + 4 <= S::CC / 4;
-            const int ci = full ? 16 * (q / 4) + 4 * b + q % 4 : 8 * (q / 2) + 2 * b + q % 2;
+            const int ci = attn_coord<S, BITS>(q, b);
             const int x = ci < S::CC ? to_fixed(qt[g * D + c * S::CC + ci], e) : 0;
             int d[4];
             if constexpr (BITS == 4) {
@@ -437,37 +478,35 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             }
             transpose_rows(y[0][i], y[1][i], y[2][i], y[3][i]);
         }
-        uint32_t krho[4], vrho[4];
-        spread_rows(__float_as_uint(k.rho), krho);
+        // the norms, to the lanes of their positions mod 16
+        norms[(lane & 15) * 4 + (lane >> 4)] = k.rho;
+        norms[64 + (lane & 15) * 4 + (lane >> 4)] = here.ok ? v.rho : 0.f;
         // the values' records as they are, for the second product
 #pragma unroll
         for (int i = 0; i < H::SW; i += 4)
             *reinterpret_cast<u32x4 *>(mine + lane * H::RS + i) =
                 u32x4{H::staged(v.w, i), H::staged(v.w, i + 1), H::staged(v.w, i + 2), H::staged(v.w, i + 3)};
-        // their norms, and the unit of w: 2^-30 of the tile's largest norm
-        const float vr = here.ok ? fabsf(v.rho) : 0.f;
-        float vmax = row_max16(vr);
-        {
-            uint32_t x[4];
-            spread_rows(__float_as_uint(vmax), x);
-            vmax = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
-                         fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
-        }
-        const int ve = __builtin_amdgcn_readfirstlane(head_exponent(vmax, 30));
-        spread_rows(__float_as_uint(here.ok ? __builtin_amdgcn_ldexpf(v.rho, ve) : 0.f), vrho);
-        // what the digit sums count: 2^-ve, the levels' scale, 256 (the
-        // lowest digit products are left out)
-        const float vunit = __builtin_amdgcn_ldexpf(a.v_dig.scale, -ve);
         __builtin_amdgcn_sched_barrier(0);
         if (b + 1 < nb) {
             here = next;
-            issue(here, a.k_idx, a.k_rho, k);
-            issue(here, a.v_idx, a.v_rho, v);
+            fetch(here);
             next = place(b + 2);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (ok_mask == 0)
             continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const f32x4 krho = *reinterpret_cast<const f32x4 *>(norms + 4 * col);
+        f32x4 vrho = *reinterpret_cast<const f32x4 *>(norms + 64 + 4 * col);
+        // the unit of w: 2^-30 of the tile's largest norm; what the digit sums
+        // count: that times the levels' scale
+        const float vmax = row_max16(fmaxf(fmaxf(fabsf(vrho[0]), fabsf(vrho[1])), fmaxf(fabsf(vrho[2]), fabsf(vrho[3]))));
+        const int ve = __builtin_amdgcn_readfirstlane(head_exponent(vmax, 30));
+        const float vunit = __builtin_amdgcn_ldexpf(a.v_dig.scale, 8 - ve);   // (sums of digits in units of 256)
+#pragma unroll
+        for (int st = 0; st < 4; st++)
+            vrho[st] = __builtin_amdgcn_ldexpf(vrho[st], ve);
 
         // 4. logits (in units of ln 2) of the lane's row and its four positions
         float val[NT][4];
@@ -482,7 +521,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             auto step = [&](auto nsc, int q0) {
                 constexpr int NS = decltype(nsc)::value;
                 uint32_t sel[NS], inv[NS], p[NS];
-                selectors<S, BITS, NS>(y[st], q0, sel);
+                attn_selectors<S, BITS, NS>(y[st], q0, sel);
                 if constexpr (BITS == 4) {
 #pragma unroll
                     for (int j = 0; j < NS; j++) {
@@ -517,7 +556,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 const int w2 = x[0][2] + x[1][1] + x[2][0];
                 const int w3 = x[0][3] + x[1][2] + x[2][1];
                 const float f = fmaf((float)w01, 65536.f, fmaf((float)w2, 256.f, (float)w3));
-                val[nt][st] = (f * f1[nt]) * (__uint_as_float(krho[st]) * f2[nt]);
+                val[nt][st] = (f * f1[nt]) * (krho[st] * f2[nt]);
             }
         }
         const bool whole = ok_mask == ~0ull && tb + 64 <= lim_min && n == ROWS;   // (uniform)
@@ -548,7 +587,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 sum += p;
                 // balanced digits: each byte of x + 128 (in the three lower
                 // places), less 128
-                const int x = (int)__builtin_rintf(p * __uint_as_float(vrho[st]));
+                const int x = (int)__builtin_rintf(p * vrho[st]);
                 u[st] = ((uint32_t)x + 0x00808080u) ^ 0x00808080u;
             }
             l[nt] = fmaf(l[nt], alpha[nt], sum);
@@ -619,11 +658,11 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                     if constexpr (VD == 2) {
                         const int hi = (x[1][3] << 8) + x[1][2] + x[0][3];
                         const int lo = ((x[1][1] + x[0][2]) << 8) + x[1][0] + x[0][1];
-                        f = fmaf((float)hi, 65536.f * 256.f, (float)lo * 256.f);
+                        f = fmaf((float)hi, 65536.f, (float)lo);
                     } else {
                         const int hi = (x[2][3] << 8) + x[2][2] + x[1][3];
                         const int lo = ((x[2][1] + x[1][2] + x[0][3]) << 8) + x[2][0] + x[1][1] + x[0][2];
-                        f = fmaf((float)hi, 65536.f * 65536.f, (float)lo * 65536.f);
+                        f = fmaf((float)hi, 65536.f, (float)lo) * 256.f;
                     }
                     acc[nt][c0 + j] = fmaf(f, vunit, acc[nt][c0 + j] * alpha[nt]);
                 }

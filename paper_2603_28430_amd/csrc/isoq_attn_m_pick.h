@@ -15,7 +15,7 @@ AttnKernel attn_m_entry(bool f16)
     const size_t lds = sizeof(uint32_t) * AttnMShape<D, BITS, NT>::lds_words();
     return {f16 ? reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 2>)
                 : reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 3>),
-            lds, 4 * NT};
+            lds, 4 * NT, false};
 }
 
 template <int D, int BITS>
@@ -41,7 +41,7 @@ AttnKernel attn_m_d(int d, int rows, bool f16)
     case 256: return attn_m_rows<256, BITS>(rows, f16);
     case 512: return attn_m_rows<512, BITS>(rows, f16);
     }
-    return {nullptr, 0, 0};
+    return {};
 }
 
 }  // namespace

@@ -25,6 +25,7 @@ struct isoq_params {
     int n_pass;                     // sets in all
     bool wide;                      // the logits need all sets and digit products
     isoq::ValueDigits vd[2];          // levels as digits for the weighted sums of attention (fp16, fp32 queries)
+    isoq::HalfLevels kh, vh;          // and in fp16, as keys' and as values' levels
 };
 
 struct isoq_sketch {

@@ -559,14 +559,17 @@ void build_value_digits(int bits, const float *levels, int digits, ValueDigits &
     const double big = std::frexp((double)levels[K - 1], &exp);
     if (!(big > 0))
         return;   // every level is zero as a float
+    double level[8];
+    for (int k = 0; k < K / 2; k++)
+        level[k] = std::ldexp((double)levels[K / 2 + k], -exp);
     const double top = digits == 2 ? 32639.0 : 8355711.0;   // 127 in every digit
-    const int tries = 4096;
+    const int tries = 1024;
     double best = INFINITY, scale = big / top;
     for (int i = 0; i < tries; i++) {
-        const double q = big / top * (1.0 + (double)i / tries);
+        const double q = big / top * (1.0 + (double)i / tries), inv = 1.0 / q;
         double sum = 0;
-        for (int k = K / 2; k < K; k++) {
-            const double u = std::ldexp((double)levels[k], -exp) / q, e = (u - std::nearbyint(u)) * q;
+        for (int k = 0; k < K / 2; k++) {
+            const double u = level[k] * inv, e = (u - std::nearbyint(u)) * q;
             sum += e * e;
         }
         if (sum < best) {
@@ -584,6 +587,63 @@ void build_value_digits(int bits, const float *levels, int digits, ValueDigits &
         }
     }
     for (int t = 0; t < digits; t++)
+        std::memcpy(out.tab[t], bytes[t], 16);
+    out.scale = (float)std::ldexp(scale, exp);
+}
+
+// fp16 bits of u, and back.
+static uint16_t to_half(double u)
+{
+    const _Float16 h = (_Float16)(float)u;
+    uint16_t bits;
+    std::memcpy(&bits, &h, 2);
+    return bits;
+}
+
+static double half_value(uint16_t bits)
+{
+    _Float16 h;
+    std::memcpy(&h, &bits, 2);
+    return (double)(float)h;
+}
+
+void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out)
+{
+    const int K = 1 << bits;
+    out = HalfLevels{};
+    int exp = 0;
+    const double big = std::frexp((double)levels[K - 1], &exp);
+    if (!(big > 0))
+        return;
+    double scale = 1.0;
+    if (!pair) {
+        double best = INFINITY;
+        for (int i = 0; i < 4096; i++) {
+            // the largest level becomes 1 .. 2
+            const double q = big / (1.0 + (double)i / 4096), inv = 1.0 / q;
+            double sum = 0;
+            for (int k = K / 2; k < K; k++) {
+                const double u = std::ldexp((double)levels[k], -exp) * inv, e = (u - half_value(to_half(u))) * q;
+                sum += e * e;
+            }
+            if (sum < best) {
+                best = sum;
+                scale = q;
+            }
+        }
+    }
+    uint8_t bytes[4][16] = {};
+    for (int k = 0; k < K; k++) {
+        const double u = std::ldexp((double)levels[k], -exp) / scale;
+        const uint16_t hi = to_half(u), lo = to_half(u - half_value(hi));
+        bytes[0][k] = (uint8_t)hi;
+        bytes[1][k] = (uint8_t)(hi >> 8);
+        if (pair) {
+            bytes[2][k] = (uint8_t)lo;
+            bytes[3][k] = (uint8_t)(lo >> 8);
+        }
+    }
+    for (int t = 0; t < 4; t++)
         std::memcpy(out.tab[t], bytes[t], 16);
     out.scale = (float)std::ldexp(scale, exp);
 }

@@ -130,6 +130,14 @@ struct ValueDigits {
     float scale;
 };
 
+// The codebook in fp16 for attention of many rows (isoq_attn_c.h): byte k of
+// tab[0] and tab[1] are the low and high byte of level k's fp16 value in units of
+// scale, of tab[2] and tab[3] those of the fp16 value of what is left (keys).
+struct HalfLevels {
+    uint32_t tab[4][4];
+    float scale;
+};
+
 // Attention logits against a paged cache of quantized keys (isoq_scores.h,
 // isoq_scores_generic.hip).
 struct SArgs {
@@ -366,6 +374,10 @@ bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> 
 // is searched for the least sum of squared errors over the levels; the largest
 // level's integer is at least half of what the digits hold.
 void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out);
+// The levels in fp16: in two parts (pair), in units of a power of two that
+// brings the largest to 0.5 .. 1; or in one, in units searched for the least sum
+// of squared errors (the largest level is 1 .. 2 then).
+void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out);
 // Lloyd-Max levels for N(0, sigma^2) (ascending, symmetrised).
 bool lloyd_levels(int bits, double sigma, int iters, double *levels);
 // Seeded raw draws (Philox4x32-10 + Box-Muller), layout of the public header.
