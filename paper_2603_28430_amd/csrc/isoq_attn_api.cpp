@@ -64,14 +64,14 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // Splits: as many as give so many workgroups (a compute unit holds 2 to 5 at
     // once; what is over evens out sequences of different lengths, and is not
     // wanted where there is one sequence, or where a split leaves its part of
-    // 128 rows in memory); none up to 1,024 positions, where a second launch
-    // takes longer than the four tiles a wave then has (one sequence of 700, 8 x 4
-    // heads: 12.1 us, with three splits 15.6).
+    // 128 rows in memory); none up to 768 positions, three tiles a wave (one
+    // sequence, 8 x 4 heads, on the GPU / with the host's calls: 700 positions 9.8 /
+    // 12.1 us with one split, 8.7 / 15.6 with three; 1,000: 12.4 / 12.4, 8.7 / 14.5).
     // (1 x 8 x 8 heads, 131,071 positions, 64 / 96 / 128 / 256 splits: 48 / 50 / 49 /
     // 53 us; 16 ragged sequences x 8 heads of up to 4,096, 3 / 4 / 6 splits: 52 / 45 /
     // 37 us; 8 x 32 heads, 32,768, 2 / 4 / 8 splits: 227 / 204 / 201 us.)
     const int64_t want = p.kern.parts ? 1024 : n_seqs == 1 ? 768 : 2048, blocks = p.groups * n_seqs;
-    const int64_t splits = p.max_pos <= 1024 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
+    const int64_t splits = p.max_pos <= 768 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
     p.chunk = (int)std::min<int64_t>(chunk, 0x7FFFFF00);

@@ -1,6 +1,8 @@
 // Attention over the paged quantized cache on the integer matrix cores (widths
 // of the tuned decoding kernels).
 //
+// A workgroup of four waves has 4 or 8 rows; its waves take 64 positions in turn.
+//
 // The logits are those of isoq_scores_m.h: rotated query and codebook as 8-bit
 // digits, products of digits summed exactly in int32 by v_mfma_i32_16x16x64_i8,
 // the level digits picked four at a time by v_perm_b32.  The sum of values is
@@ -91,40 +93,10 @@ __device__ __forceinline__ void attn_rotate(const AttnArgs &a, const AttnSeq &sq
     }
 }
 
-// Write one row's chunk of 8 coordinates of the sum of values, rotated back.
-template <int VAR, int D>
-__device__ __forceinline__ void attn_emit8(const AttnArgs &a, int64_t row, int h, int l, const float y[8])
-{
-    constexpr int LPQ = D / kCoordsPerLane, PL = kLanePL<VAR>;
-    const float *par = a.v_params + ((int64_t)(a.v_sets == 1 ? 0 : h) * LPQ + l) * PL;
-    float o[8];
-    if constexpr (VAR == VAR_BLOCK8) {
-#pragma unroll
-        for (int c = 0; c < 8; c++)
-            o[c] = 0.f;
-#pragma unroll
-        for (int r = 0; r < 8; r++) {
-            float P[8];
-            load_params<8>(par + 8 * r, P);
-#pragma unroll
-            for (int c = 0; c < 8; c++)
-                o[c] = fmaf(P[c], y[r], o[c]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    } else {
-        float P[PL];
-        load_params<PL>(par, P);
-        rotate_inverse<VAR>(P, y, o);
-    }
-    if (a.q_f16)
-        store_row_chunk<true>(static_cast<char *>(a.out) + row * D * 2 + l * 16, o);
-    else
-        store_row_chunk<false>(static_cast<char *>(a.out) + row * D * 4 + l * 32, o);
-}
-
 template <int D, int BITS, int NT>
 struct AttnMShape {
     using S = ScoreMShape<D, BITS, 0>;
+    static constexpr int WV = 4;                     // waves per workgroup
     static constexpr int ROWS = 4 * NT;              // rows per workgroup
     static constexpr int CL = D / 16;                // coordinates per lane of the second product
     // A record as staged in LDS: a lane's coordinates in groups of up to 8,
@@ -163,9 +135,9 @@ struct AttnMShape {
     static constexpr int lds_words()
     {
         // the rotated queries are gone when the waves' parts are written, and
-        // everything when the waves' sums are merged (4 x rows x D, m and l)
-        const int loop = ROWS * row_words() + (ROWS * D > 4 * wave_words() ? ROWS * D : 4 * wave_words());
-        const int merge = 4 * ROWS * D + 8 * ROWS;
+        // everything when the waves' sums are merged (waves x rows x D, m and l)
+        const int loop = ROWS * row_words() + (ROWS * D > WV * wave_words() ? ROWS * D : WV * wave_words());
+        const int merge = WV * ROWS * (D + 2);
         return loop > merge ? loop : merge;
     }
 };
@@ -263,6 +235,7 @@ template <int D, int BITS, int NT, int VD>
 __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 {
     using H = AttnMShape<D, BITS, NT>;
+    constexpr int WV = H::WV;
     using S = typename H::S;
     constexpr int64_t RB = (int64_t)D * BITS / 8;
     constexpr int QP = BITS == 4 ? 29 : 30;   // query integers below 2^QP (4 bits: digits of twice them)
@@ -279,12 +252,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     if (r0 >= total)   // (block-uniform, as every early return here)
         return;
     const int n = min(ROWS, total - r0);
-    // rows come in the tokens' order, so the last one attends to the most positions
-    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap), lim_min = sq.limit(r0 / a.group, a.cap);
     const int64_t t0l = (int64_t)blockIdx.y * a.chunk;
-    if (t0l >= lim_all && blockIdx.y > 0)
-        return;   // the join looks at the splits below a row's limit only
-    const int t0 = (int)t0l, tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+    const int t0 = (int)t0l;
 
     uint32_t *dig = smem;                                            // [ROWS][4][ROWW]
     int *sums = reinterpret_cast<int *>(dig + ROWS * 4 * S::ROWW);   // [ROWS][8]: 4 digit sums, largest magnitude
@@ -294,18 +263,44 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     uint32_t *wdig = mine + 64 * H::RS;
     float *norms = reinterpret_cast<float *>(wdig + NT * 256);
 
-    // 0. places, records and norms of the wave's positions, as in
-    //    isoq_scores_m.h: the block-table entry two batches ahead, records one
+    // 0. places of the wave's positions: what the block table says is loaded two
+    //    batches ahead, first of all, since the records' addresses wait for it
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
-    struct Place {
-        int32_t blk, pos;
-        bool ok;
+    const int tw = t0 + 64 * w + lane;
+    struct Entry {
+        int32_t blk, pos;   // cache block and position in it
     };
+    auto entry = [&](int b) {   // (positions past the last possible one: that one's)
+        const uint32_t tt = (uint32_t)min((int64_t)tw + 64 * WV * (int64_t)b, (int64_t)a.cap - 1);
+        const uint32_t bi = fast_div(tt, a.div_block);
+        return Entry{table[bi], (int)(tt - bi * a.block_size)};
+    };
+    Entry next{};
+    if (a.cap > 0)
+        next = entry(0);
+
+    // 1. rotated queries
+    for (int i = threadIdx.x; i < ROWS * 8; i += 64 * WV)
+        sums[i] = 0;
+    __syncthreads();
+    switch (a.variant) {
+    case VAR_FULL: attn_rotate<VAR_FULL, D>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_FAST: attn_rotate<VAR_FAST, D>(a, sq, h, r0, n, qt, mx); break;
+    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D>(a, sq, h, r0, n, qt, mx); break;
+    default: attn_rotate<VAR_BLOCK8, D>(a, sq, h, r0, n, qt, mx); break;
+    }
+    // the positions that the rows attend to: rows come in the tokens' order, so
+    // the last one attends to the most
+    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap), lim_min = sq.limit(r0 / a.group, a.cap);
+    if (t0l >= lim_all && blockIdx.y > 0)
+        return;   // the join looks at the splits below a row's limit only
+    const int tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+
+    // 2. records and norms of the first batch, as in isoq_scores_m.h
     struct Batch {
         uint32_t w[S::RW];
         float rho;
     };
-    const int tw = t0 + 64 * w + lane;
     const uint64_t rstride = (uint64_t)a.n_kv_heads * a.block_size, row0 = (uint64_t)h * a.block_size;
     const uint64_t bstride = rstride * RB;
     auto times = [](uint32_t blk, uint64_t stride, uint32_t add) {   // one multiply unless the stride needs 33 bits
@@ -313,16 +308,6 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         if (stride >> 32)
             o += (uint64_t)(blk * (uint32_t)(stride >> 32)) << 32;
         return o;
-    };
-    auto place = [&](int b) {
-        const int64_t tl = (int64_t)tw + 256 * (int64_t)b;
-        const uint32_t tt = (uint32_t)min(tl, (int64_t)tend - 1);
-        const uint32_t bi = fast_div(tt, a.div_block);
-        const int32_t blk = table[bi];
-        const bool ok = tl < tend && blk >= 0 && blk < a.n_blocks;
-        // an invalid position reads position 0 of the head in block 0 (always
-        // present) and gets no weight
-        return Place{ok ? blk : 0, ok ? (int)(tt - bi * a.block_size) : 0, ok};
     };
     const int64_t pstep = (int64_t)a.block_size * S::CP;
     const uint8_t *const k_idx = a.k_idx + row0 * RB, *const v_idx = a.v_idx + row0 * RB;
@@ -369,33 +354,26 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         }
         k.rho = rho[row];
     };
-    const int nb = (tend - t0 + 255) / 256;   // (0 where no position is left)
+    const int nb = (tend - t0 + 64 * WV - 1) / (64 * WV);   // (0 where no position is left)
     Batch k{}, v{};
-    Place here{}, next{};
-    auto fetch = [&](const Place &pl) {
-        const uint64_t at = times(pl.blk, bstride, 0) + (uint64_t)((uint32_t)pl.pos * S::CP);
-        const uint64_t row = times(pl.blk, rstride, pl.pos);
+    bool valid = false;   // of the lane's position of the batch at hand
+    auto fetch = [&](int b) {
+        valid = (int64_t)tw + 64 * WV * (int64_t)b < tend && next.blk >= 0 && next.blk < a.n_blocks;
+        // an invalid position reads position 0 of the head in block 0 (always
+        // present) and gets no weight
+        const uint32_t blk = valid ? (uint32_t)next.blk : 0u, pos = valid ? (uint32_t)next.pos : 0u;
+        const uint64_t at = times(blk, bstride, 0) + (uint64_t)(pos * S::CP);
+        const uint64_t row = times(blk, rstride, pos);
         issue(at, row, k_idx, k_rho, k);
         issue(at, row, v_idx, v_rho, v);
+        next = entry(b + 1);
     };
-    if (nb > 0) {
-        here = place(0);
-        fetch(here);
-        next = place(1);
-    }
+    if (nb > 0)
+        fetch(0);
 
-    // 1. rotated queries, 2. their digits, as in isoq_scores_m.h
-    for (int i = threadIdx.x; i < ROWS * 8; i += 256)
-        sums[i] = 0;
+    // 3. the queries' digits, as in isoq_scores_m.h
     __syncthreads();
-    switch (a.variant) {
-    case VAR_FULL: attn_rotate<VAR_FULL, D>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_FAST: attn_rotate<VAR_FAST, D>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D>(a, sq, h, r0, n, qt, mx); break;
-    default: attn_rotate<VAR_BLOCK8, D>(a, sq, h, r0, n, qt, mx); break;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n * 4 * S::NQ; i += 256) {
+    for (int i = threadIdx.x; i < n * 4 * S::NQ; i += 64 * WV) {
         const int g = i / (4 * S::NQ), cq = i - g * (4 * S::NQ);
         const int c = cq / S::NQ, q = cq - c * S::NQ;
         const int e = head_exponent(__uint_as_float(mx[8 * g]), QP);
@@ -460,9 +438,9 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     }
 
     for (int b = 0; b < nb; b++) {
-        const int tb = t0 + 256 * b + 64 * w;   // the wave's first position
-        const uint64_t ok_mask = __builtin_amdgcn_ballot_w64(here.ok);
-        // 3. the keys' records, chunk kq of key 16 r + col in y[r]
+        const int tb = t0 + 64 * WV * b + 64 * w;   // the wave's first position
+        const uint64_t ok_mask = __builtin_amdgcn_ballot_w64(valid);
+        // 4. the keys' records, chunk kq of key 16 r + col in y[r]
         uint32_t y[4][S::WC];
 #pragma unroll
         for (int i = 0; i < S::WC; i++) {
@@ -480,7 +458,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         }
         // the norms, to the lanes of their positions mod 16
         norms[(lane & 15) * 4 + (lane >> 4)] = k.rho;
-        norms[64 + (lane & 15) * 4 + (lane >> 4)] = here.ok ? v.rho : 0.f;
+        norms[64 + (lane & 15) * 4 + (lane >> 4)] = valid ? v.rho : 0.f;
         // the values' records as they are, for the second product
 #pragma unroll
         for (int i = 0; i < H::SW; i += 4)
@@ -488,9 +466,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 u32x4{H::staged(v.w, i), H::staged(v.w, i + 1), H::staged(v.w, i + 2), H::staged(v.w, i + 3)};
         __builtin_amdgcn_sched_barrier(0);
         if (b + 1 < nb) {
-            here = next;
-            fetch(here);
-            next = place(b + 2);
+            fetch(b + 1);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (ok_mask == 0)
@@ -508,7 +484,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         for (int st = 0; st < 4; st++)
             vrho[st] = __builtin_amdgcn_ldexpf(vrho[st], ve);
 
-        // 4. logits (in units of ln 2) of the lane's row and its four positions
+        // 5. logits (in units of ln 2) of the lane's row and its four positions
         float val[NT][4];
 #pragma unroll
         for (int st = 0; st < 4; st++) {
@@ -570,7 +546,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                     val[nt][st] = ok && tb + kk < lim[nt] ? val[nt][st] : -INFINITY;
             }
         }
-        // 5. running maximum, weights, and their digits to LDS
+        // 6. running maximum, weights, and their digits to LDS
         float alpha[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -612,7 +588,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 W[nt][c] = e;
             }
         }
-        // 6. sums of values, up to 8 of the lane's coordinates at a time
+        // 7. sums of values, up to 8 of the lane's coordinates at a time
         auto group = [&](auto nc, int c0) {
             constexpr int N = decltype(nc)::value;
             uint32_t sel[4][N];
@@ -677,7 +653,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         __builtin_amdgcn_wave_barrier();   // (the next batch's records and digits take this one's place)
     }
 
-    // 7. the four waves' m, l and sums, merged through LDS
+    // 8. the waves' m, l and sums, merged through LDS
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
         float x = l[nt];
@@ -689,8 +665,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             l[nt] = NAN;   // an infinity or NaN in the rotated query: no digits hold it
     }
     __syncthreads();
-    float *part = reinterpret_cast<float *>(smem);          // [4 waves][ROWS][D]
-    float *ml = part + 4 * ROWS * D;                        // [4 waves][ROWS][2]
+    float *part = reinterpret_cast<float *>(smem);          // [WV][ROWS][D]
+    float *ml = part + WV * ROWS * D;                       // [WV][ROWS][2]
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
         const int r = 4 * nt + kq;
@@ -702,53 +678,89 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             ml[(w * ROWS + r) * 2 + 1] = l[nt];
         }
     }
-    __syncthreads();
-    constexpr int LPQ = D / 8;
-    for (int e = threadIdx.x; e < n * LPQ; e += 256) {
-        const int r = e / LPQ, j = e - r * LPQ;
-        const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
-        const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
-        float top = -INFINITY, sum = 0.f, f[4], y[8];
+    // a lane's 8 coordinates of a row (at most one for each: ROWS D / 8 <= 256)
+    static_assert(ROWS * (D / 8) <= 256, "a chunk of 8 coordinates per lane");
+    const int e = threadIdx.x, r = e / (D / 8), j = e - r * (D / 8);
+    const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
+    const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
+    float top = -INFINITY, sum = 0.f, y[8];
+    auto merge = [&] {
 #pragma unroll
-        for (int x = 0; x < 4; x++)
+        for (int x = 0; x < WV; x++)
             top = fmaxf(top, ml[(x * ROWS + r) * 2]);
         const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int x = 0; x < 4; x++) {
-            f[x] = __builtin_amdgcn_exp2f(ml[(x * ROWS + r) * 2] - ref);
-            sum = fmaf(f[x], ml[(x * ROWS + r) * 2 + 1], sum);
-        }
-#pragma unroll
-        for (int c = 0; c < 8; c++) {
+        for (int c = 0; c < 8; c++)
             y[c] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 4; x++)
-                y[c] = fmaf(f[x], part[(x * ROWS + r) * D + 8 * j + c], y[c]);
-        }
-        if (a.n_splits > 1) {
-            float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 8 * j;
+#pragma unroll 4
+        for (int x = 0; x < WV; x++) {
+            const float f = __builtin_amdgcn_exp2f(ml[(x * ROWS + r) * 2] - ref);
+            sum = fmaf(f, ml[(x * ROWS + r) * 2 + 1], sum);
 #pragma unroll
             for (int c = 0; c < 8; c++)
-                dst[c] = y[c];
-            if (j == 0) {
-                float *to = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
-                to[0] = top;
-                to[1] = sum;
-            }
-            continue;
+                y[c] = fmaf(f, part[(x * ROWS + r) * D + 8 * j + c], y[c]);
         }
+    };
+    if (a.n_splits > 1) {
+        __syncthreads();
+        if (r >= n)
+            return;
+        merge();
+        float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 8 * j;
+#pragma unroll
+        for (int c = 0; c < 8; c++)
+            dst[c] = y[c];
+        if (j == 0) {
+            float *to = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+            to[0] = top;
+            to[1] = sum;
+        }
+        return;
+    }
+    // (the rotation's parameters are asked for before the waves wait for each other)
+    auto finish = [&](auto var) {
+        constexpr int VAR = decltype(var)::value;
+        constexpr int PL = VAR == VAR_BLOCK8 ? 8 : kLanePL<VAR>;
+        const float *par = a.v_params + ((int64_t)(a.v_sets == 1 ? 0 : h) * (D / 8) + j) * kLanePL<VAR>;
+        float P[PL];
+        if (r < n)
+            load_params<PL>(par, P);
+        __syncthreads();
+        if (r >= n)
+            return;
+        merge();
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        float o[8];
 #pragma unroll
         for (int c = 0; c < 8; c++)
             y[c] *= inv;
-        switch (a.variant) {
-        case VAR_FULL: attn_emit8<VAR_FULL, D>(a, row, h, j, y); break;
-        case VAR_FAST: attn_emit8<VAR_FAST, D>(a, row, h, j, y); break;
-        case VAR_PLANAR2D: attn_emit8<VAR_PLANAR2D, D>(a, row, h, j, y); break;
-        default: attn_emit8<VAR_BLOCK8, D>(a, row, h, j, y); break;
+        if constexpr (VAR == VAR_BLOCK8) {   // row by row
+#pragma unroll
+            for (int c = 0; c < 8; c++)
+                o[c] = 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; q++) {
+                if (q > 0)
+                    load_params<8>(par + 8 * q, P);
+#pragma unroll
+                for (int c = 0; c < 8; c++)
+                    o[c] = fmaf(P[c], y[q], o[c]);
+            }
+        } else {
+            rotate_inverse<VAR>(P, y, o);
         }
+        if (a.q_f16)
+            store_row_chunk<true>(static_cast<char *>(a.out) + row * D * 2 + j * 16, o);
+        else
+            store_row_chunk<false>(static_cast<char *>(a.out) + row * D * 4 + j * 32, o);
         if (j == 0 && a.lse)
             a.lse[row] = attn_lse(top, sum);
+    };
+    switch (a.variant) {
+    case VAR_FULL: finish(std::integral_constant<int, VAR_FULL>{}); break;
+    case VAR_FAST: finish(std::integral_constant<int, VAR_FAST>{}); break;
+    case VAR_PLANAR2D: finish(std::integral_constant<int, VAR_PLANAR2D>{}); break;
+    default: finish(std::integral_constant<int, VAR_BLOCK8>{}); break;
     }
 }
 
