@@ -50,13 +50,13 @@ struct AttnArgs {
 constexpr int kAttnMaxSplits = 256;
 
 // Width-generic kernel: one row per workgroup, grid (query head + n_q_heads
-// token, split, sequence).
+// token, sequence, split).
 const void *attn_generic_kernel_for(int variant, int bits);
 size_t attn_generic_lds(int slots, int variant);
 // Matrix-core kernel (isoq_attn_m.h; widths of the tuned decoding kernels) for
 // `rows` rows per sequence and key head: its entry, its dynamic LDS, and the
-// rows that a workgroup takes.  Grid (key head + n_kv_heads row tile, split,
-// sequence).
+// rows that a workgroup takes.  Grid (key head + n_kv_heads row tile,
+// sequence, split).
 struct AttnKernel {
     const void *fn;
     size_t lds;

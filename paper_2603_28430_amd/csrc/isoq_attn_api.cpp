@@ -61,16 +61,19 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         }
         p.groups = n_kv_heads * ((rows + p.kern.rows - 1) / p.kern.rows);
     }
-    // Splits: as many as give so many workgroups (a compute unit holds 2 to 5 at
-    // once; what is over evens out sequences of different lengths, and is not
-    // wanted where there is one sequence, or where a split leaves its part of
-    // 128 rows in memory); none up to 768 positions, three tiles a wave (one
-    // sequence, 8 x 4 heads, on the GPU / with the host's calls: 700 positions 9.8 /
-    // 12.1 us with one split, 8.7 / 15.6 with three; 1,000: 12.4 / 12.4, 8.7 / 14.5).
-    // (1 x 8 x 8 heads, 131,071 positions, 64 / 96 / 128 / 256 splits: 48 / 50 / 49 /
-    // 53 us; 16 ragged sequences x 8 heads of up to 4,096, 3 / 4 / 6 splits: 52 / 45 /
-    // 37 us; 8 x 32 heads, 32,768, 2 / 4 / 8 splits: 227 / 204 / 201 us.)
-    const int64_t want = p.kern.parts ? 1024 : n_seqs == 1 ? 768 : 2048, blocks = p.groups * n_seqs;
+    // Splits: as many as give so many workgroups, of which a compute unit holds two
+    // to four at once (two above d = 128): more than one round of them evens out
+    // sequences of different lengths, and is not wanted where there is one
+    // sequence, or where a split leaves its part of 128 rows in memory.  None up to
+    // 768 positions, three tiles a wave (one sequence, 8 x 4 heads, on the GPU / with
+    // the host's calls: 700 positions 9.8 / 12.1 us with one split, 8.7 / 15.6 with
+    // three; 1,000: 12.4 / 12.4, 8.7 / 14.5).
+    // (us at 512 / 768 / 1,024 / 1,536 / 2,048 wanted: 1 x 8 x 8 heads, 131,071
+    // positions 49 / 51 / 49 / 53 / 53; 8 x 32 x 32,768 231 / 210 / 203 / 202 / 208; 16
+    // ragged x 8 x 4 of up to 8,192 45 / 44 / 40 / 42 / 42, with 5 tokens of up to
+    // 4,096 51 / 50 / 44 / 40 / 41; 4 x 8 x 2, 8,190, d = 256 25 / 25 / 27 / 27 / 27; 512
+    // tokens 209 / 183 / 190 / 194 / 194.)
+    const int64_t want = p.kern.parts || n_seqs == 1 || pk->d > 128 ? 768 : 1536, blocks = p.groups * n_seqs;
     const int64_t splits = p.max_pos <= 768 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
@@ -250,7 +253,8 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
         if (e != hipSuccess)
             return hip_fail(e, "hipFuncSetAttribute");
     }
-    st = launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)plan.n_splits, (unsigned)n_seqs), 256, args, lds, stream);
+    // (splits last: those that some sequences do not reach come after those that all do)
+    st = launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)n_seqs, (unsigned)plan.n_splits), 256, args, lds, stream);
     if (st != ISOQ_OK || need == 0)
         return st;
     const bool few = plan.n_splits <= kAttnJoinFew;

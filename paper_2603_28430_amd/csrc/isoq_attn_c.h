@@ -63,25 +63,18 @@ struct AttnCShape {
 };
 
 // Four levels' fp16 values for four selector bytes: tables of the values' low
-// and high bytes.
+// and high bytes (4 bits: of the positive levels', whose sign bit is set where
+// `inv` says that the index is below 8).
 template <int BITS>
-__device__ __forceinline__ void level_halves(const uint32_t lo[4], const uint32_t hi[4], uint32_t sel, uint32_t upper,
+__device__ __forceinline__ void level_halves(const uint32_t lo[2], const uint32_t hi[2], uint32_t sel, uint32_t inv,
                                              uint32_t out[2])
 {
-    const uint32_t l = level_bytes<BITS>(lo, sel, upper), h = level_bytes<BITS>(hi, sel, upper);
+    const uint32_t l = __builtin_amdgcn_perm(lo[1], lo[0], sel);
+    uint32_t h = __builtin_amdgcn_perm(hi[1], hi[0], sel);
+    if constexpr (BITS == 4)
+        h = __builtin_amdgcn_bitop3_b32(h, inv, vector_const(0x80808080u), 0x78);   // h ^ (inv & 0x80)
     out[0] = __builtin_amdgcn_perm(h, l, 0x05010400u);
     out[1] = __builtin_amdgcn_perm(h, l, 0x07030602u);
-}
-
-// (4 bits) 0xFF where the index is 8 or more; the index mod 8.
-template <int BITS>
-__device__ __forceinline__ uint32_t split_index(uint32_t &sel)
-{
-    if constexpr (BITS < 4)
-        return 0u;
-    const uint32_t up = __builtin_amdgcn_perm(0u, 0u, 0x0C0C0C0Cu + ((sel >> 3) & 0x01010101u));
-    sel &= 0x07070707u;
-    return up;
 }
 
 __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
@@ -98,7 +91,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 
     const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads), rt = (int)(blockIdx.x / (uint32_t)a.n_kv_heads);
     const int h = (int)xcd_head((uint32_t)hx, (uint32_t)a.n_kv_heads, a.block_size * RB % 128 != 0);
-    const int s = blockIdx.z;
+    const int s = blockIdx.y;
     const int lane = threadIdx.x & 63, n32 = lane & 31, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnSeq sq = attn_seq(a, s);
@@ -107,8 +100,8 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
         return;
     const int n = min(C::ROWS, total - r0);
     const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap);
-    const int64_t t0l = (int64_t)blockIdx.y * a.chunk;
-    if (t0l >= lim_all && blockIdx.y > 0)
+    const int64_t t0l = (int64_t)blockIdx.z * a.chunk;
+    if (t0l >= lim_all && blockIdx.z > 0)
         return;   // the join looks at the splits below a row's limit only
     const int t0 = (int)t0l, tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
     const int nt = (tend - t0 + 63) / 64;
@@ -239,11 +232,11 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
     for (int i = threadIdx.x; i < 8 * C::ROWS; i += 256)
         mx[i] = 0;
     __syncthreads();
-    switch (a.variant) {
-    case VAR_FULL: attn_rotate<VAR_FULL, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_FAST: attn_rotate<VAR_FAST, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
-    default: attn_rotate<VAR_BLOCK8, D, C::QS>(a, sq, h, r0, n, qt, mx); break;
+    for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
+        const int q = i / (D / 8), c = i - q * (D / 8);
+        QueryChunk query;
+        attn_load_query<D>(a, sq, h, r0 + q, c, query);
+        attn_rotate_any<D>(a, h, c, query, qt + q * C::QS + 8 * c, mx + 8 * q);
     }
     __syncthreads();
     const uint32_t qmax = on ? mx[8 * r] : 0u;
@@ -303,9 +296,9 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                     uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
-                        const uint32_t up = split_index<BITS>(sel[j + k]);
-                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], up, hi + 2 * k);
-                        level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], up, lo + 2 * k);
+                        const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
+                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, hi + 2 * k);
+                        level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], inv, lo + 2 * k);
                     }
                     *reinterpret_cast<u32x4 *>(dst + C::kHi + 8 * (q0 + j)) = u32x4{hi[0], hi[1], hi[2], hi[3]};
                     *reinterpret_cast<u32x4 *>(dst + C::kLo + 8 * (q0 + j)) = u32x4{lo[0], lo[1], lo[2], lo[3]};
@@ -336,9 +329,9 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                 position_selectors<BITS, N>(x, sel);
 #pragma unroll
                 for (int c = 0; c < N; c++) {
-                    const uint32_t up = split_index<BITS>(sel[c]);
+                    const uint32_t inv = BITS == 4 ? magnitude(sel[c]) : 0u;
                     uint32_t o[2];
-                    level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], up, o);
+                    level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], inv, o);
                     *reinterpret_cast<u32x2 *>(dst + (c0 + c) * C::VROW) = u32x2{o[0], o[1]};
                 }
             };
@@ -497,7 +490,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
     if (!on)
         return;
     const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, now - 14);
-    float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 4 * half;
+    float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 4 * half;
 #pragma unroll
     for (int c = 0; c < C::CT; c++)
 #pragma unroll
@@ -506,7 +499,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                 *reinterpret_cast<f32x4 *>(dst + 32 * c + 8 * b) =
                     f32x4{acc[c][4 * b] * vs, acc[c][4 * b + 1] * vs, acc[c][4 * b + 2] * vs, acc[c][4 * b + 3] * vs};
     if (half == 0) {
-        float *ml = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+        float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
         ml[0] = m == -INFINITY ? m : m * f1;
         ml[1] = l;
     }

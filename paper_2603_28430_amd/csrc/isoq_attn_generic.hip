@@ -3,7 +3,7 @@
 // widths (and of codebooks with levels of very different sizes) that
 // isoq_attn_m.h does not take.  It is not tuned.
 //
-// Workgroup (row = query head of a token, split, sequence), 256 positions at a
+// Workgroup (row = query head of a token, sequence, split), 256 positions at a
 // time: each lane sums one key's logit over its record, slot by slot as the
 // generic stage-1 kernels write it (the query rotated once into LDS, zero
 // padded as in Sec. 5.1); then the lanes are dealt to the rotation slots of the
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     float *qt = gsm + 40 + 3 * 256;                           // T q scale, slots * SW
     float *sum = qt + a.slots * SW;                           // [256][SW] at the end
 
-    const int s = blockIdx.z, tid = threadIdx.x;
+    const int s = blockIdx.y, tid = threadIdx.x;
     const int i = blockIdx.x / a.n_q_heads, hq = blockIdx.x - i * a.n_q_heads;
     const int h = hq / a.group;
     const AttnSeq sq = attn_seq(a, s);
@@ -36,8 +36,8 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         return;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + hq;
     const int lim = sq.limit(i, a.cap);
-    const int64_t t0 = (int64_t)blockIdx.y * a.chunk;
-    if (t0 >= lim && blockIdx.y > 0)
+    const int64_t t0 = (int64_t)blockIdx.z * a.chunk;
+    if (t0 >= lim && blockIdx.z > 0)
         return;   // the join looks at the splits below lim only
     const int tend = (int)min(t0 + a.chunk, (int64_t)lim);
 
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
             y[c] *= inv;
         }
         if (a.n_splits > 1) {
-            float *dst = a.part + (row * a.n_splits + blockIdx.y) * a.width + SW * j;
+            float *dst = a.part + (row * a.n_splits + blockIdx.z) * a.width + SW * j;
 #pragma unroll
             for (int c = 0; c < SW; c++)
                 dst[c] = y[c];
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     }
     if (tid == 0) {
         if (a.n_splits > 1) {
-            float *ml = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+            float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
             ml[0] = m;
             ml[1] = l;
         } else if (a.lse) {

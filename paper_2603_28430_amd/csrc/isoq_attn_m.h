@@ -10,7 +10,8 @@
 //     sum_t w_t c[idx_tj],
 // w as a 31-bit integer cut into four digits (in units of 2^-30 of the largest
 // norm of the tile, p <= 1) and the levels as two digits (fp16 queries: a level
-// within 2^-16 of the largest) or three (fp32: 2^-24).
+// within 2^-16 of the largest) or three (fp32: 2^-24); at 4 bits the digits of
+// the eight magnitudes, complemented for the negative ones.
 //
 // Lane layout.  A tile is 64 positions of a wave and four rows (query heads of
 // new tokens that share the key head).  The logits' instruction has the rows'
@@ -35,61 +36,85 @@
 namespace isoq {
 namespace {
 
-// Bytes of a 16-lane row's maximum: every lane of the row gets it.
+// The largest of v and of the lane that a DPP control names, in one instruction:
+// left to itself, fmaxf of a moved value is a move, a second maximum that
+// quiets NaNs, and the maximum.  (The two wait states between writing a
+// register and reading it by DPP are the asm's own.)
+#define ISOQ_DPP_MAX(v, ctrl)                                                                      \
+    asm("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 " ctrl " row_mask:0xf bank_mask:0xf" : "+v"(v))
+
+// The largest of a 16-lane row, in every lane of it.
 __device__ __forceinline__ float row_max16(float v)
 {
-    v = fmaxf(v, dpp_f<DPP_QUAD_1032>(v));
-    v = fmaxf(v, dpp_f<DPP_QUAD_2301>(v));
-    v = fmaxf(v, dpp_f<DPP_ROW_HALF_MIRROR>(v));
-    return fmaxf(v, dpp_f<DPP_ROW_MIRROR>(v));
+    ISOQ_DPP_MAX(v, "quad_perm:[1,0,3,2]");
+    ISOQ_DPP_MAX(v, "quad_perm:[2,3,0,1]");
+    ISOQ_DPP_MAX(v, "row_half_mirror");
+    ISOQ_DPP_MAX(v, "row_mirror");
+    return v;
 }
 
-// Rotate the rows r0 .. r0 + n - 1 of a sequence's key head h (scale folded
-// in) into qt[n][QS]; the largest magnitude of each to mx[8 r], an infinity or
-// NaN among them.
-template <int VAR, int D, int QS = D>
-__device__ __forceinline__ void attn_rotate(const AttnArgs &a, const AttnSeq &sq, int h, int r0, int n, float *qt,
-                                            uint32_t *mx)
+// Eight coordinates of a query row, as loaded.
+struct QueryChunk {
+    Raw<true> half;
+    Raw<false> whole;
+};
+
+template <int D>
+__device__ __forceinline__ void attn_load_query(const AttnArgs &a, const AttnSeq &sq, int h, int r, int l, QueryChunk &q)
+{
+    const int i = r / a.group, g = r - i * a.group;
+    const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
+    if (a.q_f16)
+        load_row_chunk<true>(static_cast<const char *>(a.q) + row * D * 2 + l * 16, q.half);
+    else
+        load_row_chunk<false>(static_cast<const char *>(a.q) + row * D * 4 + l * 32, q.whole);
+}
+
+// Rotate chunk l of a query row of key head h (scale folded in) into qt[0 .. 7];
+// its largest magnitude, an infinity or NaN among them, to mx.
+template <int VAR, int D>
+__device__ __forceinline__ void attn_rotate(const AttnArgs &a, int h, int l, const QueryChunk &q, float *qt, uint32_t *mx)
 {
     constexpr int LPQ = D / kCoordsPerLane, PL = kLanePL<VAR>;
-    const int set = a.k_sets == 1 ? 0 : h;
-    for (int e = threadIdx.x; e < n * LPQ; e += 256) {
-        const int r = e / LPQ, l = e - r * LPQ;
-        const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
-        const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
-        float x[8], y[8], P[VAR == VAR_BLOCK8 ? 8 : PL];
-        if (a.q_f16) {
-            Raw<true> raw;
-            load_row_chunk<true>(static_cast<const char *>(a.q) + row * D * 2 + l * 16, raw);
-            unpack<true>(raw, x);
-        } else {
-            Raw<false> raw;
-            load_row_chunk<false>(static_cast<const char *>(a.q) + row * D * 4 + l * 32, raw);
-            unpack<false>(raw, x);
-        }
-        const float *par = a.k_params + ((int64_t)set * LPQ + l) * PL;
-        if constexpr (VAR == VAR_BLOCK8) {
+    float x[8], y[8], P[VAR == VAR_BLOCK8 ? 8 : PL];
+    if (a.q_f16)
+        unpack<true>(q.half, x);
+    else
+        unpack<false>(q.whole, x);
+    const float *par = a.k_params + ((int64_t)(a.k_sets == 1 ? 0 : h) * LPQ + l) * PL;
+    if constexpr (VAR == VAR_BLOCK8) {
 #pragma unroll
-            for (int q = 0; q < 8; q++) {   // row by row: all 64 parameters at once would set the kernel's registers
-                load_params<8>(par + 8 * q, P);
-                y[q] = P[0] * x[0];
+        for (int e = 0; e < 8; e++) {   // row by row: all 64 parameters at once would set the kernel's registers
+            load_params<8>(par + 8 * e, P);
+            y[e] = P[0] * x[0];
 #pragma unroll
-                for (int c = 1; c < 8; c++)
-                    y[q] = fmaf(P[c], x[c], y[q]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            load_params<PL>(par, P);
-            rotate_forward<VAR>(P, x, y);
+            for (int c = 1; c < 8; c++)
+                y[e] = fmaf(P[c], x[c], y[e]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        uint32_t m = 0;
+    } else {
+        load_params<PL>(par, P);
+        rotate_forward<VAR>(P, x, y);
+    }
+    uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const float v = y[k] * a.scale;
-            qt[r * QS + 8 * l + k] = v;
-            m = max(m, __float_as_uint(fabsf(v)));   // ordered as the magnitudes; NaN above all
-        }
-        atomicMax(mx + 8 * r, m);
+    for (int k = 0; k < 8; k++) {
+        const float v = y[k] * a.scale;
+        qt[k] = v;
+        m = max(m, __float_as_uint(fabsf(v)));   // ordered as the magnitudes; NaN above all
+    }
+    atomicMax(mx, m);
+}
+
+template <int D>
+__device__ __forceinline__ void attn_rotate_any(const AttnArgs &a, int h, int l, const QueryChunk &q, float *qt,
+                                                uint32_t *mx)
+{
+    switch (a.variant) {
+    case VAR_FULL: attn_rotate<VAR_FULL, D>(a, h, l, q, qt, mx); break;
+    case VAR_FAST: attn_rotate<VAR_FAST, D>(a, h, l, q, qt, mx); break;
+    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D>(a, h, l, q, qt, mx); break;
+    default: attn_rotate<VAR_BLOCK8, D>(a, h, l, q, qt, mx); break;
     }
 }
 
@@ -144,15 +169,17 @@ struct AttnMShape {
 
 // Selector words of the coordinates 0 .. n - 1 from byte planes: byte i of b[k]
 // is byte k of record part i (n * BITS bits each), byte i of sel[c] the index of
-// part i's coordinate c.
+// part i's coordinate c (4 bits: in its lower half; see magnitude).
 template <int BITS, int N>
 __device__ __forceinline__ void plane_selectors(const uint32_t *b, uint32_t *sel)
 {
-    constexpr uint32_t mask = BITS == 2 ? 0x03030303u : BITS == 3 ? 0x07070707u : 0x0F0F0F0Fu;
+    constexpr uint32_t mask = BITS == 2 ? 0x03030303u : 0x07070707u;
 #pragma unroll
     for (int c = 0; c < N; c++) {
         const int bit = c * BITS, k = bit >> 3, sh = bit & 7;
-        if (sh + BITS <= 8)
+        if (BITS == 4)
+            sel[c] = sh ? b[k] >> sh : b[k];
+        else if (sh + BITS <= 8)
             sel[c] = (sh ? b[k] >> sh : b[k]) & mask;
         else   // (3 bits) across two bytes
             sel[c] = bit_select(vector_const(sh == 6 ? 0x03030303u : 0x01010101u), b[k] >> sh, b[k + 1] << (8 - sh)) & mask;
@@ -184,7 +211,23 @@ __device__ __forceinline__ void attn_selectors(const uint32_t *y, int q0, uint32
             return;
         }
     }
+    if constexpr (BITS == 4) {   // a word holds 8 coordinates: its lower and its upper half-bytes
+#pragma unroll
+        for (int j = 0; j < NS; j++)
+            sel[j] = (q0 + j) % 2 ? y[(q0 + j) / 2] >> 4 : y[(q0 + j) / 2];
+        return;
+    }
     selectors<S, BITS, NS>(y, q0, sel);
+}
+
+// 4-bit indices in the lower half of each byte: 0xFF where the index is below 8,
+// and the index of the magnitude, 0 .. 7: index 8 + m has magnitude m, 7 - m is
+// its mirror image, whose digits are the complements.
+__device__ __forceinline__ uint32_t magnitude(uint32_t &sel)
+{
+    const uint32_t inv = __builtin_amdgcn_perm(0u, 0u, 0x0D0D0D0Du - ((sel >> 3) & 0x01010101u));
+    sel = __builtin_amdgcn_bitop3_b32(sel, inv, vector_const(0x07070707u), 0x28);   // (sel ^ inv) & 7
+    return inv;
 }
 
 // Chunk coordinate of byte b of quad q.
@@ -221,16 +264,6 @@ __device__ __forceinline__ void position_selectors(const uint32_t x[4], uint32_t
     plane_selectors<BITS, N>(b, sel);
 }
 
-// Level digits of four selector bytes: tab holds 8 levels (2 and 3 bits) or 16.
-template <int BITS>
-__device__ __forceinline__ uint32_t level_bytes(const uint32_t tab[4], uint32_t sel, uint32_t upper)
-{
-    if constexpr (BITS < 4)
-        return __builtin_amdgcn_perm(tab[1], tab[0], sel);
-    // sel: index mod 8; upper: 0xFF where the index is 8 or more
-    return bit_select(upper, __builtin_amdgcn_perm(tab[3], tab[2], sel), __builtin_amdgcn_perm(tab[1], tab[0], sel));
-}
-
 template <int D, int BITS, int NT, int VD>
 __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 {
@@ -244,7 +277,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 
     const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads), rt = (int)(blockIdx.x / (uint32_t)a.n_kv_heads);
     const int h = (int)xcd_head((uint32_t)hx, (uint32_t)a.n_kv_heads, a.block_size * RB % 128 != 0);
-    const int s = blockIdx.z;
+    const int s = blockIdx.y;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnSeq sq = attn_seq(a, s);
@@ -252,7 +285,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     if (r0 >= total)   // (block-uniform, as every early return here)
         return;
     const int n = min(ROWS, total - r0);
-    const int64_t t0l = (int64_t)blockIdx.y * a.chunk;
+    const int64_t t0l = (int64_t)blockIdx.z * a.chunk;
     const int t0 = (int)t0l;
 
     uint32_t *dig = smem;                                            // [ROWS][4][ROWW]
@@ -263,8 +296,15 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     uint32_t *wdig = mine + 64 * H::RS;
     float *norms = reinterpret_cast<float *>(wdig + NT * 256);
 
-    // 0. places of the wave's positions: what the block table says is loaded two
-    //    batches ahead, first of all, since the records' addresses wait for it
+    // 0. what does not wait for the lengths: the queries (a chunk of 8 coordinates
+    //    per lane), and the block table's entries for the wave's first positions
+    //    (later ones are loaded two batches ahead: the records' addresses wait
+    //    for them)
+    static_assert(ROWS * (D / 8) <= 256, "a chunk of 8 coordinates per lane");
+    const int cr = threadIdx.x / (D / 8), cl = threadIdx.x - cr * (D / 8);   // the lane's row and chunk
+    QueryChunk query;
+    if (cr < n)
+        attn_load_query<D>(a, sq, h, r0 + cr, cl, query);
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
     const int tw = t0 + 64 * w + lane;
     struct Entry {
@@ -278,23 +318,20 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     Entry next{};
     if (a.cap > 0)
         next = entry(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // the positions that the rows attend to: rows come in the tokens' order, so
+    // the last one attends to the most
+    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap), lim_min = sq.limit(r0 / a.group, a.cap);
+    if (t0l >= lim_all && blockIdx.z > 0)
+        return;   // the join looks at the splits below a row's limit only
+    const int tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
 
     // 1. rotated queries
     for (int i = threadIdx.x; i < ROWS * 8; i += 64 * WV)
         sums[i] = 0;
     __syncthreads();
-    switch (a.variant) {
-    case VAR_FULL: attn_rotate<VAR_FULL, D>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_FAST: attn_rotate<VAR_FAST, D>(a, sq, h, r0, n, qt, mx); break;
-    case VAR_PLANAR2D: attn_rotate<VAR_PLANAR2D, D>(a, sq, h, r0, n, qt, mx); break;
-    default: attn_rotate<VAR_BLOCK8, D>(a, sq, h, r0, n, qt, mx); break;
-    }
-    // the positions that the rows attend to: rows come in the tokens' order, so
-    // the last one attends to the most
-    const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap), lim_min = sq.limit(r0 / a.group, a.cap);
-    if (t0l >= lim_all && blockIdx.y > 0)
-        return;   // the join looks at the splits below a row's limit only
-    const int tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+    if (cr < n)
+        attn_rotate_any<D>(a, h, cl, query, qt + cr * D + 8 * cl, mx + 8 * cr);
 
     // 2. records and norms of the first batch, as in isoq_scores_m.h
     struct Batch {
@@ -408,7 +445,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     uint32_t A[NT][S::NQ];
     i32x4 asum[NT];
     float f1[NT], f2[NT];   // 2^-e (with the quantum) of the digits, in two factors
-    float m[NT], l[NT];     // running maximum and (the lane's part of the) sum of row 4 nt + kq
+    float m[NT], l[NT];     // running maximum and (the lane's part of the) sum of row 4 nt + kq,
+    float sw[NT];           // (4 bits) and of its weights p rho
     int lim[NT];
     float acc[NT][CL];
 #pragma unroll
@@ -431,7 +469,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             asum[nt] = *reinterpret_cast<const i32x4 *>(sums + 8 * gi);
         lim[nt] = gr < n ? sq.limit((r0 + gr) / a.group, a.cap) : 0;
         m[nt] = -INFINITY;
-        l[nt] = 0.f;
+        l[nt] = sw[nt] = 0.f;
 #pragma unroll
         for (int c = 0; c < CL; c++)
             acc[nt][c] = 0.f;
@@ -500,11 +538,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 attn_selectors<S, BITS, NS>(y[st], q0, sel);
                 if constexpr (BITS == 4) {
 #pragma unroll
-                    for (int j = 0; j < NS; j++) {
-                        const uint32_t neg = 0x0D0D0D0Du - ((sel[j] >> 3) & 0x01010101u);
-                        inv[j] = __builtin_amdgcn_perm(0u, 0u, neg);
-                        sel[j] = (sel[j] ^ inv[j]) & 0x07070707u;
-                    }
+                    for (int j = 0; j < NS; j++)
+                        inv[j] = magnitude(sel[j]);
                 }
 #pragma unroll
                 for (int t = 0; t < 3; t++) {
@@ -556,17 +591,21 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             alpha[nt] = __builtin_amdgcn_exp2f(m[nt] - ref);
             m[nt] = top;
             uint32_t u[4];
-            float sum = 0.f;
+            float sum = 0.f, wsum = 0.f;
 #pragma unroll
             for (int st = 0; st < 4; st++) {
                 const float p = __builtin_amdgcn_exp2f(val[nt][st] - ref);
                 sum += p;
                 // balanced digits: each byte of x + 128 (in the three lower
                 // places), less 128
-                const int x = (int)__builtin_rintf(p * vrho[st]);
+                const float weight = __builtin_rintf(p * vrho[st]);
+                wsum += weight;
+                const int x = (int)weight;
                 u[st] = ((uint32_t)x + 0x00808080u) ^ 0x00808080u;
             }
             l[nt] = fmaf(l[nt], alpha[nt], sum);
+            if constexpr (BITS == 4)
+                sw[nt] = fmaf(wsum, vunit, sw[nt] * alpha[nt]);
             const uint32_t a01 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), a23 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
             const uint32_t b01 = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), b23 = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
             uint32_t *dst = wdig + nt * 256 + lane;   // [digit][row][position mod 16]
@@ -607,13 +646,11 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             }
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                uint32_t up[4];
+                uint32_t inv[4];
                 if constexpr (BITS == 4) {
 #pragma unroll
-                    for (int c = 0; c < 4; c++) {
-                        up[c] = __builtin_amdgcn_perm(0u, 0u, 0x0C0C0C0Cu + ((sel[c][j] >> 3) & 0x01010101u));
-                        sel[c][j] &= 0x07070707u;
-                    }
+                    for (int c = 0; c < 4; c++)
+                        inv[c] = magnitude(sel[c][j]);
                 }
                 i32x4 d[NT][VD];
 #pragma unroll
@@ -621,7 +658,12 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                     uint32_t p[4];
 #pragma unroll
                     for (int c = 0; c < 4; c++)
-                        p[c] = level_bytes<BITS>(a.v_dig.tab[t], sel[c][j], BITS == 4 ? up[c] : 0u);
+                        p[c] = __builtin_amdgcn_perm(a.v_dig.tab[t][1], a.v_dig.tab[t][0], sel[c][j]);
+                    if constexpr (BITS == 4) {
+#pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            p[c] ^= inv[c];
+                    }
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
                         d[nt][t] = digit_mfma<4>(W[nt], p, i32x4{0, 0, 0, 0});
@@ -663,6 +705,19 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         l[nt] = x + dpp_f<DPP_ROW_MIRROR>(x);
         if (nonfinite(mx[8 * (4 * nt + kq)]) && lim[nt] > 0)
             l[nt] = NAN;   // an infinity or NaN in the rotated query: no digits hold it
+        if constexpr (BITS == 4) {
+            // the levels' half offset (build_value_digits), the same for every
+            // coordinate; vunit is in units of 256
+            float y = sw[nt];
+            y += dpp_f<DPP_QUAD_1032>(y);
+            y += dpp_f<DPP_QUAD_2301>(y);
+            y += dpp_f<DPP_ROW_HALF_MIRROR>(y);
+            y += dpp_f<DPP_ROW_MIRROR>(y);
+            y *= (VD == 2 ? 128.5f : 32896.5f) / 256.f;
+#pragma unroll
+            for (int c = 0; c < CL; c++)
+                acc[nt][c] += y;
+        }
     }
     __syncthreads();
     float *part = reinterpret_cast<float *>(smem);          // [WV][ROWS][D]
@@ -678,9 +733,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             ml[(w * ROWS + r) * 2 + 1] = l[nt];
         }
     }
-    // a lane's 8 coordinates of a row (at most one for each: ROWS D / 8 <= 256)
-    static_assert(ROWS * (D / 8) <= 256, "a chunk of 8 coordinates per lane");
-    const int e = threadIdx.x, r = e / (D / 8), j = e - r * (D / 8);
+    // the lane's 8 coordinates of a row again
+    const int r = (64 * w + lane) / (D / 8), j = (64 * w + lane) - r * (D / 8);
     const int i = (r0 + r) / a.group, g = r0 + r - i * a.group;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + g;
     float top = -INFINITY, sum = 0.f, y[8];
@@ -706,12 +760,12 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         if (r >= n)
             return;
         merge();
-        float *dst = a.part + (row * a.n_splits + blockIdx.y) * D + 8 * j;
+        float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 8 * j;
 #pragma unroll
         for (int c = 0; c < 8; c++)
             dst[c] = y[c];
         if (j == 0) {
-            float *to = a.part_ml + (row * a.n_splits + blockIdx.y) * 2;
+            float *to = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
             to[0] = top;
             to[1] = sum;
         }

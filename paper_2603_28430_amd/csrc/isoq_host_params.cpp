@@ -552,24 +552,25 @@ bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> 
 
 void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out)
 {
-    const int K = 1 << bits;
+    const int H = 1 << (bits - 1);
     out = ValueDigits{};
     // in units of a power of two that brings the largest level to 0.5 .. 1
     int exp = 0;
-    const double big = std::frexp((double)levels[K - 1], &exp);
+    const double big = std::frexp((double)levels[2 * H - 1], &exp);
     if (!(big > 0))
         return;   // every level is zero as a float
     double level[8];
-    for (int k = 0; k < K / 2; k++)
-        level[k] = std::ldexp((double)levels[K / 2 + k], -exp);
-    const double top = digits == 2 ? 32639.0 : 8355711.0;   // 127 in every digit
+    for (int k = 0; k < H; k++)
+        level[k] = std::ldexp((double)levels[H + k], -exp);
+    const double half = bits < 4 ? 0.0 : digits == 2 ? 128.5 : 32896.5;
+    const double top = (digits == 2 ? 32639.0 : 8355711.0) + half;   // 127 in every digit
     const int tries = 1024;
     double best = INFINITY, scale = big / top;
     for (int i = 0; i < tries; i++) {
         const double q = big / top * (1.0 + (double)i / tries), inv = 1.0 / q;
         double sum = 0;
-        for (int k = 0; k < K / 2; k++) {
-            const double u = level[k] * inv, e = (u - std::nearbyint(u)) * q;
+        for (int k = 0; k < H; k++) {
+            const double u = level[k] * inv - half, e = (u - std::nearbyint(u)) * q;
             sum += e * e;
         }
         if (sum < best) {
@@ -577,17 +578,21 @@ void build_value_digits(int bits, const float *levels, int digits, ValueDigits &
             scale = q;
         }
     }
-    uint8_t bytes[3][16] = {};
-    for (int k = 0; k < K; k++) {
-        long v = std::lrint(std::ldexp((double)levels[k], -exp) / scale);
-        for (int t = 0; t < digits; t++) {
-            const long d = ((v + 128) & 255) - 128;
-            bytes[t][k] = (uint8_t)(d & 255);
-            v = (v - d) / 256;
+    uint8_t bytes[3][8] = {};
+    for (int k = 0; k < H; k++) {
+        const long n = std::lrint(level[k] / scale - half);
+        for (int sign = 0; sign < (bits == 4 ? 1 : 2); sign++) {
+            long v = sign ? -n : n;
+            const int at = bits == 4 ? k : sign ? H - 1 - k : H + k;   // 4 bits: by magnitude
+            for (int t = 0; t < digits; t++) {
+                const long d = ((v + 128) & 255) - 128;
+                bytes[t][at] = (uint8_t)(d & 255);
+                v = (v - d) / 256;
+            }
         }
     }
     for (int t = 0; t < digits; t++)
-        std::memcpy(out.tab[t], bytes[t], 16);
+        std::memcpy(out.tab[t], bytes[t], 8);
     out.scale = (float)std::ldexp(scale, exp);
 }
 
@@ -632,19 +637,20 @@ void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out
             }
         }
     }
-    uint8_t bytes[4][16] = {};
-    for (int k = 0; k < K; k++) {
+    uint8_t bytes[4][8] = {};
+    for (int i = 0; i < 8 && i < K; i++) {
+        const int k = bits == 4 ? 8 + i : i;   // 4 bits: by magnitude
         const double u = std::ldexp((double)levels[k], -exp) / scale;
         const uint16_t hi = to_half(u), lo = to_half(u - half_value(hi));
-        bytes[0][k] = (uint8_t)hi;
-        bytes[1][k] = (uint8_t)(hi >> 8);
+        bytes[0][i] = (uint8_t)hi;
+        bytes[1][i] = (uint8_t)(hi >> 8);
         if (pair) {
-            bytes[2][k] = (uint8_t)lo;
-            bytes[3][k] = (uint8_t)(lo >> 8);
+            bytes[2][i] = (uint8_t)lo;
+            bytes[3][i] = (uint8_t)(lo >> 8);
         }
     }
     for (int t = 0; t < 4; t++)
-        std::memcpy(out.tab[t], bytes[t], 16);
+        std::memcpy(out.tab[t], bytes[t], 8);
     out.scale = (float)std::ldexp(scale, exp);
 }
 

@@ -124,17 +124,20 @@ struct LevelDigits {
 
 // The codebook as 8-bit digits for the weighted sums of attention (isoq_attn_m.h):
 // byte k of tab[t] is digit t (least significant first) of level k's integer,
-// n_k = d_0 + 256 d_1 (+ 65536 d_2), and scale n_k the level.
+// n_k = d_0 + 256 d_1 (+ 65536 d_2), and scale n_k the level.  At 4 bits of the
+// positive level of magnitude k, which is scale (n_k + half), half = (1 + 256 (+
+// 65536)) / 2: the complement of the digits then stands for its mirror image.
 struct ValueDigits {
-    uint32_t tab[3][4];
+    uint32_t tab[3][2];
     float scale;
 };
 
 // The codebook in fp16 for attention of many rows (isoq_attn_c.h): byte k of
 // tab[0] and tab[1] are the low and high byte of level k's fp16 value in units of
-// scale, of tab[2] and tab[3] those of the fp16 value of what is left (keys).
+// scale, of tab[2] and tab[3] those of the fp16 value of what is left (keys).  At
+// 4 bits of the positive level of magnitude k.
 struct HalfLevels {
-    uint32_t tab[4][4];
+    uint32_t tab[4][2];
     float scale;
 };
 
