@@ -401,6 +401,7 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
     p->lv = LevelDigits{};
     p->n_pass = 1;
     p->wide = false;
+    p->half_keys = false;
     p->lv_offset = 0;
     if (decode_d(d)) {
         std::vector<LevelDigits> lv;
@@ -411,8 +412,8 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             p->lv = lv[0];
             build_value_digits(bits, p->levels, 2, p->vd[0]);
             build_value_digits(bits, p->levels, 3, p->vd[1]);
-            build_half_levels(bits, p->levels, true, p->kh);
-            build_half_levels(bits, p->levels, false, p->vh);
+            p->half_keys = build_half_levels(bits, p->levels, false, p->vh) <= kHalfKeys;
+            build_half_levels(bits, p->levels, !p->half_keys, p->kh);
             p->n_pass = (int)lv.size();
             p->lv_offset = layout.size();
             const float *f = reinterpret_cast<const float *>(lv.data() + 1);

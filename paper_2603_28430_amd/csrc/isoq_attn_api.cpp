@@ -55,7 +55,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         // rows 74 us by digits, 80 us in fp16; 32: 82, 73; 64: 138, 87; 256: 464,
         // 177.  4 x 4 heads, 8,192, d = 64, 4 bits: 24 rows 27, 24; 64: 44, 27.)
         if (f16 && rows >= 32) {
-            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits);
+            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, pk->half_keys);
             if (many.fn)
                 p.kern = many;
         }
@@ -64,7 +64,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // Splits: as many as give so many workgroups, of which a compute unit holds two
     // to four at once (two above d = 128): more than one round of them evens out
     // sequences of different lengths, and is not wanted where there is one
-    // sequence, or where a split leaves its part of 128 rows in memory.  None up to
+    // sequence.  None up to
     // 768 positions, three tiles a wave (one sequence, 8 x 4 heads, on the GPU / with
     // the host's calls: 700 positions 9.8 / 12.1 us with one split, 8.7 / 15.6 with
     // three; 1,000: 12.4 / 12.4, 8.7 / 14.5).
@@ -72,8 +72,9 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // positions 49 / 51 / 49 / 53 / 53; 8 x 32 x 32,768 231 / 210 / 203 / 202 / 208; 16
     // ragged x 8 x 4 of up to 8,192 45 / 44 / 40 / 42 / 42, with 5 tokens of up to
     // 4,096 51 / 50 / 44 / 40 / 41; 4 x 8 x 2, 8,190, d = 256 25 / 25 / 27 / 27 / 27; 512
-    // tokens 209 / 183 / 190 / 194 / 194.)
-    const int64_t want = p.kern.parts || n_seqs == 1 || pk->d > 128 ? 768 : 1536, blocks = p.groups * n_seqs;
+    // tokens 209 / 183 / 190 / 194 / 194, and of two equal sequences of 8,192 315 / 350 /
+    // 333 / - / 364.)
+    const int64_t want = p.kern.parts ? 1024 : n_seqs == 1 || pk->d > 128 ? 768 : 1536, blocks = p.groups * n_seqs;
     const int64_t splits = p.max_pos <= 768 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);

@@ -5,18 +5,20 @@
 // rows per key head that decoding is what it spends its time on.  Here a
 // workgroup has 128 rows, decodes each tile once into LDS, and multiplies in
 // fp16 with fp32 sums:
-//   logits   both factors in two parts, x = hi + lo with hi = fp16(x) and lo =
-//            fp16(x - hi), three products (lo lo is left out): the rotated query
-//            row in units of a power of two that brings its largest coordinate
-//            to 8 .. 16, the codebook in units that bring its largest level to
-//            0.5 .. 1; what is left out is 2^-22 of a product, so that logits and
-//            lse keep fp32's accuracy;
-//   values   one product: w = p rho (p <= 1, in units of a power of two next to the
-//            tile's largest norm, up to 2^14) and the levels rounded to fp16 once,
-//            the levels in units for which they lie closest to fp16 numbers.  w's
-//            rounding, 2^-12 at most and of random sign from position to
-//            position, is like the output's own (fp16) rounding, not a sum of
-//            them; l sums the p before rounding, in fp32.
+//   logits   the rotated query in two parts, x = hi + lo with hi = fp16(x) and lo
+//            = fp16(x - hi), its row in units of a power of two that brings its
+//            largest coordinate to 8 .. 16; the levels likewise, and three products
+//            (lo lo is left out: 2^-22 of a product).  Levels that fp16 numbers
+//            hold to kHalfKeys of themselves in some unit (2-bit Lloyd-Max
+//            levels: 2^-21) are one part, and two products.  (3-bit levels in
+//            one part, off by up to 2^-15, would put lse off by 2e-6 to 3e-6 of
+//            its norm instead of 6e-8.)
+//   values   the weights w = p rho (p <= 1, in units of a power of two next to the
+//            tile's largest norm, up to 2^14) in two parts, the levels in one, in
+//            units for which they lie closest to fp16 numbers (off by 2e-7, 8e-6,
+//            7e-5 of the rows' root mean square at 2, 3, 4 bits): outputs are off
+//            by 2.1e-4 to 2.2e-4 of their norm, what rounding them to fp16 alone
+//            takes; w in one part 2.9e-4 to 3.2e-4.
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
@@ -39,7 +41,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int D, int BITS>
+template <int D, int BITS, bool LO>
 struct AttnCShape {
     using S = ScoreMShape<D, BITS, 0>;
     using H = AttnMShape<D, BITS, 1>;
@@ -52,7 +54,7 @@ struct AttnCShape {
     static constexpr int RV = H::SW + 1;             // words of a value's raw record
     // LDS bytes: keys hi, lo; values; raw records; per tile parity the norms
     // (K, V), the valid positions and the values' unit
-    static constexpr int kHi = 0, kLo = 64 * KROW, kV = 2 * 64 * KROW, kRawK = kV + 32 * CT * VROW,
+    static constexpr int kHi = 0, kLo = 64 * KROW, kV = (LO ? 2 : 1) * 64 * KROW, kRawK = kV + 32 * CT * VROW,
                          kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV, kTile = kNorm + 2 * 512;
     static constexpr int loop_bytes() { return kTile + 2 * 16; }
     // before the loop the rotated queries and their largest magnitudes
@@ -79,10 +81,10 @@ __device__ __forceinline__ void level_halves(const uint32_t lo[2], const uint32_
 
 __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
 
-template <int D, int BITS>
+template <int D, int BITS, bool LO>
 __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 {
-    using C = AttnCShape<D, BITS>;
+    using C = AttnCShape<D, BITS, LO>;
     using S = typename C::S;
     using H = typename C::H;
     constexpr int64_t RB = (int64_t)D * BITS / 8;
@@ -298,10 +300,12 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                     for (int k = 0; k < 2; k++) {
                         const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
                         level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, hi + 2 * k);
-                        level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], inv, lo + 2 * k);
+                        if constexpr (LO)
+                            level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], inv, lo + 2 * k);
                     }
                     *reinterpret_cast<u32x4 *>(dst + C::kHi + 8 * (q0 + j)) = u32x4{hi[0], hi[1], hi[2], hi[3]};
-                    *reinterpret_cast<u32x4 *>(dst + C::kLo + 8 * (q0 + j)) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+                    if constexpr (LO)
+                        *reinterpret_cast<u32x4 *>(dst + C::kLo + 8 * (q0 + j)) = u32x4{lo[0], lo[1], lo[2], lo[3]};
                 }
             };
 #pragma unroll
@@ -364,7 +368,8 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
                     kh[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kHi + 32 * k * C::KROW + 32 * ks);
-                    kl[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kLo + 32 * k * C::KROW + 32 * ks);
+                    if constexpr (LO)
+                        kl[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kLo + 32 * k * C::KROW + 32 * ks);
                 }
             };
             read_keys(0);
@@ -377,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                 for (int k = 0; k < 2; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(ql[ks]), st[k], 0, 0, 0);
 #pragma unroll
-                for (int k = 0; k < 2; k++)
+                for (int k = 0; k < 2 && LO; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kl[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
 #pragma unroll
                 for (int k = 0; k < 2; k++)
@@ -434,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                         acc[c][e] *= scale;
             }
             float sum = 0.f;
-            u32x4 p[4];   // positions 16 s .. 16 s + 15: B's order
+            u32x4 p[4], pl[4];   // positions 16 s .. 16 s + 15 (B's order), in two parts
 #pragma unroll
             for (int k = 0; k < 2; k++)
 #pragma unroll
@@ -449,9 +454,13 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                     }
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
+                        const int at = 2 * (b % 2) + i;
                         uint32_t o;
                         asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(o) : "v"(y[2 * i]), "v"(y[2 * i + 1]));
-                        p[2 * k + b / 2][2 * (b % 2) + i] = o;
+                        p[2 * k + b / 2][at] = o;
+                        const f16x2 r = __builtin_bit_cast(f16x2, o);
+                        asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(o) : "v"(y[2 * i] - (float)r.x), "v"(y[2 * i + 1] - (float)r.y));
+                        pl[2 * k + b / 2][at] = o;
                     }
                 }
             l = fmaf(l, alpha, sum);
@@ -469,6 +478,9 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                 if (k + 1 < 4)
                     read_values(k + 1);
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < C::CT; c++)
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(vv[k & 1][c]), as_halves(pl[k]), acc[c], 0, 0, 0);
 #pragma unroll
                 for (int c = 0; c < C::CT; c++)
                     acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(vv[k & 1][c]), as_halves(p[k]), acc[c], 0, 0, 0);

@@ -25,7 +25,8 @@ struct isoq_params {
     int n_pass;                     // sets in all
     bool wide;                      // the logits need all sets and digit products
     isoq::ValueDigits vd[2];          // levels as digits for the weighted sums of attention (fp16, fp32 queries)
-    isoq::HalfLevels kh, vh;          // and in fp16, as keys' and as values' levels
+    isoq::HalfLevels kh, vh;          // and in fp16, as keys' (two parts, unless half_keys) and as values' levels
+    bool half_keys;
 };
 
 struct isoq_sketch {

@@ -612,14 +612,14 @@ static double half_value(uint16_t bits)
     return (double)(float)h;
 }
 
-void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out)
+double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out)
 {
     const int K = 1 << bits;
     out = HalfLevels{};
     int exp = 0;
     const double big = std::frexp((double)levels[K - 1], &exp);
     if (!(big > 0))
-        return;
+        return 0.0;   // every level is zero as a float
     double scale = 1.0;
     if (!pair) {
         double best = INFINITY;
@@ -637,11 +637,14 @@ void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out
             }
         }
     }
+    double off = 0;
     uint8_t bytes[4][8] = {};
     for (int i = 0; i < 8 && i < K; i++) {
         const int k = bits == 4 ? 8 + i : i;   // 4 bits: by magnitude
         const double u = std::ldexp((double)levels[k], -exp) / scale;
         const uint16_t hi = to_half(u), lo = to_half(u - half_value(hi));
+        if (u != 0)
+            off = std::max(off, std::fabs((u - half_value(hi)) / u));
         bytes[0][i] = (uint8_t)hi;
         bytes[1][i] = (uint8_t)(hi >> 8);
         if (pair) {
@@ -652,6 +655,7 @@ void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out
     for (int t = 0; t < 4; t++)
         std::memcpy(out.tab[t], bytes[t], 8);
     out.scale = (float)std::ldexp(scale, exp);
+    return off;
 }
 
 bool build_magnitude_lut(int H, const double *tau, const double *lev, double *inv_h,

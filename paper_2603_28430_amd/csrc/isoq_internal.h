@@ -379,8 +379,11 @@ bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> 
 void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out);
 // The levels in fp16: in two parts (pair), in units of a power of two that
 // brings the largest to 0.5 .. 1; or in one, in units searched for the least sum
-// of squared errors (the largest level is 1 .. 2 then).
-void build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out);
+// of squared errors (the largest level is 1 .. 2 then).  Returns how far the
+// first part is off, at most, relative to a level.
+double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out);
+// Keys' levels in one fp16 part where it holds them to this (isoq_attn_c.h).
+constexpr double kHalfKeys = 0x1p-20;
 // Lloyd-Max levels for N(0, sigma^2) (ascending, symmetrised).
 bool lloyd_levels(int bits, double sigma, int iters, double *levels);
 // Seeded raw draws (Philox4x32-10 + Box-Muller), layout of the public header.
