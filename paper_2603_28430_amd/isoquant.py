@@ -278,6 +278,16 @@ def _placed(ref, ts):
             _device_tensors(ref, **{f"arg{i}": t for i, t in enumerate(ts)})
 
 
+def _on_current(ref, ts, stream):
+    """_placed, on the current device (where kernels are launched), which is the stream's too."""
+    _placed(ref, ts)
+    dev = ref.get_device()
+    if dev != _torch_module._C._cuda_getDevice():
+        raise ValueError(f"tensors on {ref.device}, which is not the current device")
+    if stream is not None and stream.device != ref.device:
+        raise ValueError(f"tensors on {ref.device}, stream on {stream.device}")
+
+
 def isoq_roundtrip(p: Params, x, rows_per_set: int = 1, x_hat=None, stream=None):
     """x_hat = stage-1 quantize->dequantize of x (same shape and dtype)."""
     n = _rows(x, p.d)
@@ -456,6 +466,17 @@ def isoq_kv_attn_workspace(pk: Params, pv: Params, dtype, n_tokens: int, max_q_l
                                           int(max_blocks_per_seq), int(max_len)))
 
 
+def _attn_buffers(q, out, lse, workspace, need):
+    torch = _torch_module
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    return out, lse, workspace
+
+
 def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, scale: float = 1.0,
                  q_start=None, max_q_len: int = 1, max_len=None, out=None, lse=None, workspace=None, stream=None):
     """Attention of new tokens' queries q [n_tokens, n_q_heads, d] over the paged
@@ -466,9 +487,9 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
     sequence s, at most max_q_len, which are its last positions (causal).
     Returns (out like q, lse fp32 [n_tokens, n_q_heads]); rows of no sequence
     are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
-    least isoq_kv_attn_workspace(...) bytes; by default one is allocated from
-    torch's pool on torch's current stream, so pass one where `stream` is
-    another."""
+    least isoq_kv_attn_workspace(...) bytes.  What is not passed (out, lse,
+    workspace) is allocated from torch's pool for `stream`, by default the
+    current one."""
     torch = _torch()
     if q.dim() != 3 or k_idx.dim() != 4 or k_rho.dim() != 3 or block_table.dim() != 2:
         raise ValueError("q [n_tokens, n_q_heads, d], k_idx [n_blocks, n_kv_heads, block_size, R], "
@@ -493,28 +514,23 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
             raise ValueError("without q_start there is one token a sequence")
     elif q_start.shape != (n_seqs + 1,) or q_start.dtype != torch.int32:
         raise ValueError("q_start must be int32 [n_seqs + 1]")
-    if out is None:
-        out = torch.empty_like(q)
-    elif out.shape != shape or out.dtype != q.dtype:
+    if out is not None and (out.shape != shape or out.dtype != q.dtype):
         raise ValueError("out must have q's shape and dtype")
-    if lse is None:
-        lse = torch.empty((n_tokens, n_q_heads), dtype=torch.float32, device=q.device)
-    elif lse.shape != shape[:2] or lse.dtype != torch.float32:
+    if lse is not None and (lse.shape != shape[:2] or lse.dtype != torch.float32):
         raise ValueError("lse must be fp32 [n_tokens, n_q_heads]")
     if max_len is None:
         max_len = max_blocks * block_size
     need = lib.isoq_kv_attn_workspace(pk.handle, pv.handle, code, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
                                       block_size, max_blocks, max_len)
-    tensors = (q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens, out, lse)
-    if q_start is not None:
-        tensors += (q_start,)
-    if workspace is not None:
-        if workspace.dtype != torch.uint8 or workspace.numel() < need:
-            raise ValueError(f"workspace must be uint8 of at least {need} bytes")
-        tensors += (workspace,)
-    _placed(q, tensors)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if workspace is not None and (workspace.dtype != torch.uint8 or workspace.numel() < need):
+        raise ValueError(f"workspace must be uint8 of at least {need} bytes")
+    tensors = (q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens)
+    _on_current(q, tensors + tuple(t for t in (q_start, out, lse, workspace) if t is not None), stream)
+    if stream is None:
+        out, lse, workspace = _attn_buffers(q, out, lse, workspace, need)
+    else:
+        with torch.cuda.stream(stream):
+            out, lse, workspace = _attn_buffers(q, out, lse, workspace, need)
     st = lib.isoq_kv_attn(pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs,
                           n_q_heads, n_kv_heads, k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(),
                           v_rho.data_ptr(), n_blocks, block_size, block_table.data_ptr(), max_blocks,
@@ -666,7 +682,7 @@ def isoq_kv_copy_blocks(pk: Params, block_pairs, k_idx, k_rho, v_idx=None, v_rho
     tensors = _cache_planes(pk, k_idx, k_rho, v_idx, v_rho, sketch, k_signs, k_gamma)
     if block_pairs.dim() != 2 or block_pairs.shape[1] != 2 or block_pairs.dtype != torch.int32:
         raise ValueError("block_pairs must be int32 [n_pairs, 2]")
-    _placed(k_idx, tensors + (block_pairs,))
+    _on_current(k_idx, tensors + (block_pairs,), stream)
     n_blocks, n_heads, block_size, _ = k_idx.shape
     st = lib.isoq_kv_copy_blocks(pk.handle, None if sketch is None else sketch.handle, block_pairs.data_ptr(),
                                  block_pairs.shape[0], n_heads, k_idx.data_ptr(), k_rho.data_ptr(), _ptr(v_idx),
@@ -691,7 +707,7 @@ def isoq_kv_compact(pk: Params, keep, n_keep, block_table, k_idx, k_rho, v_idx=N
         raise ValueError("n_keep [n_seqs] and block_table [n_seqs, max_blocks] need one row per sequence")
     if keep.dtype != torch.int32 or n_keep.dtype != torch.int32 or block_table.dtype != torch.int32:
         raise TypeError("keep, n_keep and block_table must be int32")
-    _placed(k_idx, tensors + (keep, n_keep, block_table))
+    _on_current(k_idx, tensors + (keep, n_keep, block_table), stream)
     st = lib.isoq_kv_compact(pk.handle, None if sketch is None else sketch.handle, keep.data_ptr(), keep_heads,
                              max_keep, n_keep.data_ptr(), n_seqs, block_table.data_ptr(), block_table.shape[1],
                              n_heads, k_idx.data_ptr(), k_rho.data_ptr(), _ptr(v_idx), _ptr(v_rho), _ptr(k_signs),

@@ -116,3 +116,25 @@ def test_page_calls_null_handles():
     assert binding.lib.isoq_kv_copy_blocks(None, None, None, 1, 1, None, None, None, None, None, None, 1, 16, None) == 3
     assert binding.lib.isoq_kv_compact(None, None, None, 1, 1, None, 1, None, 1, 1, None, None, None, None, None, None, 1,
                                        16, None) == 3
+
+
+def test_tensors_off_the_current_device(monkeypatch):
+    """Tensors, or a stream, on another device than the current one are refused (the stand-ins' device is -1)."""
+    monkeypatch.setattr(binding, "_is_gpu", lambda t: t.device.type == "cpu")
+    monkeypatch.setattr(binding, "lib", _NoPages(_NoLaunch(binding.lib)))
+    ok = good()
+    planes = {k: ok[k] for k in ("k_idx", "k_rho", "v_idx", "v_rho")}
+    calls = [lambda **kw: iq.isoq_kv_attn(**ok, **kw),
+             lambda **kw: iq.isoq_kv_copy_blocks(ok["pk"], torch.zeros((3, 2), dtype=torch.int32), **planes, **kw),
+             lambda **kw: iq.isoq_kv_compact(ok["pk"], torch.zeros((3, 1, 5), dtype=torch.int32),
+                                             torch.zeros(3, dtype=torch.int32), ok["block_table"], **planes, **kw)]
+
+    class Stream:
+        device, cuda_stream = torch.device("cuda:1"), 0
+    for call in calls:
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+        with pytest.raises(ValueError, match="not the current device"):
+            call()
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1)
+        with pytest.raises(ValueError, match="stream on cuda:1"):
+            call(stream=Stream())
