@@ -44,8 +44,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     const bool f16 = dtype == ISOQ_F16;
     const int64_t rows = (int64_t)(n_q_heads / n_kv_heads) * max_q_len;
     p.groups = (int64_t)n_q_heads * max_q_len;
-    // (wide codebooks: levels that one set of digits does not hold)
-    if (decode_d(pk->d) && !pk->wide && !pv->wide) {
+    if (pk->attn_tables && pv->attn_tables) {
         const int r = (int)std::min<int64_t>(rows, 1 << 20);
         p.kern = pk->bits == 2   ? attn_m_kernel_b2(pk->d, r, f16)
                  : pk->bits == 3 ? attn_m_kernel_b3(pk->d, r, f16)

@@ -27,6 +27,7 @@ struct isoq_params {
     isoq::ValueDigits vd[2];          // levels as digits for the weighted sums of attention (fp16, fp32 queries)
     isoq::HalfLevels kh, vh;          // and in fp16, as keys' (two parts, unless half_keys) and as values' levels
     bool half_keys;
+    bool attn_tables;                 // these tables serve (else attention decodes by the fp32 levels)
 };
 
 struct isoq_sketch {
