@@ -570,9 +570,11 @@ void build_value_digits(int bits, const float *levels, int digits, ValueDigits &
         const double q = big / top * (1.0 + (double)i / tries), inv = 1.0 / q;
         double sum = 0;
         for (int k = 0; k < H; k++) {
-            const double u = level[k] * inv - half, e = (u - std::nearbyint(u)) * q;
+            // (u below 2^24: the sum's last bit is one)
+            const double u = level[k] * inv - half, e = u - ((u + 0x1.8p52) - 0x1.8p52);
             sum += e * e;
         }
+        sum *= q * q;
         if (sum < best) {
             best = sum;
             scale = q;
@@ -638,12 +640,13 @@ double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &o
             level[k] = std::ldexp((double)levels[K / 2 + k], -exp);
         for (int i = 0; i < 4096; i++) {
             // the largest level becomes 1 .. 2
-            const double q = big / (1.0 + (double)i / 4096), inv = 1.0 / q;
+            const double inv = (1.0 + (double)i / 4096) / big, q = 1.0 / inv;
             double sum = 0;
             for (int k = 0; k < K / 2; k++) {
-                const double u = level[k] * inv, e = (u - round_half_bits(u)) * q;
+                const double u = level[k] * inv, e = u - round_half_bits(u);
                 sum += e * e;
             }
+            sum *= q * q;
             if (sum < best) {
                 best = sum;
                 scale = q;
