@@ -466,12 +466,12 @@ def isoq_kv_attn_workspace(pk: Params, pv: Params, dtype, n_tokens: int, max_q_l
                                           int(max_blocks_per_seq), int(max_len)))
 
 
-def _attn_buffers(q, out, lse, workspace, need):
+def _attn_buffers(q, rows, out, lse, workspace, need):
     torch = _torch_module
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = torch.empty(rows, dtype=torch.float32, device=q.device)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     return out, lse, workspace
@@ -516,7 +516,8 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
         raise ValueError("q_start must be int32 [n_seqs + 1]")
     if out is not None and (out.shape != shape or out.dtype != q.dtype):
         raise ValueError("out must have q's shape and dtype")
-    if lse is not None and (lse.shape != shape[:2] or lse.dtype != torch.float32):
+    rows = (n_tokens, n_q_heads)
+    if lse is not None and (lse.shape != rows or lse.dtype != torch.float32):
         raise ValueError("lse must be fp32 [n_tokens, n_q_heads]")
     if max_len is None:
         max_len = max_blocks * block_size
@@ -524,13 +525,16 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
                                       block_size, max_blocks, max_len)
     if workspace is not None and (workspace.dtype != torch.uint8 or workspace.numel() < need):
         raise ValueError(f"workspace must be uint8 of at least {need} bytes")
-    tensors = (q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens)
-    _on_current(q, tensors + tuple(t for t in (q_start, out, lse, workspace) if t is not None), stream)
+    tensors = [q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens]
+    for t in (q_start, out, lse, workspace):
+        if t is not None:
+            tensors.append(t)
+    _on_current(q, tensors, stream)
     if stream is None:
-        out, lse, workspace = _attn_buffers(q, out, lse, workspace, need)
+        out, lse, workspace = _attn_buffers(q, rows, out, lse, workspace, need)
     else:
         with torch.cuda.stream(stream):
-            out, lse, workspace = _attn_buffers(q, out, lse, workspace, need)
+            out, lse, workspace = _attn_buffers(q, rows, out, lse, workspace, need)
     st = lib.isoq_kv_attn(pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs,
                           n_q_heads, n_kv_heads, k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(),
                           v_rho.data_ptr(), n_blocks, block_size, block_table.data_ptr(), max_blocks,
