@@ -412,8 +412,7 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             p->lv = lv[0];
             build_value_digits(bits, p->levels, 2, p->vd[0]);
             build_value_digits(bits, p->levels, 3, p->vd[1]);
-            p->half_keys = build_half_levels(bits, p->levels, false, p->vh) <= kHalfKeys;
-            build_half_levels(bits, p->levels, !p->half_keys, p->kh);
+            p->half_keys = build_half_levels(bits, p->levels, p->half) <= kHalfKeys;
             // (a unit of 2^-23 of the largest level has to be a normal float, with room on both sides)
             const float top = p->levels[(1 << bits) - 1];
             p->attn_tables = !p->wide && top > 0x1p-96f && top < 0x1p96f;

@@ -7,18 +7,22 @@
 // fp16 with fp32 sums:
 //   logits   the rotated query in two parts, x = hi + lo with hi = fp16(x) and lo
 //            = fp16(x - hi), its row in units of a power of two that brings its
-//            largest coordinate to 8 .. 16; the levels likewise, and three products
-//            (lo lo is left out: 2^-22 of a product).  Levels that fp16 numbers
-//            hold to kHalfKeys of themselves in some unit (2-bit Lloyd-Max
-//            levels: 2^-21) are one part, and two products.  (3-bit levels in
-//            one part, off by up to 2^-15, would put lse off by 2e-6 to 3e-6 of
-//            its norm instead of 6e-8.)
+//            largest coordinate to 8 .. 16; the levels as fp16 numbers in units
+//            for which they lie closest to them (off by 2e-7, 1e-5, 7e-5 of their
+//            root mean square at 2, 3, 4 bits).  At 3 and 4 bits what that leaves
+//            of them is a third product, in e4m3 and with the query in e4m3, which
+//            rounds it to 2.6%: lse is off by 6e-8 of its norm at 2 and 3 bits and
+//            3e-7 at 4 (by 2e-6 to 3e-6 without it).
 //   values   the weights w = p rho (p <= 1, in units of a power of two next to the
-//            tile's largest norm, up to 2^14) in two parts, the levels in one, in
-//            units for which they lie closest to fp16 numbers (off by 2e-7, 8e-6,
-//            7e-5 of the rows' root mean square at 2, 3, 4 bits): outputs are off
-//            by 2.1e-4 to 2.2e-4 of their norm, what rounding them to fp16 alone
-//            takes; w in one part 2.9e-4 to 3.2e-4.
+//            tile's largest norm, up to 2^14) in fp16, the levels as above; what
+//            fp16 leaves of the weights is a second product, in e4m3 and with the
+//            levels in e4m3: outputs are off by 2.1e-4 to 2.2e-4 of their norm, what
+//            rounding them to fp16 alone takes; without it 2.9e-4 to 3.2e-4.
+// An e4m3 product is half a fp16 product's time, and the matrix cores' power is what
+// holds the kernel back (their clock falls to 1.9 GHz; taking a fifth of the vector
+// instructions out, or waits of waves for each other, changed nothing): with
+// both corrections in fp16, 2 x 512 tokens at 8,192 positions, 3 bits, took 383 us
+// instead of 361.  (The query's lo in e4m3 too: 340 us, and lse off by 1e-6 to 2e-6.)
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
@@ -40,6 +44,7 @@ namespace isoq {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 template <int D, int BITS, bool LO>
 struct AttnCShape {
@@ -48,20 +53,25 @@ struct AttnCShape {
     static constexpr int ROWS = 128;
     static constexpr int KS = S::NQ;                 // 16-coordinate steps of the logits' product (4 chunks of 4 NQ)
     static constexpr int KROW = 32 * KS + 16;        // bytes of a decoded key part
+    static constexpr int K8 = (KS + 3) / 4;          // 64-coordinate steps of its correction
+    static constexpr int KROW8 = LO ? 64 * K8 + 16 : 0;   // bytes of what fp16 left of a key's levels, in e4m3
     static constexpr int CT = (D + 31) / 32;         // 32-coordinate tiles of the values
     static constexpr int VROW = 2 * 64 + 16;         // bytes of a coordinate's 64 positions
+    static constexpr int VROW8 = 64 + 16;            // and in e4m3
     static constexpr int RK = 4 * S::WC + 1;         // words of a key's raw record (odd: lanes are keys)
     static constexpr int RV = H::SW + 1;             // words of a value's raw record
-    // LDS bytes: keys hi, lo; values; raw records; per tile parity the norms
-    // (K, V), the valid positions and the values' unit
-    static constexpr int kHi = 0, kLo = 64 * KROW, kV = (LO ? 2 : 1) * 64 * KROW, kRawK = kV + 32 * CT * VROW,
-                         kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV, kTile = kNorm + 2 * 512;
+    // LDS bytes: keys, and what fp16 left of them; values in fp16, e4m3; raw
+    // records; per tile parity the norms (K, V), the valid positions and the
+    // values' unit
+    static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROW8, kV8 = kV + 32 * CT * VROW,
+                         kRawK = kV8 + 32 * CT * VROW8, kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV,
+                         kTile = kNorm + 2 * 512;
     static constexpr int loop_bytes() { return kTile + 2 * 16; }
     // before the loop the rotated queries and their largest magnitudes
     static constexpr int QS = D + 1;
     static constexpr int query_bytes() { return 4 * ROWS * (QS + 8); }
     static constexpr int lds_bytes() { return loop_bytes() > query_bytes() ? loop_bytes() : query_bytes(); }
-    static_assert(kV % 16 == 0 && kRawK % 16 == 0 && kNorm % 16 == 0, "aligned parts");
+    static_assert(kRest % 16 == 0 && kV % 16 == 0 && kV8 % 16 == 0 && kRawK % 16 == 0 && kNorm % 16 == 0, "aligned parts");
 };
 
 // Four levels' fp16 values for four selector bytes: tables of the values' low
@@ -77,6 +87,26 @@ __device__ __forceinline__ void level_halves(const uint32_t lo[2], const uint32_
         h = __builtin_amdgcn_bitop3_b32(h, inv, vector_const(0x80808080u), 0x78);   // h ^ (inv & 0x80)
     out[0] = __builtin_amdgcn_perm(h, l, 0x05010400u);
     out[1] = __builtin_amdgcn_perm(h, l, 0x07030602u);
+}
+
+// Four levels' e4m3 values likewise.
+template <int BITS>
+__device__ __forceinline__ uint32_t level_bytes(const uint32_t tab[2], uint32_t sel, uint32_t inv)
+{
+    const uint32_t x = __builtin_amdgcn_perm(tab[1], tab[0], sel);
+    return BITS < 4 ? x : __builtin_amdgcn_bitop3_b32(x, inv, vector_const(0x80808080u), 0x78);   // x ^ (inv & 0x80)
+}
+
+// C + 2^exp A B^T, 32 x 32 x 64, e4m3
+__device__ __forceinline__ f32x16 mfma_bytes(i32x8 a, i32x8 b, f32x16 c, int exp)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 127 + exp, 0, 127);
+}
+
+__device__ __forceinline__ i32x8 read_bytes32(const uint8_t *src)
+{
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(src), y = *reinterpret_cast<const u32x4 *>(src + 16);
+    return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
 }
 
 __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
@@ -243,22 +273,39 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
     __syncthreads();
     const uint32_t qmax = on ? mx[8 * r] : 0u;
     const int qe = head_exponent(__uint_as_float(qmax), 4);
-    u32x4 qh[C::KS], ql[C::KS];
+    // coordinate j of a quad of the keys' order (places 4 quad .. + 3: quad NQ c + q
+    // is quad q of chunk c), in the row's units
+    auto query = [&](int quad, int j) {
+        const int c = quad / S::NQ, ci = attn_coord<S, BITS>(quad - c * S::NQ, j);
+        const float x = on && ci < S::CC ? __builtin_amdgcn_ldexpf(qt[r * C::QS + c * S::CC + ci], qe) : 0.f;
+        return nonfinite(qmax) ? 0.f : x;
+    };
+    u32x4 qh[C::KS], ql[C::KS];   // B of 16 places: 8 half + 0 .. 7
+    i32x8 q8[C::K8];              // in e4m3, of 64 places: 32 half + 0 .. 31
 #pragma unroll
     for (int st = 0; st < C::KS; st++) {
-        // places 16 st + 8 half + 0 .. 7 of the keys' order: quads 4 st + 2 half + 0, 1 of all chunks in turn
         f16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const int quad = 4 * st + 2 * half + e / 4, c = quad / S::NQ, q = quad - c * S::NQ;
-            const int ci = attn_coord<S, BITS>(q, e % 4);
-            const float x = on && ci < S::CC ? __builtin_amdgcn_ldexpf(qt[r * C::QS + c * S::CC + ci], qe) : 0.f;
-            const float v = nonfinite(qmax) ? 0.f : x;
+            const float v = query(4 * st + 2 * half + e / 4, e % 4);
             hi[e] = (_Float16)v;
             lo[e] = (_Float16)(v - (float)hi[e]);
         }
         qh[st] = __builtin_bit_cast(u32x4, hi);
         ql[st] = __builtin_bit_cast(u32x4, lo);
+    }
+    if constexpr (LO) {
+#pragma unroll
+        for (int st = 0; st < C::K8; st++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const int quad = 16 * st + 8 * half + e;
+                float x[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    x[j] = 16 * st + 16 <= 4 * C::KS || quad < 4 * C::KS ? query(quad, j) : 0.f;
+                q8[st][e] = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+            }
     }
     // a logit (in units of ln 2) is f1 times sum and norm
     const float f1 = fmaxf(__builtin_amdgcn_ldexpf(a.k_half.scale, -qe), 0x1p-126f);
@@ -275,6 +322,13 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
     if (D % 32 != 0) {   // coordinates past D: rows of zeros
         for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW / 4; i += 256)
             reinterpret_cast<uint32_t *>(lds + C::kV + D * C::VROW)[i] = 0u;
+        for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW8 / 4; i += 256)
+            reinterpret_cast<uint32_t *>(lds + C::kV8 + D * C::VROW8)[i] = 0u;
+    }
+    if (LO && C::KS % 4 != 0) {   // places past the keys'
+        constexpr int words = (64 * C::K8 - 16 * C::KS) / 4;
+        for (int i = threadIdx.x; i < 64 * words; i += 256)
+            reinterpret_cast<uint32_t *>(lds + C::kRest + (i / words) * C::KROW8 + 16 * C::KS)[i % words] = 0u;
     }
     if (nt > 0 && w < 2)
         store_raw(0);
@@ -288,24 +342,30 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 #pragma unroll
             for (int i = 0; i < S::WC; i++)
                 y[i] = src[i];
-            uint8_t *dst = lds + lane * C::KROW + w * 8 * S::NQ;
+            uint8_t *dst = lds + C::kHalf + lane * C::KROW + w * 8 * S::NQ;
+            uint8_t *rest = lds + C::kRest + lane * C::KROW8 + w * 4 * S::NQ;
             auto part = [&](auto nsc, int q0) {
                 constexpr int NS = decltype(nsc)::value;
-                uint32_t sel[NS];
+                uint32_t sel[NS], lo[NS];
                 attn_selectors<S, BITS, NS>(y, q0, sel);
 #pragma unroll
                 for (int j = 0; j < NS; j += 2) {
-                    uint32_t hi[4], lo[4];
+                    uint32_t x[4];
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
                         const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
-                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, hi + 2 * k);
+                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, x + 2 * k);
                         if constexpr (LO)
-                            level_halves<BITS>(a.k_half.tab[2], a.k_half.tab[3], sel[j + k], inv, lo + 2 * k);
+                            lo[j + k] = level_bytes<BITS>(a.k_half.tab[3], sel[j + k], inv);
                     }
-                    *reinterpret_cast<u32x4 *>(dst + C::kHi + 8 * (q0 + j)) = u32x4{hi[0], hi[1], hi[2], hi[3]};
-                    if constexpr (LO)
-                        *reinterpret_cast<u32x4 *>(dst + C::kLo + 8 * (q0 + j)) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+                    *reinterpret_cast<u32x4 *>(dst + 8 * (q0 + j)) = u32x4{x[0], x[1], x[2], x[3]};
+                }
+                if constexpr (LO && S::NQ % 4 == 0) {
+                    *reinterpret_cast<u32x4 *>(rest + 4 * q0) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+                } else if constexpr (LO) {
+#pragma unroll
+                    for (int j = 0; j < NS; j += 2)
+                        *reinterpret_cast<u32x2 *>(rest + 4 * (q0 + j)) = u32x2{lo[j], lo[j + 1]};
                 }
             };
 #pragma unroll
@@ -320,6 +380,8 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
             const uint32_t *raw = reinterpret_cast<const uint32_t *>(lds + C::kRawV) + 4 * p * C::RV;
             // place of the positions 16 s + 8 b + 4 h in a row: [16 s][h][b]
             uint8_t *dst = lds + C::kV + v * H::CL * C::VROW + 2 * (16 * (p >> 2) + 8 * (p & 1) + 4 * ((p >> 1) & 1));
+            // in e4m3, of the positions 32 k + 8 b + 4 h: [h][k][b]
+            uint8_t *dst8 = lds + C::kV8 + v * H::CL * C::VROW8 + 32 * (p & 1) + 16 * (p >> 3) + 4 * ((p >> 1) & 3);
             auto part = [&](auto nc, int c0) {
                 constexpr int N = decltype(nc)::value;
                 uint32_t x[4], sel[N];
@@ -337,6 +399,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                     uint32_t o[2];
                     level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], inv, o);
                     *reinterpret_cast<u32x2 *>(dst + (c0 + c) * C::VROW) = u32x2{o[0], o[1]};
+                    *reinterpret_cast<uint32_t *>(dst8 + (c0 + c) * C::VROW8) = level_bytes<BITS>(a.v_half.tab[2], sel[c], inv);
                 }
             };
 #pragma unroll
@@ -362,17 +425,30 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 16; e++)
                     st[k][e] = 0.f;
-            const uint8_t *key = lds + n32 * C::KROW + 16 * half;
-            u32x4 kh[2][2], kl[2][2];
+            const uint8_t *key = lds + C::kHalf + n32 * C::KROW + 16 * half;
+            const uint8_t *rest = lds + C::kRest + n32 * C::KROW8 + 32 * half;
+            u32x4 kh[2][2];
             auto read_keys = [&](int ks) {
 #pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    kh[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kHi + 32 * k * C::KROW + 32 * ks);
-                    if constexpr (LO)
-                        kl[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + C::kLo + 32 * k * C::KROW + 32 * ks);
-                }
+                for (int k = 0; k < 2; k++)
+                    kh[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + 32 * k * C::KROW + 32 * ks);
             };
-            read_keys(0);
+            if constexpr (LO) {
+                i32x8 lo[2];
+                lo[0] = read_bytes32(rest);
+#pragma unroll
+                for (int i = 0; i < 2 * C::K8; i++) {   // step i / 2, positions 32 (i mod 2) ..
+                    if (i + 1 < 2 * C::K8)
+                        lo[(i + 1) & 1] = read_bytes32(rest + 32 * ((i + 1) & 1) * C::KROW8 + 64 * ((i + 1) / 2));
+                    else
+                        read_keys(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    st[i & 1] = mfma_bytes(lo[i & 1], q8[i / 2], st[i & 1], -kLevelRest);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                read_keys(0);
+            }
 #pragma unroll
             for (int ks = 0; ks < C::KS; ks++) {
                 if (ks + 1 < C::KS)
@@ -381,9 +457,6 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
 #pragma unroll
                 for (int k = 0; k < 2; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(ql[ks]), st[k], 0, 0, 0);
-#pragma unroll
-                for (int k = 0; k < 2 && LO; k++)
-                    st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kl[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
 #pragma unroll
                 for (int k = 0; k < 2; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
@@ -439,7 +512,8 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                         acc[c][e] *= scale;
             }
             float sum = 0.f;
-            u32x4 p[4], pl[4];   // positions 16 s .. 16 s + 15 (B's order), in two parts
+            u32x4 p[4];   // positions 16 s .. 16 s + 15 (B's order)
+            i32x8 pr;     // of all 64, what fp16 left
 #pragma unroll
             for (int k = 0; k < 2; k++)
 #pragma unroll
@@ -459,28 +533,38 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                         asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(o) : "v"(y[2 * i]), "v"(y[2 * i + 1]));
                         p[2 * k + b / 2][at] = o;
                         const f16x2 r = __builtin_bit_cast(f16x2, o);
-                        asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(o) : "v"(y[2 * i] - (float)r.x), "v"(y[2 * i + 1] - (float)r.y));
-                        pl[2 * k + b / 2][at] = o;
+                        y[2 * i] -= (float)r.x;
+                        y[2 * i + 1] -= (float)r.y;
                     }
+                    pr[4 * k + b] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
                 }
             l = fmaf(l, alpha, sum);
             // 5. O^T += V^T P^T, likewise
             const uint8_t *val = lds + C::kV + n32 * C::VROW + 16 * half;
+            const uint8_t *val8 = lds + C::kV8 + n32 * C::VROW8 + 32 * half;
             u32x4 vv[2][C::CT];
+            i32x8 v8[2];
+            v8[0] = read_bytes32(val8);
             auto read_values = [&](int k) {
 #pragma unroll
                 for (int c = 0; c < C::CT; c++)
                     vv[k & 1][c] = *reinterpret_cast<const u32x4 *>(val + 32 * c * C::VROW + 32 * k);
             };
-            read_values(0);
+#pragma unroll
+            for (int c = 0; c < C::CT; c++) {
+                if (c + 1 < C::CT)
+                    v8[(c + 1) & 1] = read_bytes32(val8 + 32 * (c + 1) * C::VROW8);
+                else
+                    read_values(0);
+                __builtin_amdgcn_sched_barrier(0);
+                acc[c] = mfma_bytes(v8[c & 1], pr, acc[c], 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int k = 0; k < 4; k++) {
                 if (k + 1 < 4)
                     read_values(k + 1);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int c = 0; c < C::CT; c++)
-                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(vv[k & 1][c]), as_halves(pl[k]), acc[c], 0, 0, 0);
 #pragma unroll
                 for (int c = 0; c < C::CT; c++)
                     acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(vv[k & 1][c]), as_halves(p[k]), acc[c], 0, 0, 0);

@@ -614,6 +614,17 @@ static double half_value(uint16_t bits)
     return (double)(float)h;
 }
 
+// e4m3 bits of u, |u| below 448: 4 bits of significand, steps of 2^-9 at least.
+static uint8_t to_e4m3(double u)
+{
+    int e = 0;
+    std::frexp(u, &e);
+    const int step = std::max(e - 4, -9);
+    const double n = std::nearbyint(std::ldexp(std::fabs(u), -step));   // 0 .. 16
+    const int bits = n < 8 ? (int)n : n < 16 ? ((step + 10) << 3) + (int)n - 8 : (step + 11) << 3;
+    return (uint8_t)(bits | (std::signbit(u) && n > 0 ? 0x80 : 0));
+}
+
 // u > 0 rounded to fp16's 11 bits (a search over units does this tens of
 // thousands of times, in 4 ns instead of the conversions' 18).
 static double round_half_bits(double u)
@@ -625,7 +636,7 @@ static double round_half_bits(double u)
     return u;
 }
 
-double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out)
+double build_half_levels(int bits, const float *levels, HalfLevels &out)
 {
     const int K = 1 << bits;
     out = HalfLevels{};
@@ -633,24 +644,21 @@ double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &o
     const double big = std::frexp((double)levels[K - 1], &exp);
     if (!(big > 0))
         return 0.0;   // every level is zero as a float
-    double scale = 1.0;
-    if (!pair) {
-        double best = INFINITY, level[8];
-        for (int k = 0; k < K / 2; k++)
-            level[k] = std::ldexp((double)levels[K / 2 + k], -exp);
-        for (int i = 0; i < 4096; i++) {
-            // the largest level becomes 1 .. 2
-            const double inv = (1.0 + (double)i / 4096) / big, q = 1.0 / inv;
-            double sum = 0;
-            for (int k = 0; k < K / 2; k++) {
-                const double u = level[k] * inv, e = u - round_half_bits(u);
-                sum += e * e;
-            }
-            sum *= q * q;
-            if (sum < best) {
-                best = sum;
-                scale = q;
-            }
+    double scale = 1.0, best = INFINITY, level[8];
+    for (int k = 0; k < K / 2; k++)
+        level[k] = std::ldexp((double)levels[K / 2 + k], -exp);
+    for (int i = 0; i < 4096; i++) {
+        // the largest level becomes 1 .. 2
+        const double inv = (1.0 + (double)i / 4096) / big, q = 1.0 / inv;
+        double sum = 0;
+        for (int k = 0; k < K / 2; k++) {
+            const double u = level[k] * inv, e = u - round_half_bits(u);
+            sum += e * e;
+        }
+        sum *= q * q;
+        if (sum < best) {
+            best = sum;
+            scale = q;
         }
     }
     double off = 0;
@@ -658,15 +666,14 @@ double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &o
     for (int i = 0; i < 8 && i < K; i++) {
         const int k = bits == 4 ? 8 + i : i;   // 4 bits: by magnitude
         const double u = std::ldexp((double)levels[k], -exp) / scale;
-        const uint16_t hi = to_half(u), lo = to_half(u - half_value(hi));
+        const uint16_t hi = to_half(u);
+        const double rest = u - half_value(hi);
         if (u != 0)
-            off = std::max(off, std::fabs((u - half_value(hi)) / u));
+            off = std::max(off, std::fabs(rest / u));
         bytes[0][i] = (uint8_t)hi;
         bytes[1][i] = (uint8_t)(hi >> 8);
-        if (pair) {
-            bytes[2][i] = (uint8_t)lo;
-            bytes[3][i] = (uint8_t)(lo >> 8);
-        }
+        bytes[2][i] = to_e4m3(u);
+        bytes[3][i] = to_e4m3(std::ldexp(rest, kLevelRest));
     }
     for (int t = 0; t < 4; t++)
         std::memcpy(out.tab[t], bytes[t], 8);

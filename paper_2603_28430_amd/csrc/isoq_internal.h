@@ -134,8 +134,8 @@ struct ValueDigits {
 
 // The codebook in fp16 for attention of many rows (isoq_attn_c.h): byte k of
 // tab[0] and tab[1] are the low and high byte of level k's fp16 value in units of
-// scale, of tab[2] and tab[3] those of the fp16 value of what is left (keys).  At
-// 4 bits of the positive level of magnitude k.
+// scale, of tab[2] its e4m3 value, and of tab[3] that of 2^kLevelRest times what
+// fp16 leaves of it.  At 4 bits of the positive level of magnitude k.
 struct HalfLevels {
     uint32_t tab[4][2];
     float scale;
@@ -377,13 +377,14 @@ bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> 
 // is searched for the least sum of squared errors over the levels; the largest
 // level's integer is at least half of what the digits hold.
 void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out);
-// The levels in fp16: in two parts (pair), in units of a power of two that
-// brings the largest to 0.5 .. 1; or in one, in units searched for the least sum
-// of squared errors (the largest level is 1 .. 2 then).  Returns how far the
-// first part is off, at most, relative to a level.
-double build_half_levels(int bits, const float *levels, bool pair, HalfLevels &out);
-// Keys' levels in one fp16 part where it holds them to this (isoq_attn_c.h).
+// The levels in units searched for the least sum of the squares of what fp16
+// leaves of them (the largest level is 1 .. 2).  Returns the most that it leaves
+// of a level, relative to it.
+double build_half_levels(int bits, const float *levels, HalfLevels &out);
+// Keys' levels as they are in fp16 where it holds them to this (isoq_attn_c.h).
 constexpr double kHalfKeys = 0x1p-20;
+// (2^-11 at most, so 2^8 in e4m3, whose largest is 448)
+constexpr int kLevelRest = 19;
 // Lloyd-Max levels for N(0, sigma^2) (ascending, symmetrised).
 bool lloyd_levels(int bits, double sigma, int iters, double *levels);
 // Seeded raw draws (Philox4x32-10 + Box-Muller), layout of the public header.

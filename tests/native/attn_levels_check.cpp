@@ -1,7 +1,7 @@
 // Prints, for each codebook read from stdin (bits, then 2^bits levels), the
 // values that attention's forms of it stand for, level by level: two and three
-// digits (build_value_digits), one and two fp16 parts (build_half_levels, with
-// the error it reports first).
+// digits (build_value_digits), in fp16 (build_half_levels, with the error it
+// reports first), with what that leaves in e4m3, and in e4m3.
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -20,6 +20,13 @@ static double half(const isoq::HalfLevels &h, int t, int at)
     _Float16 v;
     std::memcpy(&v, &bits, 2);
     return (double)v;
+}
+
+static double byte(const isoq::HalfLevels &h, int t, int at)
+{
+    const int v = reinterpret_cast<const uint8_t *>(h.tab[t])[at], e = v >> 3 & 15, m = v & 7;
+    const double x = e == 0 ? std::ldexp(m, -9) : std::ldexp(8 + m, e - 10);
+    return (v & 127) == 127 ? NAN : v & 128 ? -x : x;
 }
 
 int main()
@@ -47,13 +54,17 @@ int main()
             }
             std::printf("\n");
         }
-        for (int pair = 0; pair < 2; pair++) {
-            isoq::HalfLevels h;
-            std::printf("%.17g ", isoq::build_half_levels(bits, lev, pair, h));
+        isoq::HalfLevels h;
+        const double off = isoq::build_half_levels(bits, lev, h);
+        for (int form = 0; form < 3; form++) {
+            if (form == 0)
+                std::printf("%.17g ", off);
             for (int k = 0; k < K; k++) {
                 const int at = bits < 4 ? k : k >= 8 ? k - 8 : 7 - k;
-                const double v = (half(h, 0, at) + (pair ? half(h, 2, at) : 0.0)) * h.scale;
-                std::printf("%.17g ", bits == 4 && k < 8 ? -v : v);
+                const double v = form == 2   ? byte(h, 2, at)
+                                 : form == 1 ? half(h, 0, at) + std::ldexp(byte(h, 3, at), -isoq::kLevelRest)
+                                             : half(h, 0, at);
+                std::printf("%.17g ", (bits == 4 && k < 8 ? -v : v) * h.scale);
             }
             std::printf("\n");
         }

@@ -4,11 +4,12 @@ Digits (build_value_digits): integers of the largest magnitude 32,639 (two
 digits) or 8,355,711 (three) in units of at most twice the largest level over
 that, so a level is off by half a unit, 1 / 32,639 or 1 / 8,355,711 of the
 largest one at most (and by 2^-24 of itself: the unit is a float).
-fp16 (build_half_levels): a level in one part is off by half a step, 2^-11 of
-itself, at most; the unit is chosen among 4,096 for a small error of all levels,
-of which the reported one is the largest; in two parts by 2^-22 (the first's
-half step, rounded again), and by half of 2^-24 in units in which the largest is
-0.5 to 1, where that is more.  Both: a level's mirror image is its negative.
+fp16 (build_half_levels): off by half a step, 2^-11 of a level, at most; the unit
+is chosen among 4,096 for a small error of all levels, of which the reported one
+is the largest.  With what that leaves in e4m3, whose half step is 2^-4 of it (and
+2^-10 of the unit 2^-19 where it is small): 2^-15 of the level and 2^-29 of the
+largest.  In e4m3 alone: 2^-4 of a level, and 2^-10 of the largest.  A level's mirror
+image is its negative in all of them.
 Runs on the CPU."""
 import os
 import shutil
@@ -42,22 +43,23 @@ def test_attn_levels(tmp_path):
     text = "".join("%d %s\n" % (b, " ".join("%.9g" % np.float32(v) for v in c)) for b, c, _ in books)
     out = subprocess.run([str(exe)], input=text, capture_output=True, text=True, check=True, timeout=60).stdout
     lines = [np.array(line.split(), float) for line in out.strip().splitlines()]
-    assert len(lines) == 4 * len(books)
+    assert len(lines) == 5 * len(books)
     for i, (b, c, lloyd) in enumerate(books):
         ref = np.float32(c).astype(float)
         top = ref[-1]
-        two, three, one_part, two_parts = lines[4 * i:4 * i + 4]
+        two, three, half, rest, byte = lines[5 * i:5 * i + 5]
+        off, half = half[0], half[1:]
         for vals, units in ((two, 32639), (three, 8355711)):
             assert np.all(np.abs(vals - ref) <= top / units + 2.0 ** -24 * np.abs(ref)), (b, units)
-        off, vals = one_part[0], one_part[1:]
-        assert np.all(np.abs(vals - ref) <= (off + 2.0 ** -23) * np.abs(ref)) and off <= 2.0 ** -11, (b, off)
+        left = np.abs(half - ref)
+        scale = 2.0 ** -23 * np.abs(ref)   # (the unit is a float, and so are the levels)
+        assert np.all(left <= off * np.abs(ref) + scale) and off <= 2.0 ** -11, (b, off)
+        assert np.all(np.abs(rest - ref) <= 2.0 ** -4 * left + 2.0 ** -29 * top + scale), b
+        assert np.all(np.abs(byte - ref) <= 2.0 ** -4 * np.abs(ref) + 2.0 ** -10 * top + scale), b
         if lloyd:
-            # what the kernel's comment states (of the levels' root mean square under equal weights here)
-            rms = np.sqrt(np.mean((vals - ref) ** 2) / np.mean(ref ** 2))
+            # of the levels' root mean square under equal weights: what the kernel's comment states
+            rms = np.sqrt(np.mean(left ** 2) / np.mean(ref ** 2))
             assert rms <= {2: 4e-7, 3: 1.6e-5, 4: 1e-4}[b], (b, rms)
             assert b > 2 or off <= 2.0 ** -20
-        off2, vals2 = two_parts[0], two_parts[1:]
-        assert off2 <= 2.0 ** -11
-        assert np.all(np.abs(vals2 - ref) <= 2.0 ** -22 * np.abs(ref) + 2.0 ** -25 * 2 * top), b
-        for v in (two, three, vals, vals2):
+        for v in (two, three, half, rest, byte):
             assert np.array_equal(v, -v[::-1])

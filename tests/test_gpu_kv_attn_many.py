@@ -1,12 +1,18 @@
 """Attention of 32 rows and more per key head (the fp16 matrix cores; widths up
 to 128, fp16 queries) where it can go wrong, against the definition in 64 bits;
-reference and tolerance of test_gpu_kv_attn.py.  In its terms: a query's and a
-key's two fp16 parts are off by 2^-22 of their largest coordinate's units and
-the product without the low parts by 2^-22, inside (pw + 8) 2^-23; a value's
-level in one part is off by at most 7e-5 of the levels' root mean square at 4
-bits and 8e-6 at 3, inside 1 / 32639 of the largest level (2.7 and 2.2 times
-that) times sqrt(pw).  For other codebooks the level's error is worked out from
-the levels (test_many_codebooks).  Needs an MI355X."""
+reference and tolerance of test_gpu_kv_attn.py.  In its terms: a query's two fp16
+parts are off by 2^-22 of its largest coordinate, inside (pw + 8) 2^-23.  A key's
+level is fp16 plus what that leaves (at most 1e-4 of the levels' root mean square
+at 4 bits) in e4m3, times the query in e4m3: both off by 2^-4 / sqrt(3) = 3.6% of
+that at most in the root mean square, so a coordinate's product by 5e-6, and the
+sum of d of them with independent signs by 5e-6 / sqrt(d) of ||q|| ||c[idx]||: 6.4e-7
+at d = 64, of which (64 + 8) 2^-23 is 13 times, and more above.  A value's level is
+off by at most 7e-5 of the levels' root mean square at 4 bits and 8e-6 at 3, inside
+1 / 32639 of the largest level (2.7 and 2.2 times that) times sqrt(pw); a weight by
+2^-4 of the 2^-11 that fp16 leaves of it, times a level off by 2^-4: 2^-14 of an
+independent sum, inside what is allowed for the output's own rounding.  For other
+codebooks the level's error is worked out from the levels (test_many_codebooks).
+Needs an MI355X."""
 import numpy as np
 import pytest
 
