@@ -34,7 +34,8 @@
  *     generic kernel family for every other width), d in {64, 128, 256, 512}
  *     for the KV-cache append (and, fp16 rows only, 80, 96, 160 and 192), d in
  *     {64, 80, 96, 128, 160, 192, 256, 512} for the attention-score call
- *     without the sketch, d in {64, 128, 256, 512} and (fp16 rows, or any
+ *     without the sketch and for attention (any d from 1 to 1024 by
+ *     width-generic kernels), d in {64, 128, 256, 512} and (fp16 rows, or any
  *     query type for the scores) 80, 96, 160 and 192 for the stage-2 sketch
  *     and the calls that use it (Full, Fast and 2-D handles; every other call
  *     takes all four variants).
@@ -457,9 +458,10 @@ isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, co
  *   n_keep      device, int32 [n_seqs], entries of each list that count (cut to
  *               [0, max_keep]).
  *   block_table, max_blocks_per_seq  as in isoq_kv_scores.  The blocks of a
- *               sequence that is compacted must not be another's too (copy a
- *               shared block first).  An entry whose source or destination has no
- *               block in [0, n_blocks), or lies outside the table, is skipped.
+ *               sequence that is compacted must not be another's too, nor
+ *               stand in its row twice (copy a shared block first).  An
+ *               entry whose source or destination has no block in [0,
+ *               n_blocks), or lies outside the table, is skipped.
  *   pk, sk, k_idx .. k_gamma, n_heads, n_blocks, block_size  as in
  *               isoq_kv_copy_blocks.
  * Positions from n_keep[s] on keep their contents.  A list that does not ascend

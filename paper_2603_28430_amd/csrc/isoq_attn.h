@@ -14,6 +14,7 @@
 // finishes its rows by itself.
 #pragma once
 
+#include "isoq_attn_tables.h"
 #include "isoq_internal.h"
 
 namespace isoq {

@@ -1,7 +1,9 @@
 // Attention over the paged quantized cache at any width from 1 to 1024 and with
 // any codebook, in fp32 without matrix instructions: the compatibility path of
 // widths (and of codebooks with levels of very different sizes) that
-// isoq_attn_m.h does not take.  It is not tuned.
+// isoq_attn_m.h does not take.  It is not tuned (4 sequences x 8 x 4 heads x 4,096
+// positions, 3 bits: d = 100 66 us, d = 1000 1,150; d = 128 with a codebook of
+// distant levels 80, where isoq_attn_m.h takes 12 with an ordinary one).
 //
 // Workgroup (row = query head of a token, sequence, split), 256 positions at a
 // time: each lane sums one key's logit over its record, slot by slot as the

@@ -4,13 +4,15 @@
 // Up to kAttnJoinFew splits (attn_join_few_kernel): a lane has a rotation slot of
 // a row, reads every split's m and l itself, and adds up; 256 / slots rows per
 // workgroup.  Bound by what it reads and writes (a chunk of 512 tokens, 32
-// heads, d = 128: n_splits x 8 MB).
+// heads, d = 128: n_splits x 8 MB; two of them in 3 splits 9 us), and by its
+// launch where that is little (3 to 5 us).
 //
 // More (attn_join_kernel): one workgroup per row.  A lane has a split's m and l (kAttnMaxSplits of them
 // at most), then a rotation slot of the splits g, g + groups, ... (256 / slots
 // groups, summed through LDS).  It reads n_splits (width + 2) floats a row: little
 // next to the cache of any call that splits, so the chain of dependent loads
-// is what it takes: the first splits' sums are asked for together with m and l.
+// is what it takes, 4 to 5 us (64 rows of 86 splits, 512 rows of 11): the first
+// splits' sums are asked for together with m and l.
 #include "isoq_attn_device.h"
 
 namespace isoq {

@@ -7,6 +7,7 @@
 
 #include <vector>
 
+#include "isoq_attn_tables.h"
 #include "isoq_internal.h"
 #include "isoquant.h"
 

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "isoq_attn_tables.h"
 #include "isoq_internal.h"
 
 namespace isoq {

@@ -122,25 +122,6 @@ struct LevelDigits {
     int32_t exp;
 };
 
-// The codebook as 8-bit digits for the weighted sums of attention (isoq_attn_m.h):
-// byte k of tab[t] is digit t (least significant first) of level k's integer,
-// n_k = d_0 + 256 d_1 (+ 65536 d_2), and scale n_k the level.  At 4 bits of the
-// positive level of magnitude k, which is scale (n_k + half), half = (1 + 256 (+
-// 65536)) / 2: the complement of the digits then stands for its mirror image.
-struct ValueDigits {
-    uint32_t tab[3][2];
-    float scale;
-};
-
-// The codebook in fp16 for attention of many rows (isoq_attn_c.h): byte k of
-// tab[0] and tab[1] are the low and high byte of level k's fp16 value in units of
-// scale, of tab[2] its e4m3 value, and of tab[3] that of 2^kLevelRest times what
-// fp16 leaves of it.  At 4 bits of the positive level of magnitude k.
-struct HalfLevels {
-    uint32_t tab[4][2];
-    float scale;
-};
-
 // Attention logits against a paged cache of quantized keys (isoq_scores.h,
 // isoq_scores_generic.hip).
 struct SArgs {
@@ -373,18 +354,6 @@ bool build_magnitude_lut(int H, const double *tau, const double *lev, double *in
 // square, come to 2^-24 of those that it has (a rotated query whose largest
 // coordinate is four times its root mean square).
 bool build_level_digits(int bits, const float *levels, std::vector<LevelDigits> &out);
-// The levels as integers of `digits` (2 or 3) balanced 8-bit digits.  The scale
-// is searched for the least sum of squared errors over the levels; the largest
-// level's integer is at least half of what the digits hold.
-void build_value_digits(int bits, const float *levels, int digits, ValueDigits &out);
-// The levels in units searched for the least sum of the squares of what fp16
-// leaves of them (the largest level is 1 .. 2).  Returns the most that it leaves
-// of a level, relative to it.
-double build_half_levels(int bits, const float *levels, HalfLevels &out);
-// Keys' levels as they are in fp16 where it holds them to this (isoq_attn_c.h).
-constexpr double kHalfKeys = 0x1p-20;
-// (2^-11 at most, so 2^8 in e4m3, whose largest is 448)
-constexpr int kLevelRest = 19;
 // Lloyd-Max levels for N(0, sigma^2) (ascending, symmetrised).
 bool lloyd_levels(int bits, double sigma, int iters, double *levels);
 // Seeded raw draws (Philox4x32-10 + Box-Muller), layout of the public header.

@@ -6,7 +6,7 @@
 #include <cstdio>
 #include <cstring>
 
-#include "isoq_internal.h"
+#include "isoq_attn_tables.h"
 
 static int digit(const isoq::ValueDigits &v, int t, int at)
 {
