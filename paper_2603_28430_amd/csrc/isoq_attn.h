@@ -9,7 +9,7 @@
 //     p_t = exp(s_t - m),  l = sum_t p_t,  lse = m + ln l:
 // the query is rotated once, the sum of values is rotated back once, and no
 // cached row is ever decompressed.  (Logits and m are kept in units of ln 2.)
-// A long cache is cut into splits of `chunk` positions; each leaves m, l and its
+// A long cache is cut into splits of `chunk` positions (attn_chunk); each leaves m, l and its
 // sum of values, which attn_join_kernel joins.  With one split a workgroup
 // finishes its rows by itself.
 #pragma once
@@ -37,7 +37,8 @@ struct AttnArgs {
     int32_t block_size, max_blocks;
     int32_t cap;                 // positions a sequence has at most (0: no cache)
     int32_t k_sets, v_sets, variant, q_f16;
-    int32_t chunk, n_splits;     // positions per split
+    int32_t chunk, n_splits;     // positions per split (at most, if even: attn_chunk)
+    int32_t even;
     float scale;                 // times log2(e)
     FastDiv div_block;
     int32_t d, width, slots;     // coordinates per row, padded width, its rotation slots (8 coordinates for 8-D, else 4)

@@ -51,7 +51,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
                                  : attn_m_kernel_b4(pk->d, r, f16);
         // Many rows: where decoding a tile for 128 rows at once pays for what
         // fewer leave idle (us by digits / in fp16.  16 x 8 heads, 4,096
-        // positions, d = 128, 3 bits: 24 rows 64 / 72, 32 78 / 67, 64 141 / 80, 128
+        // positions, d = 128, 3 bits: 24 rows 64 / 74, 32 78 / 69, 64 141 / 81, 128
         // 256 / 103.  2 x 8 heads, 8,192: 24 28 / 33, 32 30 / 33, 48 39 / 38, 128 70
         // / 55.  4 x 4 heads, 8,192, d = 64, 4 bits: 32 25 / 24, 64 40 / 28.)
         if (f16 && rows >= 32) {
@@ -64,7 +64,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // Splits: as many as give so many workgroups, of which a compute unit holds two
     // to four at once (two above d = 128 and in fp16): more than one round of them
     // evens out sequences of different lengths, and is not wanted where there is
-    // one sequence.  None up to
+    // one sequence, or in fp16, which cuts them evenly (attn_chunk).  None up to
     // 768 positions, three tiles a wave (one sequence, 8 x 4 heads, on the GPU / with
     // the host's calls: 700 positions 9.8 / 12.1 us with one split, 8.7 / 15.6 with
     // three; 1,000: 12.4 / 12.4, 8.7 / 14.5).
@@ -72,10 +72,11 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // positions 49 / 51 / 49 / 53 / 53; 8 x 32 x 32,768 231 / 210 / 203 / 202 / 208; 16
     // ragged x 8 x 4 of up to 8,192 45 / 44 / 40 / 42 / 42, with 5 tokens of up to
     // 4,096 51 / 50 / 44 / 40 / 41; 4 x 8 x 2, 8,190, d = 256 25 / 25 / 27 / 27 / 27.
-    // In fp16 at 512 / 640 / 768 / 1,024: two ragged chunks of up to 512 tokens and 8,192
-    // positions 239 / 216 / 216 / 270, two equal ones 318 / 345 / 343 / 340; 16 of 8
-    // tokens at 4,096 69 / 67 / 94 / 79.)
-    const int64_t want = p.kern.parts ? 640 : n_seqs == 1 || pk->d > 128 ? 768 : 1536, blocks = p.groups * n_seqs;
+    // In fp16 at 384 / 512 / 640 / 768 / 1,024: two ragged chunks of up to 512 tokens and
+    // 8,192 positions 231 / 220 / 254 / 253 / 234, two equal ones 308 / 303 / 334 / 337
+    // / 318; 16 of up to 16 tokens and 4,096 positions 89 / 78 / 77 / 89 / 84; 8 prompts
+    // of 1,024 tokens 103 / 102 / 112 / 111 / 110: one round of workgroups.)
+    const int64_t want = p.kern.parts ? 512 : n_seqs == 1 || pk->d > 128 ? 768 : 1536, blocks = p.groups * n_seqs;
     const int64_t splits = p.max_pos <= 768 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
@@ -230,6 +231,7 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
     a.q_f16 = dtype == ISOQ_F16;
     a.chunk = plan.chunk;
     a.n_splits = plan.n_splits;
+    a.even = plan.kern.parts;
     a.scale = (float)((double)scale * 1.4426950408889634);
     a.div_block = make_fastdiv((uint32_t)block_size);
     a.d = pk->d;

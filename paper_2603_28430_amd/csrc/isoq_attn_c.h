@@ -21,8 +21,11 @@
 // An e4m3 product is half a fp16 product's time, and the matrix cores' power is what
 // holds the kernel back (their clock falls to 1.9 GHz; taking a fifth of the vector
 // instructions out, or waits of waves for each other, changed nothing): with
-// both corrections in fp16, 2 x 512 tokens at 8,192 positions, 3 bits, took 383 us
-// instead of 361.  (The query's lo in e4m3 too: 340 us, and lse off by 1e-6 to 2e-6.)
+// both corrections in fp16, 2 x 512 tokens at 8,192 positions, 3 bits, took 6%
+// longer.  (The query's lo in e4m3 too: 6% less, and lse off by 1e-6 to 2e-6.)
+// They take 303 to 338 us in different runs, 407 to 450 TFLOP/s of the definition's
+// operations (4 d a row and position), twice that of the matrix cores' own; 346 at
+// 4 bits, 298 at 2, 221 at d = 64.
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
@@ -132,10 +135,11 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
         return;
     const int n = min(C::ROWS, total - r0);
     const int lim_all = sq.limit((r0 + n - 1) / a.group, a.cap);
-    const int64_t t0l = (int64_t)blockIdx.z * a.chunk;
+    const int chunk = attn_chunk(a, sq);
+    const int64_t t0l = (int64_t)blockIdx.z * chunk;
     if (t0l >= lim_all && blockIdx.z > 0)
         return;   // the join looks at the splits below a row's limit only
-    const int t0 = (int)t0l, tend = (int)min(t0l + a.chunk, (int64_t)lim_all);
+    const int t0 = (int)t0l, tend = (int)min(t0l + chunk, (int64_t)lim_all);
     const int nt = (tend - t0 + 63) / 64;
 
     // the wave's rows: one per lane of each half

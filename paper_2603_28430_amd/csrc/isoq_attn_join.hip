@@ -46,7 +46,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
         load(g + u * groups, v[u]);
     const float *ml = a.part_ml + (row * a.n_splits + min(tid, a.n_splits - 1)) * 2;
     float m = ml[0], l = ml[1];
-    const int ns = (sq.limit(i, a.cap) + a.chunk - 1) / a.chunk;   // splits that have positions of this row
+    const int chunk = attn_chunk(a, sq);
+    const int ns = (int)(((uint32_t)sq.limit(i, a.cap) + (uint32_t)chunk - 1u) / (uint32_t)chunk);   // splits that have positions of this row
     if (tid >= ns) {
         m = -INFINITY;
         l = 0.f;
@@ -120,7 +121,8 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
     if (g >= per || i >= sq.rows)
         return;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + hq;
-    const int ns = (sq.limit(i, a.cap) + a.chunk - 1) / a.chunk;   // splits that have positions of this row
+    const int chunk = attn_chunk(a, sq);
+    const int ns = (int)(((uint32_t)sq.limit(i, a.cap) + (uint32_t)chunk - 1u) / (uint32_t)chunk);   // splits that have positions of this row
     const float *p = a.part + row * a.n_splits * a.width + SW * j;
     const float *ml = a.part_ml + row * a.n_splits * 2;
     float m[N], top = -INFINITY, l = 0.f, y[SW];
