@@ -191,6 +191,32 @@ def test_attn_far_offsets(d, bits, dtype, q_lens):
     check(out, lse, reference(w, 1.3))
 
 
+@pytest.mark.parametrize("d,bits,q_len", [(64, 2, 1), (64, 3, 32), (16, 4, 1)])
+def test_attn_longest_sequences(d, bits, q_len):
+    """2,047 pages of 2^20 positions, all the same block: nearly 2^31 positions.
+    Rows without a causal border inside the last page would be those of one page
+    with lse + ln 2047; the last q_len - 1 - i positions that token i does not see
+    are 1e-8 of the weights.  A lane adds up to 2^31 / 256 / 64 tiles' weights a
+    split, an error of 2^17 2^-24 at most, of the output's norm too."""
+    bs, pages = 1 << 20, 2047
+    rng = np.random.default_rng(d)
+    pk, pv = (iq.isoq_params_init("full", d, bits, 1, seed=s) for s in (1, 2))
+    k_idx, v_idx = (torch.from_numpy(rng.integers(0, 256, (1, 1, bs, pk.record_bytes), dtype=np.uint8)).cuda() for _ in (0, 1))
+    k_rho, v_rho = (torch.from_numpy(rng.uniform(0.5, 1.5, (1, 1, bs)).astype(np.float32)).cuda() for _ in (0, 1))
+    q = torch.from_numpy(rng.standard_normal((q_len, 1, d)).astype(np.float16)).cuda()
+    start = torch.tensor([0, q_len], dtype=torch.int32, device="cuda")
+
+    def run(n):
+        table = torch.zeros((1, n), dtype=torch.int32, device="cuda")
+        lens = torch.tensor([n * bs], dtype=torch.int32, device="cuda")
+        return iq.isoq_kv_attn(pk, q, k_idx, k_rho, pv, v_idx, v_rho, table, lens, scale=d ** -0.5, q_start=start,
+                               max_q_len=q_len)
+    (one, lse_one), (out, lse) = run(1), run(pages)
+    torch.cuda.synchronize()
+    assert ((lse - lse_one).double() - np.log(pages)).abs().max() < 2.0 ** -7
+    assert (out.double() - one.double()).norm() < (2.0 ** -7 + 2.0 ** -10) * one.double().norm()
+
+
 def test_pages_far_offsets():
     w = setup("full", 128, 3, "f16", [1, 1], 4, 4, 64, [500, 70], seed=1)
     n_blocks = (1 << 32) // (4 * 64 * 48) + 1000
