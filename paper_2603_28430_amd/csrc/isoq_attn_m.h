@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         // an invalid position reads position 0 of the head in block 0 (always
         // present) and gets no weight
         const uint32_t blk = valid ? (uint32_t)next.blk : 0u, pos = valid ? (uint32_t)next.pos : 0u;
-        const uint64_t at = times(blk, bstride, 0) + (uint64_t)(pos * S::CP);
+        const uint64_t at = times(blk, bstride, 0) + (uint64_t)pos * S::CP;
         const uint64_t row = times(blk, rstride, pos);
         issue(at, row, k_idx, k_rho, k);
         issue(at, row, v_idx, v_rho, v);

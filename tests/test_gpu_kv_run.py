@@ -217,6 +217,45 @@ def test_attn_longest_sequences(d, bits, q_len):
     assert (out.double() - one.double()).norm() < (2.0 ** -7 + 2.0 ** -10) * one.double().norm()
 
 
+@pytest.mark.parametrize("d,dtype,q_len", [(64, "f32", 1), (64, "f16", 32), (60, "f32", 1)])
+def test_attn_large_block(d, dtype, q_len):
+    """One block of more than 2^28 positions, whose records' offsets in it pass 2^32.
+    All but the last 64 have zero norms: logit 0, value 0, so they add their number
+    to the sum of exponentials of those 64 alone.  Half a step of fp16 in both
+    outputs, 2^-11 of the norm each (fp32: what a sum of 2^17 weights a lane and
+    split takes, 2^-7 at most, of the zeros' share, which is below 2^-9)."""
+    bs = (1 << 32) // 15 + 1000 if d == 60 else (1 << 28) + 1000
+    rng = np.random.default_rng(d)
+    pk, pv = (iq.isoq_params_init("fast", d, 2, 1, seed=s) for s in (1, 2))
+    ndt = torch.float16 if dtype == "f16" else torch.float32
+    q = torch.from_numpy(rng.standard_normal((q_len, 1, d))).to(ndt).cuda()
+    start = torch.tensor([0, q_len], dtype=torch.int32, device="cuda")
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    small, large = [], []
+    for _ in (0, 1):
+        rec = torch.from_numpy(rng.integers(0, 256, (1, 1, 64, pk.record_bytes), dtype=np.uint8)).cuda()
+        rho = torch.from_numpy(rng.uniform(30, 60, (1, 1, 64)).astype(np.float32)).cuda()
+        small += [rec, rho]
+        idx, norm = torch.zeros((1, 1, bs, pk.record_bytes), dtype=torch.uint8, device="cuda"), torch.zeros((1, 1, bs), device="cuda")
+        idx[:, :, -64:], norm[:, :, -64:] = rec, rho   # (one piece, or records stored whole: position after position)
+        large += [idx, norm]
+    assert large[0].numel() > 1 << 32
+
+    def run(c, n):
+        return iq.isoq_kv_attn(pk, q, c[0], c[1], pv, c[2], c[3], table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+                               scale=1.0, q_start=start, max_q_len=q_len)
+    (o64, l64), (out, lse) = run(small, 64), run(large, bs)
+    torch.cuda.synchronize()
+    l64 = l64.double()
+    want = torch.logaddexp(l64, torch.full_like(l64, np.log(bs - 64)))
+    share = torch.exp(np.log(bs - 64) - want)
+    assert share.max() < 2.0 ** -9, share.max()
+    assert torch.all((lse.double() - want).abs() <= 2.0 ** -7 * share + 2.0 ** -16 + 2.0 ** -22 * want.abs())
+    ref = o64.double() * torch.exp(l64 - want)[..., None]
+    err = (out.double() - ref).norm(dim=-1)
+    assert torch.all(err <= (2.0 ** -7 * share + (2.0 ** -10 if dtype == "f16" else 2.0 ** -15)) * ref.norm(dim=-1))
+
+
 def test_pages_far_offsets():
     w = setup("full", 128, 3, "f16", [1, 1], 4, 4, 64, [500, 70], seed=1)
     n_blocks = (1 << 32) // (4 * 64 * 48) + 1000
