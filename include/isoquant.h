@@ -409,8 +409,9 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  * 2^23, max_blocks_per_seq * block_size <= 2^31 - 1024.
  * Arithmetic: logits, softmax statistics and sums in fp32 or in integers of 32
  * bits (see the kernels for what is rounded).  A query with an infinity or NaN
- * gives NaN in its row of out and lse.  The result does not depend on the order in which
- * workgroups run.
+ * gives NaN in its row of out and lse, and so does a norm of k_rho or v_rho that
+ * is one in the rows that attend to its position, not in others.  The result
+ * does not depend on the order in which workgroups run.
  */
 isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
                          const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
@@ -439,7 +440,9 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
  *               then unspecified; nothing else is touched).
  *   k_idx .. k_gamma, n_blocks, block_size  the cache, laid out as in
  *               isoq_kv_append (records 16-byte aligned).
- * Limits: n_pairs < 2^24, n_blocks * block_size < 2^31.  n_pairs = 0 is a no-op.
+ * Limits: n_pairs < 2^24, n_blocks * block_size < 2^31, and a block of one array is
+ * at most 2^27 accesses of 16 bytes (of 4, or 1, where its size asks for it).
+ * n_pairs = 0 is a no-op.
  */
 isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, const int32_t *block_pairs,
                                 int64_t n_pairs, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,

@@ -64,12 +64,12 @@ struct AttnCShape {
     static constexpr int RK = 4 * S::WC + 1;         // words of a key's raw record (odd: lanes are keys)
     static constexpr int RV = H::SW + 1;             // words of a value's raw record
     // LDS bytes: keys, and what fp16 left of them; values in fp16, e4m3; raw
-    // records; per tile parity the norms (K, V), the valid positions and the
-    // values' unit
+    // records; per tile parity the norms (K, V), the valid positions, the
+    // values' unit, and the first value and key whose norm is an infinity or NaN
     static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROW8, kV8 = kV + 32 * CT * VROW,
                          kRawK = kV8 + 32 * CT * VROW8, kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV,
                          kTile = kNorm + 2 * 512;
-    static constexpr int loop_bytes() { return kTile + 2 * 16; }
+    static constexpr int loop_bytes() { return kTile + 2 * 32; }
     // before the loop the rotated queries and their largest magnitudes
     static constexpr int QS = D + 1;
     static constexpr int query_bytes() { return 4 * ROWS * (QS + 8); }
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
     int unit = 0;
     auto store_raw = [&](int t) {   // (waves 0 and 1) into tile t's places
         float *norm = reinterpret_cast<float *>(lds + C::kNorm + 512 * (t & 1));
-        uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 16 * (t & 1));
+        uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 32 * (t & 1));
         if (w == 0) {
             uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawK) + lane * C::RK;
 #pragma unroll
@@ -234,16 +234,24 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                                                      : __builtin_amdgcn_alignbit(at + 1 < S::RW ? rec.w[at + 1] : 0u, rec.w[at], sh);
                 }
             norm[lane] = rec.ok ? rec.rho : 0.f;
+            const uint64_t odds = __builtin_amdgcn_ballot_w64(rec.ok && !(fabsf(rec.rho) < INFINITY));
             const uint64_t ok = __builtin_amdgcn_ballot_w64(rec.ok);
             if (lane == 0) {
                 tile[0] = (uint32_t)ok;
                 tile[1] = (uint32_t)(ok >> 32);
+                tile[4] = odds ? __builtin_ctzll(odds) : 0x7FFFFFFF;
             }
         } else {
             uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawV) + lane * C::RV;
 #pragma unroll
             for (int i = 0; i < H::SW; i++)
                 dst[i] = H::staged(rec.w, i);
+            // (norms that are an infinity or NaN make a NaN of the rows that attend to
+            // them in step 4, not of others: the values count as zero)
+            const bool odd = rec.ok && !(fabsf(rec.rho) < INFINITY);
+            const uint64_t odds = __builtin_amdgcn_ballot_w64(odd);
+            if (odd)
+                rec.rho = 0.f;
             float top = row_max16(rec.ok ? fabsf(rec.rho) : 0.f);
 #pragma unroll
             for (int o = 16; o < 64; o *= 2)
@@ -252,8 +260,10 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
             if (t == 0 || e > unit || e < unit - 4)
                 unit = e;
             norm[64 + lane] = rec.ok ? __builtin_amdgcn_ldexpf(rec.rho, 14 - unit) : 0.f;
-            if (lane == 0)
+            if (lane == 0) {
                 tile[2] = (uint32_t)unit;
+                tile[3] = odds ? __builtin_ctzll(odds) : 0x7FFFFFFF;
+            }
         }
     };
     int32_t next = 0;
@@ -419,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
         __syncthreads();
 
         const int tb = t0 + 64 * t;
-        const uint32_t *tile = reinterpret_cast<const uint32_t *>(lds + C::kTile + 16 * (t & 1));
+        const uint32_t *tile = reinterpret_cast<const uint32_t *>(lds + C::kTile + 32 * (t & 1));
         if (tb < lim_max) {   // (wave-uniform)
             // 3. S^T of the wave's rows and the tile's positions; a step's keys
             //    are read while the one before multiplies
@@ -543,6 +553,8 @@ __global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
                     pr[4 * k + b] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
                 }
             l = fmaf(l, alpha, sum);
+            if (min((int)tile[3], (int)tile[4]) < lim - tb)
+                l = NAN;
             // 5. O^T += V^T P^T, likewise
             const uint8_t *val = lds + C::kV + n32 * C::VROW + 16 * half;
             const uint8_t *val8 = lds + C::kV8 + n32 * C::VROW8 + 32 * half;

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     };
     for (int64_t tb = t0; tb < tend; tb += 256) {
         const int64_t t = tb + tid;
-        float v = -INFINITY, rho_v = 0.f;
+        float v = -INFINITY, rho_k = 0.f, rho_v = 0.f;
         bool ok = false;
         int blk = 0, pos = 0;
         if (t < tend) {
@@ -115,7 +115,8 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
                     dot = fmaf(qt[SW * j + c], klev[(p >> (BITS * c)) & (K - 1)], dot);
             }
             const int64_t crow = ((int64_t)blk * a.n_kv_heads + h) * a.block_size + pos;
-            v = a.k_rho[crow] * dot;
+            rho_k = a.k_rho[crow];
+            v = rho_k * dot;
             rho_v = a.v_rho[crow];
         }
         float top = v;
@@ -129,7 +130,8 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         const float mref = mnew == -INFINITY ? 0.f : mnew;
         const float alpha = __builtin_amdgcn_exp2f(m - mref);   // (m = -inf: 0)
         const float p = ok ? __builtin_amdgcn_exp2f(v - mref) : 0.f;
-        l = fmaf(l, alpha, p);
+        // (a norm that is an infinity or NaN: NaN in out and lse)
+        l = fmaf(l, alpha, fabsf(rho_k) < INFINITY && fabsf(rho_v) < INFINITY ? p : NAN);
         m = mnew;
         wt[tid] = ok ? p * rho_v : 0.f;
         place[2 * tid] = ok ? blk : -1;

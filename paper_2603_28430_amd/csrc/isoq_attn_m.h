@@ -488,6 +488,10 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     for (int b = 0; b < nb; b++) {
         const int tb = t0 + 64 * WV * b + 64 * w;   // the wave's first position
         const uint64_t ok_mask = __builtin_amdgcn_ballot_w64(valid);
+        // positions with a norm that is an infinity or NaN make a NaN of the rows
+        // that attend to them (step 6), not of others: their values count as zero
+        const bool odd = valid && !(fabsf(k.rho) < INFINITY && fabsf(v.rho) < INFINITY);
+        const uint64_t odd_mask = __builtin_amdgcn_ballot_w64(odd);
         // 4. the keys' records, chunk kq of key 16 r + col in y[r]
         uint32_t y[4][S::WC];
 #pragma unroll
@@ -506,7 +510,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         }
         // the norms, to the lanes of their positions mod 16
         norms[(lane & 15) * 4 + (lane >> 4)] = k.rho;
-        norms[64 + (lane & 15) * 4 + (lane >> 4)] = valid ? v.rho : 0.f;
+        norms[64 + (lane & 15) * 4 + (lane >> 4)] = valid && !odd ? v.rho : 0.f;
         // the values' records as they are, for the second product
 #pragma unroll
         for (int i = 0; i < H::SW; i += 4)
@@ -614,6 +618,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 u[st] = ((uint32_t)x + 0x00808080u) ^ 0x00808080u;
             }
             l[nt] = fmaf(l[nt], alpha[nt], sum);
+            if (odd_mask != 0 && tb + __builtin_ctzll(odd_mask) < lim[nt])
+                l[nt] = NAN;
             if constexpr (BITS == 4)
                 sw[nt] = fmaf(wsum, vunit, sw[nt] * alpha[nt]);
             const uint32_t a01 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), a23 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);

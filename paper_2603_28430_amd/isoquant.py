@@ -478,13 +478,14 @@ def _attn_buffers(q, rows, out, lse, workspace, need):
 
 
 def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, scale: float = 1.0,
-                 q_start=None, max_q_len: int = 1, max_len=None, out=None, lse=None, workspace=None, stream=None):
+                 q_start=None, max_q_len=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
     """Attention of new tokens' queries q [n_tokens, n_q_heads, d] over the paged
     caches k_idx, v_idx [n_blocks, n_kv_heads, block_size, R] / k_rho, v_rho
     [n_blocks, n_kv_heads, block_size] with block_table int32 [n_seqs,
     max_blocks] and seq_lens int32 [n_seqs].  One token a sequence, or with
     q_start int32 [n_seqs + 1] the tokens q_start[s] .. q_start[s + 1] - 1 of
-    sequence s, at most max_q_len, which are its last positions (causal).
+    sequence s, at most max_q_len (default: n_tokens), which are its last
+    positions (causal).
     Returns (out like q, lse fp32 [n_tokens, n_q_heads]); rows of no sequence
     are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
     least isoq_kv_attn_workspace(...) bytes.  What is not passed (out, lse,
@@ -509,6 +510,8 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
     if block_table.dtype != torch.int32 or seq_lens.dtype != torch.int32:
         raise TypeError("block_table and seq_lens must be int32")
     code = _dtype_code(q.dtype)
+    if max_q_len is None:
+        max_q_len = 1 if q_start is None else max(1, n_tokens)
     if q_start is None:
         if n_tokens != n_seqs or max_q_len != 1:
             raise ValueError("without q_start there is one token a sequence")

@@ -110,6 +110,30 @@ def test_many_nonfinite_queries(bad):
     check(out, lse, ref)
 
 
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("side", ["k", "v"])
+@pytest.mark.parametrize("d,bits,dtype,q_lens", [(128, 3, "f16", [40, 33]), (64, 4, "f16", [40, 33]), (128, 2, "f16", [3, 2]),
+                                                 (96, 4, "f32", [7, 1]), (70, 3, "f16", [3, 9])])
+def test_norms_that_are_no_numbers(d, bits, dtype, q_lens, side, bad):
+    """NaN in the rows that attend to such a position, and others as if it were not there."""
+    w = setup("full", d, bits, dtype, q_lens, 2, 2, 16, [300, 90], seed=4)
+    ref = reference(w, 1.0)
+    args = device(w)
+    hit = set()
+    at = 0
+    for s, (n, pos) in enumerate(zip(q_lens, (298, 89))):   # inside a tile, and the last position
+        c = w["sides"][0 if side == "k" else 1][2]
+        args[side + "_rho"][int(c.table[s, pos // 16]), 1, pos % 16] = bad
+        hit |= {(at + i, 1) for i in range(n) if w["seq_lens"][s] - (n - 1 - i) > pos}
+        at += n
+    out, lse = iq.isoq_kv_attn(**args, scale=1.0)
+    assert 2 <= len(hit) < len(ref)
+    for key in hit:
+        assert torch.isnan(out[key]).all() and torch.isnan(lse[key]), key
+        del ref[key]
+    check(out, lse, ref)
+
+
 @pytest.mark.parametrize("scale", [0.0, 300.0, -2.0])
 def test_many_scales(scale):
     run_case("fast", 128, 3, "f16", [17, 20], n_q=4, n_kv=1, bs=16, seq_lens=[700, 40], scale=scale, seed=8)
@@ -264,6 +288,17 @@ def test_many_streams_and_graphs():
         for i in (0, 1):
             assert torch.equal(outs[i][0], alone[i][0]) and torch.equal(outs[i][1], alone[i][1])
         assert torch.equal(again[0], alone[0][0]) and torch.equal(again[1], alone[0][1])
+
+
+def test_max_q_len_by_default():
+    """Without max_q_len every token that q_start gives is computed."""
+    w = setup("full", 128, 3, "f16", [9, 1, 30], 2, 2, 16, [50, 30, 300], seed=2)
+    args = device(w)
+    del args["max_q_len"]
+    out, lse = iq.isoq_kv_attn(**args, scale=1.3)
+    check(out, lse, reference(w, 1.3))
+    none = iq.isoq_kv_attn(**dict(args, q=args["q"][:0], q_start=torch.zeros(4, dtype=torch.int32, device="cuda")))
+    assert none[0].shape == (0, 2, 128) and none[1].shape == (0, 2)
 
 
 def test_rows_do_not_depend_on_their_company():
