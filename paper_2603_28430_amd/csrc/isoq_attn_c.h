@@ -1,7 +1,7 @@
 // Attention of many rows (chunks of new tokens) over the paged quantized cache:
 // fp16 queries, widths up to 128, on the fp16 matrix cores.
 //
-// isoq_attn_m.h decodes a tile of 64 positions for 4 or 8 rows; with hundreds of
+// isoq_attn_m.h decodes a tile of 64 positions for 4 to 12 rows; with hundreds of
 // rows per key head that decoding is what it spends its time on.  Here a
 // workgroup has 128 rows, decodes each tile once into LDS, and multiplies in
 // fp16 with fp32 sums:

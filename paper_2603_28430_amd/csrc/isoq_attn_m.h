@@ -1,7 +1,8 @@
 // Attention over the paged quantized cache on the integer matrix cores (widths
 // of the tuned decoding kernels).
 //
-// A workgroup of four waves has 4 or 8 rows; its waves take 64 positions in turn.
+// A workgroup of four waves has 4, 8 or 12 rows (isoq_attn_m_pick.h); its waves take
+// 64 positions in turn.
 //
 // The logits are those of isoq_scores_m.h: rotated query and codebook as 8-bit
 // digits, products of digits summed exactly in int32 by v_mfma_i32_16x16x64_i8,

@@ -183,6 +183,17 @@ def test_attn_groups(group):
     run_case("fast", 128, 3, "f16", [1, 1], n_q=2 * group, n_kv=2, bs=16, seq_lens=[260, 77], seed=group)
 
 
+@pytest.mark.parametrize("rows", [7, 10, 12, 19])
+@pytest.mark.parametrize("bits", [2, 3, 4])
+@pytest.mark.parametrize("d", [64, 80, 96, 128, 160, 192, 256])
+def test_attn_rows_per_workgroup(d, bits, rows):
+    """Row counts on both sides of what a workgroup takes, tokens of one head and heads of one token."""
+    run = d // 16 + bits + rows
+    dtype, variant = ("f16", "f32")[run % 2], ("full", "fast", "2d", "8d")[run % 4]
+    run_case(variant, d, bits, dtype, [rows, 3], n_q=2, n_kv=2, bs=16, seq_lens=[330, 3], seed=run)
+    run_case(variant, d, bits, dtype, [1, 1], n_q=rows, n_kv=1, bs=7, seq_lens=[270, 41], seed=run)
+
+
 @pytest.mark.parametrize("d,dtype", [(128, "f16"), (96, "f32"), (100, "f16")])
 def test_attn_lengths(d, dtype):
     """Around the tiles of 64 and 256 positions, empty and one-token sequences, a max_len that cuts."""
