@@ -37,7 +37,7 @@
 // caches take 4.1 TB/s, the decoding's vector instructions (about 750 a tile of
 // 64 positions) next to memory.  With 8 rows (one sequence x 8 key heads x 131,071)
 // 48 us, 2.3 TB/s: vector and matrix instructions.  d = 256, 2 rows, 4 x 8 heads x 8,190:
-// 24 us.  A call of one sequence and 700 positions 10 us (12.5 with the host's
+// 24 us.  A call of one sequence and 700 positions 10 us (11.4 with the host's
 // part).
 #pragma once
 

@@ -3,10 +3,10 @@
 // call's launch the small ones.
 //
 // d = 128, 3 bits: 4,096 blocks of 32 heads x 16 positions (436 MB read and
-// written) 89 us, 4.9 TB/s; 16 blocks of 8 heads 3 us (7.5 a call).  8 sequences of
+// written) 89 us, 4.9 TB/s; 16 blocks of 8 heads 3 us (7.4 a call).  8 sequences of
 // 32,768 positions compacted to half of them, chosen at random for each of 8 heads
 // (174 MB), 71 us, 2.5 TB/s: of the 64-byte lines that are read half stays, and
-// with all of them it is 3.7.  One of 1,000 positions 5 us (8.6 a call).
+// with all of them it is 3.7.  One of 1,000 positions 5 us (8.4 a call).
 #include "isoq_pages.h"
 
 #include <type_traits>
