@@ -341,27 +341,39 @@ isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const 
     if (!aligned(keep, 4) || !aligned(n_keep, 4) || !aligned(block_table, 4))
         return ISOQ_E_ALIGN;
     CompactArgs a{};
+    const bool full = (int64_t)n_heads * n_seqs >= 64;   // (CompactArgs)
+    bool whole = false;
+    int n = 0;
+    auto columns = [&](int c, int64_t offset, int width, int64_t count, int64_t step, int64_t pos_stride) {
+        a.base[n] = pl.base[c] + offset;
+        a.head_stride[n] = pl.row[c] * block_size;
+        a.block_stride[n] = a.head_stride[n] * n_heads;
+        a.width[n] = width;
+        a.step[n] = step;
+        a.pos_stride[n] = (int32_t)pos_stride;
+        a.first[n + 1] = a.first[n] + (int32_t)count;
+        n++;
+    };
     for (int c = 0; c < pl.n; c++) {
-        const int64_t row = pl.row[c];
-        a.base[c] = pl.base[c];
-        a.head_stride[c] = row * block_size;
-        a.block_stride[c] = a.head_stride[c] * n_heads;
-        const int piece = pl.record[c] ? cache_piece(row) : (int)row;
+        const int64_t row = pl.row[c], piece = pl.record[c] ? cache_piece(row) : row;
         if (piece != row) {   // pieces of 16 or 8 bytes, those of one position block_size of them apart
-            a.width[c] = a.pos_stride[c] = piece;
-            a.step[c] = (int64_t)piece * block_size;
-        } else {   // records stored whole
-            int w = 16;
-            while (row % w != 0 || !aligned(pl.base[c], (size_t)w))
-                w /= 2;
-            a.width[c] = w;
-            a.pos_stride[c] = (int32_t)row;
-            a.step[c] = w;
+            columns(c, 0, (int)piece, row / piece, piece * block_size, piece);
+            continue;
         }
-        a.first[c + 1] = a.first[c] + (int32_t)(row / a.width[c]);
+        whole = whole || (row != 4 && row != 8 && row != 16);
+        int64_t at = 0;
+        for (int width = full ? 64 : 16; at < row; width /= 2) {
+            if (full && width < 64)
+                width = (int)(row - at);
+            if (const int64_t count = (row - at) / width) {
+                columns(c, at, width, count, width, row);
+                at += count * width;
+            }
+        }
     }
-    for (int c = pl.n; c < kCachePlanes; c++)
-        a.first[c + 1] = a.first[c];
+    const int chains = a.first[n];
+    for (; n < kCompactColumns; n++)
+        a.first[n + 1] = chains;
     a.keep = keep;
     a.n_keep = n_keep;
     a.block_table = block_table;
@@ -375,7 +387,7 @@ isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const 
     if (st != ISOQ_OK)
         return st;
     void *args[] = {&a};
-    return launch_lds(compact_kernel(), dim3((unsigned)n_heads, (unsigned)n_seqs, (unsigned)a.first[pl.n]),
+    return launch_lds(compact_kernel(whole), dim3((unsigned)n_heads, (unsigned)n_seqs, (unsigned)chains),
                       kCompactThreads, args, 0, stream);
 }
 

@@ -19,11 +19,18 @@ struct CopyArgs {
 constexpr int kCopyUnits = 2048;
 const void *copy_blocks_kernel();
 
-// What moves when a sequence is compacted: a chain is `width` bytes (16, 8, 4,
-// 2 or 1) of every position of a head, the byte columns that the cache layout
-// keeps together: a record's piece, a norm, or a unit of a record stored whole.
-// Chain p of plane c is at
+// What moves when a sequence is compacted: a chain is `width` bytes of every
+// position of a head, the byte columns that the cache layout keeps together: a
+// record's piece, a norm, or a part of a record stored whole.  Chain p of column
+// set c is at
 //     base + block block_stride + head head_stride + p step + pos pos_stride.
+// A record stored whole is cut into 64 bytes a chain and the rest of it where
+// sequences and heads alone fill the card, and into 16, 8, 4, 2 and 1 where they do
+// not and more workgroups are wanted.  (us, d = 80, 3 bits, 30 bytes, by fifteen
+// chains of 2 bytes / 16, 8, 4, 2 / one: 8 x 32 heads x 12,000 positions 625 / 179 / 68,
+// 3 x 8 x 60,000 82 / 41 / 78, one head 68 / 84 / 141; d = 160, 60 bytes: 8 x 32 x 6,553 496
+// / 178 / 60, 3 x 8 x 60,000 113 / 58 / 112.)
+constexpr int kCompactColumns = 2 * 5 + 4;   // K and V records, their norms, signs, gamma
 struct CompactArgs {
     const int32_t *keep;           // [n_seqs][keep_heads][max_keep]
     const int32_t *n_keep;         // [n_seqs]
@@ -31,13 +38,14 @@ struct CompactArgs {
     int64_t n_blocks;
     int32_t keep_heads, max_keep, max_blocks, block_size;
     FastDiv div_block;
-    uint8_t *base[kCachePlanes];
-    int64_t block_stride[kCachePlanes], head_stride[kCachePlanes], step[kCachePlanes];
-    int32_t pos_stride[kCachePlanes], width[kCachePlanes];
-    int32_t first[kCachePlanes + 1];   // plane c's chains are grid z first[c] .. first[c + 1] - 1
+    uint8_t *base[kCompactColumns];
+    int64_t block_stride[kCompactColumns], head_stride[kCompactColumns], step[kCompactColumns];
+    int32_t pos_stride[kCompactColumns], width[kCompactColumns];
+    int32_t first[kCompactColumns + 1];   // set c's chains are grid z first[c] .. first[c + 1] - 1
 };
 // Grid (heads, sequences, chains), kCompactThreads threads.
 constexpr int kCompactThreads = 1024;
-const void *compact_kernel();
+// whole: some records are stored whole (widths other than 4, 8 and 16).
+const void *compact_kernel(bool whole);
 
 }  // namespace isoq

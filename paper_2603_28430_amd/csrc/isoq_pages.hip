@@ -9,8 +9,6 @@
 // with all of them it is 3.7.  One of 1,000 positions 5 us (8.4 a call).
 #include "isoq_pages.h"
 
-#include <type_traits>
-
 #include "isoq_device.h"
 
 namespace isoq {
@@ -54,17 +52,80 @@ __global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a)
     }
 }
 
-// One chain of one head of one sequence, kTile positions at a time in order.
-// In place: position i takes what was at keep[i] >= i, and keep ascends, so a
-// tile's stores (positions i) can only meet sources of its own or of earlier
+// A 16-byte unit, or less, at any address: global memory takes unaligned accesses.
+template <typename T>
+struct Unaligned {
+    T v;
+} __attribute__((packed));
+
+template <typename T>
+__device__ __forceinline__ T load_at(const uint8_t *p) { return reinterpret_cast<const Unaligned<T> *>(p)->v; }
+template <typename T>
+__device__ __forceinline__ void store_at(uint8_t *p, T v) { reinterpret_cast<Unaligned<T> *>(p)->v = v; }
+
+// 16 NU + tail bytes (tail below 16) of a position, held in registers; calls with a
+// constant tail have the conditions resolved.
+template <int NU>
+struct Bytes {
+    u32x4 unit[NU > 0 ? NU : 1];
+    u32x2 t8;
+    uint32_t t4, t2, t1;
+    __device__ __forceinline__ void load(const uint8_t *p, int tail)
+    {
+#pragma unroll
+        for (int u = 0; u < NU; u++)
+            unit[u] = load_at<u32x4>(p + 16 * u);
+        p += 16 * NU;
+        if (tail & 8)   // (uniform, as the others)
+            t8 = load_at<u32x2>(p);
+        if (tail & 4)
+            t4 = load_at<uint32_t>(p + (tail & 8));
+        if (tail & 2)
+            t2 = load_at<uint16_t>(p + (tail & 12));
+        if (tail & 1)
+            t1 = p[tail & 14];
+    }
+    __device__ __forceinline__ void store(uint8_t *p, int tail) const
+    {
+#pragma unroll
+        for (int u = 0; u < NU; u++)
+            store_at(p + 16 * u, unit[u]);
+        p += 16 * NU;
+        if (tail & 8)
+            store_at(p, t8);
+        if (tail & 4)
+            store_at(p + (tail & 8), t4);
+        if (tail & 2)
+            store_at(p + (tail & 12), (uint16_t)t2);
+        if (tail & 1)
+            p[tail & 14] = (uint8_t)t1;
+    }
+    __device__ __forceinline__ void arrived(int tail)   // a use of every register: what was loaded is there
+    {
+#pragma unroll
+        for (int u = 0; u < NU; u++)
+            asm volatile("" : "+v"(unit[u])::"memory");
+        if (tail & 8)
+            asm volatile("" : "+v"(t8)::"memory");
+        if (tail & 4)
+            asm volatile("" : "+v"(t4)::"memory");
+        if (tail & 2)
+            asm volatile("" : "+v"(t2)::"memory");
+        if (tail & 1)
+            asm volatile("" : "+v"(t1)::"memory");
+    }
+};
+
+// One chain of one head of one sequence, PER positions a lane at a time, in
+// order.  In place: position i takes what was at keep[i] >= i, and keep ascends,
+// so a tile's stores (positions i) can only meet sources of its own or of earlier
 // tiles (those of later ones are at keep[j] >= j > i).  The tile's loads have
 // arrived before any of its stores (the wait and the barrier); the next tile's
 // loads need not wait for them.
-constexpr int kPerLane = 4, kTile = kCompactThreads * kPerLane;
-
-template <typename T>
-__device__ __forceinline__ void compact_chain(const CompactArgs &a, uint8_t *base, int64_t bstride, int64_t pstride)
+template <int NU, int PER>
+__device__ __forceinline__ void compact_chain(const CompactArgs &a, uint8_t *base, int64_t bstride, int64_t pstride, int tail)
 {
+    constexpr int TILE = kCompactThreads * PER;
     const int s = blockIdx.y, n = min(max(a.n_keep[s], 0), a.max_keep);
     const int32_t *keep = a.keep + ((int64_t)s * a.keep_heads + (a.keep_heads == 1 ? 0 : blockIdx.x)) * a.max_keep;
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
@@ -79,17 +140,17 @@ __device__ __forceinline__ void compact_chain(const CompactArgs &a, uint8_t *bas
         int32_t blk = table[bi];
         ok = ok && blk >= 0 && blk < a.n_blocks;
         blk = ok ? blk : 0;
-        return reinterpret_cast<T *>(base + blk * bstride + (int64_t)(pos - bi * a.block_size) * pstride);
+        return base + blk * bstride + (int64_t)(pos - bi * a.block_size) * pstride;
     };
-    T *src[kPerLane], *dst[kPerLane];
-    bool ok[kPerLane];
+    uint8_t *src[PER], *dst[PER];
+    bool ok[PER];
     auto places = [&](int i0) {
-        int32_t from[kPerLane];
+        int32_t from[PER];
 #pragma unroll
-        for (int e = 0; e < kPerLane; e++)
+        for (int e = 0; e < PER; e++)
             from[e] = keep[min(i0 + e * kCompactThreads + (int)threadIdx.x, n - 1)];
 #pragma unroll
-        for (int e = 0; e < kPerLane; e++) {
+        for (int e = 0; e < PER; e++) {
             const int i = i0 + e * kCompactThreads + (int)threadIdx.x;
             ok[e] = i < n && from[e] != i;
             dst[e] = at((uint32_t)i, ok[e]);
@@ -99,30 +160,33 @@ __device__ __forceinline__ void compact_chain(const CompactArgs &a, uint8_t *bas
     if (n == 0)
         return;
     places(0);
-    for (int i0 = 0; i0 < n; i0 += kTile) {
-        using R = std::conditional_t<(sizeof(T) < 4), uint32_t, T>;
-        R x[kPerLane];
-        T *to[kPerLane];
-        bool on[kPerLane];
+    for (int i0 = 0; i0 < n; i0 += TILE) {
+        Bytes<NU> x[PER];
+        uint8_t *to[PER];
+        bool on[PER];
 #pragma unroll
-        for (int e = 0; e < kPerLane; e++) {
-            x[e] = *src[e];
+        for (int e = 0; e < PER; e++) {
+            x[e].load(src[e], tail);
             to[e] = dst[e];
             on[e] = ok[e];
         }
-        if (n - i0 > kTile)
-            places(i0 + kTile);
+        if (n - i0 > TILE)
+            places(i0 + TILE);
 #pragma unroll
-        for (int e = 0; e < kPerLane; e++)
-            asm volatile("" : "+v"(x[e])::"memory");   // the loads have arrived
+        for (int e = 0; e < PER; e++)
+            x[e].arrived(tail);
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kPerLane; e++)
+        for (int e = 0; e < PER; e++)
             if (on[e])
-                *to[e] = (T)x[e];
+                x[e].store(to[e], tail);
     }
 }
 
+// WHOLE: caches of records stored whole.  (A kernel of its own: its 80 registers
+// would leave the other, of half as many, one workgroup a compute unit instead of
+// two, and 56 us instead of 48 for 8 x 32 heads x 8,192 positions.)
+template <bool WHOLE>
 __global__ __launch_bounds__(kCompactThreads) void compact_positions_kernel(const CompactArgs a)
 {
     int c = 0;
@@ -130,18 +194,30 @@ __global__ __launch_bounds__(kCompactThreads) void compact_positions_kernel(cons
         c++;
     uint8_t *base = a.base[c] + blockIdx.x * a.head_stride[c] + ((int)blockIdx.z - a.first[c]) * a.step[c];
     const int64_t bs = a.block_stride[c], ps = a.pos_stride[c];
-    switch (a.width[c]) {
-    case 16: compact_chain<u32x4>(a, base, bs, ps); break;
-    case 8: compact_chain<u32x2>(a, base, bs, ps); break;
-    case 4: compact_chain<uint32_t>(a, base, bs, ps); break;
-    case 2: compact_chain<uint16_t>(a, base, bs, ps); break;
-    default: compact_chain<uint8_t>(a, base, bs, ps); break;
+    switch (const int width = a.width[c]; width) {   // (uniform) the cache layout's own widths first
+    case 4: compact_chain<0, 4>(a, base, bs, ps, 4); break;
+    case 8: compact_chain<0, 4>(a, base, bs, ps, 8); break;
+    case 16: compact_chain<1, 4>(a, base, bs, ps, 0); break;
+    default:
+        if constexpr (WHOLE) {
+            switch (width >> 4) {
+            case 0: compact_chain<0, 4>(a, base, bs, ps, width & 15); break;
+            case 1: compact_chain<1, 4>(a, base, bs, ps, width & 15); break;
+            case 2: compact_chain<2, 2>(a, base, bs, ps, width & 15); break;
+            case 3: compact_chain<3, 2>(a, base, bs, ps, width & 15); break;
+            case 4: compact_chain<4, 2>(a, base, bs, ps, 0); break;
+            }
+        }
     }
 }
 
 }  // namespace
 
 const void *copy_blocks_kernel() { return reinterpret_cast<const void *>(&copy_kernel); }
-const void *compact_kernel() { return reinterpret_cast<const void *>(&compact_positions_kernel); }
+const void *compact_kernel(bool whole)
+{
+    return whole ? reinterpret_cast<const void *>(&compact_positions_kernel<true>)
+                 : reinterpret_cast<const void *>(&compact_positions_kernel<false>);
+}
 
 }  // namespace isoq

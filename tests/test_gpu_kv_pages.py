@@ -120,6 +120,32 @@ def test_compact(variant, d, bits, heads, bs, values, m, per_head):
     run_compact(c, table, lists(rng, 4, heads if per_head else 1, lens, 150, n_keep), n_keep, bs)
 
 
+@pytest.mark.parametrize("variant,d,bits,m", [("2d", 80, 3, 64), ("full", 100, 3, 0), ("full", 160, 3, 128), ("2d", 98, 4, 0),
+                                              ("fast", 1000, 3, 0), ("2d", 7, 3, 0), ("2d", 1, 2, 0), ("fast", 80, 2, 64),
+                                              ("full", 96, 3, 128), ("2d", 250, 2, 0), ("full", 172, 3, 0)])
+def test_compact_many_heads(variant, d, bits, m):
+    """Sequences and heads that fill the card: records stored whole (1 to 375
+    bytes, with every remainder of 64 and 16 bytes) move as few chains."""
+    rng = np.random.default_rng(d + bits)
+    lens, heads, bs = [130, 40, 7], 22, 7
+    per = -(-130 // bs)
+    c = Caches(variant, d, bits, 3 * per + 1, heads, bs, True, m, seed=d)
+    table = rng.permutation(3 * per + 1)[:3 * per].reshape(3, per).astype(np.int32)
+    n_keep = np.array([61, 40, 3], np.int32)
+    run_compact(c, table, lists(rng, 3, heads, lens, 70, n_keep), n_keep, bs)
+
+
+def test_compact_long_whole_records():
+    """More than one tile of a workgroup's positions, 2 and 4 a lane, in place."""
+    rng = np.random.default_rng(1)
+    for d, bits in ((80, 3), (160, 3), (100, 2)):
+        per, heads = 626, 70
+        c = Caches("full", d, bits, per, heads, 16, seed=d)
+        table = rng.permutation(per).reshape(1, per).astype(np.int32)
+        n_keep = np.array([9003], np.int32)
+        run_compact(c, table, lists(rng, 1, heads, [10000], 9003, n_keep), n_keep, 16)
+
+
 @pytest.mark.parametrize("length,count", [(9001, 8999), (9001, 4097), (20000, 8192), (4097, 4096), (13000, 12999)])
 def test_compact_long(length, count):
     """Lists around and past a workgroup's 4,096 positions, nearly everything kept among them."""
