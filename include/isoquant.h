@@ -441,8 +441,7 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
  *   k_idx .. k_gamma, n_blocks, block_size  the cache, laid out as in
  *               isoq_kv_append (records 16-byte aligned).
  * Limits: n_pairs < 2^24, n_blocks * block_size < 2^31, and a block of one array is
- * at most 2^27 accesses of 16 bytes (of 4, or 1, where its size asks for it).
- * n_pairs = 0 is a no-op.
+ * at most 2^31 bytes.  n_pairs = 0 is a no-op.
  */
 isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, const int32_t *block_pairs,
                                 int64_t n_pairs, int n_heads, uint8_t *k_idx, float *k_rho, uint8_t *v_idx,

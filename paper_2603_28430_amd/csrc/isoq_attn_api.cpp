@@ -301,19 +301,26 @@ isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, co
     for (int c = 0; c < pl.n; c++) {
         a.plane[c] = pl.base[c];
         a.stride[c] = pl.row[c] * n_heads * block_size;
-        a.unit[c] = a.stride[c] % 16 == 0 && aligned(pl.base[c], 16) ? 16 : a.stride[c] % 4 == 0 ? 4 : 1;
-        most = std::max(most, (a.stride[c] / a.unit[c] + kCopyUnits - 1) / kCopyUnits);
+        a.unit[c] = a.stride[c] >= 16 ? 16 : a.stride[c] % 4 == 0 ? 4 : 1;
+        const int64_t units = (a.stride[c] + a.unit[c] - 1) / a.unit[c];
+        if (units > 1 << 27)
+            return ISOQ_E_UNSUPPORTED;
+        a.units[c] = (int32_t)units;
+        a.div_units[c] = make_fastdiv((uint32_t)units);
+        most = std::max(most, (n_pairs * units + kCopyUnits - 1) / kCopyUnits);
     }
-    if (most > 65535)
+    const int64_t deep = (most + kCopyGrid - 1) / kCopyGrid;
+    if (deep > 65535)
         return ISOQ_E_UNSUPPORTED;
+    a.n_pairs = n_pairs;
     a.pairs = block_pairs;
     a.n_blocks = n_blocks;
     st = check_device(pk);
     if (st != ISOQ_OK)
         return st;
     void *args[] = {&a};
-    return launch_lds(copy_blocks_kernel(), dim3((unsigned)n_pairs, (unsigned)pl.n, (unsigned)most), 256, args, 0,
-                      stream);
+    return launch_lds(copy_blocks_kernel(), dim3((unsigned)std::min<int64_t>(most, kCopyGrid), (unsigned)pl.n, (unsigned)deep),
+                      256, args, 0, stream);
 }
 
 isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const int32_t *keep, int keep_heads,

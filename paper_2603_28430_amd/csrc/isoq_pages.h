@@ -11,12 +11,15 @@ constexpr int kCachePlanes = 6;   // K and V records and norms, signs, gamma
 struct CopyArgs {
     uint8_t *plane[kCachePlanes];
     int64_t stride[kCachePlanes];   // bytes of a cache block
-    int32_t unit[kCachePlanes];     // bytes per access (16, 4 or 1): divides the stride and the plane's address
+    int32_t unit[kCachePlanes];     // bytes per access (16, 4 or 1; a block has one at least)
+    int32_t units[kCachePlanes];    // accesses per block
+    FastDiv div_units[kCachePlanes];
     const int32_t *pairs;           // [n_pairs][2] source, destination
-    int64_t n_blocks;
+    int64_t n_pairs, n_blocks;
 };
-// Grid (pairs, planes, runs of kCopyUnits accesses of a block), 256 threads.
-constexpr int kCopyUnits = 2048;
+// Grid (workgroups of kCopyUnits accesses of all pairs, planes, the same past
+// kCopyGrid), 256 threads.
+constexpr int kCopyUnits = 2048, kCopyGrid = 1 << 20;
 const void *copy_blocks_kernel();
 
 // What moves when a sequence is compacted: a chain is `width` bytes of every

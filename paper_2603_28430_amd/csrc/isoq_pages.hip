@@ -3,7 +3,8 @@
 // call's launch the small ones.
 //
 // d = 128, 3 bits: 4,096 blocks of 32 heads x 16 positions (436 MB read and
-// written) 89 us, 4.9 TB/s; 16 blocks of 8 heads 3 us (7.4 a call).  8 sequences of
+// written) 86 us, 5.0 TB/s; 16 blocks of 8 heads 4 us (7.5 a call); 20,000 blocks of
+// one head 17 us, 3.8 TB/s.  8 sequences of
 // 32,768 positions compacted to half of them, chosen at random for each of 8 heads
 // (174 MB), 71 us, 2.5 TB/s: of the 64-byte lines that are read half stays, and
 // with all of them it is 3.7.  One of 1,000 positions 5 us (8.4 a call).
@@ -13,44 +14,6 @@
 
 namespace isoq {
 namespace {
-
-// Workgroup (pair, plane, run of kCopyUnits accesses): every lane's loads go out
-// before its stores.
-template <typename T>
-__device__ __forceinline__ void copy_run(const uint8_t *src, uint8_t *dst, int64_t units, int64_t u0)
-{
-    constexpr int N = kCopyUnits / 256;
-    T x[N];
-#pragma unroll
-    for (int i = 0; i < N; i++) {   // (past the end: the last one again, not stored)
-        const int64_t u = min(u0 + 256 * i + (int64_t)threadIdx.x, units - 1);
-        x[i] = __builtin_nontemporal_load(reinterpret_cast<const T *>(src) + u);
-    }
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int64_t u = u0 + 256 * i + threadIdx.x;
-        if (u < units)
-            __builtin_nontemporal_store(x[i], reinterpret_cast<T *>(dst) + u);
-    }
-}
-
-__global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a)
-{
-    const int c = blockIdx.y;
-    const int64_t stride = a.stride[c], units = stride / a.unit[c], u0 = (int64_t)blockIdx.z * kCopyUnits;
-    if (u0 >= units)
-        return;
-    const int32_t from = a.pairs[2 * (int64_t)blockIdx.x], to = a.pairs[2 * (int64_t)blockIdx.x + 1];
-    if (from < 0 || from >= a.n_blocks || to < 0 || to >= a.n_blocks || from == to)
-        return;
-    const uint8_t *src = a.plane[c] + from * stride;
-    uint8_t *dst = a.plane[c] + to * stride;
-    switch (a.unit[c]) {
-    case 16: copy_run<u32x4>(src, dst, units, u0); break;
-    case 4: copy_run<uint32_t>(src, dst, units, u0); break;
-    default: copy_run<uint8_t>(src, dst, units, u0); break;
-    }
-}
 
 // A 16-byte unit, or less, at any address: global memory takes unaligned accesses.
 template <typename T>
@@ -62,6 +25,55 @@ template <typename T>
 __device__ __forceinline__ T load_at(const uint8_t *p) { return reinterpret_cast<const Unaligned<T> *>(p)->v; }
 template <typename T>
 __device__ __forceinline__ void store_at(uint8_t *p, T v) { reinterpret_cast<Unaligned<T> *>(p)->v = v; }
+
+// kCopyUnits accesses of a plane, pair after pair: small blocks share a workgroup
+// (one of their own cost more in launches than the copy: 20,000 blocks of 16
+// positions of one head, d = 128, 3 bits, 80 us).  A block that is no multiple of 16
+// bytes ends with an access that overlaps the one before.  Every lane's loads go out
+// before its stores.
+template <typename T>
+__device__ __forceinline__ void copy_run(const CopyArgs &a, int c)
+{
+    typedef T Any __attribute__((aligned(1)));
+    constexpr int N = kCopyUnits / 256;
+    const uint32_t units = (uint32_t)a.units[c];
+    const uint64_t first = ((uint64_t)blockIdx.z * gridDim.x + blockIdx.x) * kCopyUnits, total = (uint64_t)a.n_pairs * units;
+    if (first >= total)
+        return;
+    const uint32_t count = (uint32_t)min((uint64_t)kCopyUnits, total - first);
+    const uint64_t pair0 = first / units;
+    const uint32_t unit0 = (uint32_t)(first - pair0 * units);
+    const int64_t stride = a.stride[c];
+    uint8_t *const base = a.plane[c];
+    T x[N];
+    uint8_t *dst[N];
+    bool ok[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {   // (past the end: the last one again, not stored)
+        const uint32_t j = 256 * i + threadIdx.x, at = unit0 + min(j, count - 1), pair = fast_div(at, a.div_units[c]);
+        const int32_t *fromto = a.pairs + 2 * (pair0 + pair);
+        const int32_t from = fromto[0], to = fromto[1];
+        const bool here = from >= 0 && from < a.n_blocks;
+        ok[i] = j < count && here && to >= 0 && to < a.n_blocks && from != to;
+        const int64_t offset = min((int64_t)(at - pair * units) * (int64_t)sizeof(T), stride - (int64_t)sizeof(T));
+        dst[i] = base + (ok[i] ? to : 0) * stride + offset;
+        x[i] = __builtin_nontemporal_load(reinterpret_cast<const Any *>(base + (here ? from : 0) * stride + offset));
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (ok[i])
+            __builtin_nontemporal_store(x[i], reinterpret_cast<Any *>(dst[i]));
+}
+
+__global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a)
+{
+    const int c = blockIdx.y;
+    switch (a.unit[c]) {
+    case 16: copy_run<u32x4>(a, c); break;
+    case 4: copy_run<uint32_t>(a, c); break;
+    default: copy_run<uint8_t>(a, c); break;
+    }
+}
 
 // 16 NU + tail bytes (tail below 16) of a position, held in registers; calls with a
 // constant tail have the conditions resolved.

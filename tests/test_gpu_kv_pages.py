@@ -63,6 +63,22 @@ def test_copy_blocks(variant, d, bits, heads, bs, values, m):
     c.check(want)
 
 
+@pytest.mark.parametrize("variant,d,bits,heads,bs,n", [("2d", 80, 3, 1, 3, 3000), ("2d", 7, 3, 1, 1, 5000), ("full", 128, 3, 1, 16, 2500),
+                                                       ("2d", 1, 2, 1, 2, 9000), ("fast", 100, 3, 3, 13, 700)])
+def test_copy_many_small_blocks(variant, d, bits, heads, bs, n):
+    """Blocks of less than a workgroup's accesses, that end anywhere in them, and of less than 16 bytes."""
+    c = Caches(variant, d, bits, 2 * n + 5, heads, bs, True, 64 if d == 80 else 0, seed=d)
+    perm = np.random.default_rng(d).permutation(2 * n + 5)
+    pairs = np.stack([perm[:n], perm[n:2 * n]], 1).astype(np.int32)
+    pairs[5::97] = [-1, 3]
+    want = {k: v.copy() for k, v in c.host.items()}
+    good = pairs[pairs[:, 0] >= 0]
+    for v in want.values():
+        v[good[:, 1]] = v[good[:, 0]]
+    iq.isoq_kv_copy_blocks(c.p, torch.from_numpy(pairs).cuda(), **c.kw)
+    c.check(want)
+
+
 def test_copy_blocks_none():
     c = Caches("full", 128, 3, 4, 2, 16)
     iq.isoq_kv_copy_blocks(c.p, torch.zeros((0, 2), dtype=torch.int32, device="cuda"), **c.kw)
