@@ -75,12 +75,14 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // In fp16 at 384 / 512 / 640 / 768 / 1,024: two ragged chunks of up to 512 tokens and
     // 8,192 positions 231 / 220 / 254 / 253 / 234, two equal ones 308 / 303 / 334 / 337
     // / 318; 16 of up to 16 tokens and 4,096 positions 89 / 78 / 77 / 89 / 84; 8 prompts
-    // of 1,024 tokens 103 / 102 / 112 / 111 / 110: one round of workgroups.)
+    // of 1,024 tokens 103 / 102 / 112 / 111 / 110: one round of workgroups, which is
+    // three a compute unit at d = 64 (512 / 768 / 1,024: two ragged chunks 138 / 126 / 137,
+    // two equal ones 219 / 190 / 206, the 16 57 / 48 / 56).)
     // (Workgroups of 8 rows at 768 / 1,280 / 1,536: 8 x 8 heads, 4,096 positions 18 / 22 /
     // 22; 16 ragged x 8 x 4 of 5 tokens, mean of three 47 / 38 / 38; 4 ragged x 2 x 16, up
     // to 20,000 20 / 23 / 23; 8 ragged x 4 x 4 of 5 tokens, fp32 23 / 23 / 27.  Of 12: 8 x
     // 8 heads, 4,096 23 / 28 / 28, 8 ragged x 8, up to 8,000 34 / 35 / 35.)
-    const int64_t want = p.kern.parts                                          ? 512
+    const int64_t want = p.kern.parts                                          ? (pk->d <= 64 ? 768 : 512)
                          : n_seqs == 1 || pk->d > 128 || p.kern.rows == 12     ? 768
                          : p.kern.rows == 8                                    ? 1280
                                                                                : 1536;

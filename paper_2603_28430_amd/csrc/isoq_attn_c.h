@@ -25,7 +25,7 @@
 // longer.  (The query's lo in e4m3 too: 6% less, and lse off by 1e-6 to 2e-6.)
 // They take 303 to 338 us in different runs, 407 to 450 TFLOP/s of the definition's
 // operations (4 d a row and position), twice that of the matrix cores' own; 346 at
-// 4 bits, 298 at 2, 221 at d = 64.
+// 4 bits, 298 at 2, 190 at d = 64.
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
@@ -114,8 +114,11 @@ __device__ __forceinline__ i32x8 read_bytes32(const uint8_t *src)
 
 __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
 
+// (Up to d = 64 the registers allow three workgroups a compute unit, at 4 bits with
+// three of them spilled: 61 us instead of 71 for three ragged chunks of up to 300
+// tokens and 6,000 positions, 8 x 2 heads.)
 template <int D, int BITS, bool LO>
-__global__ __launch_bounds__(256, 2) void attn_c_kernel(const AttnArgs a)
+__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const AttnArgs a)
 {
     using C = AttnCShape<D, BITS, LO>;
     using S = typename C::S;
