@@ -51,7 +51,7 @@ def build(verbose: bool = False) -> str:
                 "isoq_generic_2d.hip", "isoq_generic_8d.hip", "isoq_qjl_append.hip", "isoq_packed.hip",
                 "isoq_packed_8d.hip", "isoq_packed_qjl.hip", "isoq_scores_generic.hip", "isoq_attn_generic.hip",
                 "isoq_attn_join.hip", "isoq_attn_m2.hip", "isoq_attn_m3.hip", "isoq_attn_m4.hip",
-                "isoq_attn_c.hip",                 "isoq_pages.hip"):
+                "isoq_attn_c.hip", "isoq_pages.hip"):
         jobs.append([HIPCC, *DEVICE_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o",
                      os.path.join(obj_dir, src + ".o")])
     for src in ("isoq_api.cpp", "isoq_attn_api.cpp", "isoq_host_params.cpp"):

@@ -23,7 +23,7 @@ struct AttnArgs {
     const void *q;               // [n_tokens][n_q_heads][d]
     void *out;                   // the same
     float *lse;                  // [n_tokens][n_q_heads], or null
-    float *part;                 // splits: sums of values [row][n_splits][width], row = token n_q_heads + head
+    float *part;                 // splits (or null: rows are finished by the kernel): sums of values [row][n_splits][width], row = token n_q_heads + head
     float *part_ml;              // splits: m, l [row][n_splits][2]
     const uint8_t *k_idx, *v_idx;
     const float *k_rho, *v_rho;
@@ -63,7 +63,7 @@ struct AttnKernel {
     const void *fn;
     size_t lds;
     int rows;
-    bool parts;   // leaves parts for the join even with one split
+    bool parts;   // the kernel of many rows
 };
 AttnKernel attn_m_kernel_b2(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b3(int d, int rows, bool f16);

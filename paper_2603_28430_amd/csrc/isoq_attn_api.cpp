@@ -31,6 +31,7 @@ struct AttnPlan {
     int64_t groups;    // workgroups per sequence and split
     int width, slots;  // rotated coordinates per row (a multiple of the slot), slots
     int chunk, n_splits;
+    bool join;         // the kernel leaves parts for a join
 };
 
 AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int n_seqs, int max_q_len, int n_q_heads,
@@ -87,17 +88,28 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
                          : p.kern.rows == 8                                    ? 1280
                                                                                : 1536;
     const int64_t blocks = p.groups * n_seqs;
-    const int64_t splits = p.max_pos <= 768 ? 1 : std::min<int64_t>((want + blocks - 1) / blocks, kAttnMaxSplits);
+    // In fp16 as many splits as fit one round, down to 128 positions each up to 768 and
+    // 256 past that: a tile takes a workgroup 4 us however few there are (32 tokens of
+    // one sequence, 8 x 4 heads, 700 positions: one split 51 us, of 256 30, of 128 25; 300
+    // tokens of 4 sequences: one 67, two 82; four of 64 tokens and 4,000, d = 64, 2 bits: of
+    // 512 39, of 384 50).
+    const bool short_many = p.kern.parts && p.max_pos <= 768;
+    const int64_t unit = short_many ? 128 : 256;
+    int64_t splits = p.kern.parts        ? std::max<int64_t>(1, want / blocks)
+                     : p.max_pos <= 768 ? 1
+                                         : (want + blocks - 1) / blocks;
+    splits = std::min<int64_t>(splits, kAttnMaxSplits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
-    chunk = std::max<int64_t>(256, (chunk + 255) / 256 * 256);
+    chunk = std::max<int64_t>(unit, (chunk + unit - 1) / unit * unit);
     p.chunk = (int)std::min<int64_t>(chunk, 0x7FFFFF00);
     p.n_splits = (int)std::max<int64_t>(1, (p.max_pos + p.chunk - 1) / p.chunk);
+    p.join = p.n_splits > 1 || (p.kern.parts && pk->variant == VAR_BLOCK8);
     return p;
 }
 
 size_t plan_bytes(const AttnPlan &p, int64_t n_tokens, int n_q_heads)
 {
-    return p.n_splits == 1 && !p.kern.parts ? 0 : sizeof(float) * (size_t)n_tokens * n_q_heads * p.n_splits * (p.width + 2);
+    return !p.join ? 0 : sizeof(float) * (size_t)n_tokens * n_q_heads * p.n_splits * (p.width + 2);
 }
 
 // Argument values of isoq_kv_attn that do not need its pointers.
@@ -214,7 +226,7 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
     a.q = q;
     a.out = out;
     a.lse = lse;
-    a.part = static_cast<float *>(workspace);
+    a.part = need ? static_cast<float *>(workspace) : nullptr;
     a.part_ml = need ? a.part + (size_t)n_tokens * n_q_heads * plan.n_splits * plan.width : nullptr;
     a.k_idx = k_idx;
     a.v_idx = v_idx;

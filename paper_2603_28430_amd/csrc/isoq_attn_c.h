@@ -595,7 +595,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         __syncthreads();
     }
 
-    // 6. the row's part, for the join
+    // 6. the row's part, for the join; or the row itself: a lane has four
+    //    consecutive coordinates at a time, a slot of the 4-D and 2-D rotations
     {
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
@@ -605,6 +606,30 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
     if (!on)
         return;
     const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, now - 14);
+    const float mref = m == -INFINITY ? m : m * f1;
+    if (!a.part) {   // (one split; 8-D slots are two lanes', and go through the join)
+        const float inv = l == 0.f ? 0.f : vs / l;
+        auto finish = [&](auto var) {
+            constexpr int VAR = decltype(var)::value;
+#pragma unroll
+            for (int c = 0; c < C::CT; c++)
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+                    if (D % 32 == 0 || 32 * c + 8 * b < D) {
+                        const float y[4] = {acc[c][4 * b] * inv, acc[c][4 * b + 1] * inv, acc[c][4 * b + 2] * inv,
+                                            acc[c][4 * b + 3] * inv};
+                        attn_emit<VAR, 4>(a, row, h, 8 * c + 2 * b + half, y);
+                    }
+        };
+        switch (a.variant) {   // (uniform)
+        case VAR_FULL: finish(std::integral_constant<int, VAR_FULL>{}); break;
+        case VAR_FAST: finish(std::integral_constant<int, VAR_FAST>{}); break;
+        case VAR_PLANAR2D: finish(std::integral_constant<int, VAR_PLANAR2D>{}); break;
+        }
+        if (half == 0 && a.lse)
+            a.lse[row] = attn_lse(mref, l);
+        return;
+    }
     float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 4 * half;
 #pragma unroll
     for (int c = 0; c < C::CT; c++)
@@ -615,7 +640,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                     f32x4{acc[c][4 * b] * vs, acc[c][4 * b + 1] * vs, acc[c][4 * b + 2] * vs, acc[c][4 * b + 3] * vs};
     if (half == 0) {
         float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
-        ml[0] = m == -INFINITY ? m : m * f1;
+        ml[0] = mref;
         ml[1] = l;
     }
 }

@@ -45,7 +45,7 @@ __device__ __forceinline__ int attn_chunk(const AttnArgs &a, const AttnSeq &sq)
     if (!a.even)
         return a.chunk;
     const uint32_t len = (uint32_t)min(max(sq.len, 0), a.cap), n = (uint32_t)a.n_splits;
-    return min(max(256, (int)((len + n - 1) / n + 63) & ~63), a.chunk);
+    return min(max(128, (int)((len + n - 1) / n + 63) & ~63), a.chunk);
 }
 
 // Slot j (SW coordinates) of row `row` (head hq of its token): the sum of
