@@ -9,8 +9,8 @@
 // the level digits picked four at a time by v_perm_b32.  The sum of values is
 // the same product the other way round: with w_t = p_t rho_vt,
 //     sum_t w_t c[idx_tj],
-// w as a 31-bit integer cut into four digits (in units of 2^-30 of the largest
-// norm of the tile, p <= 1) and the levels as two digits (fp16 queries: a level
+// w as a 31-bit integer cut into four digits (in units of 2^-30 of the row's
+// largest one in the tile) and the levels as two digits (fp16 queries: a level
 // within 2^-16 of the largest) or three (fp32: 2^-24); at 4 bits the digits of
 // the eight magnitudes, complemented for the negative ones.
 //
@@ -527,15 +527,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         const f32x4 krho = *reinterpret_cast<const f32x4 *>(norms + 4 * col);
-        f32x4 vrho = *reinterpret_cast<const f32x4 *>(norms + 64 + 4 * col);
-        // the unit of w: 2^-30 of the tile's largest norm; what the digit sums
-        // count: that times the levels' scale
-        const float vmax = row_max16(fmaxf(fmaxf(fabsf(vrho[0]), fabsf(vrho[1])), fmaxf(fabsf(vrho[2]), fabsf(vrho[3]))));
-        const int ve = __builtin_amdgcn_readfirstlane(head_exponent(vmax, 30));
-        const float vunit = __builtin_amdgcn_ldexpf(a.v_dig.scale, 8 - ve);   // (sums of digits in units of 256)
-#pragma unroll
-        for (int st = 0; st < 4; st++)
-            vrho[st] = __builtin_amdgcn_ldexpf(vrho[st], ve);
+        const f32x4 vrho = *reinterpret_cast<const f32x4 *>(norms + 64 + 4 * col);
 
         // 5. logits (in units of ln 2) of the lane's row and its four positions
         float val[NT][4];
@@ -596,8 +588,10 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                     val[nt][st] = ok && tb + kk < lim[nt] ? val[nt][st] : -INFINITY;
             }
         }
-        // 6. running maximum, weights, and their digits to LDS
-        float alpha[NT];
+        // 6. running maximum, weights, and their digits to LDS.  The unit of a row's
+        //    weights is 2^-30 of the largest of them: norms at positions that it
+        //    does not attend to, or with next to no p, leave it its bits
+        float alpha[NT], vunit[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
             float top = fmaxf(fmaxf(val[nt][0], val[nt][1]), fmaxf(val[nt][2], val[nt][3]));
@@ -606,14 +600,21 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             alpha[nt] = __builtin_amdgcn_exp2f(m[nt] - ref);
             m[nt] = top;
             uint32_t u[4];
-            float sum = 0.f, wsum = 0.f;
+            float sum = 0.f, wsum = 0.f, weights[4];
 #pragma unroll
             for (int st = 0; st < 4; st++) {
                 const float p = __builtin_amdgcn_exp2f(val[nt][st] - ref);
                 sum += p;
+                weights[st] = p * vrho[st];
+            }
+            const int ve = head_exponent(row_max16(fmaxf(fmaxf(fabsf(weights[0]), fabsf(weights[1])),
+                                                         fmaxf(fabsf(weights[2]), fabsf(weights[3])))), 30);
+            vunit[nt] = __builtin_amdgcn_ldexpf(a.v_dig.scale, 8 - ve);   // (sums of digits in units of 256)
+#pragma unroll
+            for (int st = 0; st < 4; st++) {
                 // balanced digits: each byte of x + 128 (in the three lower
                 // places), less 128
-                const float weight = __builtin_rintf(p * vrho[st]);
+                const float weight = __builtin_rintf(__builtin_amdgcn_ldexpf(weights[st], ve));
                 wsum += weight;
                 const int x = (int)weight;
                 u[st] = ((uint32_t)x + 0x00808080u) ^ 0x00808080u;
@@ -622,7 +623,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             if (odd_mask != 0 && tb + __builtin_ctzll(odd_mask) < lim[nt])
                 l[nt] = NAN;
             if constexpr (BITS == 4)
-                sw[nt] = fmaf(wsum, vunit, sw[nt] * alpha[nt]);
+                sw[nt] = fmaf(wsum, vunit[nt], sw[nt] * alpha[nt]);
             const uint32_t a01 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), a23 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
             const uint32_t b01 = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), b23 = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
             uint32_t *dst = wdig + nt * 256 + lane;   // [digit][row][position mod 16]
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                         const int lo = ((x[2][1] + x[1][2] + x[0][3]) << 8) + x[2][0] + x[1][1] + x[0][2];
                         f = fmaf((float)hi, 65536.f, (float)lo) * 256.f;
                     }
-                    acc[nt][c0 + j] = fmaf(f, vunit, acc[nt][c0 + j] * alpha[nt]);
+                    acc[nt][c0 + j] = fmaf(f, vunit[nt], acc[nt][c0 + j] * alpha[nt]);
                 }
             }
         };
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
             l[nt] = NAN;   // an infinity or NaN in the rotated query: no digits hold it
         if constexpr (BITS == 4) {
             // the levels' half offset (build_value_digits), the same for every
-            // coordinate; vunit is in units of 256
+            // coordinate; sw is in units of 256
             float y = sw[nt];
             y += dpp_f<DPP_QUAD_1032>(y);
             y += dpp_f<DPP_QUAD_2301>(y);
