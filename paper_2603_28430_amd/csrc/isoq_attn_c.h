@@ -13,8 +13,8 @@
 //            of them is a third product, in e4m3 and with the query in e4m3, which
 //            rounds it to 2.6%: lse is off by 6e-8 of its norm at 2 and 3 bits and
 //            3e-7 at 4 (by 2e-6 to 3e-6 without it).
-//   values   the weights w = p rho (p <= 1, in units of a power of two next to the
-//            tile's largest norm, up to 2^14) in fp16, the levels as above; what
+//   values   the weights w = p rho (in units of a power of two next to the row's
+//            largest, which is 2^8 .. 2^15) in fp16, the levels as above; what
 //            fp16 leaves of the weights is a second product, in e4m3 and with the
 //            levels in e4m3: outputs are off by 2.1e-4 to 2.2e-4 of their norm, what
 //            rounding them to fp16 alone takes; without it 2.9e-4 to 3.2e-4.
@@ -64,8 +64,9 @@ struct AttnCShape {
     static constexpr int RK = 4 * S::WC + 1;         // words of a key's raw record (odd: lanes are keys)
     static constexpr int RV = H::SW + 1;             // words of a value's raw record
     // LDS bytes: keys, and what fp16 left of them; values in fp16, e4m3; raw
-    // records; per tile parity the norms (K, V), the valid positions, the
-    // values' unit, and the first value and key whose norm is an infinity or NaN
+    // records; per tile parity the norms (K, V), the valid positions, the values'
+    // unit and half of their least norm in it, and the first key and value whose
+    // norm is an infinity or NaN
     static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROW8, kV8 = kV + 32 * CT * VROW,
                          kRawK = kV8 + 32 * CT * VROW8, kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV,
                          kTile = kNorm + 2 * 512;
@@ -219,9 +220,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         }
         rec.rho = rhos[crow];
     };
-    // the values' unit: norms below 2^unit; kept while the tile's largest norm
-    // is above 2^(unit - 4)
-    int unit = 0;
+    // the tiles' unit of values: norms below 2^tile_unit; kept while the tile's
+    // largest norm is above 2^(tile_unit - 4)
+    int tile_unit = 0;
     auto store_raw = [&](int t) {   // (waves 0 and 1) into tile t's places
         float *norm = reinterpret_cast<float *>(lds + C::kNorm + 512 * (t & 1));
         uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 32 * (t & 1));
@@ -255,17 +256,24 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const uint64_t odds = __builtin_amdgcn_ballot_w64(odd);
             if (odd)
                 rec.rho = 0.f;
-            float top = row_max16(rec.ok ? fabsf(rec.rho) : 0.f);
+            float top = row_max16(rec.ok ? fabsf(rec.rho) : 0.f), least = row_max16(rec.ok ? -fabsf(rec.rho) : -INFINITY);
 #pragma unroll
-            for (int o = 16; o < 64; o *= 2)
-                top = fmaxf(top, __shfl_xor(top, o));
-            const int e = __builtin_amdgcn_readfirstlane(top > 0.f ? __builtin_amdgcn_frexp_expf(top) : unit);
-            if (t == 0 || e > unit || e < unit - 4)
-                unit = e;
-            norm[64 + lane] = rec.ok ? __builtin_amdgcn_ldexpf(rec.rho, 14 - unit) : 0.f;
+            for (int half = 0; half < 2; half++)   // over the rows of 16 lanes
+#pragma unroll
+                for (float *v : {&top, &least}) {
+                    const uint32_t b = __float_as_uint(*v);
+                    const auto x = half == 0 ? __builtin_amdgcn_permlane16_swap(b, b, false, false)
+                                             : __builtin_amdgcn_permlane32_swap(b, b, false, false);
+                    *v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                }
+            const int e = __builtin_amdgcn_readfirstlane(top > 0.f ? __builtin_amdgcn_frexp_expf(top) : tile_unit);
+            if (t == 0 || e > tile_unit || e < tile_unit - 4)
+                tile_unit = e;
+            norm[64 + lane] = rec.ok ? __builtin_amdgcn_ldexpf(rec.rho, 14 - tile_unit) : 0.f;
             if (lane == 0) {
-                tile[2] = (uint32_t)unit;
-                tile[3] = odds ? __builtin_ctzll(odds) : 0x7FFFFFFF;
+                tile[2] = (uint32_t)tile_unit;
+                tile[5] = odds ? __builtin_ctzll(odds) : 0x7FFFFFFF;
+                tile[3] = __float_as_uint(__builtin_amdgcn_ldexpf(-least, 13 - tile_unit));
             }
         }
     };
@@ -334,8 +342,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
 #pragma unroll
         for (int e = 0; e < 16; e++)
             acc[c][e] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    int now = 0;   // the unit of acc
+    // the row: exponentials are relative to 2^ref, an integer next to the running
+    // maximum; acc is in units of 2^(unit - 14), in which the largest weight so far is
+    // `most` or up to 2^7 more
+    float ref = -INFINITY, l = 0.f, most = 0.f;
+    int unit = 0;
     if (D % 32 != 0) {   // coordinates past D: rows of zeros
         for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW / 4; i += 256)
             reinterpret_cast<uint32_t *>(lds + C::kV + D * C::VROW)[i] = 0u;
@@ -479,9 +490,17 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // 4. running maximum (in units of 1 / f1) and weights
+            // 4. running maximum (in units of 1 / f1) and weights, in the tile's unit.
+            //    Exponentials are 2^(logit - ref), ref an integer, so that rescalings
+            //    are exact.  Where the row's largest weight so far would lie below 2^8
+            //    or above 2^15 there, the row gets a unit of its own that brings it to
+            //    2^13 .. 2^14, so norms at positions that the row does not attend to, or
+            //    with next to no weight, cost it no bits, and a unit that falls cannot
+            //    overflow its sums.  Rare: a tile that raises ref has a weight of half
+            //    of its least norm at least.
             const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
-            const uint32_t ok0 = tile[0], ok1 = tile[1];
+            const u32x4 about = *reinterpret_cast<const u32x4 *>(tile);
+            const uint32_t ok0 = about[0], ok1 = about[1];
             const bool whole = (ok0 & ok1) == ~0u && tb + 64 <= lim_min;
 #pragma unroll
             for (int k = 0; k < 2; k++)
@@ -511,22 +530,52 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
 #pragma unroll
                 for (int e = 0; e < 16; e++)
                     top = fmaxf(top, st[k][e]);
-            {
-                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                top = fmaxf(m, fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])));
-            }
-            const float ref = (top == -INFINITY ? 0.f : top) * f1;
-            const int u = __builtin_amdgcn_readfirstlane((int)tile[2]);
-            const float alpha = __builtin_amdgcn_exp2f(fmaf(m, f1, -ref));
-            const float scale = __builtin_amdgcn_ldexpf(alpha, now - u);
-            m = top;
-            now = u;
-            if (__builtin_amdgcn_ballot_w64(scale != 1.f) != 0) {
+            auto both = [](float v) {   // the larger of the row's two lanes'
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+                return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            };
+            const float was = ref;
+            ref = fmaxf(ref, __builtin_ceilf(both(top) * f1));
+            const float base = ref == -INFINITY ? 0.f : ref;
+            const int tu = __builtin_amdgcn_readfirstlane((int)about[2]);
+            const int fall = (int)fmaxf(was - base, -1000.f);   // (there was nothing: -1000)
+            int move = most > 0.f ? fall + unit - tu : 0;   // of acc (or it is zero)
+            float up = -base, down = 1.f;
+            if (__builtin_amdgcn_ballot_w64(move != 0 || (most < 0x1p8f && ref > -INFINITY)) != 0) {
+                l = __builtin_amdgcn_ldexpf(l, fall);
+                const float before = __builtin_amdgcn_ldexpf(most, min(move, 100));
+                float large = ref > was ? __uint_as_float(about[3]) : 0.f;
+                auto off = [&] { return fmaxf(before, large) > 0x1p15f || fmaxf(before, large) < 0x1p8f; };
+                int shift = 0;   // of the tile's weights
+                if (__builtin_amdgcn_ballot_w64(off() && ref > -INFINITY) != 0) {
+                    large = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 2; k++)
+#pragma unroll
+                        for (int b = 0; b < 4; b++) {
+                            const f32x4 x = *reinterpret_cast<const f32x4 *>(norm + 64 + 32 * k + 8 * b);
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                large = fmaxf(large, fabsf(__builtin_amdgcn_exp2f(fmaf(st[k][4 * b + i], f1, -base)) * x[i]));
+                        }
+                    large = both(large);
+                    // (sums that would move by more than 2^100 keep their unit: the tile's weights are nothing next to them)
+                    if (off() && fmaxf(before, large) > 0.f)
+                        shift = move > 100 ? fall - move : min(14 - __builtin_amdgcn_frexp_expf(fmaxf(before, large)), 100);
+                }
+                unit = tu - shift;
+                move += shift;
+                most = fmaxf(__builtin_amdgcn_ldexpf(most, move), __builtin_amdgcn_ldexpf(large, shift));
+                const float scale = __builtin_amdgcn_ldexpf(1.f, min(move, 126));
 #pragma unroll
                 for (int c = 0; c < C::CT; c++)
 #pragma unroll
                     for (int e = 0; e < 16; e++)
                         acc[c][e] *= scale;
+                // (past 2^-60 the weights are zero in fp16 and e4m3 either way, and l keeps its small ones)
+                shift = max(shift, -60);
+                up += (float)shift;
+                down = __builtin_amdgcn_ldexpf(1.f, -shift);
             }
             float sum = 0.f;
             u32x4 p[4];   // positions 16 s .. 16 s + 15 (B's order)
@@ -539,7 +588,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                     float y[4];
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(st[k][4 * b + i], f1, -ref));
+                        const float e = __builtin_amdgcn_exp2f(fmaf(st[k][4 * b + i], f1, up));
                         sum += e;
                         y[i] = e * x[i];
                     }
@@ -555,8 +604,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                     }
                     pr[4 * k + b] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
                 }
-            l = fmaf(l, alpha, sum);
-            if (min((int)tile[3], (int)tile[4]) < lim - tb)
+            l = fmaf(sum, down, l);
+            if (min((int)tile[4], (int)tile[5]) < lim - tb)
                 l = NAN;
             // 5. O^T += V^T P^T, likewise
             const uint8_t *val = lds + C::kV + n32 * C::VROW + 16 * half;
@@ -605,8 +654,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         l = NAN;   // an infinity or NaN in the rotated query
     if (!on)
         return;
-    const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, now - 14);
-    const float mref = m == -INFINITY ? m : m * f1;
+    const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, unit - 14);
     if (!a.part) {   // (one split; 8-D slots are two lanes', and go through the join)
         const float inv = l == 0.f ? 0.f : vs / l;
         auto finish = [&](auto var) {
@@ -627,7 +675,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         case VAR_PLANAR2D: finish(std::integral_constant<int, VAR_PLANAR2D>{}); break;
         }
         if (half == 0 && a.lse)
-            a.lse[row] = attn_lse(mref, l);
+            a.lse[row] = attn_lse(ref, l);
         return;
     }
     float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 4 * half;
@@ -640,7 +688,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                     f32x4{acc[c][4 * b] * vs, acc[c][4 * b + 1] * vs, acc[c][4 * b + 2] * vs, acc[c][4 * b + 3] * vs};
     if (half == 0) {
         float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
-        ml[0] = mref;
+        ml[0] = ref;
         ml[1] = l;
     }
 }

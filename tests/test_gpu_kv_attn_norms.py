@@ -51,10 +51,11 @@ def run(w):
     check(out, lse, held)
 
 
-# (by digits 4, 8 and 12 rows a workgroup and more; width-generic)
+# (by digits 4, 8 and 12 rows a workgroup and more; in fp16; width-generic)
 KERNELS = [(128, 2, "f16", 3, 1), (128, 3, "f16", 2, 4), (128, 4, "f16", 3, 4), (64, 4, "f32", 3, 1), (96, 3, "f32", 2, 3),
            (80, 2, "f32", 12, 1), (256, 4, "f32", 3, 3), (192, 3, "f16", 5, 1), (512, 2, "f32", 3, 1), (128, 3, "f32", 9, 4),
-           (70, 3, "f16", 3, 2), (70, 4, "f32", 5, 1)]
+           (128, 2, "f16", 40, 1), (128, 3, "f16", 20, 2), (128, 4, "f16", 40, 4), (64, 3, "f16", 33, 1), (80, 4, "f16", 70, 2),
+           (96, 2, "f16", 9, 4), (70, 3, "f16", 3, 2), (70, 4, "f32", 5, 1)]
 
 
 @pytest.mark.parametrize("ratio", [1e6, 1e9, 1e13])
