@@ -401,7 +401,8 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
     p->lv = LevelDigits{};
     p->n_pass = 1;
     p->wide = false;
-    p->half_keys = p->attn_tables = false;
+    p->key_rest = kRestNone;
+    p->attn_tables = false;
     p->lv_offset = 0;
     if (decode_d(d)) {
         std::vector<LevelDigits> lv;
@@ -412,7 +413,8 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             p->lv = lv[0];
             build_value_digits(bits, p->levels, 2, p->vd[0]);
             build_value_digits(bits, p->levels, 3, p->vd[1]);
-            p->half_keys = build_half_levels(bits, p->levels, p->half) <= kHalfKeys;
+            const double left = build_half_levels(bits, p->levels, p->half);
+            p->key_rest = left <= kLeftNone ? kRestNone : left <= kLeftBytes ? kRestBytes : kRestHalves;
             // (a unit of 2^-23 of the largest level has to be a normal float, with room on both sides)
             const float top = p->levels[(1 << bits) - 1];
             p->attn_tables = !p->wide && top > 0x1p-96f && top < 0x1p96f;

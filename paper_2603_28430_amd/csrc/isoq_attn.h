@@ -68,9 +68,9 @@ struct AttnKernel {
 AttnKernel attn_m_kernel_b2(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b3(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b4(int d, int rows, bool f16);
-// Kernel of many rows (isoq_attn_c.h; fp16 queries, widths up to 128), the keys'
-// levels in one fp16 part (half_keys) or two; or {}.
-AttnKernel attn_c_kernel_for(int d, int bits, bool half_keys);
+// Kernel of many rows (isoq_attn_c.h; fp16 queries, widths up to 128), with what
+// fp16 leaves of the keys' levels in the form `rest` (kRestNone ..); or {}.
+AttnKernel attn_c_kernel_for(int d, int bits, int rest);
 // Join of the splits, 256 threads: up to kAttnJoinFew splits (few) grid (rows of
 // a sequence / (256 / slots), sequence), more (row, sequence); a row being query
 // head + n_q_heads token.

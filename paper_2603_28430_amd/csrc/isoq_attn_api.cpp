@@ -56,7 +56,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         // 256 / 103.  2 x 8 heads, 8,192: 24 28 / 33, 32 30 / 33, 48 39 / 38, 128 70
         // / 55.  4 x 4 heads, 8,192, d = 64, 4 bits: 32 25 / 24, 64 40 / 28.)
         if (f16 && rows >= 32) {
-            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, pk->half_keys);
+            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, pk->key_rest);
             if (many.fn)
                 p.kern = many;
         }

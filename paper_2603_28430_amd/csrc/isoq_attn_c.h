@@ -8,11 +8,13 @@
 //   logits   the rotated query in two parts, x = hi + lo with hi = fp16(x) and lo
 //            = fp16(x - hi), its row in units of a power of two that brings its
 //            largest coordinate to 8 .. 16; the levels as fp16 numbers in units
-//            for which they lie closest to them (off by 2e-7, 1e-5, 7e-5 of their
-//            root mean square at 2, 3, 4 bits).  At 3 and 4 bits what that leaves
-//            of them is a third product, in e4m3 and with the query in e4m3, which
-//            rounds it to 2.6%: lse is off by 6e-8 of its norm at 2 and 3 bits and
-//            3e-7 at 4 (by 2e-6 to 3e-6 without it).
+//            for which they lie closest to them (off by 1e-7, 6e-6, 4e-5 of their
+//            root mean square at 2, 3, 4 bits).  What that leaves of them is a
+//            third product (kRestNone ..): at 3 bits in e4m3 and with the query in
+//            e4m3, which rounds it to 2.6%, at 4 bits, and for codebooks that fp16
+//            holds as badly, in fp16.  lse is off by 5e-8 to 8e-8 of its norm, as
+//            in fp32 products (4 bits without the third product 2e-6 to 3e-6, with it
+//            in e4m3 3e-7 to 8e-7, for 318 us instead of 351).
 //   values   the weights w = p rho (in units of a power of two next to the row's
 //            largest, which is 2^8 .. 2^15) in fp16, the levels as above; what
 //            fp16 leaves of the weights is a second product, in e4m3 and with the
@@ -49,7 +51,7 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-template <int D, int BITS, bool LO>
+template <int D, int BITS, int REST>
 struct AttnCShape {
     using S = ScoreMShape<D, BITS, 0>;
     using H = AttnMShape<D, BITS, 1>;
@@ -57,7 +59,7 @@ struct AttnCShape {
     static constexpr int KS = S::NQ;                 // 16-coordinate steps of the logits' product (4 chunks of 4 NQ)
     static constexpr int KROW = 32 * KS + 16;        // bytes of a decoded key part
     static constexpr int K8 = (KS + 3) / 4;          // 64-coordinate steps of its correction
-    static constexpr int KROW8 = LO ? 64 * K8 + 16 : 0;   // bytes of what fp16 left of a key's levels, in e4m3
+    static constexpr int KROWR = REST == kRestBytes ? 64 * K8 + 16 : REST == kRestHalves ? KROW : 0;   // bytes of what fp16 left of a key's levels
     static constexpr int CT = (D + 31) / 32;         // 32-coordinate tiles of the values
     static constexpr int VROW = 2 * 64 + 16;         // bytes of a coordinate's 64 positions
     static constexpr int VROW8 = 64 + 16;            // and in e4m3
@@ -67,7 +69,7 @@ struct AttnCShape {
     // records; per tile parity the norms (K, V), the valid positions, the values'
     // unit and half of their least norm in it, and the first key and value whose
     // norm is an infinity or NaN
-    static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROW8, kV8 = kV + 32 * CT * VROW,
+    static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROWR, kV8 = kV + 32 * CT * VROW,
                          kRawK = kV8 + 32 * CT * VROW8, kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV,
                          kTile = kNorm + 2 * 512;
     static constexpr int loop_bytes() { return kTile + 2 * 32; }
@@ -118,10 +120,10 @@ __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(
 // (Up to d = 64 the registers allow three workgroups a compute unit, at 4 bits with
 // three of them spilled: 61 us instead of 71 for three ragged chunks of up to 300
 // tokens and 6,000 positions, 8 x 2 heads.)
-template <int D, int BITS, bool LO>
+template <int D, int BITS, int REST>
 __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const AttnArgs a)
 {
-    using C = AttnCShape<D, BITS, LO>;
+    using C = AttnCShape<D, BITS, REST>;
     using S = typename C::S;
     using H = typename C::H;
     constexpr int64_t RB = (int64_t)D * BITS / 8;
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         return nonfinite(qmax) ? 0.f : x;
     };
     u32x4 qh[C::KS], ql[C::KS];   // B of 16 places: 8 half + 0 .. 7
-    i32x8 q8[C::K8];              // in e4m3, of 64 places: 32 half + 0 .. 31
+    [[maybe_unused]] i32x8 q8[C::K8];   // in e4m3, of 64 places: 32 half + 0 .. 31
 #pragma unroll
     for (int st = 0; st < C::KS; st++) {
         f16x8 hi, lo;
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         qh[st] = __builtin_bit_cast(u32x4, hi);
         ql[st] = __builtin_bit_cast(u32x4, lo);
     }
-    if constexpr (LO) {
+    if constexpr (REST == kRestBytes) {
 #pragma unroll
         for (int st = 0; st < C::K8; st++)
 #pragma unroll
@@ -353,10 +355,10 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW8 / 4; i += 256)
             reinterpret_cast<uint32_t *>(lds + C::kV8 + D * C::VROW8)[i] = 0u;
     }
-    if (LO && C::KS % 4 != 0) {   // places past the keys'
+    if (REST == kRestBytes && C::KS % 4 != 0) {   // places past the keys'
         constexpr int words = (64 * C::K8 - 16 * C::KS) / 4;
         for (int i = threadIdx.x; i < 64 * words; i += 256)
-            reinterpret_cast<uint32_t *>(lds + C::kRest + (i / words) * C::KROW8 + 16 * C::KS)[i % words] = 0u;
+            reinterpret_cast<uint32_t *>(lds + C::kRest + (i / words) * C::KROWR + 16 * C::KS)[i % words] = 0u;
     }
     if (nt > 0 && w < 2)
         store_raw(0);
@@ -371,26 +373,32 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             for (int i = 0; i < S::WC; i++)
                 y[i] = src[i];
             uint8_t *dst = lds + C::kHalf + lane * C::KROW + w * 8 * S::NQ;
-            uint8_t *rest = lds + C::kRest + lane * C::KROW8 + w * 4 * S::NQ;
+            uint8_t *rest = lds + C::kRest + lane * C::KROWR + w * (REST == kRestHalves ? 8 : 4) * S::NQ;
             auto part = [&](auto nsc, int q0) {
                 constexpr int NS = decltype(nsc)::value;
-                uint32_t sel[NS], lo[NS];
+                uint32_t sel[NS];
+                [[maybe_unused]] uint32_t lo[NS];
                 attn_selectors<S, BITS, NS>(y, q0, sel);
 #pragma unroll
                 for (int j = 0; j < NS; j += 2) {
                     uint32_t x[4];
+                    [[maybe_unused]] uint32_t y[4];
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
                         const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
                         level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, x + 2 * k);
-                        if constexpr (LO)
+                        if constexpr (REST == kRestHalves)
+                            level_halves<BITS>(a.k_half.tab[4], a.k_half.tab[5], sel[j + k], inv, y + 2 * k);
+                        if constexpr (REST == kRestBytes)
                             lo[j + k] = level_bytes<BITS>(a.k_half.tab[3], sel[j + k], inv);
                     }
                     *reinterpret_cast<u32x4 *>(dst + 8 * (q0 + j)) = u32x4{x[0], x[1], x[2], x[3]};
+                    if constexpr (REST == kRestHalves)
+                        *reinterpret_cast<u32x4 *>(rest + 8 * (q0 + j)) = u32x4{y[0], y[1], y[2], y[3]};
                 }
-                if constexpr (LO && S::NQ % 4 == 0) {
+                if constexpr (REST == kRestBytes && S::NQ % 4 == 0) {
                     *reinterpret_cast<u32x4 *>(rest + 4 * q0) = u32x4{lo[0], lo[1], lo[2], lo[3]};
-                } else if constexpr (LO) {
+                } else if constexpr (REST == kRestBytes) {
 #pragma unroll
                     for (int j = 0; j < NS; j += 2)
                         *reinterpret_cast<u32x2 *>(rest + 4 * (q0 + j)) = u32x2{lo[j], lo[j + 1]};
@@ -454,20 +462,24 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 for (int e = 0; e < 16; e++)
                     st[k][e] = 0.f;
             const uint8_t *key = lds + C::kHalf + n32 * C::KROW + 16 * half;
-            const uint8_t *rest = lds + C::kRest + n32 * C::KROW8 + 32 * half;
+            const uint8_t *rest = lds + C::kRest + n32 * C::KROWR + (REST == kRestHalves ? 16 : 32) * half;
             u32x4 kh[2][2];
+            [[maybe_unused]] u32x4 kr[2][2];
             auto read_keys = [&](int ks) {
 #pragma unroll
-                for (int k = 0; k < 2; k++)
+                for (int k = 0; k < 2; k++) {
                     kh[ks & 1][k] = *reinterpret_cast<const u32x4 *>(key + 32 * k * C::KROW + 32 * ks);
+                    if constexpr (REST == kRestHalves)
+                        kr[ks & 1][k] = *reinterpret_cast<const u32x4 *>(rest + 32 * k * C::KROW + 32 * ks);
+                }
             };
-            if constexpr (LO) {
+            if constexpr (REST == kRestBytes) {
                 i32x8 lo[2];
                 lo[0] = read_bytes32(rest);
 #pragma unroll
                 for (int i = 0; i < 2 * C::K8; i++) {   // step i / 2, positions 32 (i mod 2) ..
                     if (i + 1 < 2 * C::K8)
-                        lo[(i + 1) & 1] = read_bytes32(rest + 32 * ((i + 1) & 1) * C::KROW8 + 64 * ((i + 1) / 2));
+                        lo[(i + 1) & 1] = read_bytes32(rest + 32 * ((i + 1) & 1) * C::KROWR + 64 * ((i + 1) / 2));
                     else
                         read_keys(0);
                     __builtin_amdgcn_sched_barrier(0);
@@ -486,6 +498,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 for (int k = 0; k < 2; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(ql[ks]), st[k], 0, 0, 0);
 #pragma unroll
+                for (int k = 0; k < 2 && REST == kRestHalves; k++)
+                    st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kr[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
+#pragma unroll
                 for (int k = 0; k < 2; k++)
                     st[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_halves(kh[ks & 1][k]), as_halves(qh[ks]), st[k], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
@@ -501,6 +516,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
             const u32x4 about = *reinterpret_cast<const u32x4 *>(tile);
             const uint32_t ok0 = about[0], ok1 = about[1];
+            const int tu = __builtin_amdgcn_readfirstlane((int)about[2]), half_least = __builtin_amdgcn_readfirstlane((int)about[3]);
             const bool whole = (ok0 & ok1) == ~0u && tb + 64 <= lim_min;
 #pragma unroll
             for (int k = 0; k < 2; k++)
@@ -537,14 +553,13 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const float was = ref;
             ref = fmaxf(ref, __builtin_ceilf(both(top) * f1));
             const float base = ref == -INFINITY ? 0.f : ref;
-            const int tu = __builtin_amdgcn_readfirstlane((int)about[2]);
             const int fall = (int)fmaxf(was - base, -1000.f);   // (there was nothing: -1000)
             int move = most > 0.f ? fall + unit - tu : 0;   // of acc (or it is zero)
             float up = -base, down = 1.f;
             if (__builtin_amdgcn_ballot_w64(move != 0 || (most < 0x1p8f && ref > -INFINITY)) != 0) {
                 l = __builtin_amdgcn_ldexpf(l, fall);
                 const float before = __builtin_amdgcn_ldexpf(most, min(move, 100));
-                float large = ref > was ? __uint_as_float(about[3]) : 0.f;
+                float large = ref > was ? __int_as_float(half_least) : 0.f;
                 auto off = [&] { return fmaxf(before, large) > 0x1p15f || fmaxf(before, large) < 0x1p8f; };
                 int shift = 0;   // of the tile's weights
                 if (__builtin_amdgcn_ballot_w64(off() && ref > -INFINITY) != 0) {

@@ -5,41 +5,43 @@
 namespace isoq {
 namespace {
 
-template <int D, int BITS, bool LO>
+template <int D, int BITS, int REST>
 AttnKernel attn_c_entry()
 {
-    using C = AttnCShape<D, BITS, LO>;
-    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, LO>), (size_t)C::lds_bytes(), C::ROWS, true};
+    using C = AttnCShape<D, BITS, REST>;
+    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, REST>), (size_t)C::lds_bytes(), C::ROWS, true};
 }
 
-template <int D, bool LO>
+template <int D, int REST>
 AttnKernel attn_c_bits(int bits)
 {
     switch (bits) {
-    case 2: return attn_c_entry<D, 2, LO>();
-    case 3: return attn_c_entry<D, 3, LO>();
-    case 4: return attn_c_entry<D, 4, LO>();
+    case 2: return attn_c_entry<D, 2, REST>();
+    case 3: return attn_c_entry<D, 3, REST>();
+    case 4: return attn_c_entry<D, 4, REST>();
     }
     return {};
 }
 
-template <bool LO>
+template <int REST>
 AttnKernel attn_c_d(int d, int bits)
 {
     switch (d) {
-    case 64: return attn_c_bits<64, LO>(bits);
-    case 80: return attn_c_bits<80, LO>(bits);
-    case 96: return attn_c_bits<96, LO>(bits);
-    case 128: return attn_c_bits<128, LO>(bits);
+    case 64: return attn_c_bits<64, REST>(bits);
+    case 80: return attn_c_bits<80, REST>(bits);
+    case 96: return attn_c_bits<96, REST>(bits);
+    case 128: return attn_c_bits<128, REST>(bits);
     }
     return {};
 }
 
 }  // namespace
 
-AttnKernel attn_c_kernel_for(int d, int bits, bool half_keys)
+AttnKernel attn_c_kernel_for(int d, int bits, int rest)
 {
-    return half_keys ? attn_c_d<false>(d, bits) : attn_c_d<true>(d, bits);
+    return rest == kRestNone    ? attn_c_d<kRestNone>(d, bits)
+           : rest == kRestBytes ? attn_c_d<kRestBytes>(d, bits)
+                                : attn_c_d<kRestHalves>(d, bits);
 }
 
 }  // namespace isoq

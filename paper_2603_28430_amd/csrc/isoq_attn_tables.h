@@ -18,10 +18,11 @@ struct ValueDigits {
 
 // The codebook in fp16 for attention of many rows (isoq_attn_c.h): byte k of
 // tab[0] and tab[1] are the low and high byte of level k's fp16 value in units of
-// scale, of tab[2] its e4m3 value, and of tab[3] that of 2^kLevelRest times what
-// fp16 leaves of it.  At 4 bits of the positive level of magnitude k.
+// scale, of tab[2] its e4m3 value, of tab[3] that of 2^kLevelRest times what fp16
+// leaves of it, and of tab[4] and tab[5] the bytes of that in fp16.  At 4 bits of
+// the positive level of magnitude k.
 struct HalfLevels {
-    uint32_t tab[4][2];
+    uint32_t tab[6][2];
     float scale;
 };
 
@@ -33,8 +34,12 @@ void build_value_digits(int bits, const float *levels, int digits, ValueDigits &
 // leaves of them (the largest level is 1 .. 2).  Returns the most that it leaves
 // of a level, relative to it.
 double build_half_levels(int bits, const float *levels, HalfLevels &out);
-// Keys' levels as they are in fp16 where it holds them to this (isoq_attn_c.h).
-constexpr double kHalfKeys = 0x1p-20;
+// What is multiplied of what fp16 leaves of the keys' levels (isoq_attn_c.h):
+// nothing where that is 2^-20 of them at most; in e4m3, times the query in e4m3,
+// which leaves 2^-4.8 of it, where it is 2^-14.8 (Lloyd-Max levels of 3 bits: 2^-15);
+// else in fp16 (of 4 bits: 2^-11.8).
+enum { kRestNone, kRestBytes, kRestHalves };
+constexpr double kLeftNone = 0x1p-20, kLeftBytes = 0x1.2p-15;
 // (2^-11 at most, so 2^8 in e4m3, whose largest is 448)
 constexpr int kLevelRest = 19;
 

@@ -26,8 +26,8 @@ struct isoq_params {
     int n_pass;                     // sets in all
     bool wide;                      // the logits need all sets and digit products
     isoq::ValueDigits vd[2];          // levels as digits for the weighted sums of attention (fp16, fp32 queries)
-    isoq::HalfLevels half;            // and in fp16; half_keys: fp16 leaves next to nothing of them
-    bool half_keys;
+    isoq::HalfLevels half;            // and in fp16
+    int key_rest;                     // the form of what that leaves of the keys' (kRestNone ..)
     bool attn_tables;                 // these tables serve (else attention decodes by the fp32 levels)
 };
 

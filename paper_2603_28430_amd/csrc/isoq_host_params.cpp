@@ -663,7 +663,7 @@ double build_half_levels(int bits, const float *levels, HalfLevels &out)
         }
     }
     double off = 0;
-    uint8_t bytes[4][8] = {};
+    uint8_t bytes[6][8] = {};
     for (int i = 0; i < 8 && i < K; i++) {
         const int k = bits == 4 ? 8 + i : i;   // 4 bits: by magnitude
         const double u = std::ldexp((double)levels[k], -exp) / scale;
@@ -675,8 +675,11 @@ double build_half_levels(int bits, const float *levels, HalfLevels &out)
         bytes[1][i] = (uint8_t)(hi >> 8);
         bytes[2][i] = to_e4m3(u);
         bytes[3][i] = to_e4m3(std::ldexp(rest, kLevelRest));
+        const uint16_t lo = to_half(rest);
+        bytes[4][i] = (uint8_t)lo;
+        bytes[5][i] = (uint8_t)(lo >> 8);
     }
-    for (int t = 0; t < 4; t++)
+    for (int t = 0; t < 6; t++)
         std::memcpy(out.tab[t], bytes[t], 8);
     out.scale = (float)std::ldexp(scale, exp);
     return off;
