@@ -401,8 +401,7 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
     p->lv = LevelDigits{};
     p->n_pass = 1;
     p->wide = false;
-    p->key_rest = kRestNone;
-    p->attn_tables = false;
+    p->attn_by_tables = false;
     p->lv_offset = 0;
     if (decode_d(d)) {
         std::vector<LevelDigits> lv;
@@ -411,13 +410,9 @@ isoq_status isoq_params_init(isoq_params **out, int variant, int d, int bits, in
             while (layout.size() % 4)
                 layout.push_back(0.f);
             p->lv = lv[0];
-            build_value_digits(bits, p->levels, 2, p->vd[0]);
-            build_value_digits(bits, p->levels, 3, p->vd[1]);
-            const double left = build_half_levels(bits, p->levels, p->half);
-            p->key_rest = left <= kLeftNone ? kRestNone : left <= kLeftBytes ? kRestBytes : kRestHalves;
             // (a unit of 2^-23 of the largest level has to be a normal float, with room on both sides)
             const float top = p->levels[(1 << bits) - 1];
-            p->attn_tables = !p->wide && top > 0x1p-96f && top < 0x1p96f;
+            p->attn_by_tables = !p->wide && top > 0x1p-96f && top < 0x1p96f;
             p->n_pass = (int)lv.size();
             p->lv_offset = layout.size();
             const float *f = reinterpret_cast<const float *>(lv.data() + 1);

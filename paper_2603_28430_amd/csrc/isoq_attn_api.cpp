@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
 
 #include "isoq_attn.h"
 #include "isoq_handles.h"
@@ -23,9 +24,31 @@ constexpr int64_t kAttnMaxPos = 0x7FFFFFFF - 1023;
 // Kept positions: a workgroup's first one past them still fits 31 bits.
 constexpr int kCompactMaxKeep = 0x7FFFFFFF - 8191;
 
+// The handle's tables, made by the first call that asks for them; null if there is
+// no memory.  (Host threads that come first together all make them, the same ones,
+// and keep one.)
+const AttnTables *tables_of(const isoq_params *p)
+{
+    const AttnTables *held = p->attn_tables.load(std::memory_order_acquire);
+    if (held)
+        return held;
+    AttnTables *t = new (std::nothrow) AttnTables;
+    if (!t)
+        return nullptr;
+    build_value_digits(p->bits, p->levels, 2, t->vd[0]);
+    build_value_digits(p->bits, p->levels, 3, t->vd[1]);
+    const double left = build_half_levels(p->bits, p->levels, t->half);
+    t->key_rest = left <= kLeftNone ? kRestNone : left <= kLeftBytes ? kRestBytes : kRestHalves;
+    if (p->attn_tables.compare_exchange_strong(held, t, std::memory_order_acq_rel))
+        return t;
+    delete t;
+    return held;
+}
+
 // How a call is cut up; from its sizes alone, so that isoq_kv_attn_workspace
 // answers for the call that follows.
 struct AttnPlan {
+    const AttnTables *kt, *vt;   // null where the width-generic kernel runs, or without memory
     AttnKernel kern;   // fn null: the width-generic kernel, a row per workgroup
     int64_t max_pos;   // positions a sequence has at most
     int64_t groups;    // workgroups per sequence and split
@@ -45,7 +68,11 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     const bool f16 = dtype == ISOQ_F16;
     const int64_t rows = (int64_t)(n_q_heads / n_kv_heads) * max_q_len;
     p.groups = (int64_t)n_q_heads * max_q_len;
-    if (pk->attn_tables && pv->attn_tables) {
+    if (pk->attn_by_tables && pv->attn_by_tables) {
+        p.kt = tables_of(pk);
+        p.vt = tables_of(pv);
+        if (!p.kt || !p.vt)
+            return p;
         const int r = (int)std::min<int64_t>(rows, 1 << 20);
         p.kern = pk->bits == 2   ? attn_m_kernel_b2(pk->d, r, f16)
                  : pk->bits == 3 ? attn_m_kernel_b3(pk->d, r, f16)
@@ -56,7 +83,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         // 256 / 103.  2 x 8 heads, 8,192: 24 28 / 33, 32 30 / 33, 48 39 / 38, 128 70
         // / 55.  4 x 4 heads, 8,192, d = 64, 4 bits: 32 25 / 24, 64 40 / 28.)
         if (f16 && rows >= 32) {
-            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, pk->key_rest);
+            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, p.kt->key_rest);
             if (many.fn)
                 p.kern = many;
         }
@@ -213,6 +240,8 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
         return ISOQ_E_ALIGN;
     const AttnPlan plan =
         attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len);
+    if (pk->attn_by_tables && pv->attn_by_tables && !plan.kern.fn)
+        return ISOQ_E_NOMEM;
     const size_t need = plan_bytes(plan, n_tokens, n_q_heads);
     if (need > 0 && !workspace)
         return ISOQ_E_NULL;
@@ -266,9 +295,11 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
         a.v_lev[k] = pv->levels[k];
     }
     a.k_dig = pk->lv;
-    a.v_dig = pv->vd[dtype == ISOQ_F16 ? 0 : 1];
-    a.k_half = pk->half;
-    a.v_half = pv->half;
+    if (plan.kern.fn) {
+        a.v_dig = plan.vt->vd[dtype == ISOQ_F16 ? 0 : 1];
+        a.k_half = plan.kt->half;
+        a.v_half = plan.vt->half;
+    }
     void *args[] = {&a};
     const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(pk->variant, pk->bits);
     const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, pk->variant);

@@ -1,5 +1,5 @@
 // The codebook in the forms that attention multiplies with, built on the host
-// once per handle.
+// once per handle, by its first attention.
 #pragma once
 
 #include <cstdint>
@@ -42,5 +42,11 @@ enum { kRestNone, kRestBytes, kRestHalves };
 constexpr double kLeftNone = 0x1p-20, kLeftBytes = 0x1.2p-15;
 // (2^-11 at most, so 2^8 in e4m3, whose largest is 448)
 constexpr int kLevelRest = 19;
+
+struct AttnTables {
+    ValueDigits vd[2];   // of two digits (fp16 queries), three (fp32)
+    HalfLevels half;
+    int key_rest;        // the form of what fp16 leaves of the keys' (kRestNone ..)
+};
 
 }  // namespace isoq
