@@ -408,9 +408,11 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  * Limits: n_seqs <= 65535, n_tokens * n_q_heads < 2^31, max_q_len * n_q_heads <=
  * 2^23, max_blocks_per_seq * block_size <= 2^31 - 1024.
  * Arithmetic: logits, softmax statistics and sums in fp32 or in integers of 32
- * bits (see the kernels for what is rounded).  A query with an infinity or NaN
- * gives NaN in its row of out and lse, and so does a norm of k_rho or v_rho that
- * is one in the rows that attend to its position, not in others.  The result
+ * bits (see the kernels for what is rounded); a row's result is as exact as its
+ * own weights and norms allow, whatever norms stand at other positions.  A query
+ * with an infinity or NaN gives NaN in its row of out and lse if it attends to
+ * any position, and so does a norm of k_rho or v_rho that is one in the rows that
+ * attend to its position, not in others.  The result
  * does not depend on the order in which workgroups run.
  */
 isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,

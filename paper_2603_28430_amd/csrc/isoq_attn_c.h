@@ -665,8 +665,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
     }
-    if (nonfinite(qmax) && lim > 0)
-        l = NAN;   // an infinity or NaN in the rotated query
+    if (nonfinite(qmax) && l != 0.f)
+        l = NAN;   // an infinity or NaN in the rotated query (counted as zero till here), and a position
     if (!on)
         return;
     const float vs = __builtin_amdgcn_ldexpf(a.v_half.scale, unit - 14);

@@ -78,6 +78,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     const int groups = max(1, 256 / a.slots);
     const int vg = tid / a.slots, vj = tid - vg * a.slots;
     float acc[SW], m = -INFINITY, l = 0.f;
+    bool seen = false;   // a position that is there
 #pragma unroll
     for (int c = 0; c < SW; c++)
         acc[c] = 0.f;
@@ -104,6 +105,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
             pos = (int)((uint32_t)t - bi * a.block_size);
             ok = blk >= 0 && blk < a.n_blocks;
         }
+        seen |= ok;
         if (ok) {
             const CacheSrcRt rec = source(a.k_idx, blk, pos);
             float dot = 0.f;
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         sum[tid * SW + c] = acc[c];
     __syncthreads();
     l = (red[4] + red[5]) + (red[6] + red[7]);
-    if (odd && lim > 0)   // (all of its logits may be -inf: no NaN came up by itself)
+    if (odd && __syncthreads_or(seen))   // (odd is the same in all lanes; the logits may all be -inf: no NaN came up by itself)
         l = NAN;
     const float inv = a.n_splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
     for (int j = tid; j < a.slots; j += 256) {

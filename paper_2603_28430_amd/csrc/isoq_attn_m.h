@@ -721,8 +721,8 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         x += dpp_f<DPP_QUAD_2301>(x);
         x += dpp_f<DPP_ROW_HALF_MIRROR>(x);
         l[nt] = x + dpp_f<DPP_ROW_MIRROR>(x);
-        if (nonfinite(mx[8 * (4 * nt + kq)]) && lim[nt] > 0)
-            l[nt] = NAN;   // an infinity or NaN in the rotated query: no digits hold it
+        if (nonfinite(mx[8 * (4 * nt + kq)]) && l[nt] != 0.f)
+            l[nt] = NAN;   // an infinity or NaN in the rotated query, which no digits hold, and a position
         if constexpr (BITS == 4) {
             // the levels' half offset (build_value_digits), the same for every
             // coordinate; sw is in units of 256
