@@ -399,6 +399,8 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  *   max_len     positions of the longest sequence at most, as far as the host
  *               knows (max_blocks_per_seq * block_size if it does not): a closer
  *               bound cuts long caches into better splits.
+ *   scale       up to 2.35e38 in magnitude: it is used in units of ln 2, as a float
+ *               (larger ones, infinities and NaN are ISOQ_E_INVALID).
  *   lse         device, fp32 [n_tokens][n_q_heads], or NULL.
  *   workspace   device, at least isoq_kv_attn_workspace(...) bytes for the same
  *               arguments (16-byte aligned; may be NULL where that is 0).  Its

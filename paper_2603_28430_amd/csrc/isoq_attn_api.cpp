@@ -227,7 +227,8 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
                                 max_blocks_per_seq, max_len);
     if (st != ISOQ_OK)
         return st;
-    if (n_blocks < 0 || !std::isfinite(scale) || (!q_start && (n_tokens != n_seqs || max_q_len != 1)))
+    const float scale2 = (float)((double)scale * 1.4426950408889634);   // (logits in units of ln 2)
+    if (n_blocks < 0 || !std::isfinite(scale2) || (!q_start && (n_tokens != n_seqs || max_q_len != 1)))
         return ISOQ_E_INVALID;
     if (n_tokens == 0 || n_seqs == 0)
         return ISOQ_OK;
@@ -283,7 +284,7 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
     a.chunk = plan.chunk;
     a.n_splits = plan.n_splits;
     a.even = plan.kern.parts;
-    a.scale = (float)((double)scale * 1.4426950408889634);
+    a.scale = scale2;
     a.div_block = make_fastdiv((uint32_t)block_size);
     a.d = pk->d;
     a.width = plan.width;

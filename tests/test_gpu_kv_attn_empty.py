@@ -47,3 +47,17 @@ def test_queries_that_are_no_numbers_without_positions(d, bits, dtype, n, length
             del ref[t, 1]
     assert any(np.isinf(l) for _, l, _, _ in ref.values()) and any(not np.isinf(l) for _, l, _, _ in ref.values())
     check(out, lse, ref)
+
+
+@pytest.mark.parametrize("d", [128, 70])
+def test_scales_at_the_end_of_floats(d):
+    """A scale whose multiple in units of ln 2 is no float is refused; the largest others are not."""
+    w = setup("full", d, 3, "f16", [1, 1], 2, 2, 16, [40, 3], seed=1)
+    w["q"][:] = 0
+    args = device(w)
+    for bad in (2.4e38, -3.4e38):
+        with pytest.raises(iq.IsoqError):
+            iq.isoq_kv_attn(**args, scale=bad)
+    for good in (2.3e38, -2.3e38):
+        out, lse = iq.isoq_kv_attn(**args, scale=good)
+        check(out, lse, reference(w, good))
