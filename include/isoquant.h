@@ -460,7 +460,8 @@ isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, co
  * ceil(n_keep / block_size) on are free.
  *
  *   keep        device, int32 [n_seqs][keep_heads][max_keep], each list strictly
- *               ascending; keep_heads is n_heads, or 1: one list for all heads.
+ *               ascending, from 0 or more; keep_heads is n_heads, or 1: one list
+ *               for all heads.
  *   n_keep      device, int32 [n_seqs], entries of each list that count (cut to
  *               [0, max_keep]).
  *   block_table, max_blocks_per_seq  as in isoq_kv_scores.  The blocks of a
@@ -470,9 +471,9 @@ isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, co
  *               n_blocks), or lies outside the table, is skipped.
  *   pk, sk, k_idx .. k_gamma, n_heads, n_blocks, block_size  as in
  *               isoq_kv_copy_blocks.
- * Positions from n_keep[s] on keep their contents.  A list that does not ascend
- * strictly leaves the positions below its n_keep unspecified and touches nothing
- * else.  Limits: n_seqs <= 65535, n_heads < 2^22, max_keep <= 2^31 - 8192,
+ * Positions from n_keep[s] on keep their contents.  In a list that does not ascend
+ * strictly from 0 or more, entries with keep[s][h][i] < i are skipped too.
+ * Limits: n_seqs <= 65535, n_heads < 2^22, max_keep <= 2^31 - 8192,
  * max_blocks_per_seq * block_size < 2^31.
  */
 isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const int32_t *keep, int keep_heads,

@@ -129,9 +129,10 @@ struct Bytes {
 };
 
 // One chain of one head of one sequence, PER positions a lane at a time, in
-// order.  In place: position i takes what was at keep[i] >= i, and keep ascends,
-// so a tile's stores (positions i) can only meet sources of its own or of earlier
-// tiles (those of later ones are at keep[j] >= j > i).  The tile's loads have
+// order.  In place: position i takes what was at keep[i] if that is > i (= i stays,
+// and a list that ascends from 0 has none below), so a tile's stores (positions i)
+// can only meet sources of its own or of earlier tiles (those of later ones are at
+// keep[j] > j > i).  The tile's loads have
 // arrived before any of its stores (the wait and the barrier); the next tile's
 // loads need not wait for them.
 template <int NU, int PER>
@@ -164,7 +165,7 @@ __device__ __forceinline__ void compact_chain(const CompactArgs &a, uint8_t *bas
 #pragma unroll
         for (int e = 0; e < PER; e++) {
             const int i = i0 + e * kCompactThreads + (int)threadIdx.x;
-            ok[e] = i < n && from[e] != i;
+            ok[e] = i < n && from[e] > i;
             dst[e] = at((uint32_t)i, ok[e]);
             src[e] = at((uint32_t)from[e], ok[e]);
         }
