@@ -16,7 +16,7 @@
 //            in fp32 products (4 bits without the third product 2e-6 to 3e-6, with it
 //            in e4m3 3e-7 to 8e-7, for 318 us instead of 351).
 //   values   the weights w = p rho (in units of a power of two next to the row's
-//            largest, which is 2^8 .. 2^15) in fp16, the levels as above; what
+//            largest, which is 2^4 .. 2^15) in fp16, the levels as above; what
 //            fp16 leaves of the weights is a second product, in e4m3 and with the
 //            levels in e4m3: outputs are off by 2.1e-4 to 2.2e-4 of their norm, what
 //            rounding them to fp16 alone takes; without it 2.9e-4 to 3.2e-4.
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             acc[c][e] = 0.f;
     // the row: exponentials are relative to 2^ref, an integer next to the running
     // maximum; acc is in units of 2^(unit - 14), in which the largest weight so far is
-    // `most` or up to 2^7 more
+    // `most` or up to 2^11 more
     float ref = -INFINITY, l = 0.f, most = 0.f;
     int unit = 0;
     if (D % 32 != 0) {   // coordinates past D: rows of zeros
@@ -507,12 +507,16 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             }
             // 4. running maximum (in units of 1 / f1) and weights, in the tile's unit.
             //    Exponentials are 2^(logit - ref), ref an integer, so that rescalings
-            //    are exact.  Where the row's largest weight so far would lie below 2^8
+            //    are exact.  Where the row's largest weight so far would lie below 2^4
             //    or above 2^15 there, the row gets a unit of its own that brings it to
             //    2^13 .. 2^14, so norms at positions that the row does not attend to, or
             //    with next to no weight, cost it no bits, and a unit that falls cannot
             //    overflow its sums.  Rare: a tile that raises ref has a weight of half
-            //    of its least norm at least.
+            //    of its least norm at least.  (8 prompts of 1,024 tokens whose first
+            //    position takes most of half of the rows' weight: 264 us with a value
+            //    as large as the others or 1/50 of them, 291 with 1/500, where such
+            //    rows keep a unit of their own; 2^4 holds the weight that makes the
+            //    row to 2^-14 with its rest in e4m3.)
             const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
             const u32x4 about = *reinterpret_cast<const u32x4 *>(tile);
             const uint32_t ok0 = about[0], ok1 = about[1];
@@ -556,11 +560,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const int fall = (int)fmaxf(was - base, -1000.f);   // (there was nothing: -1000)
             int move = most > 0.f ? fall + unit - tu : 0;   // of acc (or it is zero)
             float up = -base, down = 1.f;
-            if (__builtin_amdgcn_ballot_w64(move != 0 || (most < 0x1p8f && ref > -INFINITY)) != 0) {
+            if (__builtin_amdgcn_ballot_w64(move != 0 || (most < 0x1p4f && ref > -INFINITY)) != 0) {
                 l = __builtin_amdgcn_ldexpf(l, fall);
                 const float before = __builtin_amdgcn_ldexpf(most, min(move, 100));
                 float large = ref > was ? __int_as_float(half_least) : 0.f;
-                auto off = [&] { return fmaxf(before, large) > 0x1p15f || fmaxf(before, large) < 0x1p8f; };
+                auto off = [&] { return fmaxf(before, large) > 0x1p15f || fmaxf(before, large) < 0x1p4f; };
                 int shift = 0;   // of the tile's weights
                 if (__builtin_amdgcn_ballot_w64(off() && ref > -INFINITY) != 0) {
                     large = 0.f;
