@@ -20,14 +20,19 @@
 //            fp16 leaves of the weights is a second product, in e4m3 and with the
 //            levels in e4m3: outputs are off by 2.1e-4 to 2.2e-4 of their norm, what
 //            rounding them to fp16 alone takes; without it 2.9e-4 to 3.2e-4.
-// An e4m3 product is half a fp16 product's time, and the matrix cores' power is what
-// holds the kernel back (their clock falls to 1.9 GHz; taking a fifth of the vector
-// instructions out, or waits of waves for each other, changed nothing): with
-// both corrections in fp16, 2 x 512 tokens at 8,192 positions, 3 bits, took 6%
-// longer.  (The query's lo in e4m3 too: 6% less, and lse off by 1e-6 to 2e-6.)
-// They take 303 to 338 us in different runs, 407 to 450 TFLOP/s of the definition's
-// operations (4 d a row and position), twice that of the matrix cores' own; 346 at
-// 4 bits, 298 at 2, 190 at d = 64.
+// An e4m3 product is half a fp16 product's time: with both corrections in fp16, 2 x
+// 512 tokens at 8,192 positions, 3 bits, took 6% longer (with the query's lo in e4m3
+// too 6% less, and lse off by 1e-6 to 2e-6).
+//
+// What bounds it.  Two equal chunks (2 x 512 tokens at 8,192 positions, 8 x 4 heads)
+// take 307 to 326 us at 3 bits, 400 to 430 TFLOP/s of the definition's operations (4 d
+// a row and position), twice that of the matrix cores' own, and 364 once such calls
+// have followed each other for some ms and the clock has fallen; 351 to 376 and 426 at
+// 4 bits; 274 at 2 and 197 at d = 64.  Matrix cores are busy for 42% of the cycles, vector
+// instructions issue in 50%, waves wait for 28%: the two waves of a SIMD overlap the
+// two kinds little.  (A fifth fewer vector instructions, and all four waves fetching
+// records, changed nothing when tried.)  Ragged chunks of up to 512 tokens are bound
+// by what unequal sequences leave idle as well: 30%, 40%, 31%.
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each

@@ -38,8 +38,11 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 // the workgroups of a few sequences of many rows busy to the end (two ragged
 // chunks of up to 512 tokens and 8,192 positions 185 us instead of 194, mean of six;
 // four of 128 and 4,096 88 instead of 98); with one to eight rows a key head they changed
-// nothing (16 ragged sequences of up to 8,192 positions 44 and 44 us, of others
-// 36 and 36).
+// nothing where the block table is as wide as the longest sequence (16 ragged sequences
+// of up to 8,192 positions 44 and 44 us, of others 36 and 36).  Where it is wider and the
+// caller gives no max_len, a.chunk is longer than the sequences need (16 sequences of
+// 8,192 positions, 8 x 4 heads, a table of 131,072: 86 us instead of 42, one sequence 22
+// instead of 11): even parts were not measured there.
 __device__ __forceinline__ int attn_chunk(const AttnArgs &a, const AttnSeq &sq)
 {
     if (!a.even)

@@ -4,7 +4,7 @@
 // Up to kAttnJoinFew splits (attn_join_few_kernel): a lane has a rotation slot of
 // a row, reads every split's m and l itself, and adds up; 256 / slots rows per
 // workgroup.  Bound by what it reads and writes (a chunk of 512 tokens, 32
-// heads, d = 128: n_splits x 8 MB; two of them in 3 splits 9 us), and by its
+// heads, d = 128: n_splits x 8 MB; two of them in 2 splits 9 to 11 us), and by its
 // launch where that is little (3 to 5 us).
 //
 // More (attn_join_kernel): one workgroup per row.  A lane has a split's m and l (kAttnMaxSplits of them

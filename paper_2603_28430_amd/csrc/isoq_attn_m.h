@@ -30,15 +30,18 @@
 // combined by shifts and adds and enter an fp32 sum, one register per
 // coordinate and row, which the running maximum of the row rescales.
 //
-// What bounds it.  With one row a key head (8 sequences x 32 heads x 32,768
-// positions, d = 128, 3 bits: 873 MB) 199 us, 4.4 TB/s: memory, of which a large copy
-// takes 4.7.  With 4 rows (16 sequences x 8 key heads, up to 8,192 positions, 4
-// bits) 40 us, of which 10 are the workgroups' preparation and the join: long
-// caches take 4.1 TB/s, the decoding's vector instructions (about 750 a tile of
-// 64 positions) next to memory.  With 8 rows (one sequence x 8 key heads x 131,071)
-// 48 us, 2.3 TB/s: vector and matrix instructions.  d = 256, 2 rows, 4 x 8 heads x 8,190:
-// 24 us.  A call of one sequence and 700 positions 10 us (11.4 with the host's
-// part).
+// What bounds it (the kernel's time in a trace; a join of splits takes 4 to 5 us
+// more).  With one row a key head (8 sequences x 32 heads x 32,768 positions, d =
+// 128, 3 bits: 873 MB) 197 to 201 us, 4.4 TB/s where a large copy moves 4.7, and 216
+// to 222 once such calls have followed each other for some ms and the clock has
+// fallen: vector
+// instructions (87% of issue) no less than memory.  With 4 rows (16 ragged
+// sequences x 8 key heads, up to 8,192 positions, 4 bits) 41 us: the decoding's
+// vector instructions (about 750 a tile of 64 positions; 52% of issue, a third of
+// them the workgroups' preparation) and waits (37%).  With 8 rows (one sequence x 8
+// key heads x 131,071) 46 us, 2.4 TB/s: vector (64% of issue) and matrix
+// instructions (20%).  d = 256, 2 rows, 4 x 8 heads x 8,190: 21 us.  One sequence of
+// 700 positions 11 us: three tiles a wave in series, on eight workgroups.
 #pragma once
 
 #include "isoq_attn_device.h"

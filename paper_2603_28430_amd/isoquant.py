@@ -488,8 +488,11 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
     [n_blocks, n_kv_heads, block_size] with block_table int32 [n_seqs,
     max_blocks] and seq_lens int32 [n_seqs].  One token a sequence, or with
     q_start int32 [n_seqs + 1] the tokens q_start[s] .. q_start[s + 1] - 1 of
-    sequence s, at most max_q_len (default: n_tokens), which are its last
-    positions (causal).
+    sequence s, at most max_q_len, which are its last positions (causal).
+    max_q_len and max_len (the longest sequence's positions) are bounds that the
+    call is planned by, by default n_tokens and what block_table holds: give both
+    where they are known (64 single tokens at 2,000 positions, 8 x 4 heads, with
+    q_start: 39 us with max_q_len=1, 245 without).
     Returns (out like q, lse fp32 [n_tokens, n_q_heads]); rows of no sequence
     are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
     least isoq_kv_attn_workspace(...) bytes.  What is not passed (out, lse,
