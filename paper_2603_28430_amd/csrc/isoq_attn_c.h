@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
             const u32x4 about = *reinterpret_cast<const u32x4 *>(tile);
             const uint32_t ok0 = about[0], ok1 = about[1];
-            const int tu = __builtin_amdgcn_readfirstlane((int)about[2]), half_least = __builtin_amdgcn_readfirstlane((int)about[3]);
+            const int tu = (int)about[2], half_least = (int)about[3];
             const bool whole = (ok0 & ok1) == ~0u && tb + 64 <= lim_min;
 #pragma unroll
             for (int k = 0; k < 2; k++)
@@ -564,8 +564,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             const float base = ref == -INFINITY ? 0.f : ref;
             const int fall = (int)fmaxf(was - base, -1000.f);   // (there was nothing: -1000)
             int move = most > 0.f ? fall + unit - tu : 0;   // of acc (or it is zero)
+            float held = ref > -INFINITY ? most : 0x1p4f;
+            if (move != 0 || ref > was)   // (fall and the unit's change may cancel: l and unit follow all the same)
+                held = 0.f;
             float up = -base, down = 1.f;
-            if (__builtin_amdgcn_ballot_w64(move != 0 || (most < 0x1p4f && ref > -INFINITY)) != 0) {
+            if (__builtin_amdgcn_ballot_w64(held < 0x1p4f) != 0) {
                 l = __builtin_amdgcn_ldexpf(l, fall);
                 const float before = __builtin_amdgcn_ldexpf(most, min(move, 100));
                 float large = ref > was ? __int_as_float(half_least) : 0.f;

@@ -129,3 +129,17 @@ def test_norms_at_random(d, bits, dtype, n, group):
         for h in range(2):
             c.norms[0, h] = c.norms[0, h] * f
     run(w)
+
+
+@pytest.mark.parametrize("step", [5, 6, 9, -5, -7])
+@pytest.mark.parametrize("d,bits,dtype,n,group", KERNELS)
+def test_norms_fall_as_the_logits_rise(d, bits, dtype, n, group, step):
+    """From tile to tile norms by 2^-step and logits by step ln 2, so that the units of
+    weights and of exponentials move against each other and their product stays."""
+    rng = np.random.default_rng(n)
+    tiles, size = 6, 64
+    k = np.repeat(np.arange(tiles), size)
+    norms = 2.0 ** (-step * (k - tiles // 2)) * rng.uniform(0.55, 0.95, len(k))
+    logits = 40.0 + step * (k - tiles // 2) * np.log(2.0) + rng.uniform(0.0, 0.2, len(k))
+    w = steered("full", d, bits, dtype, [n], 2, group, [len(k)], logits, norms, seed=d)
+    run(w)
