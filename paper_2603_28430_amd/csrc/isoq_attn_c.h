@@ -25,10 +25,10 @@
 // too 6% less, and lse off by 1e-6 to 2e-6).
 //
 // What bounds it.  Two equal chunks (2 x 512 tokens at 8,192 positions, 8 x 4 heads)
-// take 307 to 326 us at 3 bits, 400 to 430 TFLOP/s of the definition's operations (4 d
-// a row and position), twice that of the matrix cores' own, and 364 once such calls
-// have followed each other for some ms and the clock has fallen; 351 to 376 and 426 at
-// 4 bits; 274 at 2 and 197 at d = 64.  Matrix cores are busy for 42% of the cycles, vector
+// take 307 to 333 us at 3 bits, 400 to 430 TFLOP/s of the definition's operations (4 d
+// a row and position), twice that of the matrix cores' own, and 364 to 376 once such
+// calls have followed each other for some ms and the clock has fallen; 351 to 394 and
+// 426 to 440 at 4 bits; 274 at 2 and 200 at d = 64.  Matrix cores are busy for 42% of the cycles, vector
 // instructions issue in 50%, waves wait for 28%: the two waves of a SIMD overlap the
 // two kinds little.  (A fifth fewer vector instructions, and all four waves fetching
 // records, changed nothing when tried.)  Ragged chunks of up to 512 tokens are bound

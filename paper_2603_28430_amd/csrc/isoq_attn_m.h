@@ -32,7 +32,7 @@
 //
 // What bounds it (the kernel's time in a trace; a join of splits takes 4 to 5 us
 // more).  With one row a key head (8 sequences x 32 heads x 32,768 positions, d =
-// 128, 3 bits: 873 MB) 197 to 201 us, 4.4 TB/s where a large copy moves 4.7, and 216
+// 128, 3 bits: 873 MB) 197 to 205 us, 4.3 TB/s where a large copy moves 4.7, and 216
 // to 222 once such calls have followed each other for some ms and the clock has
 // fallen: vector
 // instructions (87% of issue) no less than memory.  With 4 rows (16 ragged
