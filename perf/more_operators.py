@@ -406,7 +406,7 @@ def plain_plan(s):
     blk = table[q, (pos // bs).clamp(max=width - 1)].long()
     slots = torch.where(there_t & fine[q] & (blk >= 0), blk * bs + pos % bs, -1)
     left = there - torch.where(fine, grow, 0).sum()
-    return (lens.to(I32), start.clamp(max=tokens).to(I32), slots, pos.to(I32), left.to(I32).reshape(1), table, free)
+    return (lens.to(I32), start.to(I32), slots, pos.to(I32), left.to(I32).reshape(1), table, free)
 
 
 def plain_rope(s):
