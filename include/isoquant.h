@@ -488,6 +488,99 @@ isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const 
                             float *v_rho, uint8_t *k_signs, float *k_gamma, int64_t n_blocks, int block_size,
                             void *stream);
 
+/*
+ * isoq_kv_plan -- the block tables and slots of a step's tokens, from the
+ * sequences' lengths before and after it, on the GPU: what isoq_kv_append
+ * (slot_mapping), isoq_qk_norm_rope (positions) and isoq_kv_attn (q_start,
+ * seq_lens, block_table) take.  Nothing is read back, so that lengths may be
+ * ones that only the GPU knows (n_keep of isoq_kv_compact, drafts that were
+ * accepted), and a step can be captured into a graph.
+ *
+ *   lens, new_lens  device, int32 [n_seqs]: positions of each sequence before and
+ *               after the step (cut to 0 .. max_blocks_per_seq * block_size).  A
+ *               sequence that grows has new_lens - lens new tokens; one that
+ *               shrinks (drafts taken back, the end of a sequence: 0) has none.
+ *   block_table device, int32 [n_seqs][max_blocks_per_seq], in and out: the
+ *               first ceil(length / block_size) entries of a row are the blocks
+ *               that the sequence owns; further ones are ignored and, but for
+ *               those that it takes, left as they were.
+ *   free_blocks, n_free, max_free  device, int32 [max_free], in and out, and int32
+ *               [1]: the first *n_free entries are free blocks (cut to 0 ..
+ *               max_free).  Blocks that sequences release go behind them (past
+ *               max_free: they are lost), in the order of the sequences and their
+ *               positions; then the sequences that grow take blocks from the end.
+ *               A sequence is refused if it and those before it want more than there
+ *               are: it keeps its length and blocks, and its tokens get no slot.
+ *   seq_lens    device, int32 [n_seqs]: the lengths now (may be lens itself; not
+ *               new_lens).  seq_lens[s] != new_lens[s]: refused (or cut).
+ *   q_start     device, int32 [n_seqs + 1]: sequence s has the tokens q_start[s] ..
+ *               q_start[s + 1] - 1, those of refused sequences among them.
+ *   slot_mapping, positions  device, int64 and int32 [n_tokens]: each token's slot
+ *               (-1 for none: isoq_kv_append skips it) and position.  n_tokens may
+ *               be more than there are (a captured step of a fixed size): tokens
+ *               past the last have slot -1 and position 0.  If it is fewer, those
+ *               past n_tokens are left out, though lengths and blocks count them.
+ *   n_free_out  device, int32 [1]: free blocks left (may be n_free itself).
+ * Other buffers must not overlap.  Limits: n_seqs <= 65535, (max_blocks_per_seq + 1) *
+ * block_size < 2^31, max_free and n_tokens < 2^31.
+ */
+isoq_status isoq_kv_plan(const int32_t *lens, const int32_t *new_lens, int n_seqs, int32_t *block_table,
+                         int max_blocks_per_seq, int block_size, int32_t *free_blocks, int64_t max_free,
+                         const int32_t *n_free, int32_t *seq_lens, int32_t *q_start, int64_t *slot_mapping,
+                         int32_t *positions, int64_t n_tokens, int32_t *n_free_out, void *stream);
+
+/*
+ * Rotary positions.  A handle holds the angles by which the pairs of a head are
+ * turned: pair i of a row at position p by p * freqs[i] radians, and the pair's
+ * length is multiplied by `amplitude`.  The first rot_dim coordinates are
+ * rotated, the rest is passed on.
+ *
+ * isoq_rope_init -- build a handle on the current device.
+ *   d           width of a head, 1 .. 1024.
+ *   rot_dim     coordinates that are rotated: even, 0 .. d.
+ *   layout      ISOQ_ROPE_PAIRS: pair i is coordinates (2 i, 2 i + 1);
+ *               ISOQ_ROPE_HALVES: (i, rot_dim / 2 + i).
+ *   freqs       host, rot_dim / 2 doubles (isoq_rope_freqs, or others).
+ *   amplitude   finite (1 leaves lengths as they are).
+ * isoq_rope_freqs -- host only: base^(-2 i / rot_dim) for i < rot_dim / 2, slowed
+ * down for contexts that are `factor` times longer than the `original` positions:
+ * a pair that turns at most `low` times in those by `factor`, one that turns at
+ * least `high` times not at all, between them blended linearly in the number of
+ * turns.  factor 1: as they are; original 0: every pair by factor.
+ */
+enum { ISOQ_ROPE_PAIRS = 0, ISOQ_ROPE_HALVES = 1 };
+typedef struct isoq_rope isoq_rope;
+isoq_status isoq_rope_init(isoq_rope **out, int d, int rot_dim, int layout, const double *freqs, double amplitude);
+isoq_status isoq_rope_destroy(isoq_rope *r);
+isoq_status isoq_rope_freqs(int rot_dim, double base, double factor, double original, double low, double high,
+                            double *out);
+
+/*
+ * isoq_qk_norm_rope -- norms and rotary positions of new tokens' queries and keys
+ * in one pass: each row (a head of a token) becomes
+ *     y = weight * x / sqrt(mean(x^2) + eps)     (where there is a weight)
+ * and its rotated pairs are turned by the angles of the token's position.  q_out
+ * is what isoq_kv_attn takes, k_out what isoq_kv_append takes.
+ *
+ *   dtype       ISOQ_F16 or ISOQ_F32, the element type of q, k, q_out and k_out.
+ *   q, k        device, token t's heads at q + t * q_stride (k + t * k_stride)
+ *               elements, one after another: a part of a projection's output that
+ *               holds queries, keys and values may be passed as it is.  Aligned to
+ *               their elements; 16 bytes, with strides and widths that are
+ *               multiples of as much, are faster.  n_q_heads or n_kv_heads may be 0.
+ *   positions   device, int32 [n_tokens], any value (negative ones turn back).
+ *               Angles are exact to 2^-31 of a turn at every position.
+ *   q_weight, k_weight  device, fp32 [d], or NULL: no norm.
+ *   q_out, k_out  device, [n_tokens][heads][d] (16-byte aligned); may be q (k)
+ *               itself where its stride is n_q_heads * d (n_kv_heads * d).
+ * Arithmetic: fp32, rounded once (fp16: to nearest even).  Limits: n_tokens *
+ * (n_q_heads + n_kv_heads) < 2^31, heads <= 65535.
+ */
+isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int64_t q_stride, int n_q_heads,
+                              const void *k, int64_t k_stride, int n_kv_heads, const int32_t *positions,
+                              int64_t n_tokens, const float *q_weight, const float *k_weight, float eps, void *q_out,
+                              void *k_out, void *stream);
+
 /* Sizes: bytes of one packed index record, ceil(pw * bits / 8) with the
  * padded width pw = 4 g4 (Full, Fast) or 2 g2 (2-D); isoq_packed_bytes is
  * ceil(d * bits / 8), the same number whenever d is a multiple of 4.  Raw

@@ -51,10 +51,10 @@ def build(verbose: bool = False) -> str:
                 "isoq_generic_2d.hip", "isoq_generic_8d.hip", "isoq_qjl_append.hip", "isoq_packed.hip",
                 "isoq_packed_8d.hip", "isoq_packed_qjl.hip", "isoq_scores_generic.hip", "isoq_attn_generic.hip",
                 "isoq_attn_join.hip", "isoq_attn_m2.hip", "isoq_attn_m3.hip", "isoq_attn_m4.hip",
-                "isoq_attn_c.hip", "isoq_pages.hip"):
+                "isoq_attn_c.hip", "isoq_pages.hip", "isoq_plan.hip", "isoq_rope.hip"):
         jobs.append([HIPCC, *DEVICE_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o",
                      os.path.join(obj_dir, src + ".o")])
-    for src in ("isoq_api.cpp", "isoq_attn_api.cpp", "isoq_host_params.cpp"):
+    for src in ("isoq_api.cpp", "isoq_attn_api.cpp", "isoq_step_api.cpp", "isoq_host_params.cpp"):
         jobs.append([os.path.join(ROCM, "llvm", "bin", "clang++"), *HOST_FLAGS, *inc, "-c",
                      os.path.join(CSRC, src), "-o", os.path.join(obj_dir, src + ".o")])
     with cf.ThreadPoolExecutor(max_workers=len(jobs)) as ex:

@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libisoquant.so")
 
 ISOQ_FULL, ISOQ_FAST, ISOQ_PLANAR2D, ISOQ_BLOCK8 = 0, 1, 2, 3
 ISOQ_F32, ISOQ_F16 = 0, 1
+ISOQ_ROPE_PAIRS, ISOQ_ROPE_HALVES = 0, 1
+LAYOUTS = {"pairs": ISOQ_ROPE_PAIRS, "halves": ISOQ_ROPE_HALVES}
 VARIANTS = {"full": ISOQ_FULL, "fast": ISOQ_FAST, "2d": ISOQ_PLANAR2D, "8d": ISOQ_BLOCK8}
 
 STATUS = {0: "ISOQ_OK", 1: "ISOQ_E_INVALID", 2: "ISOQ_E_UNSUPPORTED", 3: "ISOQ_E_NULL",
@@ -70,6 +72,11 @@ def _load():
     L.isoq_kv_copy_blocks.argtypes = [vp, vp, vp, i64, c_int, vp, vp, vp, vp, vp, vp, i64, c_int, vp]
     L.isoq_kv_compact.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, vp, c_int, c_int, vp, vp, vp, vp, vp, vp, i64,
                                   c_int, vp]
+    L.isoq_kv_plan.argtypes = [vp, vp, c_int, vp, c_int, c_int, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp]
+    L.isoq_rope_init.argtypes = [ctypes.POINTER(vp), c_int, c_int, c_int, dp, ctypes.c_double]
+    L.isoq_rope_destroy.argtypes = [vp]
+    L.isoq_rope_freqs.argtypes = [c_int] + [ctypes.c_double] * 5 + [dp]
+    L.isoq_qk_norm_rope.argtypes = [vp, c_int, vp, i64, c_int, vp, i64, c_int, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp]
     L.isoq_packed_bytes.argtypes = [c_int, c_int]
     L.isoq_packed_bytes.restype = ctypes.c_size_t
     L.isoq_record_bytes.argtypes = [c_int, c_int, c_int]
@@ -88,7 +95,8 @@ def _load():
               "isoq_quantize", "isoq_dequantize", "isoq_roundtrip", "isoq_kv_append", "isoq_kv_scores", "isoq_sketch_init",
               "isoq_sketch_destroy", "isoq_sketch_export", "isoq_quantize_qjl", "isoq_kv_append_qjl",
               "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn",
-              "isoq_kv_copy_blocks", "isoq_kv_compact", "isoq_codebook_lloyd",
+              "isoq_kv_copy_blocks", "isoq_kv_compact", "isoq_kv_plan", "isoq_rope_init", "isoq_rope_destroy",
+              "isoq_rope_freqs", "isoq_qk_norm_rope", "isoq_codebook_lloyd",
               "isoq_rotation_draws"):
         getattr(L, f).restype = c_int
     return L
@@ -729,3 +737,186 @@ def isoq_kv_compact(pk: Params, keep, n_keep, block_table, k_idx, k_rho, v_idx=N
                              _ptr(k_gamma), n_blocks, block_size, _stream_ptr(stream))
     if st:
         _check(st, "isoq_kv_compact")
+
+
+def isoq_kv_plan(lens, new_lens, block_table, block_size: int, free_blocks, n_free, n_tokens=None, seq_lens=None,
+                 q_start=None, slot_mapping=None, positions=None, n_free_out=None, stream=None):
+    """Blocks and slots of a step's tokens from the sequences' lengths before and
+    after it, lens and new_lens int32 [n_seqs]: block_table int32 [n_seqs,
+    max_blocks] and free_blocks int32 [max_free], of which the first n_free (int32
+    [1]) are free, are updated; n_tokens is the most new tokens that the step may
+    have (by default as many as slot_mapping holds).  Returns (seq_lens int32
+    [n_seqs], q_start int32 [n_seqs + 1], slot_mapping int64 [n_tokens], positions
+    int32 [n_tokens], n_free_out int32 [1]): seq_lens may be lens, n_free_out
+    n_free.  See include/isoquant.h for sequences that are refused.  What is not
+    passed is allocated from torch's pool for `stream`."""
+    torch = _torch()
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be int32 [n_seqs, max_blocks]")
+    n_seqs, max_blocks = block_table.shape
+    if n_tokens is None:
+        if slot_mapping is None:
+            raise ValueError("n_tokens, or a slot_mapping of that length")
+        n_tokens = slot_mapping.numel()
+    whole = torch.int32
+    given = [("lens", lens, whole, (n_seqs,)), ("new_lens", new_lens, whole, (n_seqs,)),
+             ("block_table", block_table, whole, (n_seqs, max_blocks)), ("n_free", n_free, whole, (1,)),
+             ("free_blocks", free_blocks, whole, (free_blocks.numel(),))]
+    for name, t, dtype, shape in (("seq_lens", seq_lens, whole, (n_seqs,)), ("q_start", q_start, whole, (n_seqs + 1,)),
+                                  ("slot_mapping", slot_mapping, torch.int64, (n_tokens,)),
+                                  ("positions", positions, whole, (n_tokens,)), ("n_free_out", n_free_out, whole, (1,))):
+        if t is not None:
+            given.append((name, t, dtype, shape))
+    for name, t, dtype, shape in given:
+        if t.dtype != dtype or t.shape != shape:
+            raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    _on_current(lens, [g[1] for g in given], stream)
+    if stream is None:
+        seq_lens, q_start, slot_mapping, positions, n_free_out = _plan_buffers(
+            lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out)
+    else:
+        with torch.cuda.stream(stream):
+            seq_lens, q_start, slot_mapping, positions, n_free_out = _plan_buffers(
+                lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out)
+    st = lib.isoq_kv_plan(lens.data_ptr(), new_lens.data_ptr(), n_seqs, block_table.data_ptr(), max_blocks, block_size,
+                          free_blocks.data_ptr(), free_blocks.numel(), n_free.data_ptr(), seq_lens.data_ptr(),
+                          q_start.data_ptr(), slot_mapping.data_ptr(), positions.data_ptr(), n_tokens,
+                          n_free_out.data_ptr(), _stream_ptr(stream))
+    if st:
+        _check(st, "isoq_kv_plan")
+    return seq_lens, q_start, slot_mapping, positions, n_free_out
+
+
+def _plan_buffers(lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out):
+    if seq_lens is None:
+        seq_lens = lens.new_empty(n_seqs)
+    if q_start is None:
+        q_start = lens.new_empty(n_seqs + 1)
+    if slot_mapping is None:
+        slot_mapping = lens.new_empty(n_tokens, dtype=_torch_module.int64)
+    if positions is None:
+        positions = lens.new_empty(n_tokens)
+    if n_free_out is None:
+        n_free_out = lens.new_empty(1)
+    return seq_lens, q_start, slot_mapping, positions, n_free_out
+
+
+class Rope:
+    """Owner of an isoq_rope handle (angles of rotary positions)."""
+
+    def __init__(self, handle: int, d: int, rot_dim: int, layout: int):
+        self.handle = ctypes.c_void_p(handle)
+        self.d, self.rot_dim, self.layout = d, rot_dim, layout
+
+    def close(self):
+        if self.handle:
+            _check(lib.isoq_rope_destroy(self.handle), "isoq_rope_destroy")
+            self.handle = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def isoq_rope_freqs(rot_dim: int, base: float = 10000.0, factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                    high: float = 32.0) -> np.ndarray:
+    """Angles a position of the rot_dim / 2 pairs: base^(-2 i / rot_dim), slowed
+    down by up to `factor` for contexts longer than `original` positions (see
+    include/isoquant.h)."""
+    out = np.zeros(max(0, int(rot_dim)) // 2)
+    _check(lib.isoq_rope_freqs(int(rot_dim), float(base), float(factor), float(original), float(low), float(high),
+                               out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))), "isoq_rope_freqs")
+    return out
+
+
+def isoq_rope_init(d: int, rot_dim=None, layout="halves", freqs=None, amplitude: float = 1.0) -> Rope:
+    """Rotary positions of heads of width d on the current device: the first
+    rot_dim coordinates (all by default) in pairs (2 i, 2 i + 1), layout "pairs", or
+    (i, rot_dim / 2 + i), "halves"; freqs [rot_dim / 2] angles a position, by
+    default isoq_rope_freqs(rot_dim)."""
+    rot_dim = int(d) if rot_dim is None else int(rot_dim)
+    if isinstance(layout, str):
+        layout = LAYOUTS[layout]
+    f = np.ascontiguousarray(isoq_rope_freqs(rot_dim) if freqs is None and rot_dim > 0 else [] if freqs is None else freqs,
+                             dtype=np.float64)
+    if f.shape != (max(0, rot_dim) // 2,):
+        raise ValueError("freqs must hold rot_dim / 2 angles")
+    h = ctypes.c_void_p()
+    _check(lib.isoq_rope_init(ctypes.byref(h), int(d), rot_dim, int(layout),
+                              f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), float(amplitude)), "isoq_rope_init")
+    return Rope(h.value, int(d), rot_dim, int(layout))
+
+
+def isoq_rope_destroy(r: Rope) -> None:
+    r.close()
+
+
+def _token_stride(name, x, d):
+    """Elements between the tokens of rows [n_tokens, heads, d], whose heads lie one after another."""
+    n, heads, width = x.shape
+    token, head, one = x.stride()
+    if width != d:
+        raise ValueError(f"{name}: last dimension must be d={d}")
+    if (width > 1 and one != 1) or (heads > 1 and head != d) or (n > 1 and token < heads * d):
+        raise ValueError(f"{name}: a token's heads must be contiguous, tokens at least as far apart")
+    return token if n > 1 else heads * d
+
+
+def isoq_qk_norm_rope(rope: Rope, q, k, positions, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None,
+                      k_out=None, stream=None):
+    """Norms (where there is a weight, fp32 [d]) and rotary positions of new
+    tokens' queries q [n_tokens, n_q_heads, d] and keys k [n_tokens, n_kv_heads, d]
+    (or None): views into one projection's output may be passed, only a token's
+    heads have to be contiguous.  positions int32 [n_tokens].  Returns (q_out,
+    k_out), contiguous; they may be q and k themselves (see include/isoquant.h)."""
+    torch = _torch()
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q [n_tokens, n_q_heads, d], k [n_tokens, n_kv_heads, d]")
+    shape, d = q.shape, rope.d
+    q_stride, k_stride, kv_heads = _token_stride("q", q, d), 0, 0
+    if k is not None:
+        if k.shape[0] != shape[0] or k.dtype != q.dtype:
+            raise ValueError("q and k must have the same tokens and dtype")
+        k_stride, kv_heads = _token_stride("k", k, d), k.shape[1]
+    elif k_out is not None or k_weight is not None:
+        raise ValueError("k_out and k_weight need k")
+    code = _dtype_code(q.dtype)
+    if positions.shape != (shape[0],) or positions.dtype != torch.int32:
+        raise ValueError("positions must be int32 [n_tokens]")
+    tensors = [positions]
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if w.shape != (d,) or w.dtype != torch.float32:
+                raise ValueError("weights must be float32 [d]")
+            tensors.append(w)
+    for x, out in ((q, q_out), (k, k_out)):
+        if out is not None:
+            if out.shape != x.shape or out.dtype != x.dtype:
+                raise ValueError("q_out and k_out must have the shapes and dtype of q and k")
+            tensors.append(out)
+    for x in (q,) if k is None else (q, k):
+        if not _is_gpu(x) or x.get_device() != positions.get_device():
+            _device_tensors(positions, positions=positions)
+            raise ValueError(f"q and k must be on {positions.device}")
+    _on_current(positions, tensors, stream)
+    if stream is None:
+        q_out, k_out = _rope_buffers(q, k, q_out, k_out)
+    else:
+        with torch.cuda.stream(stream):
+            q_out, k_out = _rope_buffers(q, k, q_out, k_out)
+    st = lib.isoq_qk_norm_rope(rope.handle, code, q.data_ptr(), q_stride, shape[1], _ptr(k), k_stride, kv_heads,
+                               positions.data_ptr(), shape[0], _ptr(q_weight), _ptr(k_weight), eps, q_out.data_ptr(),
+                               _ptr(k_out), _stream_ptr(stream))
+    if st:
+        _check(st, "isoq_qk_norm_rope")
+    return q_out, k_out
+
+
+def _rope_buffers(q, k, q_out, k_out):
+    if q_out is None:
+        q_out = q.new_empty(q.shape)
+    if k_out is None and k is not None:
+        k_out = k.new_empty(k.shape)
+    return q_out, k_out
