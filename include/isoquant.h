@@ -435,6 +435,60 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
                               int64_t max_len);
 
 /*
+ * isoq_kv_attn_cross -- attention to states of another length, as a decoder's to
+ * its encoder's: isoq_kv_attn, but for one thing: every token of a sequence
+ * attends to all of its seq_lens[s] positions.  The states' keys and values are
+ * quantized once (isoq_kv_append at slots of their own) and read by every step;
+ * tokens that share states (the beams of one input) may be one sequence of several
+ * tokens.  Arguments, limits, arithmetic and workspace (isoq_kv_attn_workspace) as
+ * isoq_kv_attn.
+ */
+isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
+                               const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
+                               int n_kv_heads, const uint8_t *k_idx, const float *k_rho, const uint8_t *v_idx,
+                               const float *v_rho, int64_t n_blocks, int block_size, const int32_t *block_table,
+                               int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len, float scale, void *out,
+                               float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * isoq_kv_attn_prefix -- isoq_kv_attn for sequences that share long beginnings (an
+ * instruction, a document): a prefix's positions are in the cache once and are
+ * attended to by the rows of all its sequences together, the sequences' own
+ * positions follow them.  A token attends to all positions of its prefix and, as
+ * in isoq_kv_attn, to its sequence's own up to itself.
+ *
+ *   block_table, seq_lens, max_len  the sequences' own positions (their new tokens
+ *               are the last of those).
+ *   prefix_start  device, int32 [n_prefixes + 1], ascending: prefix p is shared by
+ *               the sequences prefix_start[p] .. prefix_start[p + 1] - 1, which stand
+ *               side by side.  Sequences of none have only their own positions.
+ *               NULL: n_prefixes is 1 (or 0) and all sequences share it.
+ *   prefix_table, prefix_lens  device, int32 [n_prefixes][max_prefix_blocks] and
+ *               [n_prefixes]: the prefixes' blocks and lengths, as block_table and
+ *               seq_lens (the same cache and block_size).
+ *   max_prefix_tokens  tokens of all sequences of one prefix at most (n_tokens if the
+ *               host does not know); a prefix's tokens from there on are left as they
+ *               were in out and lse.  max_prefix_len: positions of the longest prefix at
+ *               most (max_prefix_blocks * block_size if it does not know).
+ *   workspace   at least isoq_kv_attn_prefix_workspace(...) bytes.
+ * n_prefixes <= 65535; max_prefix_tokens (or n_tokens) * n_q_heads <= 2^23.
+ * Everything else as isoq_kv_attn.
+ */
+isoq_status isoq_kv_attn_prefix(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
+                                const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
+                                int n_kv_heads, const uint8_t *k_idx, const float *k_rho, const uint8_t *v_idx,
+                                const float *v_rho, int64_t n_blocks, int block_size, const int32_t *block_table,
+                                int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len,
+                                const int32_t *prefix_table, int max_prefix_blocks, const int32_t *prefix_lens,
+                                int64_t max_prefix_len, const int32_t *prefix_start, int n_prefixes,
+                                int64_t max_prefix_tokens, float scale, void *out, float *lse, void *workspace,
+                                size_t workspace_bytes, void *stream);
+size_t isoq_kv_attn_prefix_workspace(const isoq_params *pk, const isoq_params *pv, int dtype, int64_t n_tokens,
+                                     int max_q_len, int n_seqs, int n_q_heads, int n_kv_heads, int block_size,
+                                     int max_blocks_per_seq, int64_t max_len, int n_prefixes, int64_t max_prefix_tokens,
+                                     int max_prefix_blocks, int64_t max_prefix_len);
+
+/*
  * isoq_kv_copy_blocks -- copy whole cache blocks inside a paged cache (forking
  * a sequence whose last block is shared, copy on write; moving blocks): for
  * every pair (source, destination) of block_pairs, the records and norms of

@@ -23,13 +23,14 @@ struct AttnArgs {
     const void *q;               // [n_tokens][n_q_heads][d]
     void *out;                   // the same
     float *lse;                  // [n_tokens][n_q_heads], or null
-    float *part;                 // splits (or null: rows are finished by the kernel): sums of values [row][n_splits][width], row = token n_q_heads + head
-    float *part_ml;              // splits: m, l [row][n_splits][2]
+    float *part;                 // splits (or null: rows are finished by the kernel): sums of values [row][part_splits][width], row = token n_q_heads + head
+    float *part_ml;              // splits: m, l [row][part_splits][2]
     const uint8_t *k_idx, *v_idx;
     const float *k_rho, *v_rho;
     const int32_t *block_table;  // [n_seqs][max_blocks]
     const int32_t *seq_lens;     // [n_seqs]
     const int32_t *q_start;      // [n_seqs + 1], or null: one token each
+    const int32_t *shared;       // [n + 1] where n_all > 0 (null: one, of all): "sequence" p is what the sequences shared[p] .. shared[p + 1] - 1 have in common, with all their tokens
     const float *k_params, *v_params;
     int64_t n_blocks;
     int64_t set_stride;          // parameter floats per set
@@ -39,6 +40,9 @@ struct AttnArgs {
     int32_t k_sets, v_sets, variant, q_f16;
     int32_t chunk, n_splits;     // positions per split (at most, if even: attn_chunk)
     int32_t even;
+    int32_t part_splits, part_first;   // splits of a row in part, this launch's from part_first on
+    int32_t full;                // every token attends to all positions (else: to those up to its own)
+    int32_t n_all;               // sequences that `shared` is about, or 0: not about shared prefixes
     float scale;                 // times log2(e)
     FastDiv div_block;
     int32_t d, width, slots;     // coordinates per row, padded width, its rotation slots (8 coordinates for 8-D, else 4)
@@ -76,5 +80,16 @@ AttnKernel attn_c_kernel_for(int d, int bits, int rest);
 // head + n_q_heads token.
 constexpr int kAttnJoinFew = 8;
 const void *attn_join_kernel_for(int variant, bool few);
+
+// Attention behind shared prefixes (isoq_kv_attn_prefix): the prefixes' splits, which
+// follow the sequences' own in part, for the join (its second argument).
+struct AttnPrefix {
+    const int32_t *start;     // [n + 1] first sequence of each prefix, or null: all sequences share one
+    const int32_t *lens;      // [n]
+    int32_t n, n_seqs;
+    int32_t max_tokens;       // tokens that share a prefix at most
+    int32_t cap, chunk, n_splits, even;   // as in AttnArgs
+};
+const void *attn_prefix_join_kernel_for(int variant, bool few);
 
 }  // namespace isoq

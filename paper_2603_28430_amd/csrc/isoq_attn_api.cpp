@@ -58,7 +58,8 @@ struct AttnPlan {
 };
 
 AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int n_seqs, int max_q_len, int n_q_heads,
-                   int n_kv_heads, int block_size, int max_blocks_per_seq, int64_t max_len)
+                   int n_kv_heads, int block_size, int max_blocks_per_seq, int64_t max_len,
+                   int max_splits = kAttnMaxSplits)
 {
     AttnPlan p{};
     const int sw = pk->variant == VAR_BLOCK8 ? 8 : 4;
@@ -125,7 +126,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     int64_t splits = p.kern.parts        ? std::max<int64_t>(1, want / blocks)
                      : p.max_pos <= 768 ? 1
                                          : (want + blocks - 1) / blocks;
-    splits = std::min<int64_t>(splits, kAttnMaxSplits);
+    splits = std::min<int64_t>(splits, max_splits);
     int64_t chunk = (p.max_pos + splits - 1) / splits;
     chunk = std::max<int64_t>(unit, (chunk + unit - 1) / unit * unit);
     p.chunk = (int)std::min<int64_t>(chunk, 0x7FFFFF00);
@@ -200,6 +201,230 @@ isoq_status cache_planes(const isoq_params *pk, const isoq_sketch *sk, uint8_t *
     return ISOQ_OK;
 }
 
+// One attention call's arguments; the prefix's where n_prefixes > 0.
+struct AttnCall {
+    const isoq_params *pk, *pv;
+    int dtype;
+    const void *q;
+    const int32_t *q_start;
+    int64_t n_tokens;
+    int max_q_len, n_seqs, n_q_heads, n_kv_heads;
+    const uint8_t *k_idx;
+    const float *k_rho;
+    const uint8_t *v_idx;
+    const float *v_rho;
+    int64_t n_blocks;
+    int block_size;
+    const int32_t *block_table;
+    int max_blocks;
+    const int32_t *seq_lens;
+    int64_t max_len;
+    const int32_t *prefix_table;
+    int max_prefix_blocks;
+    const int32_t *prefix_lens;
+    int64_t max_prefix_len;
+    const int32_t *prefix_start;
+    int n_prefixes;
+    int64_t max_prefix_tokens;
+    float scale;
+    void *out;
+    float *lse;
+    void *workspace;
+    size_t workspace_bytes;
+    void *stream;
+    bool full;
+};
+
+// A launch's arguments, but for the parts' places.
+AttnArgs attn_args(const AttnCall &c, const AttnPlan &plan, float scale2)
+{
+    const isoq_params *pk = c.pk, *pv = c.pv;
+    AttnArgs a{};
+    a.q = c.q;
+    a.out = c.out;
+    a.lse = c.lse;
+    a.k_idx = c.k_idx;
+    a.v_idx = c.v_idx;
+    a.k_rho = c.k_rho;
+    a.v_rho = c.v_rho;
+    a.block_table = c.block_table;
+    a.seq_lens = c.seq_lens;
+    a.q_start = c.q_start;
+    a.k_params = pk->dparams;
+    a.v_params = pv->dparams;
+    a.n_blocks = c.n_blocks;
+    a.set_stride = (int64_t)slots_per_set(pk->variant, pk->d) * params_per_slot(pk->variant);
+    a.n_tokens = (int32_t)c.n_tokens;
+    a.max_q_len = c.max_q_len;
+    a.n_q_heads = c.n_q_heads;
+    a.n_kv_heads = c.n_kv_heads;
+    a.group = c.n_q_heads / c.n_kv_heads;
+    a.block_size = c.block_size;
+    a.max_blocks = c.max_blocks;
+    a.cap = c.n_blocks == 0 ? 0 : (int32_t)plan.max_pos;
+    a.k_sets = pk->n_sets;
+    a.v_sets = pv->n_sets;
+    a.variant = pk->variant;
+    a.q_f16 = c.dtype == ISOQ_F16;
+    a.chunk = plan.chunk;
+    a.n_splits = a.part_splits = plan.n_splits;
+    a.even = plan.kern.parts;
+    a.full = c.full;
+    a.scale = scale2;
+    a.div_block = make_fastdiv((uint32_t)c.block_size);
+    a.d = pk->d;
+    a.width = plan.width;
+    a.slots = plan.slots;
+    a.rec = (int32_t)record_bytes(pk->variant, pk->d, pk->bits);
+    a.rec_lp = a.rec % 16 == 0 ? 4 : a.rec % 8 == 0 ? 3 : -1;   // cache_piece
+    for (int k = 0; k < (1 << pk->bits); k++) {
+        a.k_lev[k] = pk->levels[k];
+        a.v_lev[k] = pv->levels[k];
+    }
+    a.k_dig = pk->lv;
+    if (plan.kern.fn) {
+        a.v_dig = plan.vt->vd[c.dtype == ISOQ_F16 ? 0 : 1];
+        a.k_half = plan.kt->half;
+        a.v_half = plan.vt->half;
+    }
+    return a;
+}
+
+isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, int n_seqs)
+{
+    void *args[] = {&a};
+    const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(c.pk->variant, c.pk->bits);
+    const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, c.pk->variant);
+    if (!fn)
+        return ISOQ_E_UNSUPPORTED;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess)
+            return hip_fail(e, "hipFuncSetAttribute");
+    }
+    // (splits last: those that some sequences do not reach come after those that all do)
+    return launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)n_seqs, (unsigned)plan.n_splits), 256, args, lds, c.stream);
+}
+
+// The plans of a call: of the sequences' own positions, and of the prefixes'.
+struct AttnPlans {
+    AttnPlan own, pre;
+    bool prefix;
+    size_t bytes;
+    bool ok;   // (false: no memory for a handle's tables)
+};
+
+AttnPlans attn_plans(const AttnCall &c)
+{
+    AttnPlans p{};
+    const isoq_params *pk = c.pk;
+    p.prefix = c.n_prefixes > 0 && c.max_prefix_blocks > 0 && c.max_prefix_len > 0 && c.max_prefix_tokens > 0;
+    const int most = p.prefix ? kAttnMaxSplits / 2 : kAttnMaxSplits;   // (a row's join takes both kinds)
+    p.own = attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads, c.block_size, c.max_blocks,
+                      c.max_len, most);
+    const bool tables = pk->attn_by_tables && c.pv->attn_by_tables;
+    p.ok = !tables || p.own.kern.fn;
+    if (!p.prefix) {
+        p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
+        return p;
+    }
+    p.pre = attn_plan(pk, c.pv, c.dtype, c.n_prefixes, (int)c.max_prefix_tokens, c.n_q_heads, c.n_kv_heads, c.block_size,
+                      c.max_prefix_blocks, c.max_prefix_len, most);
+    p.ok = p.ok && (!tables || p.pre.kern.fn);
+    p.bytes = sizeof(float) * (size_t)c.n_tokens * c.n_q_heads * (p.own.n_splits + p.pre.n_splits) * (p.own.width + 2);
+    return p;
+}
+
+isoq_status check_prefix(const AttnCall &c)
+{
+    if (c.n_prefixes < 0 || c.max_prefix_blocks < 0 || c.max_prefix_len < 0 || c.max_prefix_tokens < 0 ||
+        (!c.prefix_start && c.n_prefixes > 1))
+        return ISOQ_E_INVALID;
+    if (c.n_prefixes > 65535 || (int64_t)c.max_prefix_blocks * c.block_size > kAttnMaxPos ||
+        c.max_prefix_tokens > kAttnMaxRows / c.n_q_heads)
+        return ISOQ_E_UNSUPPORTED;
+    return ISOQ_OK;
+}
+
+isoq_status attn_call(AttnCall c)
+{
+    isoq_status st = check_attn(c.pk, c.pv, c.dtype, c.n_tokens, c.max_q_len, c.n_seqs, c.n_q_heads, c.n_kv_heads,
+                                c.block_size, c.max_blocks, c.max_len);
+    if (st == ISOQ_OK)
+        st = check_prefix(c);
+    if (st != ISOQ_OK)
+        return st;
+    const float scale2 = (float)((double)c.scale * 1.4426950408889634);   // (logits in units of ln 2)
+    if (c.n_blocks < 0 || !std::isfinite(scale2) || (!c.q_start && (c.n_tokens != c.n_seqs || c.max_q_len != 1)))
+        return ISOQ_E_INVALID;
+    if (c.n_tokens == 0 || c.n_seqs == 0)
+        return ISOQ_OK;
+    c.max_prefix_tokens = std::min(c.max_prefix_tokens, c.n_tokens);
+    if (c.n_blocks == 0)
+        c.n_prefixes = 0;
+    const bool no_keys = c.n_blocks == 0 || c.max_blocks == 0 || c.max_len == 0;
+    const AttnPlans plans = attn_plans(c);
+    if (!c.q || !c.out || !c.seq_lens || (!no_keys && !c.block_table) ||
+        (plans.prefix && (!c.prefix_table || !c.prefix_lens)) ||
+        ((!no_keys || plans.prefix) && (!c.k_idx || !c.k_rho || !c.v_idx || !c.v_rho)))
+        return ISOQ_E_NULL;
+    if (!aligned(c.q, 16) || !aligned(c.out, 16) || !aligned(c.k_idx, 16) || !aligned(c.v_idx, 16) || !aligned(c.k_rho, 4) ||
+        !aligned(c.v_rho, 4) || !aligned(c.block_table, 4) || !aligned(c.seq_lens, 4) || !aligned(c.q_start, 4) ||
+        !aligned(c.lse, 4) || !aligned(c.workspace, 16) || !aligned(c.prefix_table, 4) || !aligned(c.prefix_lens, 4) ||
+        !aligned(c.prefix_start, 4))
+        return ISOQ_E_ALIGN;
+    if (!plans.ok)
+        return ISOQ_E_NOMEM;
+    const size_t need = plans.bytes;
+    if (need > 0 && !c.workspace)
+        return ISOQ_E_NULL;
+    if (need > c.workspace_bytes)
+        return ISOQ_E_INVALID;
+    st = check_device(c.pk);
+    if (st != ISOQ_OK)
+        return st;
+
+    const AttnPlan &plan = plans.own;
+    AttnArgs a = attn_args(c, plan, scale2);
+    if (no_keys)
+        a.cap = 0;
+    if (plans.prefix)
+        a.part_splits += plans.pre.n_splits;
+    if (need) {
+        a.part = static_cast<float *>(c.workspace);
+        a.part_ml = a.part + (size_t)c.n_tokens * c.n_q_heads * a.part_splits * plan.width;
+    }
+    AttnPrefix p{};
+    if (plans.prefix) {
+        AttnCall shared = c;   // every token of a prefix's sequences, all its positions
+        shared.block_table = c.prefix_table;
+        shared.max_blocks = c.max_prefix_blocks;
+        shared.seq_lens = c.prefix_lens;
+        shared.max_q_len = (int)c.max_prefix_tokens;
+        shared.full = true;
+        AttnArgs b = attn_args(shared, plans.pre, scale2);
+        b.shared = c.prefix_start;
+        b.n_all = c.n_seqs;
+        b.part = a.part;
+        b.part_ml = a.part_ml;
+        b.part_splits = a.part_splits;
+        b.part_first = a.n_splits;
+        p = AttnPrefix{c.prefix_start, c.prefix_lens, c.n_prefixes, c.n_seqs, (int32_t)c.max_prefix_tokens,
+                       b.cap, b.chunk, b.n_splits, b.even};
+        st = launch_attn(shared, plans.pre, b, c.n_prefixes);
+        if (st != ISOQ_OK)
+            return st;
+    }
+    st = launch_attn(c, plan, a, c.n_seqs);
+    if (st != ISOQ_OK || need == 0)
+        return st;
+    const bool few = a.part_splits <= kAttnJoinFew;
+    const unsigned rows = (unsigned)c.n_q_heads * (unsigned)c.max_q_len, per = few ? 256 / plan.slots : 1;
+    void *args[] = {&a, &p};
+    const void *join = plans.prefix ? attn_prefix_join_kernel_for(c.pk->variant, few) : attn_join_kernel_for(c.pk->variant, few);
+    return launch_lds(join, dim3((rows + per - 1) / per, (unsigned)c.n_seqs), 256, args, 0, c.stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -223,102 +448,69 @@ isoq_status isoq_kv_attn(const isoq_params *pk, const isoq_params *pv, int dtype
                          int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len, float scale, void *out,
                          float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
-    isoq_status st = check_attn(pk, pv, dtype, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads, block_size,
-                                max_blocks_per_seq, max_len);
-    if (st != ISOQ_OK)
-        return st;
-    const float scale2 = (float)((double)scale * 1.4426950408889634);   // (logits in units of ln 2)
-    if (n_blocks < 0 || !std::isfinite(scale2) || (!q_start && (n_tokens != n_seqs || max_q_len != 1)))
-        return ISOQ_E_INVALID;
-    if (n_tokens == 0 || n_seqs == 0)
-        return ISOQ_OK;
-    const bool no_keys = n_blocks == 0 || max_blocks_per_seq == 0 || max_len == 0;
-    if (!q || !out || !seq_lens || (!no_keys && (!k_idx || !k_rho || !v_idx || !v_rho || !block_table)))
-        return ISOQ_E_NULL;
-    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_idx, 16) || !aligned(v_idx, 16) || !aligned(k_rho, 4) ||
-        !aligned(v_rho, 4) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(q_start, 4) ||
-        !aligned(lse, 4) || !aligned(workspace, 16))
-        return ISOQ_E_ALIGN;
-    const AttnPlan plan =
-        attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len);
-    if (pk->attn_by_tables && pv->attn_by_tables && !plan.kern.fn)
-        return ISOQ_E_NOMEM;
-    const size_t need = plan_bytes(plan, n_tokens, n_q_heads);
-    if (need > 0 && !workspace)
-        return ISOQ_E_NULL;
-    if (need > workspace_bytes)
-        return ISOQ_E_INVALID;
-    st = check_device(pk);
-    if (st != ISOQ_OK)
-        return st;
+    return attn_call(AttnCall{pk, pv, dtype, q, q_start, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads, k_idx, k_rho,
+                              v_idx, v_rho, n_blocks, block_size, block_table, max_blocks_per_seq, seq_lens, max_len,
+                              nullptr, 0, nullptr, 0, nullptr, 0, 0, scale, out, lse, workspace, workspace_bytes, stream,
+                              false});
+}
 
-    AttnArgs a{};
-    a.q = q;
-    a.out = out;
-    a.lse = lse;
-    a.part = need ? static_cast<float *>(workspace) : nullptr;
-    a.part_ml = need ? a.part + (size_t)n_tokens * n_q_heads * plan.n_splits * plan.width : nullptr;
-    a.k_idx = k_idx;
-    a.v_idx = v_idx;
-    a.k_rho = k_rho;
-    a.v_rho = v_rho;
-    a.block_table = block_table;
-    a.seq_lens = seq_lens;
-    a.q_start = q_start;
-    a.k_params = pk->dparams;
-    a.v_params = pv->dparams;
-    a.n_blocks = n_blocks;
-    a.set_stride = (int64_t)slots_per_set(pk->variant, pk->d) * params_per_slot(pk->variant);
-    a.n_tokens = (int32_t)n_tokens;
-    a.max_q_len = max_q_len;
-    a.n_q_heads = n_q_heads;
-    a.n_kv_heads = n_kv_heads;
-    a.group = n_q_heads / n_kv_heads;
-    a.block_size = block_size;
-    a.max_blocks = max_blocks_per_seq;
-    a.cap = no_keys ? 0 : (int32_t)plan.max_pos;
-    a.k_sets = pk->n_sets;
-    a.v_sets = pv->n_sets;
-    a.variant = pk->variant;
-    a.q_f16 = dtype == ISOQ_F16;
-    a.chunk = plan.chunk;
-    a.n_splits = plan.n_splits;
-    a.even = plan.kern.parts;
-    a.scale = scale2;
-    a.div_block = make_fastdiv((uint32_t)block_size);
-    a.d = pk->d;
-    a.width = plan.width;
-    a.slots = plan.slots;
-    a.rec = (int32_t)record_bytes(pk->variant, pk->d, pk->bits);
-    a.rec_lp = a.rec % 16 == 0 ? 4 : a.rec % 8 == 0 ? 3 : -1;   // cache_piece
-    for (int k = 0; k < (1 << pk->bits); k++) {
-        a.k_lev[k] = pk->levels[k];
-        a.v_lev[k] = pv->levels[k];
-    }
-    a.k_dig = pk->lv;
-    if (plan.kern.fn) {
-        a.v_dig = plan.vt->vd[dtype == ISOQ_F16 ? 0 : 1];
-        a.k_half = plan.kt->half;
-        a.v_half = plan.vt->half;
-    }
-    void *args[] = {&a};
-    const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(pk->variant, pk->bits);
-    const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, pk->variant);
-    if (!fn)
-        return ISOQ_E_UNSUPPORTED;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess)
-            return hip_fail(e, "hipFuncSetAttribute");
-    }
-    // (splits last: those that some sequences do not reach come after those that all do)
-    st = launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)n_seqs, (unsigned)plan.n_splits), 256, args, lds, stream);
-    if (st != ISOQ_OK || need == 0)
-        return st;
-    const bool few = plan.n_splits <= kAttnJoinFew;
-    const unsigned rows = (unsigned)n_q_heads * (unsigned)max_q_len, per = few ? 256 / plan.slots : 1;
-    return launch_lds(attn_join_kernel_for(pk->variant, few), dim3((rows + per - 1) / per, (unsigned)n_seqs), 256, args, 0,
-                      stream);
+isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
+                               const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
+                               int n_kv_heads, const uint8_t *k_idx, const float *k_rho, const uint8_t *v_idx,
+                               const float *v_rho, int64_t n_blocks, int block_size, const int32_t *block_table,
+                               int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len, float scale, void *out,
+                               float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attn_call(AttnCall{pk, pv, dtype, q, q_start, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads, k_idx, k_rho,
+                              v_idx, v_rho, n_blocks, block_size, block_table, max_blocks_per_seq, seq_lens, max_len,
+                              nullptr, 0, nullptr, 0, nullptr, 0, 0, scale, out, lse, workspace, workspace_bytes, stream,
+                              true});
+}
+
+size_t isoq_kv_attn_prefix_workspace(const isoq_params *pk, const isoq_params *pv, int dtype, int64_t n_tokens,
+                                     int max_q_len, int n_seqs, int n_q_heads, int n_kv_heads, int block_size,
+                                     int max_blocks_per_seq, int64_t max_len, int n_prefixes, int64_t max_prefix_tokens,
+                                     int max_prefix_blocks, int64_t max_prefix_len)
+{
+    AttnCall c{};
+    c.pk = pk;
+    c.pv = pv;
+    c.dtype = dtype;
+    c.n_tokens = n_tokens;
+    c.max_q_len = max_q_len;
+    c.n_seqs = n_seqs;
+    c.n_q_heads = n_q_heads;
+    c.n_kv_heads = n_kv_heads;
+    c.block_size = block_size;
+    c.max_blocks = max_blocks_per_seq;
+    c.max_len = max_len;
+    c.max_prefix_blocks = max_prefix_blocks;
+    c.max_prefix_len = max_prefix_len;
+    c.n_prefixes = n_prefixes;
+    c.max_prefix_tokens = std::min(max_prefix_tokens, n_tokens);
+    static const int32_t some = 0;
+    c.prefix_start = &some;   // (only whether there is one matters here)
+    if (check_attn(pk, pv, dtype, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq,
+                   max_len) != ISOQ_OK ||
+        check_prefix(c) != ISOQ_OK || n_tokens == 0 || n_seqs == 0)
+        return 0;
+    return attn_plans(c).bytes;
+}
+
+isoq_status isoq_kv_attn_prefix(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
+                                const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
+                                int n_kv_heads, const uint8_t *k_idx, const float *k_rho, const uint8_t *v_idx,
+                                const float *v_rho, int64_t n_blocks, int block_size, const int32_t *block_table,
+                                int max_blocks_per_seq, const int32_t *seq_lens, int64_t max_len,
+                                const int32_t *prefix_table, int max_prefix_blocks, const int32_t *prefix_lens,
+                                int64_t max_prefix_len, const int32_t *prefix_start, int n_prefixes,
+                                int64_t max_prefix_tokens, float scale, void *out, float *lse, void *workspace,
+                                size_t workspace_bytes, void *stream)
+{
+    return attn_call(AttnCall{pk, pv, dtype, q, q_start, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads, k_idx, k_rho,
+                              v_idx, v_rho, n_blocks, block_size, block_table, max_blocks_per_seq, seq_lens, max_len,
+                              prefix_table, max_prefix_blocks, prefix_lens, max_prefix_len, prefix_start, n_prefixes,
+                              max_prefix_tokens, scale, out, lse, workspace, workspace_bytes, stream, false});
 }
 
 isoq_status isoq_kv_copy_blocks(const isoq_params *pk, const isoq_sketch *sk, const int32_t *block_pairs,

@@ -705,7 +705,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             a.lse[row] = attn_lse(ref, l);
         return;
     }
-    float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 4 * half;
+    float *dst = a.part + attn_part(a, row, blockIdx.z) * D + 4 * half;
 #pragma unroll
     for (int c = 0; c < C::CT; c++)
 #pragma unroll
@@ -714,7 +714,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 *reinterpret_cast<f32x4 *>(dst + 32 * c + 8 * b) =
                     f32x4{acc[c][4 * b] * vs, acc[c][4 * b + 1] * vs, acc[c][4 * b + 2] * vs, acc[c][4 * b + 3] * vs};
     if (half == 0) {
-        float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
+        float *ml = a.part_ml + attn_part(a, row, blockIdx.z) * 2;
         ml[0] = ref;
         ml[1] = l;
     }

@@ -12,20 +12,26 @@ namespace {
 // The new tokens of sequence s: rows first .. first + n - 1 of q, of which
 // `rows` are computed (max_q_len at most), and its length.
 struct AttnSeq {
-    int first, n, rows, len;
-    // Positions that token i attends to: those up to its own, the newest token
-    // being the last position.
+    int first, n, rows, len, full;
+    // Positions that token i attends to: all, or those up to its own, the newest
+    // token being the last position.
     __device__ __forceinline__ int limit(int i, int cap) const
     {
-        const int64_t l = (int64_t)len - (n - 1 - i);
+        const int64_t l = (int64_t)len - (full ? 0 : n - 1 - i);
         return (int)(l < 0 ? 0 : l < cap ? l : cap);
     }
 };
 
 __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 {
-    AttnSeq q{s, 1, 1, a.seq_lens[s]};
-    if (a.q_start) {   // (clamped: no row outside q is touched, whatever q_start holds)
+    AttnSeq q{s, 1, 1, a.seq_lens[s], a.full};
+    if (a.n_all > 0) {   // (clamped likewise)
+        const int from = a.shared ? min(max(a.shared[s], 0), a.n_all) : 0;
+        const int to = a.shared ? min(max(a.shared[s + 1], from), a.n_all) : a.n_all;
+        q.first = a.q_start ? min(max(a.q_start[from], 0), a.n_tokens) : from;
+        q.n = (a.q_start ? min(max(a.q_start[to], q.first), a.n_tokens) : to) - q.first;
+        q.rows = min(q.n, a.max_q_len);
+    } else if (a.q_start) {   // (clamped: no row outside q is touched, whatever q_start holds)
         q.first = min(max(a.q_start[s], 0), a.n_tokens);
         q.n = min(max(a.q_start[s + 1], q.first), a.n_tokens) - q.first;
         q.rows = min(q.n, a.max_q_len);
@@ -43,12 +49,23 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 // caller gives no max_len, a.chunk is longer than the sequences need (16 sequences of
 // 8,192 positions, 8 x 4 heads, a table of 131,072: 86 us instead of 42, one sequence 22
 // instead of 11): even parts were not measured there.
+__device__ __forceinline__ int attn_chunk(int len, int even, int cap, int n_splits, int chunk)
+{
+    if (!even)
+        return chunk;
+    const uint32_t l = (uint32_t)min(max(len, 0), cap), n = (uint32_t)n_splits;
+    return min(max(128, (int)((l + n - 1) / n + 63) & ~63), chunk);
+}
+
 __device__ __forceinline__ int attn_chunk(const AttnArgs &a, const AttnSeq &sq)
 {
-    if (!a.even)
-        return a.chunk;
-    const uint32_t len = (uint32_t)min(max(sq.len, 0), a.cap), n = (uint32_t)a.n_splits;
-    return min(max(128, (int)((len + n - 1) / n + 63) & ~63), a.chunk);
+    return attn_chunk(sq.len, a.even, a.cap, a.n_splits, a.chunk);
+}
+
+// Where a launch's split z of a row is, in part and part_ml.
+__device__ __forceinline__ int64_t attn_part(const AttnArgs &a, int64_t row, int z)
+{
+    return row * a.part_splits + a.part_first + z;
 }
 
 // Slot j (SW coordinates) of row `row` (head hq of its token): the sum of

@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     l = (red[4] + red[5]) + (red[6] + red[7]);
     if (odd && __syncthreads_or(seen))   // (odd is the same in all lanes; the logits may all be -inf: no NaN came up by itself)
         l = NAN;
-    const float inv = a.n_splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const float inv = a.part ? 1.f : l == 0.f ? 0.f : 1.f / l;
     for (int j = tid; j < a.slots; j += 256) {
         float y[SW];
 #pragma unroll
@@ -180,8 +180,8 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
                 y[c] += sum[(g * a.slots + j) * SW + c];
             y[c] *= inv;
         }
-        if (a.n_splits > 1) {
-            float *dst = a.part + (row * a.n_splits + blockIdx.z) * a.width + SW * j;
+        if (a.part) {
+            float *dst = a.part + attn_part(a, row, blockIdx.z) * a.width + SW * j;
 #pragma unroll
             for (int c = 0; c < SW; c++)
                 dst[c] = y[c];
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         }
     }
     if (tid == 0) {
-        if (a.n_splits > 1) {
-            float *ml = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
+        if (a.part) {
+            float *ml = a.part_ml + attn_part(a, row, blockIdx.z) * 2;
             ml[0] = m;
             ml[1] = l;
         } else if (a.lse) {

@@ -18,8 +18,57 @@
 namespace isoq {
 namespace {
 
-template <int VAR>
-__global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
+// A row's splits: `own` of its sequence from `at` on, then `all - own` of its
+// prefix, `jump` places further (in part and part_ml).
+struct RowSplits {
+    int64_t at;
+    int own, all, jump;
+    __device__ __forceinline__ int64_t place(int k) const { return at + k + (k < own ? 0 : jump); }
+};
+// (without a prefix jump is 0, and place() waits for no length)
+
+__device__ __forceinline__ int splits_of(int positions, int chunk)
+{
+    return (int)(((uint32_t)positions + (uint32_t)chunk - 1u) / (uint32_t)chunk);
+}
+
+// The splits that have positions of token i of sequence s (all = -1: the row is left
+// as it is).
+template <bool PREFIX>
+__device__ __forceinline__ RowSplits row_splits(const AttnArgs &a, const AttnPrefix &p, const AttnSeq &sq, int s, int i,
+                                                int64_t row)
+{
+    const int own = splits_of(sq.limit(i, a.cap), attn_chunk(a, sq));
+    RowSplits r{row * a.part_splits, PREFIX ? own : 0, own, 0};
+    if constexpr (PREFIX) {
+        int g = 0, first = 0, end = p.n_seqs;   // the prefix, and its sequences
+        if (p.start) {
+            for (int hi = p.n; g + 1 < hi;) {
+                const int mid = (g + hi) >> 1;
+                if (p.start[mid] <= s)
+                    g = mid;
+                else
+                    hi = mid;
+            }
+            first = max(p.start[g], 0);
+            end = p.start[g + 1];
+        }
+        if (s >= first && s < end) {
+            const int token = a.q_start ? min(max(a.q_start[min(first, p.n_seqs)], 0), a.n_tokens) : first;
+            if (sq.first + i - token >= p.max_tokens) {
+                r.all = -1;
+                return r;
+            }
+            const int len = p.lens[g];
+            r.all += splits_of(min(max(len, 0), p.cap), attn_chunk(len, p.even, p.cap, p.n_splits, p.chunk));
+            r.jump = a.n_splits - r.own;
+        }
+    }
+    return r;
+}
+
+template <int VAR, bool PREFIX>
+__device__ __forceinline__ void attn_join_row(const AttnArgs &a, const AttnPrefix &pre)
 {
     constexpr int SW = kGenSW<VAR>, AHEAD = 4;
     __shared__ float weight[kAttnMaxSplits], red[8];
@@ -31,12 +80,16 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
     if (i >= sq.rows)
         return;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + hq;
+    const RowSplits rs = row_splits<PREFIX>(a, pre, sq, blockIdx.y, i, row);
+    const int ns = rs.all;
+    if (PREFIX && ns < 0)   // (block-uniform)
+        return;
     const int groups = max(1, 256 / a.slots);
     const int g = tid / a.slots, j = tid - g * a.slots;
-    const float *p = a.part + row * a.n_splits * a.width + SW * j;
     f32x4 v[AHEAD][SW / 4];
+    const int last = PREFIX ? max(0, ns - 1) : a.n_splits - 1;   // (of one sequence's own splits: before their number is known)
     auto load = [&](int k, f32x4 *x) {   // (past the last split: that one again, not used)
-        const f32x4 *src = reinterpret_cast<const f32x4 *>(p + (int64_t)min(k, a.n_splits - 1) * a.width);
+        const f32x4 *src = reinterpret_cast<const f32x4 *>(a.part + rs.place(min(k, last)) * a.width + SW * j);
 #pragma unroll
         for (int c = 0; c < SW / 4; c++)
             x[c] = src[c];
@@ -44,10 +97,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
 #pragma unroll
     for (int u = 0; u < AHEAD; u++)
         load(g + u * groups, v[u]);
-    const float *ml = a.part_ml + (row * a.n_splits + min(tid, a.n_splits - 1)) * 2;
+    const float *ml = a.part_ml + rs.place(min(tid, last)) * 2;
     float m = ml[0], l = ml[1];
-    const int chunk = attn_chunk(a, sq);
-    const int ns = (int)(((uint32_t)sq.limit(i, a.cap) + (uint32_t)chunk - 1u) / (uint32_t)chunk);   // splits that have positions of this row
     if (tid >= ns) {
         m = -INFINITY;
         l = 0.f;
@@ -111,8 +162,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
         a.lse[row] = attn_lse(top, l);
 }
 
-template <int VAR>
-__global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
+template <int VAR, bool PREFIX>
+__device__ __forceinline__ void attn_join_rows(const AttnArgs &a, const AttnPrefix &pre)
 {
     constexpr int SW = kGenSW<VAR>, N = kAttnJoinFew;
     const AttnSeq sq = attn_seq(a, blockIdx.y);
@@ -121,19 +172,19 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
     if (g >= per || i >= sq.rows)
         return;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + hq;
-    const int chunk = attn_chunk(a, sq);
-    const int ns = (int)(((uint32_t)sq.limit(i, a.cap) + (uint32_t)chunk - 1u) / (uint32_t)chunk);   // splits that have positions of this row
-    const float *p = a.part + row * a.n_splits * a.width + SW * j;
-    const float *ml = a.part_ml + row * a.n_splits * 2;
+    const RowSplits rs = row_splits<PREFIX>(a, pre, sq, blockIdx.y, i, row);
+    const int ns = rs.all;
+    if (PREFIX && ns < 0)
+        return;
     float m[N], top = -INFINITY, l = 0.f, y[SW];
     f32x4 v[N][SW / 4];
 #pragma unroll
     for (int k = 0; k < N; k++)
         if (k < ns) {
-            m[k] = ml[2 * k];
+            m[k] = a.part_ml[rs.place(k) * 2];
 #pragma unroll
             for (int c = 0; c < SW / 4; c++)
-                v[k][c] = *reinterpret_cast<const f32x4 *>(p + (int64_t)k * a.width + 4 * c);
+                v[k][c] = *reinterpret_cast<const f32x4 *>(a.part + rs.place(k) * a.width + SW * j + 4 * c);
         }
 #pragma unroll
     for (int k = 0; k < N; k++)
@@ -147,7 +198,7 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
     for (int k = 0; k < N; k++)
         if (k < ns) {
             const float f = __builtin_amdgcn_exp2f(m[k] - ref);
-            l = fmaf(f, ml[2 * k + 1], l);
+            l = fmaf(f, a.part_ml[rs.place(k) * 2 + 1], l);
 #pragma unroll
             for (int c = 0; c < SW; c++)
                 y[c] = fmaf(f, v[k][c / 4][c % 4], y[c]);
@@ -162,23 +213,53 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
 }
 
 template <int VAR>
-const void *join_kernel(bool few)
+__global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
 {
+    attn_join_row<VAR, false>(a, AttnPrefix{});
+}
+
+template <int VAR>
+__global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
+{
+    attn_join_rows<VAR, false>(a, AttnPrefix{});
+}
+
+template <int VAR>
+__global__ __launch_bounds__(256) void attn_prefix_join_kernel(const AttnArgs a, const AttnPrefix p)
+{
+    attn_join_row<VAR, true>(a, p);
+}
+
+template <int VAR>
+__global__ __launch_bounds__(256) void attn_prefix_join_few_kernel(const AttnArgs a, const AttnPrefix p)
+{
+    attn_join_rows<VAR, true>(a, p);
+}
+
+template <int VAR>
+const void *join_kernel(bool prefix, bool few)
+{
+    if (prefix)
+        return few ? reinterpret_cast<const void *>(&attn_prefix_join_few_kernel<VAR>)
+                   : reinterpret_cast<const void *>(&attn_prefix_join_kernel<VAR>);
     return few ? reinterpret_cast<const void *>(&attn_join_few_kernel<VAR>)
                : reinterpret_cast<const void *>(&attn_join_kernel<VAR>);
 }
 
-}  // namespace
-
-const void *attn_join_kernel_for(int variant, bool few)
+const void *join_of(int variant, bool prefix, bool few)
 {
     switch (variant) {
-    case VAR_FULL: return join_kernel<VAR_FULL>(few);
-    case VAR_FAST: return join_kernel<VAR_FAST>(few);
-    case VAR_PLANAR2D: return join_kernel<VAR_PLANAR2D>(few);
-    case VAR_BLOCK8: return join_kernel<VAR_BLOCK8>(few);
+    case VAR_FULL: return join_kernel<VAR_FULL>(prefix, few);
+    case VAR_FAST: return join_kernel<VAR_FAST>(prefix, few);
+    case VAR_PLANAR2D: return join_kernel<VAR_PLANAR2D>(prefix, few);
+    case VAR_BLOCK8: return join_kernel<VAR_BLOCK8>(prefix, few);
     }
     return nullptr;
 }
+
+}  // namespace
+
+const void *attn_join_kernel_for(int variant, bool few) { return join_of(variant, false, few); }
+const void *attn_prefix_join_kernel_for(int variant, bool few) { return join_of(variant, true, few); }
 
 }  // namespace isoq

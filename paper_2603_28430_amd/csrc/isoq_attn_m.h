@@ -776,17 +776,17 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 y[c] = fmaf(f, part[(x * ROWS + r) * D + 8 * j + c], y[c]);
         }
     };
-    if (a.n_splits > 1) {
+    if (a.part) {
         __syncthreads();
         if (r >= n)
             return;
         merge();
-        float *dst = a.part + (row * a.n_splits + blockIdx.z) * D + 8 * j;
+        float *dst = a.part + attn_part(a, row, blockIdx.z) * D + 8 * j;
 #pragma unroll
         for (int c = 0; c < 8; c++)
             dst[c] = y[c];
         if (j == 0) {
-            float *to = a.part_ml + (row * a.n_splits + blockIdx.z) * 2;
+            float *to = a.part_ml + attn_part(a, row, blockIdx.z) * 2;
             to[0] = top;
             to[1] = sum;
         }

@@ -69,6 +69,10 @@ def _load():
                                c_int, vp, i64, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     L.isoq_kv_attn_workspace.argtypes = [vp, vp, c_int, i64, c_int, c_int, c_int, c_int, c_int, c_int, i64]
     L.isoq_kv_attn_workspace.restype = ctypes.c_size_t
+    L.isoq_kv_attn_cross.argtypes = L.isoq_kv_attn.argtypes
+    L.isoq_kv_attn_prefix.argtypes = L.isoq_kv_attn.argtypes[:20] + [vp, c_int, vp, i64, vp, c_int, i64] + L.isoq_kv_attn.argtypes[20:]
+    L.isoq_kv_attn_prefix_workspace.argtypes = L.isoq_kv_attn_workspace.argtypes + [c_int, i64, c_int, i64]
+    L.isoq_kv_attn_prefix_workspace.restype = ctypes.c_size_t
     L.isoq_kv_copy_blocks.argtypes = [vp, vp, vp, i64, c_int, vp, vp, vp, vp, vp, vp, i64, c_int, vp]
     L.isoq_kv_compact.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, vp, c_int, c_int, vp, vp, vp, vp, vp, vp, i64,
                                   c_int, vp]
@@ -94,7 +98,8 @@ def _load():
     for f in ("isoq_params_init", "isoq_params_destroy", "isoq_params_export", "isoq_params_info",
               "isoq_quantize", "isoq_dequantize", "isoq_roundtrip", "isoq_kv_append", "isoq_kv_scores", "isoq_sketch_init",
               "isoq_sketch_destroy", "isoq_sketch_export", "isoq_quantize_qjl", "isoq_kv_append_qjl",
-              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn",
+              "isoq_kv_scores_qjl", "isoq_kv_scores_filled", "isoq_kv_attn", "isoq_kv_attn_cross",
+              "isoq_kv_attn_prefix",
               "isoq_kv_copy_blocks", "isoq_kv_compact", "isoq_kv_plan", "isoq_rope_init", "isoq_rope_destroy",
               "isoq_rope_freqs", "isoq_qk_norm_rope", "isoq_codebook_lloyd",
               "isoq_rotation_draws"):
@@ -490,7 +495,8 @@ def _attn_buffers(q, k_idx, k_rho, out, lse, workspace, need):
 
 
 def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, scale: float = 1.0,
-                 q_start=None, max_q_len=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
+                 q_start=None, max_q_len=None, max_len=None, out=None, lse=None, workspace=None, stream=None,
+                 causal: bool = True, prefix=None):
     """Attention of new tokens' queries q [n_tokens, n_q_heads, d] over the paged
     caches k_idx, v_idx [n_blocks, n_kv_heads, block_size, R] / k_rho, v_rho
     [n_blocks, n_kv_heads, block_size] with block_table int32 [n_seqs,
@@ -505,7 +511,8 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
     are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
     least isoq_kv_attn_workspace(...) bytes.  What is not passed (out, lse,
     workspace) is allocated from torch's pool for `stream`, by default the
-    current one."""
+    current one.  causal=False is isoq_kv_attn_cross; prefix, the arguments of
+    isoq_kv_attn_prefix."""
     torch = _torch()
     shape, cache, table = q.shape, k_idx.shape, block_table.shape
     if len(shape) != 3 or len(cache) != 4 or len(table) != 2:
@@ -538,28 +545,104 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
         raise ValueError("lse must be fp32 [n_tokens, n_q_heads]")
     if max_len is None:
         max_len = max_blocks * block_size
-    need = lib.isoq_kv_attn_workspace(pk.handle, pv.handle, code, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
-                                      block_size, max_blocks, max_len)
+    if prefix is None:
+        need = lib.isoq_kv_attn_workspace(pk.handle, pv.handle, code, n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
+                                          block_size, max_blocks, max_len)
+    else:
+        need = lib.isoq_kv_attn_prefix_workspace(pk.handle, pv.handle, code, n_tokens, max_q_len, n_seqs, n_q_heads,
+                                                 n_kv_heads, block_size, max_blocks, max_len, *prefix.sizes)
     if workspace is not None and (workspace.dtype != torch.uint8 or workspace.numel() < need):
         raise ValueError(f"workspace must be uint8 of at least {need} bytes")
     tensors = [q, k_idx, k_rho, v_idx, v_rho, block_table, seq_lens]
     for t in (q_start, out, lse, workspace):
         if t is not None:
             tensors.append(t)
+    if prefix is not None:
+        tensors += prefix.tensors
     _on_current(q, tensors, stream)
     if stream is None:
         out, lse, workspace = _attn_buffers(q, k_idx, k_rho, out, lse, workspace, need)
     else:
         with torch.cuda.stream(stream):
             out, lse, workspace = _attn_buffers(q, k_idx, k_rho, out, lse, workspace, need)
-    st = lib.isoq_kv_attn(pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs,
-                          n_q_heads, n_kv_heads, k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(),
-                          v_rho.data_ptr(), n_blocks, block_size, block_table.data_ptr(), max_blocks,
-                          seq_lens.data_ptr(), max_len, scale, out.data_ptr(), lse.data_ptr(), _ptr(workspace),
-                          0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if prefix is None:
+        st = (lib.isoq_kv_attn if causal else lib.isoq_kv_attn_cross)(
+            pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
+            k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(), v_rho.data_ptr(), n_blocks, block_size,
+            block_table.data_ptr(), max_blocks, seq_lens.data_ptr(), max_len, scale, out.data_ptr(), lse.data_ptr(),
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    else:
+        st = lib.isoq_kv_attn_prefix(
+            pk.handle, pv.handle, code, q.data_ptr(), _ptr(q_start), n_tokens, max_q_len, n_seqs, n_q_heads, n_kv_heads,
+            k_idx.data_ptr(), k_rho.data_ptr(), v_idx.data_ptr(), v_rho.data_ptr(), n_blocks, block_size,
+            block_table.data_ptr(), max_blocks, seq_lens.data_ptr(), max_len, *prefix.args, scale, out.data_ptr(),
+            lse.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream))
     if st:
-        _check(st, "isoq_kv_attn")
+        _check(st, "isoq_kv_attn" if causal and prefix is None else "isoq_kv_attn_cross" if prefix is None else
+               "isoq_kv_attn_prefix")
     return out, lse
+
+
+def isoq_kv_attn_cross(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, scale: float = 1.0,
+                       q_start=None, max_q_len=None, max_len=None, out=None, lse=None, workspace=None, stream=None):
+    """isoq_kv_attn with every token of a sequence attending to all of its
+    seq_lens positions: a decoder's attention to its encoder's states, which stand
+    in the cache (see include/isoquant.h).  Arguments and results as isoq_kv_attn."""
+    return isoq_kv_attn(pk, q, k_idx, k_rho, pv, v_idx, v_rho, block_table, seq_lens, scale, q_start, max_q_len, max_len,
+                        out, lse, workspace, stream, False)
+
+
+class _Prefix:
+    """The arguments of isoq_kv_attn_prefix beyond those of isoq_kv_attn, checked."""
+    __slots__ = ("tensors", "sizes", "args")
+
+    def __init__(self, table, lens, start, max_tokens, max_len, n_tokens, block_size):
+        whole = _torch_module.int32
+        if table.dim() != 2 or lens.shape != (table.shape[0],) or table.dtype != whole or lens.dtype != whole:
+            raise ValueError("prefix_table int32 [n_prefixes, max_prefix_blocks], prefix_lens int32 [n_prefixes]")
+        n, blocks = table.shape
+        self.tensors = [table, lens]
+        if start is not None:
+            if start.shape != (n + 1,) or start.dtype != whole:
+                raise ValueError("prefix_start must be int32 [n_prefixes + 1]")
+            self.tensors.append(start)
+        elif n > 1:
+            raise ValueError("several prefixes need prefix_start")
+        max_tokens = n_tokens if max_tokens is None else max_tokens
+        max_len = blocks * block_size if max_len is None else max_len
+        self.sizes = (n, max_tokens, blocks, max_len)
+        self.args = (table.data_ptr(), blocks, lens.data_ptr(), max_len, _ptr(start), n, max_tokens)
+
+
+def isoq_kv_attn_prefix(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_table, seq_lens, prefix_table,
+                        prefix_lens, prefix_start=None, scale: float = 1.0, q_start=None, max_q_len=None, max_len=None,
+                        max_prefix_tokens=None, max_prefix_len=None, out=None, lse=None, workspace=None, stream=None):
+    """isoq_kv_attn for sequences that share long beginnings: prefix_table int32
+    [n_prefixes, max_prefix_blocks] and prefix_lens int32 [n_prefixes] are in the
+    same cache once, and prefix p is what the sequences prefix_start[p] ..
+    prefix_start[p + 1] - 1 (int32 [n_prefixes + 1]; None: one prefix, of all) begin
+    with; block_table and seq_lens are the sequences' own positions after it.
+    max_prefix_tokens: tokens of one prefix's sequences at most (by default all
+    there are); max_prefix_len: positions of the longest prefix at most.  Other
+    arguments and results as isoq_kv_attn, workspace of at least
+    isoq_kv_attn_prefix_workspace(...) bytes."""
+    _torch()
+    if q.dim() != 3 or k_idx.dim() != 4:
+        raise ValueError("q [n_tokens, n_q_heads, d], k_idx [n_blocks, n_kv_heads, block_size, R]")
+    prefix = _Prefix(prefix_table, prefix_lens, prefix_start, max_prefix_tokens, max_prefix_len, q.shape[0], k_idx.shape[2])
+    return isoq_kv_attn(pk, q, k_idx, k_rho, pv, v_idx, v_rho, block_table, seq_lens, scale, q_start, max_q_len, max_len,
+                        out, lse, workspace, stream, True, prefix)
+
+
+def isoq_kv_attn_prefix_workspace(pk: Params, pv: Params, dtype, n_tokens: int, max_q_len: int, n_seqs: int,
+                                  n_q_heads: int, n_kv_heads: int, block_size: int, max_blocks_per_seq: int, max_len: int,
+                                  n_prefixes: int, max_prefix_tokens: int, max_prefix_blocks: int,
+                                  max_prefix_len: int) -> int:
+    """Bytes of workspace that isoq_kv_attn_prefix takes for these sizes (see include/isoquant.h)."""
+    return int(lib.isoq_kv_attn_prefix_workspace(pk.handle, pv.handle, _dtype_code(dtype), int(n_tokens), int(max_q_len),
+                                                 int(n_seqs), int(n_q_heads), int(n_kv_heads), int(block_size),
+                                                 int(max_blocks_per_seq), int(max_len), int(n_prefixes),
+                                                 int(max_prefix_tokens), int(max_prefix_blocks), int(max_prefix_len)))
 
 
 class Sketch:
