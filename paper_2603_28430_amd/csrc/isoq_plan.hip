@@ -9,6 +9,7 @@
 //     tokens    token i of a sequence has position lens + i.
 // Three prefix sums over the sequences (new tokens, blocks taken, blocks
 // released), so the result does not depend on the order in which anything runs.
+// Sums saturate at 2^31 - 1, past every list and every token.
 #include <hip/hip_runtime.h>
 
 #include "isoq_device.h"
@@ -16,6 +17,8 @@
 
 namespace isoq {
 namespace {
+
+__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
 
 struct PlanSeq {
     int old, want, have, need;
@@ -39,114 +42,234 @@ __device__ __forceinline__ PlanSeq plan_seq(const PlanArgs &a, int s)
     return q;
 }
 
-// Slot and position of token t, once the sequences' lengths, first tokens and
-// blocks are there.
-__device__ __forceinline__ void plan_token(const PlanArgs &a, int t)
+// Slot and position of token t of sequence s, which are there.
+__device__ __forceinline__ void plan_place(const PlanArgs &a, int t, int s, int pos, bool fine)
 {
-    int lo = 0, hi = a.n_seqs;   // the first sequence that ends past t
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_start[mid + 1] > t)
-            hi = mid;
-        else
-            lo = mid + 1;
-    }
     int64_t slot = -1;
-    int pos = 0;
-    if (lo < a.n_seqs) {
-        const int first = a.q_start[lo], len = a.seq_lens[lo];
-        const bool fine = len == min(max(a.new_lens[lo], 0), a.cap);   // not refused
-        pos = (fine ? len - (a.q_start[lo + 1] - first) : len) + (t - first);
-        const uint32_t j = fast_div((uint32_t)pos, a.div_block);
-        if (fine && pos >= 0 && j < (uint32_t)a.max_blocks) {
-            const int blk = a.block_table[(int64_t)lo * a.max_blocks + j];
-            if (blk >= 0)
-                slot = (int64_t)blk * a.block_size + (pos - (int)(j * (uint32_t)a.block_size));
-        }
+    const uint32_t j = fast_div((uint32_t)pos, a.div_block);
+    if (fine && pos >= 0 && j < (uint32_t)a.max_blocks) {
+        const int blk = a.block_table[(int64_t)s * a.max_blocks + j];
+        if (blk >= 0)
+            slot = (int64_t)blk * a.block_size + (pos - (int)(j * (uint32_t)a.block_size));
     }
     a.slots[t] = slot;
     a.positions[t] = pos;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_all_kernel(const PlanArgs a)
+// The first sequence that ends past token t; start[s] .. start[s + 1] - 1 are those of s.
+__device__ __forceinline__ int plan_find(const int *start, int n, int t)
+{
+    int lo = 0;
+    for (int hi = n; lo < hi;) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid + 1] > t)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo;
+}
+
+// Slot and position of token t, once the sequences' lengths, first tokens and
+// blocks are there.
+__device__ __forceinline__ void plan_token(const PlanArgs &a, int t)
+{
+    const int s = plan_find(a.q_start, a.n_seqs, t);
+    if (s >= a.n_seqs) {
+        a.slots[t] = -1;
+        a.positions[t] = 0;
+        return;
+    }
+    const int first = a.q_start[s], len = a.seq_lens[s];
+    const bool fine = len == min(max(a.new_lens[s], 0), a.cap);   // not refused
+    plan_place(a, t, s, (fine ? len - (a.q_start[s + 1] - first) : len) + (t - first), fine);
+}
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int v)
+{
+#define ISOQ_SCAN_STEP(ctrl, rows) \
+    v = add_sat(v, __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xF, false))
+    ISOQ_SCAN_STEP(0x111, 0xF);   // row_shr 1, 2, 4, 8: within 16 lanes
+    ISOQ_SCAN_STEP(0x112, 0xF);
+    ISOQ_SCAN_STEP(0x114, 0xF);
+    ISOQ_SCAN_STEP(0x118, 0xF);
+    ISOQ_SCAN_STEP(0x142, 0xA);   // row_bcast 15: lane 15's to 16 .. 31, lane 47's to 48 .. 63
+    ISOQ_SCAN_STEP(0x143, 0xC);   // row_bcast 31: lane 31's to 32 .. 63
+#undef ISOQ_SCAN_STEP
+    return v;
+}
+
+// A sequence's blocks to move, a list of which the waves work off: free[from ..] to
+// its row downwards (taken), or its row to free[from ..] (released).
+struct PlanMove {
+    int seq, at, from, count;   // count < 0: released
+};
+
+// ONE: a sequence a thread at most, held in registers, and the token search in LDS;
+// else consecutive ones a thread, read again in every pass.
+template <bool ONE>
+__device__ __forceinline__ void plan_body(const PlanArgs &a)
 {
     constexpr int WAVES = kPlanThreads / 64;
-    __shared__ int64_t wave_sum[3][WAVES], most[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int per = (a.n_seqs + kPlanThreads - 1) / kPlanThreads;   // consecutive sequences a thread
+    // blocks that a thread moves by itself; more go to the list
+    constexpr int FEW = 2;
+    __shared__ int wave_sum[3][WAVES], most[WAVES], listed[2];
+    __shared__ PlanMove list[kPlanThreads];
+    __shared__ int start[ONE ? kPlanThreads + 1 : 1];
+    __shared__ int begin[ONE ? kPlanThreads : 1];   // position of its first new token, or ~ that where it is refused
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int per = ONE ? 1 : (a.n_seqs + kPlanThreads - 1) / kPlanThreads;
     const int s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
 
-    int64_t sum[3] = {0, 0, 0}, before[3], total[3];
+    if (tid < 2)
+        listed[tid] = 0;
+    const int n_free = *a.n_free;
+    PlanSeq mine{0, 0, 0, 0};
+    if (ONE && s0 < s1)
+        mine = plan_seq(a, s0);
+    auto seq = [&](int s) { return ONE ? mine : plan_seq(a, s); };
+    int sum[3] = {0, 0, 0}, before[3], total[3];
     for (int s = s0; s < s1; s++) {
-        const PlanSeq q = plan_seq(a, s);
-        sum[0] += q.fresh();
-        sum[1] += q.grow();
-        sum[2] += q.drop();
+        const PlanSeq q = seq(s);
+        sum[0] = add_sat(sum[0], q.fresh());
+        sum[1] = add_sat(sum[1], q.grow());
+        sum[2] = add_sat(sum[2], q.drop());
     }
+#pragma unroll
     for (int k = 0; k < 3; k++) {
-        int64_t x = sum[k];
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = __shfl_up((long long)x, o);
-            if (lane >= o)
-                x += y;
-        }
-        before[k] = x - sum[k];
+        const int x = wave_scan(sum[k]);
+        const int y = __builtin_amdgcn_update_dpp(0, x, 0x138, 0xF, 0xF, false);   // wave_shr 1
+        before[k] = lane == 0 ? 0 : y;
         if (lane == 63)
             wave_sum[k][w] = x;
     }
     __syncthreads();
+#pragma unroll
     for (int k = 0; k < 3; k++) {
         total[k] = 0;
+#pragma unroll
         for (int x = 0; x < WAVES; x++) {
             if (x == w)
-                before[k] += total[k];
-            total[k] += wave_sum[k][x];
+                before[k] = add_sat(before[k], total[k]);
+            total[k] = add_sat(total[k], wave_sum[k][x]);
         }
     }
-    const int64_t held = min(max((int64_t)*a.n_free, (int64_t)0), a.max_free);
-    const int64_t there = min(held + total[2], a.max_free);
+    const int max_free = (int)a.max_free;
+    const int held = min(max(n_free, 0), max_free);
+    const int there = min(add_sat(held, total[2]), max_free);
+
+    auto move = [&](const PlanMove &m, int first, int step) {
+        int *row = a.block_table + (int64_t)m.seq * a.max_blocks + m.at;
+        if (m.count < 0) {
+            const int n = min(-m.count, max_free - m.from);   // (from <= max_free)
+#pragma unroll 4
+            for (int j = first; j < n; j += step)
+                a.free_blocks[m.from + j] = row[j];
+        } else {
+#pragma unroll 4
+            for (int j = first; j < m.count; j += step)
+                row[j] = a.free_blocks[m.from - j];
+        }
+    };
+    auto put = [&](int which, const PlanMove &m) {
+        if (abs(m.count) <= FEW)
+            move(m, 0, 1);
+        else
+            list[atomicAdd(&listed[which], 1)] = m;
+    };
+    // the list's moves: all waves to one of many blocks, else a wave each
+    auto work_off = [&](int which) {
+        __syncthreads();
+        const int n = listed[which];
+        for (int x = 0; x < n; x++) {
+            const PlanMove m = list[x];
+            if (abs(m.count) > 512)
+                move(m, tid, kPlanThreads);
+            else if (x % WAVES == w)
+                move(m, lane, 64);
+        }
+        __syncthreads();
+        if constexpr (!ONE) {   // (the next sequences' moves take its place)
+            if (tid == 0)
+                listed[which] = 0;
+            __syncthreads();
+        }
+    };
 
     // what is released first: those that grow may take it
-    int64_t at = held + before[2];
-    for (int s = s0; s < s1; s++) {
-        const PlanSeq q = plan_seq(a, s);
-        for (int j = q.need; j < q.have; j++, at++)
-            if (at < a.max_free)
-                a.free_blocks[at] = a.block_table[(int64_t)s * a.max_blocks + j];
-    }
-    __syncthreads();
-    int64_t first = before[0], taken = before[1], most_taken = 0;
-    for (int s = s0; s < s1; s++) {
-        const PlanSeq q = plan_seq(a, s);
-        const bool fine = q.grow() == 0 || taken + q.grow() <= there;
-        if (fine) {
-            for (int j = q.have; j < q.need; j++)
-                a.block_table[(int64_t)s * a.max_blocks + j] = a.free_blocks[there - 1 - (taken + j - q.have)];
-            if (q.grow() > 0)
-                most_taken = taken + q.grow();
+    if (total[2] > 0) {
+        for (int k = 0, at = add_sat(held, before[2]); k < per; k++) {   // (a list of a thread's k-th sequences)
+            const int s = s0 + k;
+            if (s < s1) {
+                const PlanSeq q = seq(s);
+                if (q.drop() > 0 && at < max_free)
+                    put(0, PlanMove{s, q.need, at, -q.drop()});
+                at = add_sat(at, q.drop());
+            }
+            work_off(0);
         }
-        a.q_start[s] = (int)min(first, (int64_t)0x7FFFFFFF);
-        a.seq_lens[s] = fine ? q.want : q.old;
-        first += q.fresh();
-        taken += q.grow();
     }
+    int first = before[0], taken = before[1], most_taken = 0;
+    for (int k = 0; k < per; k++) {
+        const int s = s0 + k;
+        if (s < s1) {
+            const PlanSeq q = seq(s);
+            const int upto = add_sat(taken, q.grow());
+            const bool fine = q.grow() == 0 || upto <= there;
+            if (fine && q.grow() > 0) {
+                put(1, PlanMove{s, q.have, there - 1 - taken, q.grow()});
+                most_taken = upto;
+            }
+            a.q_start[s] = first;
+            a.seq_lens[s] = fine ? q.want : q.old;
+            if constexpr (ONE) {
+                start[s] = first;
+                begin[s] = fine ? q.old : ~q.old;
+            }
+            first = add_sat(first, q.fresh());
+            taken = upto;
+        }
+        if (!ONE || total[1] > 0)
+            work_off(1);
+    }
+#pragma unroll
     for (int o = 32; o > 0; o >>= 1)
-        most_taken = max(most_taken, (int64_t)__shfl_xor((long long)most_taken, o));
+        most_taken = max(most_taken, __shfl_xor(most_taken, o));
     if (lane == 0)
         most[w] = most_taken;
+    if (tid == 0) {
+        a.q_start[a.n_seqs] = total[0];
+        if constexpr (ONE)
+            start[a.n_seqs] = total[0];
+    }
     __syncthreads();
     if (tid == 0) {
+#pragma unroll
         for (int x = 1; x < WAVES; x++)
             most_taken = max(most_taken, most[x]);
-        a.q_start[a.n_seqs] = (int)min(total[0], (int64_t)0x7FFFFFFF);
-        *a.n_free_out = (int)(there - most_taken);
+        *a.n_free_out = there - most_taken;
     }
-    if (a.tokens_too) {
-        __syncthreads();
-        for (int t = tid; t < a.n_tokens; t += kPlanThreads)
+    if (!a.tokens_too)
+        return;
+    for (int t = tid; t < a.n_tokens; t += kPlanThreads) {
+        if constexpr (ONE) {
+            const int s = plan_find(start, a.n_seqs, t);
+            if (s >= a.n_seqs) {
+                a.slots[t] = -1;
+                a.positions[t] = 0;
+                continue;
+            }
+            const int b = begin[s];
+            plan_place(a, t, s, (b < 0 ? ~b : b) + (t - start[s]), b >= 0);
+        } else {
             plan_token(a, t);
+        }
     }
 }
+
+__global__ __launch_bounds__(kPlanThreads) void plan_one_kernel(const PlanArgs a) { plan_body<true>(a); }
+__global__ __launch_bounds__(kPlanThreads) void plan_many_kernel(const PlanArgs a) { plan_body<false>(a); }
 
 __global__ __launch_bounds__(256) void plan_slots_kernel(const PlanArgs a)
 {
@@ -157,7 +280,10 @@ __global__ __launch_bounds__(256) void plan_slots_kernel(const PlanArgs a)
 
 }  // namespace
 
-const void *plan_kernel() { return reinterpret_cast<const void *>(&plan_all_kernel); }
+const void *plan_kernel(bool one)
+{
+    return one ? reinterpret_cast<const void *>(&plan_one_kernel) : reinterpret_cast<const void *>(&plan_many_kernel);
+}
 const void *plan_tokens_kernel() { return reinterpret_cast<const void *>(&plan_slots_kernel); }
 
 }  // namespace isoq

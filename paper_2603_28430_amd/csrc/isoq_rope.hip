@@ -13,6 +13,8 @@
 namespace isoq {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // cos and sin of p 2^-32 turns: by the Taylor series on an eighth of a turn
 // either side of the nearest quarter (cut at x^11 / 11! and x^12 / 12!, 2e-9 and
 // 1e-10 at the ends).
@@ -40,7 +42,7 @@ __device__ __forceinline__ uint32_t turns_of(uint64_t per_position, int32_t posi
     return (uint32_t)((per_position * (uint64_t)(int64_t)position) >> 32);
 }
 
-// A row a wave: lane i has the coordinates i, 64 + i, ... and, for each, the other
+// Any other width: a row a wave; lane i has the coordinates i, 64 + i, ... and, for each, the other
 // of its pair.
 template <bool F16, bool HALVES, int N>
 __global__ __launch_bounds__(256) void rope_rows_kernel(const RopeArgs a)
@@ -95,6 +97,172 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(const RopeArgs a)
     }
 }
 
+// Rows whose width and rotated part are pairs of 16-byte chunks.  L lanes have a
+// row, a wave 64 / L rows of one token at a time; a lane has two chunks of CH
+// coordinates, half of the rotated part (or of the rest) apart, so that both layouts
+// have their pairs in one lane: coordinates i of both chunks, or 2 i and 2 i + 1 of
+// each.  cos and sin are a lane's own for all of its token's rows, with the weight
+// and the amplitude multiplied in: a pair is four products of its two coordinates.
+template <bool F16, bool HALVES, int L>
+__global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
+{
+    constexpr int CH = F16 ? 8 : 4, V = 64 / L;
+    using T = std::conditional_t<F16, _Float16, float>;
+    const int lane = threadIdx.x & 63, sub = lane & (L - 1), g = lane / L;
+    const uint32_t wid = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t t = wid / (uint32_t)a.parts, part = wid - t * a.parts;
+    if (t >= (uint32_t)a.n_tokens)
+        return;
+    const int nr = a.half / CH, nz = (a.d - 2 * a.half) / (2 * CH);   // lanes of a row that rotate, that pass on
+    const bool turned = sub < nr, there = sub < nr + nz;
+    const int oa = turned ? sub * CH : 2 * a.half + (sub - nr) * CH, ob = oa + (turned ? a.half : nz * CH);
+
+    float c[CH], s[CH];
+    if (turned) {
+        const int32_t pos = a.positions[t];
+#pragma unroll
+        for (int i = 0; i < CH; i++) {
+            const int p = HALVES ? oa + i : (i < CH / 2 ? oa : ob - CH) / 2 + i;
+            turn_cos_sin(turns_of(a.turns[p], pos), c[i], s[i]);
+        }
+    }
+    const int its[2] = {(a.heads[0] + V - 1) / V, (a.heads[1] + V - 1) / V}, all = its[0] + its[1];
+    const int from = (int)(part * (uint32_t)all / (uint32_t)a.parts), to = (int)((part + 1) * (uint32_t)all / (uint32_t)a.parts);
+#pragma unroll 1
+    for (int k = 0; k < 2; k++) {
+        const int lo = max(from - (k ? its[0] : 0), 0), hi = min(to - (k ? its[0] : 0), its[k]);
+        if (lo >= hi)
+            continue;
+        const float *weight = a.weight[k];
+        float wa[CH], wb[CH];
+#pragma unroll
+        for (int i = 0; i < CH; i++)
+            wa[i] = wb[i] = 1.f;
+        if (weight && there) {
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(weight + oa + i), y = *reinterpret_cast<const f32x4 *>(weight + ob + i);
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    wa[i + j] = x[j];
+                    wb[i + j] = y[j];
+                }
+            }
+        }
+        // pair i: (x, y) -> (x cx - y sy, x sx + y cy)
+        float cx[CH], sx[CH], cy[CH], sy[CH];
+#pragma unroll
+        for (int i = 0; i < CH; i++) {
+            const float wx = HALVES ? wa[i] : i < CH / 2 ? wa[2 * i % CH] : wb[2 * i % CH];
+            const float wy = HALVES ? wb[i] : i < CH / 2 ? wa[(2 * i + 1) % CH] : wb[(2 * i + 1) % CH];
+            const float ca = a.amplitude * c[i], sa = a.amplitude * s[i];
+            cx[i] = wx * ca;
+            sx[i] = wx * sa;
+            cy[i] = wy * ca;
+            sy[i] = wy * sa;
+        }
+        const int heads = a.heads[k];
+        const T *x = static_cast<const T *>(a.x[k]) + t * a.stride[k];
+        T *out = static_cast<T *>(a.out[k]) + (int64_t)t * heads * a.d;
+        u32x4 ra, rb, na{}, nb{};
+        auto load = [&](int it) {
+            const int h = it * V + g;
+            if (there && h < heads) {
+                na = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + (int64_t)h * a.d + oa));
+                nb = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + (int64_t)h * a.d + ob));
+            }
+        };
+        load(lo);
+        for (int it = lo; it < hi; it++) {
+            ra = na;
+            rb = nb;
+            if (it + 1 < hi)
+                load(it + 1);
+            float xa[CH], xb[CH];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t ea = ra[i], eb = rb[i];
+                if constexpr (F16) {
+                    const f16x2 p = __builtin_bit_cast(f16x2, ea), q = __builtin_bit_cast(f16x2, eb);
+                    xa[2 * i] = (float)p.x;
+                    xa[2 * i + 1] = (float)p.y;
+                    xb[2 * i] = (float)q.x;
+                    xb[2 * i + 1] = (float)q.y;
+                } else {
+                    xa[i] = __uint_as_float(ea);
+                    xb[i] = __uint_as_float(eb);
+                }
+            }
+            if (weight) {   // (uniform)
+                float sum = 0.f;
+                if (there) {
+#pragma unroll
+                    for (int i = 0; i < CH; i++)
+                        sum = fmaf(xb[i], xb[i], fmaf(xa[i], xa[i], sum));
+                }
+                const float scale = 1.f / sqrtf(row_sum<L>(sum) / (float)a.d + a.eps);
+#pragma unroll
+                for (int i = 0; i < CH; i++) {
+                    xa[i] *= scale;
+                    xb[i] *= scale;
+                }
+            }
+            float ya[CH], yb[CH];
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < CH; i++) {
+                    const float px = HALVES ? xa[i] : i < CH / 2 ? xa[2 * i % CH] : xb[2 * i % CH];
+                    const float py = HALVES ? xb[i] : i < CH / 2 ? xa[(2 * i + 1) % CH] : xb[(2 * i + 1) % CH];
+                    const float u = fmaf(px, cx[i], -(py * sy[i])), v = fmaf(px, sx[i], py * cy[i]);
+                    if constexpr (HALVES) {
+                        ya[i] = u;
+                        yb[i] = v;
+                    } else {
+                        (i < CH / 2 ? ya : yb)[2 * i % CH] = u;
+                        (i < CH / 2 ? ya : yb)[(2 * i + 1) % CH] = v;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < CH; i++) {
+                    ya[i] = xa[i] * wa[i];
+                    yb[i] = xb[i] * wb[i];
+                }
+            }
+            u32x4 oa4, ob4;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if constexpr (F16) {
+                    const f16x2 p{(_Float16)ya[2 * i], (_Float16)ya[2 * i + 1]}, q{(_Float16)yb[2 * i], (_Float16)yb[2 * i + 1]};
+                    oa4[i] = __builtin_bit_cast(uint32_t, p);
+                    ob4[i] = __builtin_bit_cast(uint32_t, q);
+                } else {
+                    oa4[i] = __float_as_uint(ya[i]);
+                    ob4[i] = __float_as_uint(yb[i]);
+                }
+            }
+            const int h = it * V + g;
+            if (there && h < heads) {
+                *reinterpret_cast<u32x4 *>(out + (int64_t)h * a.d + oa) = oa4;
+                *reinterpret_cast<u32x4 *>(out + (int64_t)h * a.d + ob) = ob4;
+            }
+        }
+    }
+}
+
+template <bool F16, bool HALVES>
+const void *rope_lanes(int lanes)
+{
+    switch (lanes) {
+    case 4: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 4>);
+    case 8: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 8>);
+    case 16: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 16>);
+    case 32: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 32>);
+    case 64: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 64>);
+    }
+    return nullptr;
+}
+
 template <bool F16, bool HALVES>
 const void *rope_steps(int log2_steps)
 {
@@ -109,6 +277,12 @@ const void *rope_steps(int log2_steps)
 }
 
 }  // namespace
+
+const void *rope_tile_kernel_for(bool f16, bool halves, int lanes)
+{
+    return f16 ? (halves ? rope_lanes<true, true>(lanes) : rope_lanes<true, false>(lanes))
+               : (halves ? rope_lanes<false, true>(lanes) : rope_lanes<false, false>(lanes));
+}
 
 const void *rope_kernel(bool f16, bool halves, int log2_steps)
 {

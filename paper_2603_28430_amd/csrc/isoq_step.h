@@ -27,7 +27,7 @@ struct PlanArgs {
 // One workgroup of kPlanThreads; then, where it does not do that itself, slots and
 // positions: 256 threads, a token each.
 constexpr int kPlanThreads = 1024;
-const void *plan_kernel();
+const void *plan_kernel(bool one);   // one: up to kPlanThreads sequences
 const void *plan_tokens_kernel();
 
 struct RopeArgs {
@@ -40,7 +40,11 @@ struct RopeArgs {
     const uint64_t *turns;         // [half] turns a position, in units of 2^-64
     int32_t n_tokens, d, half;     // half: pairs that are rotated
     float eps, amplitude;
+    int32_t parts;                 // waves that share a token's rows (rope_tile_kernel)
 };
+// Widths of 16-byte chunks in pairs (rope_tile_kernel): a lane has two chunks of a
+// row, lanes (4 .. 64, a power of two) a row.  Grid of four waves, `parts` a token.
+const void *rope_tile_kernel_for(bool f16, bool halves, int lanes);
 // A row a wave, rows token by token (queries, then keys), four waves a workgroup;
 // for widths up to 64 << log2_steps (log2_steps <= 4).
 const void *rope_kernel(bool f16, bool halves, int log2_steps);

@@ -18,6 +18,9 @@ using namespace isoq;
 // Tokens up to which the one workgroup of the plan writes slots and positions too.
 constexpr int64_t kPlanTokensHere = 4096;
 
+// Waves up to which a token's rows are shared out.
+constexpr int64_t kRopeWaves = 8192;
+
 constexpr double kTwoPi = 6.283185307179586476925;
 
 }  // namespace
@@ -71,7 +74,7 @@ isoq_status isoq_kv_plan(const int32_t *lens, const int32_t *new_lens, int n_seq
     a.tokens_too = n_tokens <= kPlanTokensHere;
     a.div_block = make_fastdiv((uint32_t)block_size);
     void *args[] = {&a};
-    const isoq_status st = launch_lds(plan_kernel(), dim3(1), kPlanThreads, args, 0, stream);
+    const isoq_status st = launch_lds(plan_kernel(n_seqs <= kPlanThreads), dim3(1), kPlanThreads, args, 0, stream);
     if (st != ISOQ_OK || a.tokens_too)
         return st;
     return launch_lds(plan_tokens_kernel(), dim3((unsigned)((n_tokens + 255) / 256)), 256, args, 0, stream);
@@ -212,12 +215,27 @@ isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int6
     a.half = r->rot_dim / 2;
     a.eps = eps;
     a.amplitude = r->amplitude;
+    const bool f16 = dtype == ISOQ_F16, halves = r->layout == ISOQ_ROPE_HALVES;
+    void *args[] = {&a};
+    // 16-byte chunks in pairs, where all rows have them
+    const int chunk = f16 ? 8 : 4, pairs = r->d / (2 * chunk);
+    auto placed = [&](const void *x, int64_t stride, int n) {
+        return n == 0 || (aligned(x, 16) && (n_tokens == 1 || stride % chunk == 0));
+    };
+    if (r->d % (2 * chunk) == 0 && a.half % chunk == 0 && pairs <= 64 && placed(q, q_stride, n_q_heads) &&
+        placed(k, k_stride, n_kv_heads) && aligned(q_weight, 16) && aligned(k_weight, 16)) {
+        int lanes = 4;
+        while (lanes < pairs)
+            lanes *= 2;
+        const int64_t rows = 64 / lanes, most = (n_q_heads + rows - 1) / rows + (n_kv_heads + rows - 1) / rows;
+        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, kRopeWaves / n_tokens));
+        return launch_lds(rope_tile_kernel_for(f16, halves, lanes), dim3((unsigned)((n_tokens * a.parts + 3) / 4)), 256,
+                          args, 0, stream);
+    }
     int steps = 0;
     while ((64 << steps) < r->d)
         steps++;
-    void *args[] = {&a};
-    return launch_lds(rope_kernel(dtype == ISOQ_F16, r->layout == ISOQ_ROPE_HALVES, steps),
-                      dim3((unsigned)((n_tokens * heads + 3) / 4)), 256, args, 0, stream);
+    return launch_lds(rope_kernel(f16, halves, steps), dim3((unsigned)((n_tokens * heads + 3) / 4)), 256, args, 0, stream);
 }
 
 }  // extern "C"
