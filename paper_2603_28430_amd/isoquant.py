@@ -834,40 +834,42 @@ def isoq_kv_plan(lens, new_lens, block_table, block_size: int, free_blocks, n_fr
     n_free.  See include/isoquant.h for sequences that are refused.  What is not
     passed is allocated from torch's pool for `stream`."""
     torch = _torch()
-    if block_table.dim() != 2:
-        raise ValueError("block_table must be int32 [n_seqs, max_blocks]")
-    n_seqs, max_blocks = block_table.shape
+    table = block_table.shape
+    if len(table) != 2 or free_blocks.dim() != 1:
+        raise ValueError("block_table [n_seqs, max_blocks], free_blocks [max_free]")
+    n_seqs, max_blocks = table
+    if lens.shape != (n_seqs,) or new_lens.shape != (n_seqs,) or n_free.shape != (1,):
+        raise ValueError("lens and new_lens need one entry per row of block_table, n_free one")
+    whole = torch.int32
+    if (lens.dtype != whole or new_lens.dtype != whole or block_table.dtype != whole or free_blocks.dtype != whole
+            or n_free.dtype != whole):
+        raise TypeError("lens, new_lens, block_table, free_blocks and n_free must be int32")
     if n_tokens is None:
         if slot_mapping is None:
             raise ValueError("n_tokens, or a slot_mapping of that length")
         n_tokens = slot_mapping.numel()
-    whole = torch.int32
-    given = [("lens", lens, whole, (n_seqs,)), ("new_lens", new_lens, whole, (n_seqs,)),
-             ("block_table", block_table, whole, (n_seqs, max_blocks)), ("n_free", n_free, whole, (1,)),
-             ("free_blocks", free_blocks, whole, (free_blocks.numel(),))]
-    for name, t, dtype, shape in (("seq_lens", seq_lens, whole, (n_seqs,)), ("q_start", q_start, whole, (n_seqs + 1,)),
-                                  ("slot_mapping", slot_mapping, torch.int64, (n_tokens,)),
-                                  ("positions", positions, whole, (n_tokens,)), ("n_free_out", n_free_out, whole, (1,))):
+    tensors = [lens, new_lens, block_table, free_blocks, n_free]
+    for t, n in ((seq_lens, n_seqs), (q_start, n_seqs + 1), (slot_mapping, n_tokens), (positions, n_tokens), (n_free_out, 1)):
         if t is not None:
-            given.append((name, t, dtype, shape))
-    for name, t, dtype, shape in given:
-        if t.dtype != dtype or t.shape != shape:
-            raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    _on_current(lens, [g[1] for g in given], stream)
+            if t.shape != (n,) or t.dtype != (torch.int64 if t is slot_mapping else whole):
+                raise ValueError("seq_lens [n_seqs], q_start [n_seqs + 1], positions [n_tokens] and n_free_out [1] must be "
+                                 "int32, slot_mapping [n_tokens] int64")
+            tensors.append(t)
+    _on_current(lens, tensors, stream)
+    outs = seq_lens, q_start, slot_mapping, positions, n_free_out
     if stream is None:
-        seq_lens, q_start, slot_mapping, positions, n_free_out = _plan_buffers(
-            lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out)
+        outs = _plan_buffers(lens, n_seqs, n_tokens, *outs)
     else:
         with torch.cuda.stream(stream):
-            seq_lens, q_start, slot_mapping, positions, n_free_out = _plan_buffers(
-                lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out)
+            outs = _plan_buffers(lens, n_seqs, n_tokens, *outs)
+    seq_lens, q_start, slot_mapping, positions, n_free_out = outs
     st = lib.isoq_kv_plan(lens.data_ptr(), new_lens.data_ptr(), n_seqs, block_table.data_ptr(), max_blocks, block_size,
                           free_blocks.data_ptr(), free_blocks.numel(), n_free.data_ptr(), seq_lens.data_ptr(),
                           q_start.data_ptr(), slot_mapping.data_ptr(), positions.data_ptr(), n_tokens,
                           n_free_out.data_ptr(), _stream_ptr(stream))
     if st:
         _check(st, "isoq_kv_plan")
-    return seq_lens, q_start, slot_mapping, positions, n_free_out
+    return outs
 
 
 def _plan_buffers(lens, n_seqs, n_tokens, seq_lens, q_start, slot_mapping, positions, n_free_out):
@@ -936,13 +938,11 @@ def isoq_rope_destroy(r: Rope) -> None:
     r.close()
 
 
-def _token_stride(name, x, d):
+def _token_stride(name, x):
     """Elements between the tokens of rows [n_tokens, heads, d], whose heads lie one after another."""
-    n, heads, width = x.shape
+    n, heads, d = x.shape
     token, head, one = x.stride()
-    if width != d:
-        raise ValueError(f"{name}: last dimension must be d={d}")
-    if (width > 1 and one != 1) or (heads > 1 and head != d) or (n > 1 and token < heads * d):
+    if (d > 1 and one != 1) or (heads > 1 and head != d) or (n > 1 and token < heads * d):
         raise ValueError(f"{name}: a token's heads must be contiguous, tokens at least as far apart")
     return token if n > 1 else heads * d
 
@@ -955,20 +955,29 @@ def isoq_qk_norm_rope(rope: Rope, q, k, positions, q_weight=None, k_weight=None,
     heads have to be contiguous.  positions int32 [n_tokens].  Returns (q_out,
     k_out), contiguous; they may be q and k themselves (see include/isoquant.h)."""
     torch = _torch()
-    if q.dim() != 3 or (k is not None and k.dim() != 3):
-        raise ValueError("q [n_tokens, n_q_heads, d], k [n_tokens, n_kv_heads, d]")
-    shape, d = q.shape, rope.d
-    q_stride, k_stride, kv_heads = _token_stride("q", q, d), 0, 0
-    if k is not None:
-        if k.shape[0] != shape[0] or k.dtype != q.dtype:
-            raise ValueError("q and k must have the same tokens and dtype")
-        k_stride, kv_heads = _token_stride("k", k, d), k.shape[1]
-    elif k_out is not None or k_weight is not None:
-        raise ValueError("k_out and k_weight need k")
-    code = _dtype_code(q.dtype)
-    if positions.shape != (shape[0],) or positions.dtype != torch.int32:
+    shape, d, dtype = q.shape, rope.d, q.dtype
+    if len(shape) != 3 or shape[2] != d:
+        raise ValueError(f"q must be [n_tokens, n_q_heads, {d}]")
+    n_tokens, n_q_heads, _ = shape
+    q_stride = n_q_heads * d if q.is_contiguous() else _token_stride("q", q)
+    code = _dtype_code(dtype)
+    if positions.shape != (n_tokens,) or positions.dtype != torch.int32:
         raise ValueError("positions must be int32 [n_tokens]")
     tensors = [positions]
+    device = positions.get_device()
+    if not _is_gpu(q) or q.get_device() != device:
+        raise ValueError(f"q must be on {positions.device}, got {q.device}")
+    k_stride = n_kv_heads = 0
+    if k is not None:
+        rows = k.shape
+        if len(rows) != 3 or rows[0] != n_tokens or rows[2] != d or k.dtype != dtype:
+            raise ValueError(f"k must be {dtype} [n_tokens, n_kv_heads, {d}]")
+        n_kv_heads = rows[1]
+        k_stride = n_kv_heads * d if k.is_contiguous() else _token_stride("k", k)
+        if not _is_gpu(k) or k.get_device() != device:
+            raise ValueError(f"k must be on {positions.device}, got {k.device}")
+    elif k_out is not None or k_weight is not None:
+        raise ValueError("k_out and k_weight need k")
     for w in (q_weight, k_weight):
         if w is not None:
             if w.shape != (d,) or w.dtype != torch.float32:
@@ -976,21 +985,17 @@ def isoq_qk_norm_rope(rope: Rope, q, k, positions, q_weight=None, k_weight=None,
             tensors.append(w)
     for x, out in ((q, q_out), (k, k_out)):
         if out is not None:
-            if out.shape != x.shape or out.dtype != x.dtype:
+            if out.shape != x.shape or out.dtype != dtype:
                 raise ValueError("q_out and k_out must have the shapes and dtype of q and k")
             tensors.append(out)
-    for x in (q,) if k is None else (q, k):
-        if not _is_gpu(x) or x.get_device() != positions.get_device():
-            _device_tensors(positions, positions=positions)
-            raise ValueError(f"q and k must be on {positions.device}")
     _on_current(positions, tensors, stream)
     if stream is None:
         q_out, k_out = _rope_buffers(q, k, q_out, k_out)
     else:
         with torch.cuda.stream(stream):
             q_out, k_out = _rope_buffers(q, k, q_out, k_out)
-    st = lib.isoq_qk_norm_rope(rope.handle, code, q.data_ptr(), q_stride, shape[1], _ptr(k), k_stride, kv_heads,
-                               positions.data_ptr(), shape[0], _ptr(q_weight), _ptr(k_weight), eps, q_out.data_ptr(),
+    st = lib.isoq_qk_norm_rope(rope.handle, code, q.data_ptr(), q_stride, n_q_heads, _ptr(k), k_stride, n_kv_heads,
+                               positions.data_ptr(), n_tokens, _ptr(q_weight), _ptr(k_weight), eps, q_out.data_ptr(),
                                _ptr(k_out), _stream_ptr(stream))
     if st:
         _check(st, "isoq_qk_norm_rope")
