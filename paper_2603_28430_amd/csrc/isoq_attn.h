@@ -68,13 +68,14 @@ struct AttnKernel {
     size_t lds;
     int rows;
     bool parts;   // the kernel of many rows
+    int threads;
 };
 AttnKernel attn_m_kernel_b2(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b3(int d, int rows, bool f16);
 AttnKernel attn_m_kernel_b4(int d, int rows, bool f16);
 // Kernel of many rows (isoq_attn_c.h; fp16 queries, widths up to 128), with what
 // fp16 leaves of the keys' levels in the form `rest` (kRestNone ..); or {}.
-AttnKernel attn_c_kernel_for(int d, int bits, int rest);
+AttnKernel attn_c_kernel_for(int d, int bits, int rest, int rows);
 // Join of the splits, 256 threads: up to kAttnJoinFew splits (few) grid (rows of
 // a sequence / (256 / slots), sequence), more (row, sequence); a row being query
 // head + n_q_heads token.

@@ -84,7 +84,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         // 256 / 103.  2 x 8 heads, 8,192: 24 28 / 33, 32 30 / 33, 48 39 / 38, 128 70
         // / 55.  4 x 4 heads, 8,192, d = 64, 4 bits: 32 25 / 24, 64 40 / 28.)
         if (f16 && rows >= 32) {
-            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, p.kt->key_rest);
+            const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, p.kt->key_rest, r);
             if (many.fn)
                 p.kern = many;
         }
@@ -111,7 +111,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // 22; 16 ragged x 8 x 4 of 5 tokens, mean of three 47 / 38 / 38; 4 ragged x 2 x 16, up
     // to 20,000 20 / 23 / 23; 8 ragged x 4 x 4 of 5 tokens, fp32 23 / 23 / 27.  Of 12: 8 x
     // 8 heads, 4,096 23 / 28 / 28, 8 ragged x 8, up to 8,000 34 / 35 / 35.)
-    const int64_t want = p.kern.parts                                          ? (pk->d <= 64 ? 768 : 512)
+    const int64_t want = p.kern.parts                                          ? (p.kern.rows > 128 ? 256 : pk->d <= 64 ? 768 : 512)
                          : n_seqs == 1 || pk->d > 128 || p.kern.rows == 12     ? 768
                          : p.kern.rows == 8                                    ? 1280
                                                                                : 1536;
@@ -303,7 +303,8 @@ isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, in
             return hip_fail(e, "hipFuncSetAttribute");
     }
     // (splits last: those that some sequences do not reach come after those that all do)
-    return launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)n_seqs, (unsigned)plan.n_splits), 256, args, lds, c.stream);
+    return launch_lds(fn, dim3((unsigned)plan.groups, (unsigned)n_seqs, (unsigned)plan.n_splits),
+                      plan.kern.fn ? plan.kern.threads : 256, args, lds, c.stream);
 }
 
 // The plans of a call: of the sequences' own positions, and of the prefixes'.

@@ -56,11 +56,12 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-template <int D, int BITS, int REST>
+template <int D, int BITS, int REST, int W>
 struct AttnCShape {
     using S = ScoreMShape<D, BITS, 0>;
     using H = AttnMShape<D, BITS, 1>;
-    static constexpr int ROWS = 128;
+    static constexpr int ROWS = 32 * W;              // a wave has 32
+    static constexpr bool AHEAD = W > 4;             // tiles are decoded one ahead, into the other of two buffers
     static constexpr int KS = S::NQ;                 // 16-coordinate steps of the logits' product (4 chunks of 4 NQ)
     static constexpr int KROW = 32 * KS + 16;        // bytes of a decoded key part
     static constexpr int K8 = (KS + 3) / 4;          // 64-coordinate steps of its correction
@@ -70,20 +71,91 @@ struct AttnCShape {
     static constexpr int VROW8 = 64 + 16;            // and in e4m3
     static constexpr int RK = 4 * S::WC + 1;         // words of a key's raw record (odd: lanes are keys)
     static constexpr int RV = H::SW + 1;             // words of a value's raw record
-    // LDS bytes: keys, and what fp16 left of them; values in fp16, e4m3; raw
-    // records; per tile parity the norms (K, V), the valid positions, the values'
-    // unit and half of their least norm in it, and the first key and value whose
-    // norm is an infinity or NaN
+    // LDS bytes: keys, and what fp16 left of them; values in fp16, e4m3 (two
+    // buffers of these with AHEAD); raw records (two); of 2 or 4 tiles the norms (K,
+    // V), the valid positions, the values' unit and half of their least norm in it,
+    // and the first key and value whose norm is an infinity or NaN
+    static constexpr int NB = AHEAD ? 2 : 1, NT = AHEAD ? 4 : 2;
     static constexpr int kHalf = 0, kRest = 64 * KROW, kV = kRest + 64 * KROWR, kV8 = kV + 32 * CT * VROW,
-                         kRawK = kV8 + 32 * CT * VROW8, kRawV = kRawK + 4 * 64 * RK, kNorm = kRawV + 4 * 64 * RV,
-                         kTile = kNorm + 2 * 512;
-    static constexpr int loop_bytes() { return kTile + 2 * 32; }
-    // before the loop the rotated queries and their largest magnitudes
-    static constexpr int QS = D + 1;
-    static constexpr int query_bytes() { return 4 * ROWS * (QS + 8); }
+                         kBuffer = kV8 + 32 * CT * VROW8;
+    static constexpr int kRawK = NB * kBuffer, kRawV = kRawK + 4 * 64 * RK, kRaw = 4 * 64 * (RK + RV),
+                         kNorm = kRawK + NB * kRaw, kTile = kNorm + NT * 512;
+    static constexpr int loop_bytes() { return kTile + NT * 32; }
+    // before the loop the rotated queries, in the keys' order of coordinates (reads of
+    // 16 bytes by consecutive rows touch every bank once)
+    static constexpr int QS = 16 * KS + 4;
+    static constexpr int query_bytes() { return 4 * ROWS * QS; }
     static constexpr int lds_bytes() { return loop_bytes() > query_bytes() ? loop_bytes() : query_bytes(); }
-    static_assert(kRest % 16 == 0 && kV % 16 == 0 && kV8 % 16 == 0 && kRawK % 16 == 0 && kNorm % 16 == 0, "aligned parts");
+    static_assert(kRest % 16 == 0 && kV % 16 == 0 && kV8 % 16 == 0 && kBuffer % 16 == 0 && kRaw % 16 == 0, "aligned parts");
+    static_assert(lds_bytes() <= 160 * 1024, "a compute unit's LDS");
+
+    // place of coordinate e of a row in that order: quad q of chunk c and byte b of it (attn_coord)
+    static __device__ __forceinline__ int place(int e)
+    {
+        const int c = e / S::CC, ci = e - c * S::CC;
+        int q, b;
+        if (BITS == 3 && 32 * (ci / 32 + 1) <= S::CC) {
+            q = ci / 32 * 8 + ci % 8;
+            b = ci % 32 / 8;
+        } else if (BITS == 2 && 16 * (ci / 16 + 1) <= S::CC) {
+            q = ci / 16 * 4 + ci % 4;
+            b = ci % 16 / 4;
+        } else {
+            q = ci / 8 * 2 + ci % 2;
+            b = ci % 8 / 2;
+        }
+        return 4 * (c * S::NQ + q) + b;
+    }
 };
+
+// The workgroup's n query rows from r0 on, rotated (scale folded in), into qt.  A
+// thread keeps its chunk of 8 coordinates, whose parameters and places it has once,
+// and asks for four rows at a time.
+template <int VAR, class C, int D, int THREADS>
+__device__ __forceinline__ void attn_c_queries(const AttnArgs &a, const AttnSeq &sq, int h, int r0, int n, float *qt)
+{
+    constexpr int NCH = D / 8, PER = THREADS / NCH, PL = kLanePL<VAR>, U = 4;
+    const int c = threadIdx.x % NCH, first = threadIdx.x / NCH;
+    if (first >= PER)
+        return;
+    float P[PL];
+    load_params<PL>(a.k_params + ((int64_t)(a.k_sets == 1 ? 0 : h) * NCH + c) * PL, P);
+    int at[8];
+#pragma unroll
+    for (int k = 0; k < 8; k++)
+        at[k] = C::place(8 * c + k);
+    for (int q = first; q < n; q += U * PER) {
+        Raw<true> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int r = r0 + min(q + u * PER, n - 1), i = r / a.group;
+            const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + h * a.group + (r - i * a.group);
+            load_row_chunk<true>(static_cast<const char *>(a.q) + row * D * 2 + c * 16, raw[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            float x[8], y[8];
+            unpack<true>(raw[u], x);
+            if constexpr (VAR == VAR_BLOCK8) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    y[e] = P[8 * e] * x[0];
+#pragma unroll
+                    for (int k = 1; k < 8; k++)
+                        y[e] = fmaf(P[8 * e + k], x[k], y[e]);
+                }
+            } else {
+                rotate_forward<VAR>(P, x, y);
+            }
+            if (q + u * PER < n) {
+                float *dst = qt + (q + u * PER) * C::QS;
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    dst[at[k]] = y[k] * a.scale;
+            }
+        }
+    }
+}
 
 // Four levels' fp16 values for four selector bytes: tables of the values' low
 // and high bytes (4 bits: of the positive levels', whose sign bit is set where
@@ -125,10 +197,10 @@ __device__ __forceinline__ f16x8 as_halves(u32x4 v) { return __builtin_bit_cast(
 // (Up to d = 64 the registers allow three workgroups a compute unit, at 4 bits with
 // three of them spilled: 61 us instead of 71 for three ragged chunks of up to 300
 // tokens and 6,000 positions, 8 x 2 heads.)
-template <int D, int BITS, int REST>
-__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const AttnArgs a)
+template <int D, int BITS, int REST, int W>
+__global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : D <= 64 ? 3 : 2) void attn_c_kernel(const AttnArgs a)
 {
-    using C = AttnCShape<D, BITS, REST>;
+    using C = AttnCShape<D, BITS, REST, W>;
     using S = typename C::S;
     using H = typename C::H;
     constexpr int64_t RB = (int64_t)D * BITS / 8;
@@ -163,12 +235,14 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
     const int lim_min = 32 * w + 32 <= n ? sq.limit((r0 + 32 * w) / a.group, a.cap) : 0;
     const int lim_max = 32 * w < n ? sq.limit((r0 + min(32 * w + 31, n - 1)) / a.group, a.cap) : 0;
 
-    // 0. records of the next tile: waves 0 (K) and 1 (V), a position per lane
+    // 0. records of the next tile: waves WK (K) and WV (V), a position per lane
+    constexpr int WK = W > 4 ? 1 : 0, WV = W > 4 ? 2 : 1;
+    const bool fetches = w == WK || w == WV;
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
     const uint64_t rstride = (uint64_t)a.n_kv_heads * a.block_size, row0 = (uint64_t)h * a.block_size;
     const uint64_t bstride = rstride * RB;
-    const uint8_t *const idx = (w == 0 ? a.k_idx : a.v_idx) + row0 * RB;
-    const float *const rhos = (w == 0 ? a.k_rho : a.v_rho) + row0;
+    const uint8_t *const idx = (w == WK ? a.k_idx : a.v_idx) + row0 * RB;
+    const float *const rhos = (w == WK ? a.k_rho : a.v_rho) + row0;
     const int64_t pstep = (int64_t)a.block_size * S::CP;
     struct Batch {
         uint32_t w[S::RW];
@@ -188,6 +262,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         const uint32_t pos = rec.ok ? tt - fast_div(tt, a.div_block) * a.block_size : 0u;
         const uint8_t *src = idx + b * bstride + (uint64_t)pos * S::CP;
         const uint64_t crow = b * rstride + pos;
+        rec.rho = rhos[crow];
         if constexpr (S::LW == 4) {
 #pragma unroll
             for (int v = 0; v < S::RW / 4; v++) {
@@ -225,16 +300,16 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 rec.w[v] = odd ? __builtin_amdgcn_alignbit(x[v], x[v - 1], 16) : x[v];
             rec.w[S::RW - 1] = odd ? x[S::RW - 2] >> 16 : hw;
         }
-        rec.rho = rhos[crow];
     };
     // the tiles' unit of values: norms below 2^tile_unit; kept while the tile's
     // largest norm is above 2^(tile_unit - 4)
     int tile_unit = 0;
-    auto store_raw = [&](int t) {   // (waves 0 and 1) into tile t's places
-        float *norm = reinterpret_cast<float *>(lds + C::kNorm + 512 * (t & 1));
-        uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 32 * (t & 1));
-        if (w == 0) {
-            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawK) + lane * C::RK;
+    auto store_raw = [&](int t) {   // (waves WK and WV) into tile t's places
+        float *norm = reinterpret_cast<float *>(lds + C::kNorm + 512 * (t & (C::NT - 1)));
+        uint32_t *tile = reinterpret_cast<uint32_t *>(lds + C::kTile + 32 * (t & (C::NT - 1)));
+        const int raw = C::kRaw * (t & (C::NB - 1));
+        if (w == WK) {
+            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawK + raw) + lane * C::RK;
 #pragma unroll
             for (int c = 0; c < 4; c++)
 #pragma unroll
@@ -253,7 +328,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 tile[4] = odds ? __builtin_ctzll(odds) : 0x7FFFFFFF;
             }
         } else {
-            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawV) + lane * C::RV;
+            uint32_t *dst = reinterpret_cast<uint32_t *>(lds + C::kRawV + raw) + lane * C::RV;
 #pragma unroll
             for (int i = 0; i < H::SW; i++)
                 dst[i] = H::staged(rec.w, i);
@@ -285,33 +360,49 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         }
     };
     int32_t next = 0;
-    if (nt > 0 && w < 2) {
+    if (nt > 0 && fetches) {
         fetch(0, block_of(0));
         next = block_of(1);
     }
 
     // 1. rotated queries, and the wave's rows of them as fp16 pairs in registers
     float *qt = reinterpret_cast<float *>(smem);
-    uint32_t *mx = smem + C::ROWS * C::QS;   // [ROWS][8], as attn_rotate has them
-    for (int i = threadIdx.x; i < 8 * C::ROWS; i += 256)
-        mx[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n * (D / 8); i += 256) {
-        const int q = i / (D / 8), c = i - q * (D / 8);
-        QueryChunk query;
-        attn_load_query<D>(a, sq, h, r0 + q, c, query);
-        attn_rotate_any<D>(a, h, c, query, qt + q * C::QS + 8 * c, mx + 8 * q);
+    if (4 * S::NQ > S::CC) {   // places past a chunk's coordinates
+        constexpr int pad = 4 * S::NQ - S::CC;
+        // (the rows' zeros first: a chunk's last places are not the last of its quads)
+        for (int i = threadIdx.x; i < C::ROWS * C::QS; i += 64 * W)
+            qt[i] = 0.f;
+        static_assert(pad >= 0, "");
+        __syncthreads();
+    }
+    switch (a.variant) {   // (uniform)
+    case VAR_FULL: attn_c_queries<VAR_FULL, C, D, 64 * W>(a, sq, h, r0, n, qt); break;
+    case VAR_FAST: attn_c_queries<VAR_FAST, C, D, 64 * W>(a, sq, h, r0, n, qt); break;
+    case VAR_PLANAR2D: attn_c_queries<VAR_PLANAR2D, C, D, 64 * W>(a, sq, h, r0, n, qt); break;
+    default: attn_c_queries<VAR_BLOCK8, C, D, 64 * W>(a, sq, h, r0, n, qt); break;
     }
     __syncthreads();
-    const uint32_t qmax = on ? mx[8 * r] : 0u;
+    // the lane's places, 16 st + 8 half + 0 .. 7, and the row's largest magnitude (an
+    // infinity or NaN among them) of both lanes'
+    const float *mine = qt + r * C::QS;
+    f32x4 qv[C::KS][2];
+    uint32_t qmax = 0;
+#pragma unroll
+    for (int st = 0; st < C::KS; st++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            qv[st][e] = *reinterpret_cast<const f32x4 *>(mine + 16 * st + 8 * half + 4 * e);
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                qmax = max(qmax, __float_as_uint(fabsf(qv[st][e][k])));
+        }
+    {
+        const auto x = __builtin_amdgcn_permlane32_swap(qmax, qmax, false, false);
+        qmax = on ? max(x[0], x[1]) : 0u;
+    }
     const int qe = head_exponent(__uint_as_float(qmax), 4);
-    // coordinate j of a quad of the keys' order (places 4 quad .. + 3: quad NQ c + q
-    // is quad q of chunk c), in the row's units
-    auto query = [&](int quad, int j) {
-        const int c = quad / S::NQ, ci = attn_coord<S, BITS>(quad - c * S::NQ, j);
-        const float x = on && ci < S::CC ? __builtin_amdgcn_ldexpf(qt[r * C::QS + c * S::CC + ci], qe) : 0.f;
-        return nonfinite(qmax) ? 0.f : x;
-    };
+    const bool counts = on && !nonfinite(qmax);
+    auto scaled = [&](float x) { return counts ? __builtin_amdgcn_ldexpf(x, qe) : 0.f; };   // in the row's units
     u32x4 qh[C::KS], ql[C::KS];   // B of 16 places: 8 half + 0 .. 7
     [[maybe_unused]] i32x8 q8[C::K8];   // in e4m3, of 64 places: 32 half + 0 .. 31
 #pragma unroll
@@ -319,7 +410,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         f16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float v = query(4 * st + 2 * half + e / 4, e % 4);
+            const float v = scaled(qv[st][e / 4][e % 4]);
             hi[e] = (_Float16)v;
             lo[e] = (_Float16)(v - (float)hi[e]);
         }
@@ -331,12 +422,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
         for (int st = 0; st < C::K8; st++)
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const int quad = 16 * st + 8 * half + e;
-                float x[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    x[j] = 16 * st + 16 <= 4 * C::KS || quad < 4 * C::KS ? query(quad, j) : 0.f;
-                q8[st][e] = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+                f32x4 x{0.f, 0.f, 0.f, 0.f};
+                if (16 * st + 8 * half < 4 * C::KS)   // (whole groups of 8 quads)
+                    x = *reinterpret_cast<const f32x4 *>(mine + 64 * st + 32 * half + 4 * e);
+                q8[st][e] = __builtin_amdgcn_cvt_pk_fp8_f32(
+                    scaled(x[2]), scaled(x[3]), __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[0]), scaled(x[1]), 0, false), true);
             }
     }
     // a logit (in units of ln 2) is f1 times sum and norm
@@ -354,109 +444,108 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
     // `most` or up to 2^11 more
     float ref = -INFINITY, l = 0.f, most = 0.f;
     int unit = 0;
-    if (D % 32 != 0) {   // coordinates past D: rows of zeros
-        for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW / 4; i += 256)
-            reinterpret_cast<uint32_t *>(lds + C::kV + D * C::VROW)[i] = 0u;
-        for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW8 / 4; i += 256)
-            reinterpret_cast<uint32_t *>(lds + C::kV8 + D * C::VROW8)[i] = 0u;
+    for (int b = 0; b < C::NB; b++) {
+        uint8_t *buf = lds + b * C::kBuffer;
+        if (D % 32 != 0) {   // coordinates past D: rows of zeros
+            for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW / 4; i += 64 * W)
+                reinterpret_cast<uint32_t *>(buf + C::kV + D * C::VROW)[i] = 0u;
+            for (int i = threadIdx.x; i < (32 * C::CT - D) * C::VROW8 / 4; i += 64 * W)
+                reinterpret_cast<uint32_t *>(buf + C::kV8 + D * C::VROW8)[i] = 0u;
+        }
+        if (REST == kRestBytes && C::KS % 4 != 0) {   // places past the keys'
+            constexpr int words = (64 * C::K8 - 16 * C::KS) / 4;
+            for (int i = threadIdx.x; i < 64 * words; i += 64 * W)
+                reinterpret_cast<uint32_t *>(buf + C::kRest + (i / words) * C::KROWR + 16 * C::KS)[i % words] = 0u;
+        }
     }
-    if (REST == kRestBytes && C::KS % 4 != 0) {   // places past the keys'
-        constexpr int words = (64 * C::K8 - 16 * C::KS) / 4;
-        for (int i = threadIdx.x; i < 64 * words; i += 256)
-            reinterpret_cast<uint32_t *>(lds + C::kRest + (i / words) * C::KROWR + 16 * C::KS)[i % words] = 0u;
-    }
-    if (nt > 0 && w < 2)
-        store_raw(0);
-    __syncthreads();
 
-    for (int t = 0; t < nt; t++) {
-        // 2. decode the tile; the next one's records are asked for
-        {
-            const uint32_t *src = reinterpret_cast<const uint32_t *>(lds + C::kRawK) + lane * C::RK + w * S::WC;
-            uint32_t y[S::WC];
+    // 2. decode tile t into its buffer: four waves its keys, a chunk of the
+    //    coordinates each, four waves (the same ones, or the next) its values
+    const int part4 = w & 3;
+    auto decode_keys = [&](int t) {
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(lds + C::kRawK + C::kRaw * (t & (C::NB - 1))) + lane * C::RK + part4 * S::WC;
+        uint32_t y[S::WC];
 #pragma unroll
-            for (int i = 0; i < S::WC; i++)
-                y[i] = src[i];
-            uint8_t *dst = lds + C::kHalf + lane * C::KROW + w * 8 * S::NQ;
-            uint8_t *rest = lds + C::kRest + lane * C::KROWR + w * (REST == kRestHalves ? 8 : 4) * S::NQ;
-            auto part = [&](auto nsc, int q0) {
-                constexpr int NS = decltype(nsc)::value;
-                uint32_t sel[NS];
-                [[maybe_unused]] uint32_t lo[NS];
-                attn_selectors<S, BITS, NS>(y, q0, sel);
+        for (int i = 0; i < S::WC; i++)
+            y[i] = src[i];
+        uint8_t *buf = lds + C::kBuffer * (t & (C::NB - 1));
+        uint8_t *dst = buf + C::kHalf + lane * C::KROW + part4 * 8 * S::NQ;
+        uint8_t *rest = buf + C::kRest + lane * C::KROWR + part4 * (REST == kRestHalves ? 8 : 4) * S::NQ;
+        auto part = [&](auto nsc, int q0) {
+            constexpr int NS = decltype(nsc)::value;
+            uint32_t sel[NS];
+            [[maybe_unused]] uint32_t lo[NS];
+            attn_selectors<S, BITS, NS>(y, q0, sel);
 #pragma unroll
-                for (int j = 0; j < NS; j += 2) {
-                    uint32_t x[4];
-                    [[maybe_unused]] uint32_t y[4];
+            for (int j = 0; j < NS; j += 2) {
+                uint32_t x[4];
+                [[maybe_unused]] uint32_t y[4];
 #pragma unroll
-                    for (int k = 0; k < 2; k++) {
-                        const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
-                        level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, x + 2 * k);
-                        if constexpr (REST == kRestHalves)
-                            level_halves<BITS>(a.k_half.tab[4], a.k_half.tab[5], sel[j + k], inv, y + 2 * k);
-                        if constexpr (REST == kRestBytes)
-                            lo[j + k] = level_bytes<BITS>(a.k_half.tab[3], sel[j + k], inv);
-                    }
-                    *reinterpret_cast<u32x4 *>(dst + 8 * (q0 + j)) = u32x4{x[0], x[1], x[2], x[3]};
+                for (int k = 0; k < 2; k++) {
+                    const uint32_t inv = BITS == 4 ? magnitude(sel[j + k]) : 0u;
+                    level_halves<BITS>(a.k_half.tab[0], a.k_half.tab[1], sel[j + k], inv, x + 2 * k);
                     if constexpr (REST == kRestHalves)
-                        *reinterpret_cast<u32x4 *>(rest + 8 * (q0 + j)) = u32x4{y[0], y[1], y[2], y[3]};
+                        level_halves<BITS>(a.k_half.tab[4], a.k_half.tab[5], sel[j + k], inv, y + 2 * k);
+                    if constexpr (REST == kRestBytes)
+                        lo[j + k] = level_bytes<BITS>(a.k_half.tab[3], sel[j + k], inv);
                 }
-                if constexpr (REST == kRestBytes && S::NQ % 4 == 0) {
-                    *reinterpret_cast<u32x4 *>(rest + 4 * q0) = u32x4{lo[0], lo[1], lo[2], lo[3]};
-                } else if constexpr (REST == kRestBytes) {
+                *reinterpret_cast<u32x4 *>(dst + 8 * (q0 + j)) = u32x4{x[0], x[1], x[2], x[3]};
+                if constexpr (REST == kRestHalves)
+                    *reinterpret_cast<u32x4 *>(rest + 8 * (q0 + j)) = u32x4{y[0], y[1], y[2], y[3]};
+            }
+            if constexpr (REST == kRestBytes && S::NQ % 4 == 0) {
+                *reinterpret_cast<u32x4 *>(rest + 4 * q0) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+            } else if constexpr (REST == kRestBytes) {
 #pragma unroll
-                    for (int j = 0; j < NS; j += 2)
-                        *reinterpret_cast<u32x2 *>(rest + 4 * (q0 + j)) = u32x2{lo[j], lo[j + 1]};
-                }
-            };
+                for (int j = 0; j < NS; j += 2)
+                    *reinterpret_cast<u32x2 *>(rest + 4 * (q0 + j)) = u32x2{lo[j], lo[j + 1]};
+            }
+        };
 #pragma unroll
-            for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
-                part(std::integral_constant<int, 4>{}, q0);
-            if constexpr (S::NQ % 4 != 0)
-                part(std::integral_constant<int, 2>{}, S::NQ - 2);
-        }
-        {
-            // lane word 4 w + lane / 16 of the positions 4 p .. 4 p + 3, p = lane mod 16
-            const int p = lane & 15, v = 4 * w + (lane >> 4);
-            const uint32_t *raw = reinterpret_cast<const uint32_t *>(lds + C::kRawV) + 4 * p * C::RV;
-            // place of the positions 16 s + 8 b + 4 h in a row: [16 s][h][b]
-            uint8_t *dst = lds + C::kV + v * H::CL * C::VROW + 2 * (16 * (p >> 2) + 8 * (p & 1) + 4 * ((p >> 1) & 1));
-            // in e4m3, of the positions 32 k + 8 b + 4 h: [h][k][b]
-            uint8_t *dst8 = lds + C::kV8 + v * H::CL * C::VROW8 + 32 * (p & 1) + 16 * (p >> 3) + 4 * ((p >> 1) & 3);
-            auto part = [&](auto nc, int c0) {
-                constexpr int N = decltype(nc)::value;
-                uint32_t x[4], sel[N];
+        for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
+            part(std::integral_constant<int, 4>{}, q0);
+        if constexpr (S::NQ % 4 != 0)
+            part(std::integral_constant<int, 2>{}, S::NQ - 2);
+    };
+    auto decode_values = [&](int t) {
+        // lane word 4 part4 + lane / 16 of the positions 4 p .. 4 p + 3, p = lane mod 16
+        const int p = lane & 15, v = 4 * part4 + (lane >> 4);
+        const uint32_t *raw = reinterpret_cast<const uint32_t *>(lds + C::kRawV + C::kRaw * (t & (C::NB - 1))) + 4 * p * C::RV;
+        uint8_t *buf = lds + C::kBuffer * (t & (C::NB - 1));
+        // place of the positions 16 s + 8 b + 4 h in a row: [16 s][h][b]
+        uint8_t *dst = buf + C::kV + v * H::CL * C::VROW + 2 * (16 * (p >> 2) + 8 * (p & 1) + 4 * ((p >> 1) & 1));
+        // in e4m3, of the positions 32 k + 8 b + 4 h: [h][k][b]
+        uint8_t *dst8 = buf + C::kV8 + v * H::CL * C::VROW8 + 32 * (p & 1) + 16 * (p >> 3) + 4 * ((p >> 1) & 3);
+        auto part = [&](auto nc, int c0) {
+            constexpr int N = decltype(nc)::value;
+            uint32_t x[4], sel[N];
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    if constexpr (H::HALF)
-                        x[i] = reinterpret_cast<const uint16_t *>(raw + i * C::RV)[2 * c0 + v];
-                    else
-                        x[i] = raw[i * C::RV + 2 * c0 + v];
-                }
-                position_selectors<BITS, N>(x, sel);
+            for (int i = 0; i < 4; i++) {
+                if constexpr (H::HALF)
+                    x[i] = reinterpret_cast<const uint16_t *>(raw + i * C::RV)[2 * c0 + v];
+                else
+                    x[i] = raw[i * C::RV + 2 * c0 + v];
+            }
+            position_selectors<BITS, N>(x, sel);
 #pragma unroll
-                for (int c = 0; c < N; c++) {
-                    const uint32_t inv = BITS == 4 ? magnitude(sel[c]) : 0u;
-                    uint32_t o[2];
-                    level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], inv, o);
-                    *reinterpret_cast<u32x2 *>(dst + (c0 + c) * C::VROW) = u32x2{o[0], o[1]};
-                    *reinterpret_cast<uint32_t *>(dst8 + (c0 + c) * C::VROW8) = level_bytes<BITS>(a.v_half.tab[2], sel[c], inv);
-                }
-            };
+            for (int c = 0; c < N; c++) {
+                const uint32_t inv = BITS == 4 ? magnitude(sel[c]) : 0u;
+                uint32_t o[2];
+                level_halves<BITS>(a.v_half.tab[0], a.v_half.tab[1], sel[c], inv, o);
+                *reinterpret_cast<u32x2 *>(dst + (c0 + c) * C::VROW) = u32x2{o[0], o[1]};
+                *reinterpret_cast<uint32_t *>(dst8 + (c0 + c) * C::VROW8) = level_bytes<BITS>(a.v_half.tab[2], sel[c], inv);
+            }
+        };
 #pragma unroll
-            for (int c0 = 0; c0 + 8 <= H::CL; c0 += 8)
-                part(std::integral_constant<int, 8>{}, c0);
-            if constexpr (H::CL % 8 != 0)
-                part(std::integral_constant<int, H::CL % 8>{}, H::CL / 8 * 8);
-        }
-        if (t + 1 < nt && w < 2) {
-            fetch(t + 1, next);
-            next = block_of(t + 2);
-        }
-        __syncthreads();
-
+        for (int c0 = 0; c0 + 8 <= H::CL; c0 += 8)
+            part(std::integral_constant<int, 8>{}, c0);
+        if constexpr (H::CL % 8 != 0)
+            part(std::integral_constant<int, H::CL % 8>{}, H::CL / 8 * 8);
+    };
+    auto attend = [&](int t) {
         const int tb = t0 + 64 * t;
-        const uint32_t *tile = reinterpret_cast<const uint32_t *>(lds + C::kTile + 32 * (t & 1));
+        const uint8_t *buf = lds + C::kBuffer * (t & (C::NB - 1));
+        const uint32_t *tile = reinterpret_cast<const uint32_t *>(lds + C::kTile + 32 * (t & (C::NT - 1)));
         if (tb < lim_max) {   // (wave-uniform)
             // 3. S^T of the wave's rows and the tile's positions; a step's keys
             //    are read while the one before multiplies
@@ -466,8 +555,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
 #pragma unroll
                 for (int e = 0; e < 16; e++)
                     st[k][e] = 0.f;
-            const uint8_t *key = lds + C::kHalf + n32 * C::KROW + 16 * half;
-            const uint8_t *rest = lds + C::kRest + n32 * C::KROWR + (REST == kRestHalves ? 16 : 32) * half;
+            const uint8_t *key = buf + C::kHalf + n32 * C::KROW + 16 * half;
+            const uint8_t *rest = buf + C::kRest + n32 * C::KROWR + (REST == kRestHalves ? 16 : 32) * half;
             u32x4 kh[2][2];
             [[maybe_unused]] u32x4 kr[2][2];
             auto read_keys = [&](int ks) {
@@ -522,7 +611,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             //    as large as the others or 1/50 of them, 291 with 1/500, where such
             //    rows keep a unit of their own; 2^4 holds the weight that makes the
             //    row to 2^-14 with its rest in e4m3.)
-            const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & 1)) + 4 * half;
+            const float *norm = reinterpret_cast<const float *>(lds + C::kNorm + 512 * (t & (C::NT - 1))) + 4 * half;
             const u32x4 about = *reinterpret_cast<const u32x4 *>(tile);
             const uint32_t ok0 = about[0], ok1 = about[1];
             const int tu = (int)about[2], half_least = (int)about[3];
@@ -635,8 +724,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
             if (min((int)tile[4], (int)tile[5]) < lim - tb)
                 l = NAN;
             // 5. O^T += V^T P^T, likewise
-            const uint8_t *val = lds + C::kV + n32 * C::VROW + 16 * half;
-            const uint8_t *val8 = lds + C::kV8 + n32 * C::VROW8 + 32 * half;
+            const uint8_t *val = buf + C::kV + n32 * C::VROW + 16 * half;
+            const uint8_t *val8 = buf + C::kV8 + n32 * C::VROW8 + 32 * half;
             u32x4 vv[2][C::CT];
             i32x8 v8[2];
             v8[0] = read_bytes32(val8);
@@ -666,9 +755,56 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void attn_c_kernel(const Attn
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (t + 1 < nt && w < 2)
-            store_raw(t + 1);
+    };
+    if constexpr (!C::AHEAD) {
+        if (nt > 0 && fetches)
+            store_raw(0);
         __syncthreads();
+        for (int t = 0; t < nt; t++) {
+            decode_keys(t);
+            decode_values(t);
+            if (t + 1 < nt && fetches) {   // (waves WK and WV fetch the next tile's records while all compute)
+                fetch(t + 1, next);
+                next = block_of(t + 2);
+            }
+            __syncthreads();
+            attend(t);
+            if (t + 1 < nt && fetches)
+                store_raw(t + 1);
+            __syncthreads();
+        }
+    } else if (nt > 0) {
+        // the first four waves decode the next tile's keys before they attend to this
+        // one, the next four its values after it: of the two waves of a SIMD one has
+        // vector instructions while the other has matrix products
+        if (fetches) {
+            store_raw(0);
+            if (nt > 1)
+                fetch(1, next);
+            next = block_of(2);
+        }
+        __syncthreads();
+        if (w < 4)
+            decode_values(0);
+        else
+            decode_keys(0);
+        if (nt > 1 && fetches)
+            store_raw(1);
+        __syncthreads();
+        for (int t = 0; t < nt; t++) {
+            if (t + 2 < nt && fetches) {
+                fetch(t + 2, next);
+                next = block_of(t + 3);
+            }
+            if (w >= 4 && t + 1 < nt)
+                decode_keys(t + 1);
+            attend(t);
+            if (w < 4 && t + 1 < nt)
+                decode_values(t + 1);
+            if (t + 2 < nt && fetches)
+                store_raw(t + 2);
+            __syncthreads();
+        }
     }
 
     // 6. the row's part, for the join; or the row itself: a lane has four

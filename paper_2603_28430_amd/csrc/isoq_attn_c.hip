@@ -5,43 +5,49 @@
 namespace isoq {
 namespace {
 
-template <int D, int BITS, int REST>
+template <int D, int BITS, int REST, int W>
 AttnKernel attn_c_entry()
 {
-    using C = AttnCShape<D, BITS, REST>;
-    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, REST>), (size_t)C::lds_bytes(), C::ROWS, true};
+    using C = AttnCShape<D, BITS, REST, W>;
+    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, REST, W>), (size_t)C::lds_bytes(), C::ROWS, true, 64 * W};
 }
 
-template <int D, int REST>
+template <int D, int REST, int W>
 AttnKernel attn_c_bits(int bits)
 {
     switch (bits) {
-    case 2: return attn_c_entry<D, 2, REST>();
-    case 3: return attn_c_entry<D, 3, REST>();
-    case 4: return attn_c_entry<D, 4, REST>();
+    case 2: return attn_c_entry<D, 2, REST, W>();
+    case 3: return attn_c_entry<D, 3, REST, W>();
+    case 4: return attn_c_entry<D, 4, REST, W>();
+    }
+    return {};
+}
+
+template <int REST, int W>
+AttnKernel attn_c_d(int d, int bits)
+{
+    switch (d) {
+    case 64: return attn_c_bits<64, REST, W>(bits);
+    case 80: return attn_c_bits<80, REST, W>(bits);
+    case 96: return attn_c_bits<96, REST, W>(bits);
+    case 128: return attn_c_bits<128, REST, W>(bits);
     }
     return {};
 }
 
 template <int REST>
-AttnKernel attn_c_d(int d, int bits)
+AttnKernel attn_c_rows(int d, int bits, int rows)
 {
-    switch (d) {
-    case 64: return attn_c_bits<64, REST>(bits);
-    case 80: return attn_c_bits<80, REST>(bits);
-    case 96: return attn_c_bits<96, REST>(bits);
-    case 128: return attn_c_bits<128, REST>(bits);
-    }
-    return {};
+    return rows > 128 ? attn_c_d<REST, 8>(d, bits) : attn_c_d<REST, 4>(d, bits);
 }
 
 }  // namespace
 
-AttnKernel attn_c_kernel_for(int d, int bits, int rest)
+AttnKernel attn_c_kernel_for(int d, int bits, int rest, int rows)
 {
-    return rest == kRestNone    ? attn_c_d<kRestNone>(d, bits)
-           : rest == kRestBytes ? attn_c_d<kRestBytes>(d, bits)
-                                : attn_c_d<kRestHalves>(d, bits);
+    return rest == kRestNone    ? attn_c_rows<kRestNone>(d, bits, rows)
+           : rest == kRestBytes ? attn_c_rows<kRestBytes>(d, bits, rows)
+                                : attn_c_rows<kRestHalves>(d, bits, rows);
 }
 
 }  // namespace isoq
