@@ -204,17 +204,18 @@ __device__ __forceinline__ void transpose_rows(uint32_t &x0, uint32_t &x1, uint3
     x3 = d[1];
 }
 
-// acc += A B over one k-step of 4 (K = 64) or 2 (K = 32) quads.
+// acc += A B over one k-step of 4 quads, or of 2 and as many zeros.  (Both by the
+// instruction of K = 64: one of K = 32 that takes the sum of the other as its third
+// operand within 5 cycles of its issue reads what stood there before, which the
+// compiler does not know: attention at d = 96, 3 bits, 5 to 8 rows was off that way
+// in one schedule.  The matrix cores are not what bounds these kernels.)
 template <int NS>
 __device__ __forceinline__ i32x4 digit_mfma(const uint32_t *a, const uint32_t *b, i32x4 acc)
 {
-    if constexpr (NS == 4) {
-        const i32x4 av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3]}, bv = {(int)b[0], (int)b[1], (int)b[2], (int)b[3]};
-        return __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, acc, 0, 0, 0);
-    } else {
-        const long av = (long)(((uint64_t)a[1] << 32) | a[0]), bv = (long)(((uint64_t)b[1] << 32) | b[0]);
-        return __builtin_amdgcn_mfma_i32_16x16x32_i8(av, bv, acc, 0, 0, 0);
-    }
+    static_assert(NS == 4 || NS == 2, "");
+    const i32x4 av = {(int)a[0], (int)a[1], NS == 4 ? (int)a[2 % NS] : 0, NS == 4 ? (int)a[3 % NS] : 0};
+    const i32x4 bv = {(int)b[0], (int)b[1], (int)b[2 % NS], (int)b[3 % NS]};
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, acc, 0, 0, 0);
 }
 
 // Whether a magnitude (its bits) is infinite or NaN.
