@@ -42,7 +42,11 @@ struct AttnArgs {
     int32_t even;
     int32_t part_splits, part_first;   // splits of a row in part, this launch's from part_first on
     int32_t full;                // every token attends to all positions (else: to those up to its own)
-    int32_t n_all;               // sequences that `shared` is about, or 0: not about shared prefixes
+    int32_t n_all;               // sequences that `shared` is about, or 0: the launch is not about what they share
+    // where n_pre > 0, positions that come before the sequences' own: of n_pre prefixes,
+    // prefix p of the sequences pre_start[p] .. pre_start[p + 1] - 1 (null: of all)
+    int32_t n_pre, n_seqs, pre_blocks, pre_tokens, pre_cap;
+    const int32_t *pre_start, *pre_table, *pre_lens;
     float scale;                 // times log2(e)
     FastDiv div_block;
     int32_t d, width, slots;     // coordinates per row, padded width, its rotation slots (8 coordinates for 8-D, else 4)

@@ -58,14 +58,13 @@ struct AttnPlan {
 };
 
 AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int n_seqs, int max_q_len, int n_q_heads,
-                   int n_kv_heads, int block_size, int max_blocks_per_seq, int64_t max_len,
-                   int max_splits = kAttnMaxSplits)
+                   int n_kv_heads, int64_t max_pos, bool few_rows = false, int max_splits = kAttnMaxSplits)
 {
     AttnPlan p{};
     const int sw = pk->variant == VAR_BLOCK8 ? 8 : 4;
     p.slots = (padded_width(pk->variant, pk->d) + sw - 1) / sw;
     p.width = p.slots * sw;
-    p.max_pos = std::min<int64_t>(max_len, (int64_t)max_blocks_per_seq * block_size);
+    p.max_pos = max_pos;
     const bool f16 = dtype == ISOQ_F16;
     const int64_t rows = (int64_t)(n_q_heads / n_kv_heads) * max_q_len;
     p.groups = (int64_t)n_q_heads * max_q_len;
@@ -83,7 +82,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
         // positions, d = 128, 3 bits: 24 rows 64 / 74, 32 78 / 69, 64 141 / 81, 128
         // 256 / 103.  2 x 8 heads, 8,192: 24 28 / 33, 32 30 / 33, 48 39 / 38, 128 70
         // / 55.  4 x 4 heads, 8,192, d = 64, 4 bits: 32 25 / 24, 64 40 / 28.)
-        if (f16 && rows >= 32) {
+        if (f16 && rows >= 32 && !few_rows) {
             const AttnKernel many = attn_c_kernel_for(pk->d, pk->bits, p.kt->key_rest, r);
             if (many.fn)
                 p.kern = many;
@@ -261,13 +260,14 @@ AttnArgs attn_args(const AttnCall &c, const AttnPlan &plan, float scale2)
     a.group = c.n_q_heads / c.n_kv_heads;
     a.block_size = c.block_size;
     a.max_blocks = c.max_blocks;
-    a.cap = c.n_blocks == 0 ? 0 : (int32_t)plan.max_pos;
+    a.cap = c.n_blocks == 0 ? 0 : (int32_t)std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size);
     a.k_sets = pk->n_sets;
     a.v_sets = pv->n_sets;
     a.variant = pk->variant;
     a.q_f16 = c.dtype == ISOQ_F16;
     a.chunk = plan.chunk;
     a.n_splits = a.part_splits = plan.n_splits;
+    a.n_seqs = c.n_seqs;
     a.even = plan.kern.parts;
     a.full = c.full;
     a.scale = scale2;
@@ -310,28 +310,70 @@ isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, in
 // The plans of a call: of the sequences' own positions, and of the prefixes'.
 struct AttnPlans {
     AttnPlan own, pre;
-    bool prefix;
+    bool prefix;   // in launches and parts of their own
+    bool ahead;    // before each sequence's own positions, in one launch (own is the plan of both)
     size_t bytes;
     bool ok;   // (false: no memory for a handle's tables)
 };
+
+// What a tile of keys (64 positions) of a key head costs a workgroup of `rows` rows of a
+// kernel, four rows by digits being 1: a third more for each further four by digits
+// (isoq_attn_m_pick.h), 10 for 128 rows in fp16, by its waves that have rows.
+double tile_cost(const AttnPlan &p, int64_t rows)
+{
+    if (!p.kern.fn)
+        return (double)rows;
+    if (p.kern.parts)
+        return 2.5 * (double)std::max<int64_t>(4, (rows + 31) / 32);
+    return (double)((rows + p.kern.rows - 1) / p.kern.rows) * (0.6 + 0.1 * p.kern.rows);
+}
+
+// Whether the prefix is read anew by every sequence, in front of its own positions, in
+// one launch: `ahead` of both together, against `pre` of the prefix for all its rows
+// together (a launch, parts and a join of its own).  Where the products differ by less
+// than 10 to 20 us of work.  (us, shared / ahead, sequences of 100 positions of their own
+// behind one prefix: 8 x 4 heads, d = 128, fp16: 16 of 2,000 32 / 21, of 8,000 37 / 38, 32
+// 36 / 25, 47 / 58, 64 48 / 39, 63 / 103; 5 tokens each: 4 of 8,000 39 / 41, 16 of 2,000 50 /
+// 37, 64 78 / 93; fp32: 32 of 8,000 67 / 60, 64 102 / 108; 8 x 1, d = 64: 16 of 2,000 17 / 16,
+// of 8,000 19 / 28; 4 x 5, d = 96, fp32, 5 tokens: 16 of 2,000 31 / 31, of 8,000 59 / 73.)
+bool prefix_ahead(const AttnCall &c, const AttnPlan &ahead, const AttnPlan &pre)
+{
+    const int64_t group = c.n_q_heads / c.n_kv_heads;
+    const double tiles = (double)pre.max_pos * c.n_kv_heads;
+    const double anew = tiles * c.n_seqs * tile_cost(ahead, group * c.max_q_len);
+    const double once = tiles * c.n_prefixes * tile_cost(pre, group * c.max_prefix_tokens);
+    return ahead.max_pos <= kAttnMaxPos &&
+           anew <= once + (pre.kern.parts ? 0.75e6 : 0.5e6) + 60.0 * (double)c.n_tokens * c.n_q_heads;
+}
 
 AttnPlans attn_plans(const AttnCall &c)
 {
     AttnPlans p{};
     const isoq_params *pk = c.pk;
     p.prefix = c.n_prefixes > 0 && c.max_prefix_blocks > 0 && c.max_prefix_len > 0 && c.max_prefix_tokens > 0;
-    const int most = p.prefix ? kAttnMaxSplits / 2 : kAttnMaxSplits;   // (a row's join takes both kinds)
-    p.own = attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads, c.block_size, c.max_blocks,
-                      c.max_len, most);
     const bool tables = pk->attn_by_tables && c.pv->attn_by_tables;
-    p.ok = !tables || p.own.kern.fn;
+    const int most = p.prefix ? kAttnMaxSplits / 2 : kAttnMaxSplits;   // (a row's join takes both kinds)
+    if (p.prefix) {
+        const int64_t own = std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size);
+        const int64_t shared = std::min<int64_t>(c.max_prefix_len, (int64_t)c.max_prefix_blocks * c.block_size);
+        p.pre = attn_plan(pk, c.pv, c.dtype, c.n_prefixes, (int)c.max_prefix_tokens, c.n_q_heads, c.n_kv_heads, shared,
+                          false, most);
+        p.own = attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads, own + shared, true);
+        p.ok = !tables || (p.own.kern.fn && p.pre.kern.fn);
+        if (prefix_ahead(c, p.own, p.pre)) {
+            p.prefix = false;
+            p.ahead = true;
+            p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
+            return p;
+        }
+    }
+    p.own = attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads,
+                      std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size), false, most);
+    p.ok = !tables || (p.own.kern.fn && (!p.prefix || p.pre.kern.fn));
     if (!p.prefix) {
         p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
         return p;
     }
-    p.pre = attn_plan(pk, c.pv, c.dtype, c.n_prefixes, (int)c.max_prefix_tokens, c.n_q_heads, c.n_kv_heads, c.block_size,
-                      c.max_prefix_blocks, c.max_prefix_len, most);
-    p.ok = p.ok && (!tables || p.pre.kern.fn);
     p.bytes = sizeof(float) * (size_t)c.n_tokens * c.n_q_heads * (p.own.n_splits + p.pre.n_splits) * (p.own.width + 2);
     return p;
 }
@@ -366,8 +408,8 @@ isoq_status attn_call(AttnCall c)
     const bool no_keys = c.n_blocks == 0 || c.max_blocks == 0 || c.max_len == 0;
     const AttnPlans plans = attn_plans(c);
     if (!c.q || !c.out || !c.seq_lens || (!no_keys && !c.block_table) ||
-        (plans.prefix && (!c.prefix_table || !c.prefix_lens)) ||
-        ((!no_keys || plans.prefix) && (!c.k_idx || !c.k_rho || !c.v_idx || !c.v_rho)))
+        ((plans.prefix || plans.ahead) && (!c.prefix_table || !c.prefix_lens)) ||
+        ((!no_keys || plans.prefix || plans.ahead) && (!c.k_idx || !c.k_rho || !c.v_idx || !c.v_rho)))
         return ISOQ_E_NULL;
     if (!aligned(c.q, 16) || !aligned(c.out, 16) || !aligned(c.k_idx, 16) || !aligned(c.v_idx, 16) || !aligned(c.k_rho, 4) ||
         !aligned(c.v_rho, 4) || !aligned(c.block_table, 4) || !aligned(c.seq_lens, 4) || !aligned(c.q_start, 4) ||
@@ -389,6 +431,15 @@ isoq_status attn_call(AttnCall c)
     AttnArgs a = attn_args(c, plan, scale2);
     if (no_keys)
         a.cap = 0;
+    if (plans.ahead) {
+        a.n_pre = c.n_prefixes;
+        a.pre_blocks = c.max_prefix_blocks;
+        a.pre_tokens = (int32_t)c.max_prefix_tokens;
+        a.pre_cap = (int32_t)std::min<int64_t>(c.max_prefix_len, (int64_t)c.max_prefix_blocks * c.block_size);
+        a.pre_start = c.prefix_start;
+        a.pre_table = c.prefix_table;
+        a.pre_lens = c.prefix_lens;
+    }
     if (plans.prefix)
         a.part_splits += plans.pre.n_splits;
     if (need) {
@@ -400,6 +451,7 @@ isoq_status attn_call(AttnCall c)
         AttnCall shared = c;   // every token of a prefix's sequences, all its positions
         shared.block_table = c.prefix_table;
         shared.max_blocks = c.max_prefix_blocks;
+        shared.max_len = c.max_prefix_len;
         shared.seq_lens = c.prefix_lens;
         shared.max_q_len = (int)c.max_prefix_tokens;
         shared.full = true;
@@ -438,7 +490,8 @@ size_t isoq_kv_attn_workspace(const isoq_params *pk, const isoq_params *pv, int 
                    max_len) != ISOQ_OK ||
         n_tokens == 0 || n_seqs == 0)
         return 0;
-    return plan_bytes(attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads, block_size, max_blocks_per_seq, max_len),
+    return plan_bytes(attn_plan(pk, pv, dtype, n_seqs, max_q_len, n_q_heads, n_kv_heads,
+                                std::min<int64_t>(max_len, (int64_t)max_blocks_per_seq * block_size)),
                       n_tokens, n_q_heads);
 }
 

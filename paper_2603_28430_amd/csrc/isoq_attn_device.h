@@ -9,22 +9,50 @@
 namespace isoq {
 namespace {
 
+// The prefix that sequence s has of `n` (start[p] .. start[p + 1] - 1 share prefix p;
+// start null: all share one), or none, and the first of its tokens.
+struct PrefixOf {
+    int index, token;
+    bool any;
+};
+
+__device__ __forceinline__ PrefixOf prefix_of(const AttnArgs &a, const int32_t *start, int n, int n_seqs, int s)
+{
+    PrefixOf p{0, 0, true};
+    int first = 0, end = n_seqs;
+    if (start) {
+        for (int hi = n; p.index + 1 < hi;) {
+            const int mid = (p.index + hi) >> 1;
+            if (start[mid] <= s)
+                p.index = mid;
+            else
+                hi = mid;
+        }
+        first = max(start[p.index], 0);
+        end = start[p.index + 1];
+    }
+    p.any = s >= first && s < end;
+    p.token = a.q_start ? min(max(a.q_start[min(first, n_seqs)], 0), a.n_tokens) : first;
+    return p;
+}
+
 // The new tokens of sequence s: rows first .. first + n - 1 of q, of which
 // `rows` are computed (max_q_len at most), and its length.
 struct AttnSeq {
     int first, n, rows, len, full;
+    int base, prefix;   // positions of its prefix that come first, which prefix (0: none, or the first)
     // Positions that token i attends to: all, or those up to its own, the newest
     // token being the last position.
     __device__ __forceinline__ int limit(int i, int cap) const
     {
         const int64_t l = (int64_t)len - (full ? 0 : n - 1 - i);
-        return (int)(l < 0 ? 0 : l < cap ? l : cap);
+        return base + (int)(l < 0 ? 0 : l < cap ? l : cap);
     }
 };
 
 __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 {
-    AttnSeq q{s, 1, 1, a.seq_lens[s], a.full};
+    AttnSeq q{s, 1, 1, a.seq_lens[s], a.full, 0, 0};
     if (a.n_all > 0) {   // (clamped likewise)
         const int from = a.shared ? min(max(a.shared[s], 0), a.n_all) : 0;
         const int to = a.shared ? min(max(a.shared[s + 1], from), a.n_all) : a.n_all;
@@ -36,7 +64,32 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
         q.n = min(max(a.q_start[s + 1], q.first), a.n_tokens) - q.first;
         q.rows = min(q.n, a.max_q_len);
     }
+    if (a.n_pre > 0) {
+        const PrefixOf p = prefix_of(a, a.pre_start, a.n_pre, a.n_seqs, s);
+        if (p.any) {
+            q.prefix = p.index;
+            q.base = min(max(a.pre_lens[p.index], 0), a.pre_cap);
+            q.rows = min(q.rows, max(a.pre_tokens - (q.first - p.token), 0));
+        }
+    }
     return q;
+}
+
+// Position t's entry of the block tables: its prefix's, then its own.
+struct AttnEntry {
+    int32_t blk, pos;   // cache block and position in it
+};
+
+__device__ __forceinline__ AttnEntry attn_entry(const AttnArgs &a, const AttnSeq &sq, const int32_t *table, int t)
+{
+    uint32_t tt = (uint32_t)min(t, a.cap - 1);
+    if (a.n_pre > 0) {
+        const bool own = t >= sq.base && a.cap > 0;
+        tt = (uint32_t)(own ? min(t - sq.base, a.cap - 1) : min(t, a.pre_cap - 1));
+        table = own ? table : a.pre_table + (int64_t)sq.prefix * a.pre_blocks;
+    }
+    const uint32_t bi = fast_div(tt, a.div_block);
+    return AttnEntry{table[bi], (int)(tt - bi * a.block_size)};
 }
 
 // Positions per split of a sequence: a.chunk, which the longest possible one needs, or

@@ -100,9 +100,9 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         bool ok = false;
         int blk = 0, pos = 0;
         if (t < tend) {
-            const uint32_t bi = fast_div((uint32_t)t, a.div_block);
-            blk = table[bi];
-            pos = (int)((uint32_t)t - bi * a.block_size);
+            const AttnEntry e = attn_entry(a, sq, table, (int)t);
+            blk = e.blk;
+            pos = e.pos;
             ok = blk >= 0 && blk < a.n_blocks;
         }
         seen |= ok;

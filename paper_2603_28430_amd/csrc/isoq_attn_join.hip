@@ -41,25 +41,13 @@ __device__ __forceinline__ RowSplits row_splits(const AttnArgs &a, const AttnPre
     const int own = splits_of(sq.limit(i, a.cap), attn_chunk(a, sq));
     RowSplits r{row * a.part_splits, PREFIX ? own : 0, own, 0};
     if constexpr (PREFIX) {
-        int g = 0, first = 0, end = p.n_seqs;   // the prefix, and its sequences
-        if (p.start) {
-            for (int hi = p.n; g + 1 < hi;) {
-                const int mid = (g + hi) >> 1;
-                if (p.start[mid] <= s)
-                    g = mid;
-                else
-                    hi = mid;
-            }
-            first = max(p.start[g], 0);
-            end = p.start[g + 1];
-        }
-        if (s >= first && s < end) {
-            const int token = a.q_start ? min(max(a.q_start[min(first, p.n_seqs)], 0), a.n_tokens) : first;
-            if (sq.first + i - token >= p.max_tokens) {
+        const PrefixOf g = prefix_of(a, p.start, p.n, p.n_seqs, s);
+        if (g.any) {
+            if (sq.first + i - g.token >= p.max_tokens) {
                 r.all = -1;
                 return r;
             }
-            const int len = p.lens[g];
+            const int len = p.lens[g.index];
             r.all += splits_of(min(max(len, 0), p.cap), attn_chunk(len, p.even, p.cap, p.n_splits, p.chunk));
             r.jump = a.n_splits - r.own;
         }

@@ -321,16 +321,11 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
         attn_load_query<D>(a, sq, h, r0 + cr, cl, query);
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
     const int tw = t0 + 64 * w + lane;
-    struct Entry {
-        int32_t blk, pos;   // cache block and position in it
-    };
     auto entry = [&](int b) {   // (positions past the last possible one: that one's)
-        const uint32_t tt = (uint32_t)min((int64_t)tw + 64 * WV * (int64_t)b, (int64_t)a.cap - 1);
-        const uint32_t bi = fast_div(tt, a.div_block);
-        return Entry{table[bi], (int)(tt - bi * a.block_size)};
+        return attn_entry(a, sq, table, (int)min((int64_t)tw + 64 * WV * (int64_t)b, (int64_t)0x7FFFFFFF));
     };
-    Entry next{};
-    if (a.cap > 0)
+    AttnEntry next{};
+    if (a.cap > 0 || a.n_pre > 0)
         next = entry(0);
     __builtin_amdgcn_sched_barrier(0);
     // the positions that the rows attend to: rows come in the tokens' order, so

@@ -3,7 +3,9 @@
 test_gpu_kv_attn.py derives: the sums run over the prefix's and the sequence's own
 positions together, joined once more (fp32, inside the 2^-19 of the weights).
 
-Prefixes are further sequences of test_gpu_kv_attn.py's caches, without tokens.
+Prefixes are further sequences of test_gpu_kv_attn.py's caches, without tokens.  Each case
+runs twice: short prefixes are read anew by every sequence, and with a wide prefix table
+(as for 100,000 positions) by launches of their own for the rows of all.
 Slots that no position uses hold norms of NaN.  Needs an MI355X."""
 import numpy as np
 import pytest
@@ -100,14 +102,24 @@ def prefix_case(variant, d, bits, dtype, q_lens, n_q, n_kv, bs, seq_lens, prefix
         used = [sum(q_lens[starts[p]:starts[p + 1]]) for p in range(m)]
         args["max_prefix_tokens"] = max(1, max(used))
     args.update(kw)
-    out = torch.full_like(args["q"], CANARY)
-    lse = torch.full(args["q"].shape[:2], CANARY, device="cuda")
-    iq.isoq_kv_attn_prefix(**args, out=out, lse=lse)
-    torch.cuda.synchronize()
-    check(out, lse, reference(w, scale, prefix_of, max_len=kw.get("max_len"), max_prefix_len=kw.get("max_prefix_len")))
+    ref = reference(w, scale, prefix_of, max_len=kw.get("max_len"), max_prefix_len=kw.get("max_prefix_len"))
     total = sum(q_lens)
-    assert torch.all(out[total:] == torch.full_like(out[total:], CANARY)) and torch.all(lse[total:] == CANARY)
+    narrow = args["prefix_table"]
+    for table in (widen(narrow, bs), narrow):
+        args["prefix_table"] = table
+        out = torch.full_like(args["q"], CANARY)
+        lse = torch.full(args["q"].shape[:2], CANARY, device="cuda")
+        iq.isoq_kv_attn_prefix(**args, out=out, lse=lse)
+        torch.cuda.synchronize()
+        check(out, lse, ref)
+        assert torch.all(out[total:] == torch.full_like(out[total:], CANARY)) and torch.all(lse[total:] == CANARY)
     return w, args, out, lse
+
+
+def widen(table, bs, positions=100000):
+    """A prefix table of so many positions, the further entries outside the cache."""
+    more = max(0, -(-positions // bs) - table.shape[1])
+    return torch.cat([table, table.new_full((table.shape[0], more), -5)], 1).contiguous()
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
@@ -157,6 +169,8 @@ def test_several_tokens(q_lens, seq_lens, d, bits, dtype, group):
 
 def test_many_splits():
     """More splits than the join of few takes, of the prefix, of the sequences and of both."""
+    prefix_case("fast", 128, 3, "f16", [1] * 40, 2, 1, 16, [5] * 39 + [4000], [12000], seed=5)   # (both launches, both with splits)
+    prefix_case("full", 192, 4, "f32", [1] * 9, 2, 1, 16, [5] * 8 + [2000], [9000], seed=6)
     prefix_case("fast", 128, 3, "f16", [1], 2, 1, 16, [30], [20000], seed=1)
     prefix_case("fast", 64, 4, "f32", [1], 2, 1, 16, [15000], [20], seed=2)
     prefix_case("fast", 128, 2, "f16", [1, 1], 2, 1, 16, [9000, 3], [12000], seed=3)
@@ -167,8 +181,9 @@ def test_bounds_that_cut():
     """max_len and max_prefix_len below the lengths; max_prefix_tokens below a prefix's tokens: those rows are left alone."""
     prefix_case("full", 128, 3, "f16", [1] * 3, 4, 2, 16, [100, 30, 65], [300], max_len=64, max_prefix_len=130, seed=1)
     w, args, out, lse = prefix_case("full", 128, 3, "f16", [2, 3, 2, 1], 4, 2, 16, [100, 30, 65, 9], [300, 40], [3, 1], seed=2)
-    for most in (1, 2, 5, 6):
-        args["max_prefix_tokens"] = most
+    narrow = args["prefix_table"]
+    for most, table in ((m, x) for m in (1, 2, 5, 6) for x in (narrow, widen(narrow, 16))):
+        args["max_prefix_tokens"], args["prefix_table"] = most, table
         o, l = torch.full_like(out, CANARY), torch.full_like(lse, CANARY)
         iq.isoq_kv_attn_prefix(**args, out=o, lse=l)
         left = torch.arange(len(out), device="cuda")
@@ -183,7 +198,7 @@ def test_no_prefix_is_isoq_kv_attn():
     plain = {k: v for k, v in args.items() if not k.startswith("prefix")}
     ref = iq.isoq_kv_attn(**plain)
     for kw in (dict(prefix_table=args["prefix_table"][:, :0].contiguous()), dict(max_prefix_len=0),
-               dict(prefix_table=args["prefix_table"][:0], prefix_lens=args["prefix_lens"][:0])):
+               dict(prefix_table=args["prefix_table"][:0], prefix_lens=args["prefix_lens"][:0])):   # (no prefix at all)
         got = iq.isoq_kv_attn_prefix(**dict(args, **kw))
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
 
@@ -194,16 +209,24 @@ def test_empty_rows_whatever_the_query_holds():
     args["q"][0] = float("nan")
     args["q"][2, 1] = float("inf")
     args["q"][3, 0] = float("nan")
-    out, lse = iq.isoq_kv_attn_prefix(**args)
+    for table in (args["prefix_table"], widen(args["prefix_table"], 16)):
+        out, lse = iq.isoq_kv_attn_prefix(**dict(args, prefix_table=table))
+        empty_rows(out, lse)
+
+
+def empty_rows(out, lse):
     assert (out[:2] == 0).all() and (lse[:2] == -float("inf")).all()
     assert lse[2, 1].isnan() and lse[3, 0].isnan() and out[3, 0].isnan().all()
     assert lse[2, 0].isfinite() and lse[3, 1:].isfinite().all()
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("d", [128, 90])
-def test_invalid_pages_and_odd_norms(d):
+def test_invalid_pages_and_odd_norms(d, wide):
     """Prefix blocks outside the cache are left out; a norm that is no number reaches the rows that share it, not others."""
     w, args, out, lse = prefix_case("full", d, 3, "f16", [1] * 4, 4, 2, 16, [20, 5, 40, 0], [100, 64], [2, 2], seed=d)
+    if wide:
+        args["prefix_table"] = widen(args["prefix_table"], 16)
     good = iq.isoq_kv_attn_prefix(**args)
     bad = args["prefix_table"].clone()
     bad[0, 1:6] = torch.tensor([-1, 10 ** 6, -7, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)
@@ -222,12 +245,18 @@ def test_invalid_pages_and_odd_norms(d):
     assert got[1][:2, :2].isnan().all() and got[1][:2, 2:].isfinite().all() and torch.equal(got[0][2:], good[0][2:])
 
 
-def test_streams_workspaces_and_graphs():
+@pytest.mark.parametrize("wide", [False, True])
+def test_streams_workspaces_and_graphs(wide):
     """A stream and a workspace of its own; two graphs with a workspace each, replayed with other lengths and eager work between."""
     w, args, out, lse = prefix_case("full", 128, 3, "f16", [1] * 20, 8, 2, 16, list(range(20)), [700], seed=7)
+    if wide:
+        args["prefix_table"] = widen(args["prefix_table"], 16)
+        out, lse = iq.isoq_kv_attn_prefix(**args)
     n_seqs, blocks = args["block_table"].shape
+    shared = args["prefix_table"].shape[1]
     need = iq.isoq_kv_attn_prefix_workspace(args["pk"], args["pv"], torch.float16, 20, 1, n_seqs, 8, 2, 16, blocks,
-                                            blocks * 16, 1, 20, blocks, blocks * 16)
+                                            blocks * 16, 1, 20, shared, shared * 16)
+    assert need > 0
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     stream = torch.cuda.Stream()
     torch.cuda.synchronize()
