@@ -13,8 +13,6 @@
 namespace isoq {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 // cos and sin of p 2^-32 turns: by the Taylor series on an eighth of a turn
 // either side of the nearest quarter (cut at x^11 / 11! and x^12 / 12!, 2e-9 and
 // 1e-10 at the ends).
@@ -97,32 +95,62 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(const RopeArgs a)
     }
 }
 
-// Rows whose width and rotated part are pairs of 16-byte chunks.  L lanes have a
-// row, a wave 64 / L rows of one token at a time; a lane has two chunks of CH
-// coordinates, half of the rotated part (or of the rest) apart, so that both layouts
-// have their pairs in one lane: coordinates i of both chunks, or 2 i and 2 i + 1 of
-// each.  cos and sin are a lane's own for all of its token's rows, with the weight
-// and the amplitude multiplied in: a pair is four products of its two coordinates.
-template <bool F16, bool HALVES, int L>
+// CH elements as one access.
+template <bool F16, int CH>
+struct RopeChunk {
+    using T = std::conditional_t<F16, _Float16, float>;
+    T x[CH];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (CH * sizeof(T) == 16) {
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+            __builtin_memcpy(x, &v, 16);
+        } else {
+            __builtin_memcpy(x, __builtin_assume_aligned(p, CH * sizeof(T)), CH * sizeof(T));
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        __builtin_memcpy(__builtin_assume_aligned(p, CH * sizeof(T)), x, CH * sizeof(T));
+    }
+};
+
+// Rows by chunks of CH coordinates (16 bytes where widths and places allow it).  L
+// lanes have a row, a wave 64 / L rows of one token at a time; a lane has two chunks,
+// half of the rotated part (or of the rest) apart, so that both layouts have their pairs
+// in one lane: coordinates i of both chunks, or 2 i and 2 i + 1 of each.  cos and sin
+// are a lane's own for all of its token's rows, with the weight and the amplitude
+// multiplied in: a pair is four products of its two coordinates.
+//
+// What bounds it: memory.  32,768 tokens of 32 + 8 heads, d = 128, fp16, 671 MB: 125
+// us, 5.4 TB/s, where a large copy moves 4.8.  (A row a wave with cos and sin for every
+// element, rope_rows_kernel: 789.)  32 tokens: 4 us, next to its launch; the binding's
+// host time, 11 us, is what a call takes.
+template <bool F16, bool HALVES, int CH, int L>
 __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
 {
-    constexpr int CH = F16 ? 8 : 4, V = 64 / L;
-    using T = std::conditional_t<F16, _Float16, float>;
+    static_assert(HALVES || CH % 2 == 0, "pairs inside a chunk");
+    constexpr int V = 64 / L;
+    using Chunk = RopeChunk<F16, CH>;
+    using T = typename Chunk::T;
     const int lane = threadIdx.x & 63, sub = lane & (L - 1), g = lane / L;
     const uint32_t wid = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t t = wid / (uint32_t)a.parts, part = wid - t * a.parts;
     if (t >= (uint32_t)a.n_tokens)
         return;
-    const int nr = a.half / CH, nz = (a.d - 2 * a.half) / (2 * CH);   // lanes of a row that rotate, that pass on
+    // chunks that rotate, that are passed on; lanes for each
+    const int cr = 2 * a.half / CH, cz = (a.d - 2 * a.half) / CH, nr = (cr + 1) / 2, nz = (cz + 1) / 2;
     const bool turned = sub < nr, there = sub < nr + nz;
-    const int oa = turned ? sub * CH : 2 * a.half + (sub - nr) * CH, ob = oa + (turned ? a.half : nz * CH);
+    const int ka = turned ? sub : sub - nr, kb = ka + (turned ? nr : nz);
+    const bool both = kb < (turned ? cr : cz);   // (an odd chunk has no other)
+    const int oa = (turned ? 0 : 2 * a.half) + ka * CH, ob = oa + (both ? (kb - ka) * CH : 0);
 
     float c[CH], s[CH];
     if (turned) {
         const int32_t pos = a.positions[t];
 #pragma unroll
         for (int i = 0; i < CH; i++) {
-            const int p = HALVES ? oa + i : (i < CH / 2 ? oa : ob - CH) / 2 + i;
+            const int p = HALVES ? oa + i : i < CH / 2 ? oa / 2 + i : ob / 2 + i - CH / 2;
             turn_cos_sin(turns_of(a.turns[p], pos), c[i], s[i]);
         }
     }
@@ -140,13 +168,9 @@ __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
             wa[i] = wb[i] = 1.f;
         if (weight && there) {
 #pragma unroll
-            for (int i = 0; i < CH; i += 4) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(weight + oa + i), y = *reinterpret_cast<const f32x4 *>(weight + ob + i);
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    wa[i + j] = x[j];
-                    wb[i + j] = y[j];
-                }
+            for (int i = 0; i < CH; i++) {
+                wa[i] = weight[oa + i];
+                wb[i] = weight[ob + i];
             }
         }
         // pair i: (x, y) -> (x cx - y sy, x sx + y cy)
@@ -164,12 +188,12 @@ __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
         const int heads = a.heads[k];
         const T *x = static_cast<const T *>(a.x[k]) + t * a.stride[k];
         T *out = static_cast<T *>(a.out[k]) + (int64_t)t * heads * a.d;
-        u32x4 ra, rb, na{}, nb{};
+        Chunk ra, rb, na{}, nb{};
         auto load = [&](int it) {
             const int h = it * V + g;
             if (there && h < heads) {
-                na = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + (int64_t)h * a.d + oa));
-                nb = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + (int64_t)h * a.d + ob));
+                na.load(x + (int64_t)h * a.d + oa);
+                nb.load(x + (int64_t)h * a.d + ob);
             }
         };
         load(lo);
@@ -180,25 +204,16 @@ __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
                 load(it + 1);
             float xa[CH], xb[CH];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t ea = ra[i], eb = rb[i];
-                if constexpr (F16) {
-                    const f16x2 p = __builtin_bit_cast(f16x2, ea), q = __builtin_bit_cast(f16x2, eb);
-                    xa[2 * i] = (float)p.x;
-                    xa[2 * i + 1] = (float)p.y;
-                    xb[2 * i] = (float)q.x;
-                    xb[2 * i + 1] = (float)q.y;
-                } else {
-                    xa[i] = __uint_as_float(ea);
-                    xb[i] = __uint_as_float(eb);
-                }
+            for (int i = 0; i < CH; i++) {
+                xa[i] = (float)ra.x[i];
+                xb[i] = (float)rb.x[i];
             }
             if (weight) {   // (uniform)
                 float sum = 0.f;
                 if (there) {
 #pragma unroll
                     for (int i = 0; i < CH; i++)
-                        sum = fmaf(xb[i], xb[i], fmaf(xa[i], xa[i], sum));
+                        sum = fmaf(both ? xb[i] : 0.f, xb[i], fmaf(xa[i], xa[i], sum));
                 }
                 const float scale = 1.f / sqrtf(row_sum<L>(sum) / (float)a.d + a.eps);
 #pragma unroll
@@ -229,38 +244,41 @@ __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
                     yb[i] = xb[i] * wb[i];
                 }
             }
-            u32x4 oa4, ob4;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                if constexpr (F16) {
-                    const f16x2 p{(_Float16)ya[2 * i], (_Float16)ya[2 * i + 1]}, q{(_Float16)yb[2 * i], (_Float16)yb[2 * i + 1]};
-                    oa4[i] = __builtin_bit_cast(uint32_t, p);
-                    ob4[i] = __builtin_bit_cast(uint32_t, q);
-                } else {
-                    oa4[i] = __float_as_uint(ya[i]);
-                    ob4[i] = __float_as_uint(yb[i]);
-                }
+            for (int i = 0; i < CH; i++) {
+                ra.x[i] = (T)ya[i];
+                rb.x[i] = (T)yb[i];
             }
             const int h = it * V + g;
             if (there && h < heads) {
-                *reinterpret_cast<u32x4 *>(out + (int64_t)h * a.d + oa) = oa4;
-                *reinterpret_cast<u32x4 *>(out + (int64_t)h * a.d + ob) = ob4;
+                ra.store(out + (int64_t)h * a.d + oa);
+                if (both)
+                    rb.store(out + (int64_t)h * a.d + ob);
             }
         }
     }
 }
 
-template <bool F16, bool HALVES>
+template <bool F16, bool HALVES, int CH>
 const void *rope_lanes(int lanes)
 {
     switch (lanes) {
-    case 4: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 4>);
-    case 8: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 8>);
-    case 16: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 16>);
-    case 32: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 32>);
-    case 64: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, 64>);
+    case 4: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, CH, 4>);
+    case 8: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, CH, 8>);
+    case 16: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, CH, 16>);
+    case 32: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, CH, 32>);
+    case 64: return reinterpret_cast<const void *>(&rope_tile_kernel<F16, HALVES, CH, 64>);
     }
     return nullptr;
+}
+
+template <bool F16, bool HALVES>
+const void *rope_chunks(int chunk, int lanes)
+{
+    if constexpr (HALVES)
+        if (chunk == 1)
+            return rope_lanes<F16, HALVES, 1>(lanes);
+    return chunk == 2 ? rope_lanes<F16, HALVES, 2>(lanes) : rope_lanes<F16, HALVES, F16 ? 8 : 4>(lanes);
 }
 
 template <bool F16, bool HALVES>
@@ -278,10 +296,10 @@ const void *rope_steps(int log2_steps)
 
 }  // namespace
 
-const void *rope_tile_kernel_for(bool f16, bool halves, int lanes)
+const void *rope_tile_kernel_for(bool f16, bool halves, int chunk, int lanes)
 {
-    return f16 ? (halves ? rope_lanes<true, true>(lanes) : rope_lanes<true, false>(lanes))
-               : (halves ? rope_lanes<false, true>(lanes) : rope_lanes<false, false>(lanes));
+    return f16 ? (halves ? rope_chunks<true, true>(chunk, lanes) : rope_chunks<true, false>(chunk, lanes))
+               : (halves ? rope_chunks<false, true>(chunk, lanes) : rope_chunks<false, false>(chunk, lanes));
 }
 
 const void *rope_kernel(bool f16, bool halves, int log2_steps)

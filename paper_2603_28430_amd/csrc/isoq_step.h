@@ -42,9 +42,10 @@ struct RopeArgs {
     float eps, amplitude;
     int32_t parts;                 // waves that share a token's rows (rope_tile_kernel)
 };
-// Widths of 16-byte chunks in pairs (rope_tile_kernel): a lane has two chunks of a
-// row, lanes (4 .. 64, a power of two) a row.  Grid of four waves, `parts` a token.
-const void *rope_tile_kernel_for(bool f16, bool halves, int lanes);
+// Rows by chunks of `chunk` coordinates (16 bytes, 2 or, in halves, 1), which divide the width and
+// the rotated part (in halves each half), lanes (4 .. 64, a power of two) a row. Grid
+// of four waves, `parts` a token.
+const void *rope_tile_kernel_for(bool f16, bool halves, int chunk, int lanes);
 // A row a wave, rows token by token (queries, then keys), four waves a workgroup;
 // for widths up to 64 << log2_steps (log2_steps <= 4).
 const void *rope_kernel(bool f16, bool halves, int log2_steps);

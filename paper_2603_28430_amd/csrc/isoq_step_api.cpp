@@ -217,20 +217,23 @@ isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int6
     a.amplitude = r->amplitude;
     const bool f16 = dtype == ISOQ_F16, halves = r->layout == ISOQ_ROPE_HALVES;
     void *args[] = {&a};
-    // 16-byte chunks in pairs, where all rows have them
-    const int chunk = f16 ? 8 : 4, pairs = r->d / (2 * chunk);
-    auto placed = [&](const void *x, int64_t stride, int n) {
-        return n == 0 || (aligned(x, 16) && (n_tokens == 1 || stride % chunk == 0));
-    };
-    if (r->d % (2 * chunk) == 0 && a.half % chunk == 0 && pairs <= 64 && placed(q, q_stride, n_q_heads) &&
-        placed(k, k_stride, n_kv_heads) && aligned(q_weight, 16) && aligned(k_weight, 16)) {
+    // the largest chunks that all rows are made of
+    for (const int chunk : {f16 ? 8 : 4, 2, 1}) {
+        const int cr = 2 * a.half / chunk, cz = (r->d - 2 * a.half) / chunk, pairs = (cr + 1) / 2 + (cz + 1) / 2;
+        const size_t bytes = chunk * es;
+        auto placed = [&](const void *x, int64_t stride, int n) {
+            return n == 0 || (aligned(x, bytes) && (n_tokens == 1 || stride % chunk == 0));
+        };
+        if (r->d % chunk != 0 || (halves ? a.half : 2 * a.half) % chunk != 0 || (!halves && chunk % 2 != 0) || pairs > 64 ||
+            !placed(q, q_stride, n_q_heads) || !placed(k, k_stride, n_kv_heads))
+            continue;
         int lanes = 4;
         while (lanes < pairs)
             lanes *= 2;
         const int64_t rows = 64 / lanes, most = (n_q_heads + rows - 1) / rows + (n_kv_heads + rows - 1) / rows;
         a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, kRopeWaves / n_tokens));
-        return launch_lds(rope_tile_kernel_for(f16, halves, lanes), dim3((unsigned)((n_tokens * a.parts + 3) / 4)), 256,
-                          args, 0, stream);
+        return launch_lds(rope_tile_kernel_for(f16, halves, chunk, lanes), dim3((unsigned)((n_tokens * a.parts + 3) / 4)),
+                          256, args, 0, stream);
     }
     int steps = 0;
     while ((64 << steps) < r->d)
