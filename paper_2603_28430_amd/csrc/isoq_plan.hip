@@ -106,32 +106,43 @@ struct PlanMove {
     int seq, at, from, count;   // count < 0: released
 };
 
-// ONE: a sequence a thread at most, held in registers, and the token search in LDS;
-// else consecutive ones a thread, read again in every pass.
-template <bool ONE>
+// N > 0: up to N consecutive sequences a thread, held in registers, and the token
+// search in LDS; 0: any number, read again in every pass.
+template <int N>
 __device__ __forceinline__ void plan_body(const PlanArgs &a)
 {
     constexpr int WAVES = kPlanThreads / 64;
     // blocks that a thread moves by itself; more go to the list
     constexpr int FEW = 2;
-    __shared__ int wave_sum[3][WAVES], most[WAVES], listed[2];
+    __shared__ int wave_sum[3][WAVES], most[WAVES], listed[4];
     __shared__ PlanMove list[kPlanThreads];
-    __shared__ int start[ONE ? kPlanThreads + 1 : 1];
-    __shared__ int begin[ONE ? kPlanThreads : 1];   // position of its first new token, or ~ that where it is refused
+    __shared__ int start[N ? N * kPlanThreads + 1 : 1];
+    __shared__ int begin[N ? N * kPlanThreads : 1];   // position of its first new token, or ~ that where it is refused
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int per = ONE ? 1 : (a.n_seqs + kPlanThreads - 1) / kPlanThreads;
+    const int per = N ? N : (a.n_seqs + kPlanThreads - 1) / kPlanThreads;
     const int s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
 
-    if (tid < 2)
+    if (tid < 4)
         listed[tid] = 0;
     const int n_free = *a.n_free;
-    PlanSeq mine{0, 0, 0, 0};
-    if (ONE && s0 < s1)
-        mine = plan_seq(a, s0);
-    auto seq = [&](int s) { return ONE ? mine : plan_seq(a, s); };
+    PlanSeq mine[N ? N : 1];
+    if constexpr (N > 0) {
+#pragma unroll
+        for (int k = 0; k < N; k++)
+            mine[k] = s0 + k < s1 ? plan_seq(a, s0 + k) : PlanSeq{0, 0, 0, 0};
+    }
+    auto seq = [&](int k) {
+        if constexpr (N > 0)
+            return mine[k];
+        else
+            return plan_seq(a, s0 + k);
+    };
     int sum[3] = {0, 0, 0}, before[3], total[3];
-    for (int s = s0; s < s1; s++) {
-        const PlanSeq q = seq(s);
+#pragma unroll N > 0 ? N : 1
+    for (int k = 0; k < per; k++) {
+        if (s0 + k >= s1)
+            break;
+        const PlanSeq q = seq(k);
         sum[0] = add_sat(sum[0], q.fresh());
         sum[1] = add_sat(sum[1], q.grow());
         sum[2] = add_sat(sum[2], q.drop());
@@ -159,50 +170,80 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
     const int held = min(max(n_free, 0), max_free);
     const int there = min(add_sat(held, total[2]), max_free);
 
+    auto blocks = [&](const PlanMove &m) { return m.count < 0 ? min(-m.count, max_free - m.from) : m.count; };   // (released: from <= max_free)
+    auto source = [&](const PlanMove &m, int j) {
+        return m.count < 0 ? a.block_table + (int64_t)m.seq * a.max_blocks + m.at + j : a.free_blocks + (m.from - j);
+    };
+    auto target = [&](const PlanMove &m, int j) {
+        return m.count < 0 ? a.free_blocks + (m.from + j) : a.block_table + (int64_t)m.seq * a.max_blocks + m.at + j;
+    };
     auto move = [&](const PlanMove &m, int first, int step) {
-        int *row = a.block_table + (int64_t)m.seq * a.max_blocks + m.at;
-        if (m.count < 0) {
-            const int n = min(-m.count, max_free - m.from);   // (from <= max_free)
-#pragma unroll 4
-            for (int j = first; j < n; j += step)
-                a.free_blocks[m.from + j] = row[j];
-        } else {
-#pragma unroll 4
-            for (int j = first; j < m.count; j += step)
-                row[j] = a.free_blocks[m.from - j];
+        const int n = blocks(m);
+        for (int64_t j = first; j < n; j += 4 * step) {   // (four loads, then four stores: the lists do not overlap)
+            int v[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (j + u * step < n)
+                    v[u] = *source(m, (int)j + u * step);
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (j + u * step < n)
+                    *target(m, (int)j + u * step) = v[u];
         }
     };
+    // few blocks at once; more by the lists: from the front those for a wave, from the back those for all
     auto put = [&](int which, const PlanMove &m) {
-        if (abs(m.count) <= FEW)
+        const int n = blocks(m);
+        if (n <= FEW)
             move(m, 0, 1);
-        else
+        else if (n <= kPlanThreads / 2)
             list[atomicAdd(&listed[which], 1)] = m;
+        else
+            list[kPlanThreads - 1 - atomicAdd(&listed[2 + which], 1)] = m;
     };
-    // the list's moves: all waves to one of many blocks, else a wave each
     auto work_off = [&](int which) {
+        constexpr int U = 4;   // moves at once: their loads wait together
         __syncthreads();
-        const int n = listed[which];
-        for (int x = 0; x < n; x++) {
-            const PlanMove m = list[x];
-            if (abs(m.count) > 512)
-                move(m, tid, kPlanThreads);
-            else if (x % WAVES == w)
-                move(m, lane, 64);
+        const int n = listed[which], many = listed[2 + which];
+        for (int x = 0; x < many; x++)
+            move(list[kPlanThreads - 1 - x], tid, kPlanThreads);
+        for (int x = U * w; x < n; x += U * WAVES) {
+            PlanMove m[U];
+            int v[U], count[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                m[u] = list[min(x + u, n - 1)];
+                count[u] = x + u < n ? blocks(m[u]) : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (lane < count[u])
+                    v[u] = *source(m[u], lane);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (lane < count[u])
+                    *target(m[u], lane) = v[u];
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (count[u] > 64)
+                    move(m[u], 64 + lane, 64);
         }
         __syncthreads();
-        if constexpr (!ONE) {   // (the next sequences' moves take its place)
-            if (tid == 0)
-                listed[which] = 0;
+        if constexpr (N != 1) {   // (the next sequences' moves take its place)
+            if (tid < 4)
+                listed[tid] = 0;
             __syncthreads();
         }
     };
 
     // what is released first: those that grow may take it
     if (total[2] > 0) {
-        for (int k = 0, at = add_sat(held, before[2]); k < per; k++) {   // (a list of a thread's k-th sequences)
+        int at = add_sat(held, before[2]);
+#pragma unroll N > 0 ? N : 1
+        for (int k = 0; k < per; k++) {   // (a list of the threads' k-th sequences)
             const int s = s0 + k;
             if (s < s1) {
-                const PlanSeq q = seq(s);
+                const PlanSeq q = seq(k);
                 if (q.drop() > 0 && at < max_free)
                     put(0, PlanMove{s, q.need, at, -q.drop()});
                 at = add_sat(at, q.drop());
@@ -211,10 +252,11 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
         }
     }
     int first = before[0], taken = before[1], most_taken = 0;
+#pragma unroll N > 0 ? N : 1
     for (int k = 0; k < per; k++) {
         const int s = s0 + k;
         if (s < s1) {
-            const PlanSeq q = seq(s);
+            const PlanSeq q = seq(k);
             const int upto = add_sat(taken, q.grow());
             const bool fine = q.grow() == 0 || upto <= there;
             if (fine && q.grow() > 0) {
@@ -223,14 +265,14 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
             }
             a.q_start[s] = first;
             a.seq_lens[s] = fine ? q.want : q.old;
-            if constexpr (ONE) {
+            if constexpr (N > 0) {
                 start[s] = first;
                 begin[s] = fine ? q.old : ~q.old;
             }
             first = add_sat(first, q.fresh());
             taken = upto;
         }
-        if (!ONE || total[1] > 0)
+        if (total[1] > 0)   // (uniform)
             work_off(1);
     }
 #pragma unroll
@@ -240,7 +282,7 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
         most[w] = most_taken;
     if (tid == 0) {
         a.q_start[a.n_seqs] = total[0];
-        if constexpr (ONE)
+        if constexpr (N > 0)
             start[a.n_seqs] = total[0];
     }
     __syncthreads();
@@ -253,7 +295,7 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
     if (!a.tokens_too)
         return;
     for (int t = tid; t < a.n_tokens; t += kPlanThreads) {
-        if constexpr (ONE) {
+        if constexpr (N > 0) {
             const int s = plan_find(start, a.n_seqs, t);
             if (s >= a.n_seqs) {
                 a.slots[t] = -1;
@@ -268,8 +310,11 @@ __device__ __forceinline__ void plan_body(const PlanArgs &a)
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_one_kernel(const PlanArgs a) { plan_body<true>(a); }
-__global__ __launch_bounds__(kPlanThreads) void plan_many_kernel(const PlanArgs a) { plan_body<false>(a); }
+template <int N>
+__global__ __launch_bounds__(kPlanThreads) void plan_all_kernel(const PlanArgs a)
+{
+    plan_body<N>(a);
+}
 
 __global__ __launch_bounds__(256) void plan_slots_kernel(const PlanArgs a)
 {
@@ -280,9 +325,11 @@ __global__ __launch_bounds__(256) void plan_slots_kernel(const PlanArgs a)
 
 }  // namespace
 
-const void *plan_kernel(bool one)
+const void *plan_kernel(int n_seqs)
 {
-    return one ? reinterpret_cast<const void *>(&plan_one_kernel) : reinterpret_cast<const void *>(&plan_many_kernel);
+    return n_seqs <= kPlanThreads       ? reinterpret_cast<const void *>(&plan_all_kernel<1>)
+           : n_seqs <= 4 * kPlanThreads ? reinterpret_cast<const void *>(&plan_all_kernel<4>)
+                                        : reinterpret_cast<const void *>(&plan_all_kernel<0>);
 }
 const void *plan_tokens_kernel() { return reinterpret_cast<const void *>(&plan_slots_kernel); }
 

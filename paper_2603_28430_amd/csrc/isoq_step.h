@@ -27,7 +27,7 @@ struct PlanArgs {
 // One workgroup of kPlanThreads; then, where it does not do that itself, slots and
 // positions: 256 threads, a token each.
 constexpr int kPlanThreads = 1024;
-const void *plan_kernel(bool one);   // one: up to kPlanThreads sequences
+const void *plan_kernel(int n_seqs);
 const void *plan_tokens_kernel();
 
 struct RopeArgs {

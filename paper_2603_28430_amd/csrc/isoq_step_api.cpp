@@ -74,7 +74,7 @@ isoq_status isoq_kv_plan(const int32_t *lens, const int32_t *new_lens, int n_seq
     a.tokens_too = n_tokens <= kPlanTokensHere;
     a.div_block = make_fastdiv((uint32_t)block_size);
     void *args[] = {&a};
-    const isoq_status st = launch_lds(plan_kernel(n_seqs <= kPlanThreads), dim3(1), kPlanThreads, args, 0, stream);
+    const isoq_status st = launch_lds(plan_kernel(n_seqs), dim3(1), kPlanThreads, args, 0, stream);
     if (st != ISOQ_OK || a.tokens_too)
         return st;
     return launch_lds(plan_tokens_kernel(), dim3((unsigned)((n_tokens + 255) / 256)), 256, args, 0, stream);
