@@ -466,12 +466,13 @@ isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int
  *   prefix_table, prefix_lens  device, int32 [n_prefixes][max_prefix_blocks] and
  *               [n_prefixes]: the prefixes' blocks and lengths, as block_table and
  *               seq_lens (the same cache and block_size).
- *   max_prefix_tokens  tokens of all sequences of one prefix at most (n_tokens if the
- *               host does not know); a prefix's tokens from there on are left as they
- *               were in out and lse.  max_prefix_len: positions of the longest prefix at
- *               most (max_prefix_blocks * block_size if it does not know).
+ *   max_prefix_tokens  tokens of all sequences of one prefix at most, 1 or more (n_tokens
+ *               if the host does not know); a prefix's tokens from there on are left as
+ *               they were in out and lse.  max_prefix_len: positions of the longest prefix
+ *               at most (max_prefix_blocks * block_size if it does not know).  Where that,
+ *               max_prefix_blocks or n_blocks is 0 the call is isoq_kv_attn's.
  *   workspace   at least isoq_kv_attn_prefix_workspace(...) bytes.
- * n_prefixes <= 65535; max_prefix_tokens (or n_tokens) * n_q_heads <= 2^23.
+ * n_prefixes <= 65535; max_prefix_tokens (or n_tokens, if fewer) * n_q_heads <= 2^23.
  * Everything else as isoq_kv_attn.
  */
 isoq_status isoq_kv_attn_prefix(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
@@ -576,7 +577,8 @@ isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const 
  *               past n_tokens are left out, though lengths and blocks count them.
  *   n_free_out  device, int32 [1]: free blocks left (may be n_free itself).
  * Other buffers must not overlap.  Limits: n_seqs <= 65535, (max_blocks_per_seq + 1) *
- * block_size < 2^31, max_free and n_tokens < 2^31.
+ * block_size < 2^31, max_free, n_tokens and the new tokens of a step < 2^31 (q_start
+ * stays at 2^31 - 1 past them).
  */
 isoq_status isoq_kv_plan(const int32_t *lens, const int32_t *new_lens, int n_seqs, int32_t *block_table,
                          int max_blocks_per_seq, int block_size, int32_t *free_blocks, int64_t max_free,

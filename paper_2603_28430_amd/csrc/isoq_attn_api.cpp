@@ -381,7 +381,7 @@ AttnPlans attn_plans(const AttnCall &c)
 isoq_status check_prefix(const AttnCall &c)
 {
     if (c.n_prefixes < 0 || c.max_prefix_blocks < 0 || c.max_prefix_len < 0 || c.max_prefix_tokens < 0 ||
-        (!c.prefix_start && c.n_prefixes > 1))
+        (c.n_prefixes > 0 && c.max_prefix_tokens == 0 && c.n_tokens > 0) || (!c.prefix_start && c.n_prefixes > 1))
         return ISOQ_E_INVALID;
     if (c.n_prefixes > 65535 || (int64_t)c.max_prefix_blocks * c.block_size > kAttnMaxPos ||
         c.max_prefix_tokens > kAttnMaxRows / c.n_q_heads)
@@ -393,6 +393,7 @@ isoq_status attn_call(AttnCall c)
 {
     isoq_status st = check_attn(c.pk, c.pv, c.dtype, c.n_tokens, c.max_q_len, c.n_seqs, c.n_q_heads, c.n_kv_heads,
                                 c.block_size, c.max_blocks, c.max_len);
+    c.max_prefix_tokens = std::min(c.max_prefix_tokens, c.n_tokens);
     if (st == ISOQ_OK)
         st = check_prefix(c);
     if (st != ISOQ_OK)
@@ -402,11 +403,12 @@ isoq_status attn_call(AttnCall c)
         return ISOQ_E_INVALID;
     if (c.n_tokens == 0 || c.n_seqs == 0)
         return ISOQ_OK;
-    c.max_prefix_tokens = std::min(c.max_prefix_tokens, c.n_tokens);
-    if (c.n_blocks == 0)
-        c.n_prefixes = 0;
     const bool no_keys = c.n_blocks == 0 || c.max_blocks == 0 || c.max_len == 0;
-    const AttnPlans plans = attn_plans(c);
+    AttnPlans plans = attn_plans(c);
+    if (c.n_blocks == 0 && (plans.prefix || plans.ahead)) {   // (less than isoq_kv_attn_prefix_workspace says)
+        plans.prefix = plans.ahead = false;
+        plans.bytes = plan_bytes(plans.own, c.n_tokens, c.n_q_heads);
+    }
     if (!c.q || !c.out || !c.seq_lens || (!no_keys && !c.block_table) ||
         ((plans.prefix || plans.ahead) && (!c.prefix_table || !c.prefix_lens)) ||
         ((!no_keys || plans.prefix || plans.ahead) && (!c.k_idx || !c.k_rho || !c.v_idx || !c.v_rho)))

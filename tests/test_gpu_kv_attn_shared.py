@@ -203,6 +203,24 @@ def test_no_prefix_is_isoq_kv_attn():
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
 
 
+@pytest.mark.parametrize("wide", [False, True])
+def test_bounds_of_tokens_and_an_empty_cache(wide):
+    """No tokens of a prefix are refused (they would be left out), more than there are are as many as there are; a
+    cache without blocks gives 0 and -inf, with the workspace that the call asks for."""
+    w, args, out, lse = prefix_case("full", 128, 3, "f16", [1] * 5, 4, 2, 16, [100, 0, 70, 9, 40], [200, 40], [3, 1], seed=2)
+    if wide:
+        args["prefix_table"] = widen(args["prefix_table"], 16)
+    for most in (0, -1):
+        with pytest.raises(iq.IsoqError):
+            iq.isoq_kv_attn_prefix(**dict(args, max_prefix_tokens=most))
+    a, b = (iq.isoq_kv_attn_prefix(**dict(args, max_prefix_tokens=most)) for most in (2 ** 40, 5))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    none = {x: args[x][:0] for x in ("k_idx", "k_rho", "v_idx", "v_rho")}
+    for kw in ({}, dict(block_table=widen(args["block_table"], 16))):
+        got = iq.isoq_kv_attn_prefix(**dict(args, **none, **kw))
+        assert (got[0] == 0).all() and (got[1] == -float("inf")).all()
+
+
 def test_empty_rows_whatever_the_query_holds():
     """Neither prefix nor own positions: out 0 and lse -inf, also of a query that is no number; with a position, NaN."""
     w, args, out, lse = prefix_case("full", 128, 3, "f16", [1] * 4, 4, 2, 16, [0, 0, 3, 0], [0, 20], [3, 1], seed=5)
