@@ -47,6 +47,9 @@ struct AttnArgs {
     // prefix p of the sequences pre_start[p] .. pre_start[p + 1] - 1 (null: of all)
     int32_t n_pre, n_seqs, pre_blocks, pre_tokens, pre_cap;
     const int32_t *pre_start, *pre_table, *pre_lens;
+    // or (fold > 0) ones that an earlier launch attended to, in fold splits of pre_chunk positions
+    // at most, which are the parts: the kernel adds them to its rows (isoq_attn_m.h)
+    int32_t fold, pre_chunk, pre_even;
     float scale;                 // times log2(e)
     FastDiv div_block;
     int32_t d, width, slots;     // coordinates per row, padded width, its rotation slots (8 coordinates for 8-D, else 4)

@@ -311,6 +311,7 @@ isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, in
 struct AttnPlans {
     AttnPlan own, pre;
     bool prefix;   // in launches and parts of their own
+    bool fold;     // which the kernel of the own positions, in one split, adds itself
     bool ahead;    // before each sequence's own positions, in one launch (own is the plan of both)
     size_t bytes;
     bool ok;   // (false: no memory for a handle's tables)
@@ -374,7 +375,9 @@ AttnPlans attn_plans(const AttnCall &c)
         p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
         return p;
     }
-    p.bytes = sizeof(float) * (size_t)c.n_tokens * c.n_q_heads * (p.own.n_splits + p.pre.n_splits) * (p.own.width + 2);
+    p.fold = p.own.kern.fn && !p.own.join;
+    p.bytes = sizeof(float) * (size_t)c.n_tokens * c.n_q_heads * ((p.fold ? 0 : p.own.n_splits) + p.pre.n_splits) *
+              (p.own.width + 2);
     return p;
 }
 
@@ -406,7 +409,7 @@ isoq_status attn_call(AttnCall c)
     const bool no_keys = c.n_blocks == 0 || c.max_blocks == 0 || c.max_len == 0;
     AttnPlans plans = attn_plans(c);
     if (c.n_blocks == 0 && (plans.prefix || plans.ahead)) {   // (less than isoq_kv_attn_prefix_workspace says)
-        plans.prefix = plans.ahead = false;
+        plans.prefix = plans.ahead = plans.fold = false;
         plans.bytes = plan_bytes(plans.own, c.n_tokens, c.n_q_heads);
     }
     if (!c.q || !c.out || !c.seq_lens || (!no_keys && !c.block_table) ||
@@ -433,7 +436,7 @@ isoq_status attn_call(AttnCall c)
     AttnArgs a = attn_args(c, plan, scale2);
     if (no_keys)
         a.cap = 0;
-    if (plans.ahead) {
+    if (plans.ahead || plans.fold) {
         a.n_pre = c.n_prefixes;
         a.pre_blocks = c.max_prefix_blocks;
         a.pre_tokens = (int32_t)c.max_prefix_tokens;
@@ -443,7 +446,12 @@ isoq_status attn_call(AttnCall c)
         a.pre_lens = c.prefix_lens;
     }
     if (plans.prefix)
-        a.part_splits += plans.pre.n_splits;
+        a.part_splits = (plans.fold ? 0 : a.n_splits) + plans.pre.n_splits;
+    if (plans.fold) {
+        a.fold = plans.pre.n_splits;
+        a.pre_chunk = plans.pre.chunk;
+        a.pre_even = plans.pre.kern.parts;
+    }
     if (need) {
         a.part = static_cast<float *>(c.workspace);
         a.part_ml = a.part + (size_t)c.n_tokens * c.n_q_heads * a.part_splits * plan.width;
@@ -463,7 +471,7 @@ isoq_status attn_call(AttnCall c)
         b.part = a.part;
         b.part_ml = a.part_ml;
         b.part_splits = a.part_splits;
-        b.part_first = a.n_splits;
+        b.part_first = plans.fold ? 0 : a.n_splits;
         p = AttnPrefix{c.prefix_start, c.prefix_lens, c.n_prefixes, c.n_seqs, (int32_t)c.max_prefix_tokens,
                        b.cap, b.chunk, b.n_splits, b.even};
         st = launch_attn(shared, plans.pre, b, c.n_prefixes);
@@ -471,7 +479,7 @@ isoq_status attn_call(AttnCall c)
             return st;
     }
     st = launch_attn(c, plan, a, c.n_seqs);
-    if (st != ISOQ_OK || need == 0)
+    if (st != ISOQ_OK || need == 0 || plans.fold)
         return st;
     const bool few = a.part_splits <= kAttnJoinFew;
     const unsigned rows = (unsigned)c.n_q_heads * (unsigned)c.max_q_len, per = few ? 256 / plan.slots : 1;

@@ -9,6 +9,29 @@
 namespace isoq {
 namespace {
 
+// Positions per split of a sequence: a.chunk, which the longest possible one needs, or
+// (even) what cuts its own length into n_splits equal parts.  Equal parts keep
+// the workgroups of a few sequences of many rows busy to the end (two ragged
+// chunks of up to 512 tokens and 8,192 positions 185 us instead of 194, mean of six;
+// four of 128 and 4,096 88 instead of 98); with one to eight rows a key head they changed
+// nothing where the block table is as wide as the longest sequence (16 ragged sequences
+// of up to 8,192 positions 44 and 44 us, of others 36 and 36).  Where it is wider and the
+// caller gives no max_len, a.chunk is longer than the sequences need (16 sequences of
+// 8,192 positions, 8 x 4 heads, a table of 131,072: 86 us instead of 42, one sequence 22
+// instead of 11): even parts were not measured there.
+__device__ __forceinline__ int attn_chunk(int len, int even, int cap, int n_splits, int chunk)
+{
+    if (!even)
+        return chunk;
+    const uint32_t l = (uint32_t)min(max(len, 0), cap), n = (uint32_t)n_splits;
+    return min(max(128, (int)((l + n - 1) / n + 63) & ~63), chunk);
+}
+
+__device__ __forceinline__ int splits_of(int positions, int chunk)
+{
+    return (int)(((uint32_t)positions + (uint32_t)chunk - 1u) / (uint32_t)chunk);
+}
+
 // The prefix that sequence s has of `n` (start[p] .. start[p + 1] - 1 share prefix p;
 // start null: all share one), or none, and the first of its tokens.
 struct PrefixOf {
@@ -41,6 +64,7 @@ __device__ __forceinline__ PrefixOf prefix_of(const AttnArgs &a, const int32_t *
 struct AttnSeq {
     int first, n, rows, len, full;
     int base, prefix;   // positions of its prefix that come first, which prefix (0: none, or the first)
+    int folded;         // splits of its prefix to be added
     // Positions that token i attends to: all, or those up to its own, the newest
     // token being the last position.
     __device__ __forceinline__ int limit(int i, int cap) const
@@ -52,7 +76,7 @@ struct AttnSeq {
 
 __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 {
-    AttnSeq q{s, 1, 1, a.seq_lens[s], a.full, 0, 0};
+    AttnSeq q{s, 1, 1, a.seq_lens[s], a.full, 0, 0, 0};
     if (a.n_all > 0) {   // (clamped likewise)
         const int from = a.shared ? min(max(a.shared[s], 0), a.n_all) : 0;
         const int to = a.shared ? min(max(a.shared[s + 1], from), a.n_all) : a.n_all;
@@ -68,7 +92,11 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
         const PrefixOf p = prefix_of(a, a.pre_start, a.n_pre, a.n_seqs, s);
         if (p.any) {
             q.prefix = p.index;
-            q.base = min(max(a.pre_lens[p.index], 0), a.pre_cap);
+            const int len = min(max(a.pre_lens[p.index], 0), a.pre_cap);
+            if (a.fold > 0)
+                q.folded = splits_of(len, attn_chunk(len, a.pre_even, a.pre_cap, a.fold, a.pre_chunk));
+            else
+                q.base = len;
             q.rows = min(q.rows, max(a.pre_tokens - (q.first - p.token), 0));
         }
     }
@@ -90,24 +118,6 @@ __device__ __forceinline__ AttnEntry attn_entry(const AttnArgs &a, const AttnSeq
     }
     const uint32_t bi = fast_div(tt, a.div_block);
     return AttnEntry{table[bi], (int)(tt - bi * a.block_size)};
-}
-
-// Positions per split of a sequence: a.chunk, which the longest possible one needs, or
-// (even) what cuts its own length into n_splits equal parts.  Equal parts keep
-// the workgroups of a few sequences of many rows busy to the end (two ragged
-// chunks of up to 512 tokens and 8,192 positions 185 us instead of 194, mean of six;
-// four of 128 and 4,096 88 instead of 98); with one to eight rows a key head they changed
-// nothing where the block table is as wide as the longest sequence (16 ragged sequences
-// of up to 8,192 positions 44 and 44 us, of others 36 and 36).  Where it is wider and the
-// caller gives no max_len, a.chunk is longer than the sequences need (16 sequences of
-// 8,192 positions, 8 x 4 heads, a table of 131,072: 86 us instead of 42, one sequence 22
-// instead of 11): even parts were not measured there.
-__device__ __forceinline__ int attn_chunk(int len, int even, int cap, int n_splits, int chunk)
-{
-    if (!even)
-        return chunk;
-    const uint32_t l = (uint32_t)min(max(len, 0), cap), n = (uint32_t)n_splits;
-    return min(max(128, (int)((l + n - 1) / n + 63) & ~63), chunk);
 }
 
 __device__ __forceinline__ int attn_chunk(const AttnArgs &a, const AttnSeq &sq)

@@ -27,11 +27,6 @@ struct RowSplits {
 };
 // (without a prefix jump is 0, and place() waits for no length)
 
-__device__ __forceinline__ int splits_of(int positions, int chunk)
-{
-    return (int)(((uint32_t)positions + (uint32_t)chunk - 1u) / (uint32_t)chunk);
-}
-
 // The splits that have positions of token i of sequence s (all = -1: the row is left
 // as it is).
 template <bool PREFIX>
