@@ -354,8 +354,8 @@ AttnPlans attn_plans(const AttnCall &c)
     p.prefix = c.n_prefixes > 0 && c.max_prefix_blocks > 0 && c.max_prefix_len > 0 && c.max_prefix_tokens > 0;
     const bool tables = pk->attn_by_tables && c.pv->attn_by_tables;
     const int most = p.prefix ? kAttnMaxSplits / 2 : kAttnMaxSplits;   // (a row's join takes both kinds)
+    const int64_t own = std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size);
     if (p.prefix) {
-        const int64_t own = std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size);
         const int64_t shared = std::min<int64_t>(c.max_prefix_len, (int64_t)c.max_prefix_blocks * c.block_size);
         p.pre = attn_plan(pk, c.pv, c.dtype, c.n_prefixes, (int)c.max_prefix_tokens, c.n_q_heads, c.n_kv_heads, shared,
                           false, most);
@@ -368,8 +368,17 @@ AttnPlans attn_plans(const AttnCall &c)
             return p;
         }
     }
-    p.own = attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads,
-                      std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size), false, most);
+    auto plan_own = [&](int splits) {
+        return attn_plan(pk, c.pv, c.dtype, c.n_seqs, c.max_q_len, c.n_q_heads, c.n_kv_heads, own, false, splits);
+    };
+    p.own = plan_own(most);
+    // (One split, whose kernel needs no join, where that leaves two workgroups a compute unit and
+    // few tiles a wave: us in splits / in one, behind 8,000 positions, 64 x 8 x 4 heads, up to
+    // 1,000 positions of their own 70 / 61, 2,000 78 / 75, 4,000 98 / 102, fp32, 1,500 114 /
+    // 112; 32 x 8 x 4 behind 30,000, 1,000 74 / 72, 2,000 79 / 82; 16 x 4 x 8, 1,000 97 / 113.)
+    if (p.prefix && p.own.kern.fn && !p.own.kern.parts && p.own.n_splits > 1 && own <= 2048 &&
+        p.own.groups * c.n_seqs >= 512)
+        p.own = plan_own(1);
     p.ok = !tables || (p.own.kern.fn && (!p.prefix || p.pre.kern.fn));
     if (!p.prefix) {
         p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
