@@ -331,20 +331,23 @@ double tile_cost(const AttnPlan &p, int64_t rows)
 
 // Whether the prefix is read anew by every sequence, in front of its own positions, in
 // one launch: `ahead` of both together, against `pre` of the prefix for all its rows
-// together (a launch, parts and a join of its own).  Where the products differ by less
-// than 10 to 20 us of work.  (us, shared / ahead, sequences of 100 positions of their own
-// behind one prefix: 8 x 4 heads, d = 128, fp16: 16 of 2,000 32 / 21, of 8,000 37 / 38, 32
-// 36 / 25, 47 / 58, 64 48 / 39, 63 / 103; 5 tokens each: 4 of 8,000 39 / 41, 16 of 2,000 50 /
-// 37, 64 78 / 93; fp32: 32 of 8,000 67 / 60, 64 102 / 108; 8 x 1, d = 64: 16 of 2,000 17 / 16,
-// of 8,000 19 / 28; 4 x 5, d = 96, fp32, 5 tokens: 16 of 2,000 31 / 31, of 8,000 59 / 73.)
+// together (a launch and parts of its own).  Where the products differ by less than the
+// further launch and the parts take, 4 us by digits and 13 and more in fp16, a unit of
+// work being 22 us in a million, in fp16 half of that.  (us, shared / ahead, behind one
+// prefix, 100 positions of their own: 8 x 4 heads, d = 128, fp16: 16 sequences of 2,000 28
+// / 20, of 8,000 31 / 38, 32 of 2,000 30 / 24, of 4,000 31 / 36, 64 of 1,000 37 / 25, of
+// 2,000 38 / 36, of 4,000 40 / 57; 5 tokens each: 8 of 2,000 31 / 23, 16 40 / 35, 64 56 / 93, 4 of
+// 8,000 33 / 39; fp32: 4 of 2,000 15 / 13, 32 23 / 24, 64 35 / 38, of 4,000 52 / 59; 8 x 1, d =
+// 64: 16 of 2,000 13 / 15, 64 23 / 28; 4 x 5, d = 96, fp32, 5 tokens: 16 of 2,000 31 / 30, of 4,000
+// 41 / 44, of 8,000 57 / 72; d = 256, 2 x 4: 16 of 8,000 31 / 27, 64 of 4,000 37 / 39.)
 bool prefix_ahead(const AttnCall &c, const AttnPlan &ahead, const AttnPlan &pre)
 {
     const int64_t group = c.n_q_heads / c.n_kv_heads;
     const double tiles = (double)pre.max_pos * c.n_kv_heads;
     const double anew = tiles * c.n_seqs * tile_cost(ahead, group * c.max_q_len);
     const double once = tiles * c.n_prefixes * tile_cost(pre, group * c.max_prefix_tokens);
-    return ahead.max_pos <= kAttnMaxPos &&
-           anew <= once + (pre.kern.parts ? 0.75e6 : 0.5e6) + 60.0 * (double)c.n_tokens * c.n_q_heads;
+    const double rows = (double)c.n_tokens * c.n_q_heads;
+    return ahead.max_pos <= kAttnMaxPos && anew <= (pre.kern.parts ? 0.5 * once + 0.6e6 + 130.0 * rows : once + 0.2e6);
 }
 
 AttnPlans attn_plans(const AttnCall &c)
