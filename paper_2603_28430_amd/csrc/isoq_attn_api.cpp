@@ -110,9 +110,12 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // 22; 16 ragged x 8 x 4 of 5 tokens, mean of three 47 / 38 / 38; 4 ragged x 2 x 16, up
     // to 20,000 20 / 23 / 23; 8 ragged x 4 x 4 of 5 tokens, fp32 23 / 23 / 27.  Of 12: 8 x
     // 8 heads, 4,096 23 / 28 / 28, 8 ragged x 8, up to 8,000 34 / 35 / 35.)
+    // (Of 4, ragged, at 1,024 / 1,280 / 1,536: 16 x 16 heads, up to 1,500 17.5 / 17.5 / 19.1,
+    // 32 x 8 x 4 18.3 / 18.1 / 20.2, fp32 18.2 / 18.3 / 20.1; 32 x 8 x 4 of up to 8,000 54 / 52 / 48,
+    // 8 x 32, up to 32,768 160 / 159 / 140.)
     const int64_t want = p.kern.parts                                          ? (p.kern.rows > 128 ? 256 : pk->d <= 64 ? 768 : 512)
                          : n_seqs == 1 || pk->d > 128 || p.kern.rows == 12     ? 768
-                         : p.kern.rows == 8                                    ? 1280
+                         : p.kern.rows == 8 || p.max_pos <= 2048               ? 1280
                                                                                : 1536;
     const int64_t blocks = p.groups * n_seqs;
     // In fp16 as many splits as fit one round, down to 128 positions each up to 768 and
