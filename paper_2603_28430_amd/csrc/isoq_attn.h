@@ -63,15 +63,15 @@ struct AttnArgs {
 constexpr int kAttnMaxSplits = 256;
 
 // Width-generic kernel: one row per workgroup, grid (query head + n_q_heads
-// token, sequence, split).
-const void *attn_generic_kernel_for(int variant, int bits);
+// token, sequence, split).  (pre, here and below: for launches with n_pre > 0.)
+const void *attn_generic_kernel_for(int variant, int bits, bool pre);
 size_t attn_generic_lds(int slots, int variant);
 // Matrix-core kernel (isoq_attn_m.h; widths of the tuned decoding kernels) for
 // `rows` rows per sequence and key head: its entry, its dynamic LDS, and the
 // rows that a workgroup takes.  Grid (key head + n_kv_heads row tile,
 // sequence, split).
 struct AttnKernel {
-    const void *fn;
+    const void *fn, *fn_pre;   // fn_pre: of launches with n_pre > 0 (kernel of many rows: none)
     size_t lds;
     int rows;
     bool parts;   // the kernel of many rows
@@ -87,7 +87,7 @@ AttnKernel attn_c_kernel_for(int d, int bits, int rest, int rows);
 // a sequence / (256 / slots), sequence), more (row, sequence); a row being query
 // head + n_q_heads token.
 constexpr int kAttnJoinFew = 8;
-const void *attn_join_kernel_for(int variant, bool few);
+const void *attn_join_kernel_for(int variant, bool few, bool pre);
 
 // Attention behind shared prefixes (isoq_kv_attn_prefix): the prefixes' splits, which
 // follow the sequences' own in part, for the join (its second argument).

@@ -296,7 +296,10 @@ AttnArgs attn_args(const AttnCall &c, const AttnPlan &plan, float scale2)
 isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, int n_seqs)
 {
     void *args[] = {&a};
-    const void *fn = plan.kern.fn ? plan.kern.fn : attn_generic_kernel_for(c.pk->variant, c.pk->bits);
+    const bool pre = a.n_pre > 0;
+    const void *fn = !plan.kern.fn ? attn_generic_kernel_for(c.pk->variant, c.pk->bits, pre)
+                     : pre         ? plan.kern.fn_pre
+                                   : plan.kern.fn;
     const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, c.pk->variant);
     if (!fn)
         return ISOQ_E_UNSUPPORTED;
@@ -499,7 +502,8 @@ isoq_status attn_call(AttnCall c)
     const bool few = a.part_splits <= kAttnJoinFew;
     const unsigned rows = (unsigned)c.n_q_heads * (unsigned)c.max_q_len, per = few ? 256 / plan.slots : 1;
     void *args[] = {&a, &p};
-    const void *join = plans.prefix ? attn_prefix_join_kernel_for(c.pk->variant, few) : attn_join_kernel_for(c.pk->variant, few);
+    const void *join = plans.prefix ? attn_prefix_join_kernel_for(c.pk->variant, few)
+                                    : attn_join_kernel_for(c.pk->variant, few, plans.ahead);
     return launch_lds(join, dim3((rows + per - 1) / per, (unsigned)c.n_seqs), 256, args, 0, c.stream);
 }
 

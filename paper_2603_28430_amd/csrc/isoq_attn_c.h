@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : D <= 64 ? 3 : 2) void attn_
     const int s = blockIdx.y;
     const int lane = threadIdx.x & 63, n32 = lane & 31, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnSeq sq = attn_seq(a, s);
+    const AttnSeq sq = attn_seq<false>(a, s);
     const int r0 = rt * C::ROWS, total = sq.rows * a.group;
     if (r0 >= total)   // (block-uniform, as every early return here)
         return;

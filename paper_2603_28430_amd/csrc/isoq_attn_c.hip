@@ -9,7 +9,7 @@ template <int D, int BITS, int REST, int W>
 AttnKernel attn_c_entry()
 {
     using C = AttnCShape<D, BITS, REST, W>;
-    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, REST, W>), (size_t)C::lds_bytes(), C::ROWS, true, 64 * W};
+    return {reinterpret_cast<const void *>(&attn_c_kernel<D, BITS, REST, W>), nullptr, (size_t)C::lds_bytes(), C::ROWS, true, 64 * W};
 }
 
 template <int D, int REST, int W>

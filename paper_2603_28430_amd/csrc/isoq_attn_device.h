@@ -74,6 +74,9 @@ struct AttnSeq {
     }
 };
 
+// (PRE: launches with n_pre > 0, whose kernels are instantiations of their own: what they ask
+// for took the others 1 to 2%)
+template <bool PRE>
 __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
 {
     AttnSeq q{s, 1, 1, a.seq_lens[s], a.full, 0, 0, 0};
@@ -88,7 +91,7 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int s)
         q.n = min(max(a.q_start[s + 1], q.first), a.n_tokens) - q.first;
         q.rows = min(q.n, a.max_q_len);
     }
-    if (a.n_pre > 0) {
+    if constexpr (PRE) {
         const PrefixOf p = prefix_of(a, a.pre_start, a.n_pre, a.n_seqs, s);
         if (p.any) {
             q.prefix = p.index;
@@ -108,10 +111,11 @@ struct AttnEntry {
     int32_t blk, pos;   // cache block and position in it
 };
 
+template <bool PRE>
 __device__ __forceinline__ AttnEntry attn_entry(const AttnArgs &a, const AttnSeq &sq, const int32_t *table, int t)
 {
     uint32_t tt = (uint32_t)min(t, a.cap - 1);
-    if (a.n_pre > 0) {
+    if constexpr (PRE) {
         const bool own = t >= sq.base && a.cap > 0;
         tt = (uint32_t)(own ? min(t - sq.base, a.cap - 1) : min(t, a.pre_cap - 1));
         table = own ? table : a.pre_table + (int64_t)sq.prefix * a.pre_blocks;

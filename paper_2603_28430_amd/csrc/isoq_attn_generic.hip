@@ -16,7 +16,7 @@
 namespace isoq {
 namespace {
 
-template <int VAR, int BITS>
+template <int VAR, int BITS, bool PRE>
 __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
 {
     constexpr int SW = kGenSW<VAR>;
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     const int s = blockIdx.y, tid = threadIdx.x;
     const int i = blockIdx.x / a.n_q_heads, hq = blockIdx.x - i * a.n_q_heads;
     const int h = hq / a.group;
-    const AttnSeq sq = attn_seq(a, s);
+    const AttnSeq sq = attn_seq<PRE>(a, s);
     if (i >= sq.rows)   // (block-uniform, as every early return here)
         return;
     const int64_t row = (int64_t)(sq.first + i) * a.n_q_heads + hq;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
         bool ok = false;
         int blk = 0, pos = 0;
         if (t < tend) {
-            const AttnEntry e = attn_entry(a, sq, table, (int)t);
+            const AttnEntry e = attn_entry<PRE>(a, sq, table, (int)t);
             blk = e.blk;
             pos = e.pos;
             ok = blk >= 0 && blk < a.n_blocks;
@@ -200,26 +200,26 @@ __global__ __launch_bounds__(256) void generic_attn_kernel(const AttnArgs a)
     }
 }
 
-template <int VAR>
+template <int VAR, bool PRE>
 const void *gen_attn_bits(int bits)
 {
     switch (bits) {
-    case 2: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 2>);
-    case 3: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 3>);
-    case 4: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 4>);
+    case 2: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 2, PRE>);
+    case 3: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 3, PRE>);
+    case 4: return reinterpret_cast<const void *>(&generic_attn_kernel<VAR, 4, PRE>);
     }
     return nullptr;
 }
 
 }  // namespace
 
-const void *attn_generic_kernel_for(int variant, int bits)
+const void *attn_generic_kernel_for(int variant, int bits, bool pre)
 {
     switch (variant) {
-    case VAR_FULL: return gen_attn_bits<VAR_FULL>(bits);
-    case VAR_FAST: return gen_attn_bits<VAR_FAST>(bits);
-    case VAR_PLANAR2D: return gen_attn_bits<VAR_PLANAR2D>(bits);
-    case VAR_BLOCK8: return gen_attn_bits<VAR_BLOCK8>(bits);
+    case VAR_FULL: return pre ? gen_attn_bits<VAR_FULL, true>(bits) : gen_attn_bits<VAR_FULL, false>(bits);
+    case VAR_FAST: return pre ? gen_attn_bits<VAR_FAST, true>(bits) : gen_attn_bits<VAR_FAST, false>(bits);
+    case VAR_PLANAR2D: return pre ? gen_attn_bits<VAR_PLANAR2D, true>(bits) : gen_attn_bits<VAR_PLANAR2D, false>(bits);
+    case VAR_BLOCK8: return pre ? gen_attn_bits<VAR_BLOCK8, true>(bits) : gen_attn_bits<VAR_BLOCK8, false>(bits);
     }
     return nullptr;
 }

@@ -50,7 +50,7 @@ __device__ __forceinline__ RowSplits row_splits(const AttnArgs &a, const AttnPre
     return r;
 }
 
-template <int VAR, bool PREFIX>
+template <int VAR, bool PREFIX, bool PRE>
 __device__ __forceinline__ void attn_join_row(const AttnArgs &a, const AttnPrefix &pre)
 {
     constexpr int SW = kGenSW<VAR>, AHEAD = 4;
@@ -58,7 +58,7 @@ __device__ __forceinline__ void attn_join_row(const AttnArgs &a, const AttnPrefi
     __shared__ float sum[256 * SW];
     static_assert(kAttnMaxSplits <= 256, "a split per lane");
     const int tid = threadIdx.x;
-    const AttnSeq sq = attn_seq(a, blockIdx.y);
+    const AttnSeq sq = attn_seq<PRE>(a, blockIdx.y);
     const int i = blockIdx.x / a.n_q_heads, hq = blockIdx.x - i * a.n_q_heads;
     if (i >= sq.rows)
         return;
@@ -145,11 +145,11 @@ __device__ __forceinline__ void attn_join_row(const AttnArgs &a, const AttnPrefi
         a.lse[row] = attn_lse(top, l);
 }
 
-template <int VAR, bool PREFIX>
+template <int VAR, bool PREFIX, bool PRE>
 __device__ __forceinline__ void attn_join_rows(const AttnArgs &a, const AttnPrefix &pre)
 {
     constexpr int SW = kGenSW<VAR>, N = kAttnJoinFew;
-    const AttnSeq sq = attn_seq(a, blockIdx.y);
+    const AttnSeq sq = attn_seq<PRE>(a, blockIdx.y);
     const int g = threadIdx.x / a.slots, j = threadIdx.x - g * a.slots, per = 256 / a.slots;
     const int r = blockIdx.x * per + g, i = r / a.n_q_heads, hq = r - i * a.n_q_heads;
     if (g >= per || i >= sq.rows)
@@ -195,54 +195,65 @@ __device__ __forceinline__ void attn_join_rows(const AttnArgs &a, const AttnPref
         a.lse[row] = attn_lse(top, l);
 }
 
-template <int VAR>
+template <int VAR, bool PRE>
 __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a)
 {
-    attn_join_row<VAR, false>(a, AttnPrefix{});
+    attn_join_row<VAR, false, PRE>(a, AttnPrefix{});
 }
 
-template <int VAR>
+template <int VAR, bool PRE>
 __global__ __launch_bounds__(256) void attn_join_few_kernel(const AttnArgs a)
 {
-    attn_join_rows<VAR, false>(a, AttnPrefix{});
+    attn_join_rows<VAR, false, PRE>(a, AttnPrefix{});
 }
 
 template <int VAR>
 __global__ __launch_bounds__(256) void attn_prefix_join_kernel(const AttnArgs a, const AttnPrefix p)
 {
-    attn_join_row<VAR, true>(a, p);
+    attn_join_row<VAR, true, false>(a, p);
 }
 
 template <int VAR>
 __global__ __launch_bounds__(256) void attn_prefix_join_few_kernel(const AttnArgs a, const AttnPrefix p)
 {
-    attn_join_rows<VAR, true>(a, p);
+    attn_join_rows<VAR, true, false>(a, p);
 }
+
+// Splits of the sequences' own positions (kOwn), with a prefix ahead of them (kAhead), and of
+// both (kBoth).
+enum JoinOf { kOwn, kAhead, kBoth };
 
 template <int VAR>
-const void *join_kernel(bool prefix, bool few)
+const void *join_kernel(JoinOf of, bool few)
 {
-    if (prefix)
+    switch (of) {
+    case kOwn:
+        return few ? reinterpret_cast<const void *>(&attn_join_few_kernel<VAR, false>)
+                   : reinterpret_cast<const void *>(&attn_join_kernel<VAR, false>);
+    case kAhead:
+        return few ? reinterpret_cast<const void *>(&attn_join_few_kernel<VAR, true>)
+                   : reinterpret_cast<const void *>(&attn_join_kernel<VAR, true>);
+    case kBoth:
         return few ? reinterpret_cast<const void *>(&attn_prefix_join_few_kernel<VAR>)
                    : reinterpret_cast<const void *>(&attn_prefix_join_kernel<VAR>);
-    return few ? reinterpret_cast<const void *>(&attn_join_few_kernel<VAR>)
-               : reinterpret_cast<const void *>(&attn_join_kernel<VAR>);
+    }
+    return nullptr;
 }
 
-const void *join_of(int variant, bool prefix, bool few)
+const void *join_of(int variant, JoinOf of, bool few)
 {
     switch (variant) {
-    case VAR_FULL: return join_kernel<VAR_FULL>(prefix, few);
-    case VAR_FAST: return join_kernel<VAR_FAST>(prefix, few);
-    case VAR_PLANAR2D: return join_kernel<VAR_PLANAR2D>(prefix, few);
-    case VAR_BLOCK8: return join_kernel<VAR_BLOCK8>(prefix, few);
+    case VAR_FULL: return join_kernel<VAR_FULL>(of, few);
+    case VAR_FAST: return join_kernel<VAR_FAST>(of, few);
+    case VAR_PLANAR2D: return join_kernel<VAR_PLANAR2D>(of, few);
+    case VAR_BLOCK8: return join_kernel<VAR_BLOCK8>(of, few);
     }
     return nullptr;
 }
 
 }  // namespace
 
-const void *attn_join_kernel_for(int variant, bool few) { return join_of(variant, false, few); }
-const void *attn_prefix_join_kernel_for(int variant, bool few) { return join_of(variant, true, few); }
+const void *attn_join_kernel_for(int variant, bool few, bool pre) { return join_of(variant, pre ? kAhead : kOwn, few); }
+const void *attn_prefix_join_kernel_for(int variant, bool few) { return join_of(variant, kBoth, few); }
 
 }  // namespace isoq

@@ -278,7 +278,7 @@ __device__ __forceinline__ void position_selectors(const uint32_t x[4], uint32_t
     plane_selectors<BITS, N>(b, sel);
 }
 
-template <int D, int BITS, int NT, int VD>
+template <int D, int BITS, int NT, int VD, bool PRE>
 __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 {
     using H = AttnMShape<D, BITS, NT>;
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     const int s = blockIdx.y;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnSeq sq = attn_seq(a, s);
+    const AttnSeq sq = attn_seq<PRE>(a, s);
     const int r0 = rt * ROWS, total = sq.rows * a.group;   // rows of the sequence's key head
     if (r0 >= total)   // (block-uniform, as every early return here)
         return;
@@ -322,10 +322,10 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     const int32_t *table = a.block_table + (int64_t)s * a.max_blocks;
     const int tw = t0 + 64 * w + lane;
     auto entry = [&](int b) {   // (positions past the last possible one: that one's)
-        return attn_entry(a, sq, table, (int)min((int64_t)tw + 64 * WV * (int64_t)b, (int64_t)0x7FFFFFFF));
+        return attn_entry<PRE>(a, sq, table, (int)min((int64_t)tw + 64 * WV * (int64_t)b, (int64_t)0x7FFFFFFF));
     };
     AttnEntry next{};
-    if (a.cap > 0 || a.n_pre > 0)
+    if (PRE || a.cap > 0)
         next = entry(0);
     __builtin_amdgcn_sched_barrier(0);
     // the positions that the rows attend to: rows come in the tokens' order, so
@@ -738,7 +738,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
     // (and the parts of the rows' prefix, which lie as the lanes' sums do: a wave adds every
     // WV-th.  64 sequences of 8 x 4 heads with 32 parts a row, d = 128: 4.2 us more, a join
     // 9.8)
-    if (sq.folded > 0) {   // (uniform)
+    if (PRE && sq.folded > 0) {   // (uniform)
         constexpr int U = CL <= 8 ? 4 : CL <= 16 ? 2 : 1;
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -806,7 +806,7 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
                 y[c] = fmaf(f, part[(x * ROWS + r) * D + 8 * j + c], y[c]);
         }
     };
-    if (a.part && a.fold == 0) {
+    if (a.part && !(PRE && a.fold > 0)) {
         __syncthreads();
         if (r >= n)
             return;

@@ -9,13 +9,19 @@
 namespace isoq {
 namespace {
 
+template <int D, int BITS, int NT, bool PRE>
+const void *attn_m_entry_of(bool f16)
+{
+    return f16 ? reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 2, PRE>)
+               : reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 3, PRE>);
+}
+
 template <int D, int BITS, int NT>
 AttnKernel attn_m_entry(bool f16)
 {
     const size_t lds = sizeof(uint32_t) * AttnMShape<D, BITS, NT>::lds_words();
-    return {f16 ? reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 2>)
-                : reinterpret_cast<const void *>(&attn_m_kernel<D, BITS, NT, 3>),
-            lds, 4 * NT, false, 64 * AttnMShape<D, BITS, NT>::WV};
+    return {attn_m_entry_of<D, BITS, NT, false>(f16), attn_m_entry_of<D, BITS, NT, true>(f16), lds, 4 * NT, false,
+            64 * AttnMShape<D, BITS, NT>::WV};
 }
 
 // 4, 8 or 12 rows a workgroup.  A tile is decoded once for them, and the rest of
