@@ -106,6 +106,7 @@ AttnPlan attn_plan(const isoq_params *pk, const isoq_params *pv, int dtype, int 
     // of 1,024 tokens 103 / 102 / 112 / 111 / 110: one round of workgroups, which is
     // three a compute unit at d = 64 (512 / 768 / 1,024: two ragged chunks 138 / 126 / 137,
     // two equal ones 219 / 190 / 206, the 16 57 / 48 / 56).)
+    // (Those figures are of 128 rows a workgroup.  Of 256, one a compute unit: one round is 256.)
     // (Workgroups of 8 rows at 768 / 1,280 / 1,536: 8 x 8 heads, 4,096 positions 18 / 22 /
     // 22; 16 ragged x 8 x 4 of 5 tokens, mean of three 47 / 38 / 38; 4 ragged x 2 x 16, up
     // to 20,000 20 / 23 / 23; 8 ragged x 4 x 4 of 5 tokens, fp32 23 / 23 / 27.  Of 12: 8 x

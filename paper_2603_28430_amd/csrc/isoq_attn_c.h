@@ -3,8 +3,8 @@
 //
 // isoq_attn_m.h decodes a tile of 64 positions for 4 to 12 rows; with hundreds of
 // rows per key head that decoding is what it spends its time on.  Here a
-// workgroup has 128 rows, decodes each tile once into LDS, and multiplies in
-// fp16 with fp32 sums:
+// workgroup has 128 rows (W = 4 waves) or 256 (W = 8), decodes each tile once into
+// LDS, and multiplies in fp16 with fp32 sums:
 //   logits   the rotated query in two parts, x = hi + lo with hi = fp16(x) and lo
 //            = fp16(x - hi), its row in units of a power of two that brings its
 //            largest coordinate to 8 .. 16; the levels as fp16 numbers in units
@@ -22,17 +22,26 @@
 //            rounding them to fp16 alone takes; without it 2.9e-4 to 3.2e-4.
 // An e4m3 product is half a fp16 product's time: with both corrections in fp16, 2 x
 // 512 tokens at 8,192 positions, 3 bits, took 6% longer (with the query's lo in e4m3
-// too 6% less, and lse off by 1e-6 to 2e-6).
+// too 6% less, and lse off by 1e-6 to 2e-6; both, and 318 / 351 above, with 128 rows).
 //
 // What bounds it.  Two equal chunks (2 x 512 tokens at 8,192 positions, 8 x 4 heads)
-// take 307 to 333 us at 3 bits, 400 to 430 TFLOP/s of the definition's operations (4 d
-// a row and position), twice that of the matrix cores' own, and 364 to 376 once such
-// calls have followed each other for some ms and the clock has fallen; 351 to 394 and
-// 426 to 440 at 4 bits; 274 at 2 and 200 at d = 64.  Matrix cores are busy for 42% of the cycles, vector
-// instructions issue in 50%, waves wait for 28%: the two waves of a SIMD overlap the
-// two kinds little.  (A fifth fewer vector instructions, and all four waves fetching
-// records, changed nothing when tried.)  Ragged chunks of up to 512 tokens are bound
-// by what unequal sequences leave idle as well: 30%, 40%, 31%.
+// take 271 us at 3 bits, 490 TFLOP/s of the definition's operations (4 d a row and
+// position), twice that of the matrix cores' own, and 282 to 304 once such calls have
+// followed each other for some ms and the clock has fallen; 304 to 376 at 4 bits, 247 to
+// 298 at 2, 187 to 194 at d = 64.  (128 rows: 307 to 376, 351 to 440, 274, 200.)  256 rows at
+// 131,071 positions, 8 heads, take 271 to 313 (128 rows: 335).  Matrix cores are busy for 53%
+// of the cycles (128 rows: 42%), vector instructions issue in 53% (50%), waves wait for 25%
+// (28%): a tile of 64 positions takes the two waves of a SIMD 7,500 cycles, of which vector
+// instructions issue in 6,350 and matrix products in 4,096 (measured one by one).  Ragged
+// chunks of up to 512 tokens are bound by what unequal sequences leave idle as well (38%,
+// 43%, 29%), short contexts by 8 us of preparation (the queries' rotation, a chain of loads)
+// and 3 of storing the parts, before and after tiles of 3 us each.
+//
+// 256 rows.  A tile's decoding serves twice the rows, and a SIMD's two waves do
+// different things at a time: tiles are decoded one ahead, into the other of two
+// buffers, by the first four waves (values) after they have attended to the present
+// one, by the next four (keys) before.  (Keys and values read two tiles ahead, a third
+// wave to fetch, wave priorities, all waves decoding at once: no faster.)
 //
 // Layout (v_mfma_f32_32x32x16_f16).  S^T = K Q^T: a wave has 32 rows as columns,
 // lane 32 h + n the row n and the positions 8 b + 4 h + i (b, i = 0 .. 3) of each
@@ -41,11 +50,11 @@
 // are in the same order: [16 s][h][b][i].  K rows and V^T rows lie in LDS with
 // 16 bytes of padding (reads of 16 bytes by 16 rows touch every bank once).
 //
-// Decoding.  Wave c spreads chunk c (a quarter of the coordinates) of 64 keys;
+// Decoding.  Wave c (of four) spreads chunk c (a quarter of the coordinates) of 64 keys;
 // values are decoded four positions at a time (position_selectors), which
 // gives V^T's rows directly.  A level's two bytes are two v_perm_b32 for four
-// coordinates, two more put them together.  Waves 0 and 1 fetch the records of
-// the next tile (K, V) while all compute.
+// coordinates, two more put them together.  Two waves fetch the records of a later
+// tile (K, V) while all compute.
 #pragma once
 
 #include "isoq_attn_m.h"

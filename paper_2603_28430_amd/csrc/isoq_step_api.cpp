@@ -15,11 +15,16 @@ namespace {
 
 using namespace isoq;
 
-// Tokens up to which the one workgroup of the plan writes slots and positions too.
+// Tokens up to which the one workgroup of the plan writes slots and positions too (us by a
+// second launch / by itself: 512 single tokens 7.9 / 5.5, 2,048 11.7 / 9.7, 4,096 14.1 / 14.2, 8,192
+// 33 / 47; a prompt of 2,048 7.4 / 6.0, of 4,096 7.7 / 6.9, two of 4,096 8.1 / 9.1).
 constexpr int64_t kPlanTokensHere = 4096;
 
-// Waves up to which a token's rows are shared out.
-constexpr int64_t kRopeWaves = 8192;
+// Waves up to which a token's rows are shared out (us with one wave a token / up to 2,048 / 4,096 /
+// 8,192 / 16,384; d = 128, fp16, 40 heads: 32 tokens 6.7 / 4.1 / 4.1 / 4.1 / 4.1, 512 7.4 / 6.0 /
+// 5.7 / 5.7 / 5.7, 2,048 12.9 / 13.1 / 12.0 / 15.2 / 15.3, 4,096 17.9 / 18.0 / 18.1 / 20.1 / 25.9;
+// fp32, 72 heads: 1,000 20.9 / 16.5 / 15.7 / 16.8 / 19.2).
+constexpr int64_t kRopeWaves = 4096;
 
 constexpr double kTwoPi = 6.283185307179586476925;
 
