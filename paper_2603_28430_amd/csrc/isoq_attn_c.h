@@ -216,7 +216,13 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : D <= 64 ? 3 : 2) void attn_
     extern __shared__ __align__(16) uint32_t smem[];
     uint8_t *const lds = reinterpret_cast<uint8_t *>(smem);
 
-    const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads), rt = (int)(blockIdx.x / (uint32_t)a.n_kv_heads);
+    // (the sequences' first row tiles are not the same places of the grid: where most have no
+    // others, as single tokens next to a chunk, every 64th workgroup had work, and they went to
+    // one of an XCD's four shader engines, 15 such sequences and one of 512 tokens, 8 x 4 heads,
+    // 8,192 positions 1,062 us)
+    const uint32_t tiles = gridDim.x / (uint32_t)a.n_kv_heads;
+    const int hx = (int)(blockIdx.x % (uint32_t)a.n_kv_heads);
+    const int rt = (int)((blockIdx.x / (uint32_t)a.n_kv_heads + blockIdx.y + blockIdx.z) % tiles);
     const int h = (int)xcd_head((uint32_t)hx, (uint32_t)a.n_kv_heads, a.block_size * RB % 128 != 0);
     const int s = blockIdx.y;
     const int lane = threadIdx.x & 63, n32 = lane & 31, half = lane >> 5;
