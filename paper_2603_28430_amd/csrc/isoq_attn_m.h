@@ -278,8 +278,19 @@ __device__ __forceinline__ void position_selectors(const uint32_t x[4], uint32_t
     plane_selectors<BITS, N>(b, sel);
 }
 
+// Waves a SIMD that the registers are to allow, where the compiler alone takes a few more than
+// leave that number (with none to ten of them spilled).  (us left to the compiler / so, 8
+// sequences of 8,192 positions, 8 heads: 12 rows a head, fp16, d = 80, 2 bits 34 / 30, 3 bits 37 /
+// 32, d = 96, 2 bits 36 / 32; 8 rows, fp32, d = 128, 3 bits 34 / 32; 2 x 512 tokens, 8 x 4 heads,
+// fp32, 3 bits 1,070 / 971.)
+constexpr int attn_m_waves(int d, int bits, int nt, int vd)
+{
+    return nt == 2 ? (vd == 2 && d * bits <= 240 ? 4 : d * bits <= 384 && d <= 128 ? 3 : 1)
+                   : (nt == 3 && vd == 2 && d * bits <= 288 && d <= 96 ? 3 : 1);
+}
+
 template <int D, int BITS, int NT, int VD, bool PRE>
-__global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
+__global__ __launch_bounds__(256, attn_m_waves(D, BITS, NT, VD)) void attn_m_kernel(const AttnArgs a)
 {
     using H = AttnMShape<D, BITS, NT>;
     constexpr int WV = H::WV;
@@ -562,8 +573,12 @@ __global__ __launch_bounds__(256) void attn_m_kernel(const AttnArgs a)
 #pragma unroll
             for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
                 step(std::integral_constant<int, 4>{}, q0);
-            if constexpr (S::NQ % 4 != 0)
+            if constexpr (S::NQ % 4 != 0) {
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+                    digit_wait(d[nt]);
                 step(std::integral_constant<int, 2>{}, S::NQ - 2);
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {

@@ -204,18 +204,30 @@ __device__ __forceinline__ void transpose_rows(uint32_t &x0, uint32_t &x1, uint3
     x3 = d[1];
 }
 
-// acc += A B over one k-step of 4 quads, or of 2 and as many zeros.  (Both by the
-// instruction of K = 64: one of K = 32 that takes the sum of the other as its third
-// operand within 5 cycles of its issue reads what stood there before, which the
-// compiler does not know: attention at d = 96, 3 bits, 5 to 8 rows was off that way
-// in one schedule.  The matrix cores are not what bounds these kernels.)
+// acc += A B over one k-step of 4 quads, or of 2.
 template <int NS>
 __device__ __forceinline__ i32x4 digit_mfma(const uint32_t *a, const uint32_t *b, i32x4 acc)
 {
     static_assert(NS == 4 || NS == 2, "");
-    const i32x4 av = {(int)a[0], (int)a[1], NS == 4 ? (int)a[2 % NS] : 0, NS == 4 ? (int)a[3 % NS] : 0};
-    const i32x4 bv = {(int)b[0], (int)b[1], (int)b[2 % NS], (int)b[3 % NS]};
-    return __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, acc, 0, 0, 0);
+    if constexpr (NS == 4) {
+        const i32x4 av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3]};
+        const i32x4 bv = {(int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, acc, 0, 0, 0);
+    } else {
+        const uint64_t av = a[0] | (uint64_t)a[1] << 32, bv = b[0] | (uint64_t)b[1] << 32;
+        return __builtin_amdgcn_mfma_i32_16x16x32_i8((int64_t)av, (int64_t)bv, acc, 0, 0, 0);
+    }
+}
+
+// Between the steps of 4 that made the sums d and one of 2 that goes on with them: an
+// instruction of K = 32 that takes the sum of one of K = 64 as its third operand within 5
+// cycles of its issue, and writes another place, reads what stood there before, which the
+// compiler does not know (attention at d = 96, 3 bits, 5 to 8 rows was off that way in one
+// schedule).  8 cycles, which the sums pass through.  (A step of 2 with zeros to K = 64 takes
+// registers: d = 96, 4 bits, 8 rows, attention 34 us instead of 31, logits 20 instead of 18.)
+__device__ __forceinline__ void digit_wait(i32x4 *d)
+{
+    asm volatile("s_nop 7" : "+v"(d[0]), "+v"(d[1]), "+v"(d[2]));
 }
 
 // Whether a magnitude (its bits) is infinite or NaN.
@@ -770,8 +782,12 @@ __global__ __launch_bounds__(256) void score_m_kernel(const SMArgs a)
 #pragma unroll
                         for (int q0 = 0; q0 + 4 <= S::NQ; q0 += 4)
                             step(std::integral_constant<int, 4>{}, q0);
-                        if constexpr (S::NQ % 4 != 0)
+                        if constexpr (S::NQ % 4 != 0) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+                                digit_wait(acc[nt]);
                             step(std::integral_constant<int, 2>{}, S::NQ - 2);
+                        }
                         // one 16-key group's selectors and digits at a time
                         __builtin_amdgcn_sched_barrier(0);
                     }
