@@ -25,11 +25,11 @@
 // too 6% less, and lse off by 1e-6 to 2e-6; both, and 318 / 351 above, with 128 rows).
 //
 // What bounds it.  Two equal chunks (2 x 512 tokens at 8,192 positions, 8 x 4 heads)
-// take 271 us at 3 bits, 490 TFLOP/s of the definition's operations (4 d a row and
-// position), twice that of the matrix cores' own, and 282 to 304 once such calls have
-// followed each other for some ms and the clock has fallen; 304 to 376 at 4 bits, 247 to
-// 298 at 2, 187 to 194 at d = 64.  (128 rows: 307 to 376, 351 to 440, 274, 200.)  256 rows at
-// 131,071 positions, 8 heads, take 271 to 313 (128 rows: 335).  Matrix cores are busy for 53%
+// take 266 us at 3 bits, 500 TFLOP/s of the definition's operations (4 d a row and
+// position), twice that of the matrix cores' own, and 280 to 301 once such calls have
+// followed each other for some ms and the clock has fallen; 293 to 352 at 4 bits, 243 to
+// 289 at 2, 187 to 192 at d = 64.  (128 rows: 307 to 376, 351 to 440, 274, 200.)  256 rows at
+// 131,071 positions, 8 heads, take 267 to 306 (128 rows: 335).  Matrix cores are busy for 53%
 // of the cycles (128 rows: 42%), vector instructions issue in 53% (50%), waves wait for 25%
 // (28%): a tile of 64 positions takes the two waves of a SIMD 7,500 cycles, of which vector
 // instructions issue in 6,350 and matrix products in 4,096 (measured one by one).  Ragged

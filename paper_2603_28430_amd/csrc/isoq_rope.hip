@@ -126,8 +126,8 @@ struct RopeChunk {
 // What bounds it: memory.  32,768 tokens of 32 + 8 heads, d = 128, fp16, 671 MB: 125
 // us, 5.4 TB/s, where a large copy moves 4.8.  (A row a wave with cos and sin for every
 // element, rope_rows_kernel: 789.)  32 tokens: 4 us, next to its launch; the binding's
-// host time, 11 us, is what a call takes.  4,133 tokens of 10 heads, d = 90, fp32, in chunks of
-// two: 30 MB, 10 us (rope_rows_kernel 14).
+// host time, 9 us, is what a call takes.  4,133 tokens of 10 heads, d = 90, fp32, in chunks of
+// two: 30 MB, 9 us (rope_rows_kernel 14).
 template <bool F16, bool HALVES, int CH, int L>
 __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
 {
