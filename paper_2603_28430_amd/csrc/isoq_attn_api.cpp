@@ -294,16 +294,18 @@ AttnArgs attn_args(const AttnCall &c, const AttnPlan &plan, float scale2)
     return a;
 }
 
-isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, AttnArgs &a, int n_seqs)
+// The kernel of a plan (pre: of launches with n_pre > 0), or null where there is none.
+const void *attn_fn(const AttnCall &c, const AttnPlan &plan, bool pre)
+{
+    return !plan.kern.fn ? attn_generic_kernel_for(c.pk->variant, c.pk->bits, pre)
+           : pre         ? plan.kern.fn_pre
+                         : plan.kern.fn;
+}
+
+isoq_status launch_attn(const AttnCall &c, const AttnPlan &plan, const void *fn, AttnArgs &a, int n_seqs)
 {
     void *args[] = {&a};
-    const bool pre = a.n_pre > 0;
-    const void *fn = !plan.kern.fn ? attn_generic_kernel_for(c.pk->variant, c.pk->bits, pre)
-                     : pre         ? plan.kern.fn_pre
-                                   : plan.kern.fn;
     const size_t lds = plan.kern.fn ? plan.kern.lds : attn_generic_lds(plan.slots, c.pk->variant);
-    if (!fn)
-        return ISOQ_E_UNSUPPORTED;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
@@ -394,7 +396,7 @@ AttnPlans attn_plans(const AttnCall &c)
         p.bytes = plan_bytes(p.own, c.n_tokens, c.n_q_heads);
         return p;
     }
-    p.fold = p.own.kern.fn && !p.own.join;
+    p.fold = p.own.kern.fn_pre && !p.own.join;   // (the kernel of many rows has no form that adds them)
     p.bytes = sizeof(float) * (size_t)c.n_tokens * c.n_q_heads * ((p.fold ? 0 : p.own.n_splits) + p.pre.n_splits) *
               (p.own.width + 2);
     return p;
@@ -452,6 +454,9 @@ isoq_status attn_call(AttnCall c)
         return st;
 
     const AttnPlan &plan = plans.own;
+    const void *fn = attn_fn(c, plan, plans.ahead || plans.fold), *fn_prefix = plans.prefix ? attn_fn(c, plans.pre, false) : fn;
+    if (!fn || !fn_prefix)   // (before anything is launched)
+        return ISOQ_E_UNSUPPORTED;
     AttnArgs a = attn_args(c, plan, scale2);
     if (no_keys)
         a.cap = 0;
@@ -493,11 +498,11 @@ isoq_status attn_call(AttnCall c)
         b.part_first = plans.fold ? 0 : a.n_splits;
         p = AttnPrefix{c.prefix_start, c.prefix_lens, c.n_prefixes, c.n_seqs, (int32_t)c.max_prefix_tokens,
                        b.cap, b.chunk, b.n_splits, b.even};
-        st = launch_attn(shared, plans.pre, b, c.n_prefixes);
+        st = launch_attn(shared, plans.pre, fn_prefix, b, c.n_prefixes);
         if (st != ISOQ_OK)
             return st;
     }
-    st = launch_attn(c, plan, a, c.n_seqs);
+    st = launch_attn(c, plan, fn, a, c.n_seqs);
     if (st != ISOQ_OK || need == 0 || plans.fold)
         return st;
     const bool few = a.part_splits <= kAttnJoinFew;
