@@ -470,9 +470,10 @@ isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int
  *               if the host does not know); a prefix's tokens from there on are left as
  *               they were in out and lse.  max_prefix_len: positions of the longest prefix
  *               at most (max_prefix_blocks * block_size if it does not know).  Where that,
- *               max_prefix_blocks or n_blocks is 0 the call is isoq_kv_attn's.
+ *               n_prefixes, max_prefix_blocks or n_blocks is 0 the call is isoq_kv_attn's.
  *   workspace   at least isoq_kv_attn_prefix_workspace(...) bytes.
- * n_prefixes <= 65535; max_prefix_tokens (or n_tokens, if fewer) * n_q_heads <= 2^23.
+ * n_prefixes <= 65535; where it, max_prefix_blocks and max_prefix_len are not 0, max_prefix_tokens
+ * (or n_tokens, if fewer) * n_q_heads <= 2^23.
  * Everything else as isoq_kv_attn.
  */
 isoq_status isoq_kv_attn_prefix(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,

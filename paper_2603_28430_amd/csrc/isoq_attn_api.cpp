@@ -359,11 +359,17 @@ bool prefix_ahead(const AttnCall &c, const AttnPlan &ahead, const AttnPlan &pre)
     return ahead.max_pos <= kAttnMaxPos && anew <= (pre.kern.parts ? 0.5 * once + 0.6e6 + 130.0 * rows : once + 0.2e6);
 }
 
+// Whether a call has a prefix to attend to.
+bool has_prefix(const AttnCall &c)
+{
+    return c.n_prefixes > 0 && c.max_prefix_blocks > 0 && c.max_prefix_len > 0 && c.max_prefix_tokens > 0;
+}
+
 AttnPlans attn_plans(const AttnCall &c)
 {
     AttnPlans p{};
     const isoq_params *pk = c.pk;
-    p.prefix = c.n_prefixes > 0 && c.max_prefix_blocks > 0 && c.max_prefix_len > 0 && c.max_prefix_tokens > 0;
+    p.prefix = has_prefix(c);
     const bool tables = pk->attn_by_tables && c.pv->attn_by_tables;
     const int most = p.prefix ? kAttnMaxSplits / 2 : kAttnMaxSplits;   // (a row's join takes both kinds)
     const int64_t own = std::min<int64_t>(c.max_len, (int64_t)c.max_blocks * c.block_size);
@@ -408,7 +414,7 @@ isoq_status check_prefix(const AttnCall &c)
         (c.n_prefixes > 0 && c.max_prefix_tokens == 0 && c.n_tokens > 0) || (!c.prefix_start && c.n_prefixes > 1))
         return ISOQ_E_INVALID;
     if (c.n_prefixes > 65535 || (int64_t)c.max_prefix_blocks * c.block_size > kAttnMaxPos ||
-        c.max_prefix_tokens > kAttnMaxRows / c.n_q_heads)
+        (has_prefix(c) && c.max_prefix_tokens > kAttnMaxRows / c.n_q_heads))
         return ISOQ_E_UNSUPPORTED;
     return ISOQ_OK;
 }

@@ -88,3 +88,24 @@ for k in range(6000):
     st, held = prefix(*case, most=rng.choice([None, some(1, 300), 2 ** 40]))
     assert st == 0 and 1 <= len(held) <= 3, (case, st, len(held))
 """)
+
+
+def test_without_a_prefix_its_bounds_do_not_count(tmp_path):
+    """No prefix, or none with positions: isoq_kv_attn's launches and workspace, for more tokens than a prefix may have."""
+    run(tmp_path, CALLS + """
+for variant, d, dtype in (("full", 128, iq.ISOQ_F16), ("fast", 100, iq.ISOQ_F32)):
+    h, sizes = handle(variant, d, 3), (600 * 512, 512, 600, 32, 8)
+    need = lib.isoq_kv_attn_workspace(h, h, dtype, *sizes, 16, 64, 1024)
+    assert lib.isoq_kv_attn(h, h, dtype, P, P, *sizes, P, P, P, P, 1000, 16, P, 64, P, 1024, 1.0, P, P, P, need, None) == 0
+    plain = [bytes(x) for x in launches()]
+    for prefixes, blocks, length in ((0, 4, 64), (1, 0, 64), (1, 4, 0), (0, 0, 0), (1, 4, 64)):
+        more = prefixes, sizes[0], blocks, length
+        size = lib.isoq_kv_attn_prefix_workspace(h, h, dtype, *sizes, 16, 64, 1024, *more)
+        st = lib.isoq_kv_attn_prefix(h, h, dtype, P, P, *sizes, P, P, P, P, 1000, 16, P, 64, P, 1024, P, blocks, P, length, P,
+                                     prefixes, sizes[0], 1.0, P, P, P, need, None)
+        held = [bytes(x) for x in launches()]
+        if prefixes and blocks and length:   # (more rows than one prefix may have)
+            assert st == 2 and not held and size == 0
+        else:
+            assert st == 0 and held == plain and size == need, (prefixes, blocks, length, st)
+""")
