@@ -26,6 +26,31 @@ constexpr int64_t kPlanTokensHere = 4096;
 // fp32, 72 heads: 1,000 20.9 / 16.5 / 15.7 / 16.8 / 19.2).
 constexpr int64_t kRopeWaves = 4096;
 
+// Waves of a launch: a grid has fewer than 2^32 threads.
+constexpr int64_t kRopeLaunch = (1 << 26) - 4;
+
+// `waves` of them a token, four a workgroup; in launches of as many tokens as one takes, in
+// multiples of 16, so that rows of any width stay at multiples of 16 bytes.
+isoq_status launch_rope(const void *fn, const RopeArgs &all, int64_t n_tokens, int64_t waves, size_t es, void *stream)
+{
+    const int64_t most = kRopeLaunch / waves / 16 * 16;
+    for (int64_t t = 0; t < n_tokens; t += most) {
+        RopeArgs a = all;
+        a.n_tokens = (int32_t)std::min(most, n_tokens - t);
+        a.positions += t;
+        for (int k = 0; k < 2; k++)
+            if (a.heads[k] > 0) {
+                a.x[k] = static_cast<const char *>(a.x[k]) + t * a.stride[k] * (int64_t)es;
+                a.out[k] = static_cast<char *>(a.out[k]) + t * a.heads[k] * a.d * (int64_t)es;
+            }
+        void *args[] = {&a};
+        const isoq_status st = launch_lds(fn, dim3((unsigned)((a.n_tokens * waves + 3) / 4)), 256, args, 0, stream);
+        if (st != ISOQ_OK)
+            return st;
+    }
+    return ISOQ_OK;
+}
+
 constexpr double kTwoPi = 6.283185307179586476925;
 
 }  // namespace
@@ -215,13 +240,11 @@ isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int6
     a.heads[1] = n_kv_heads;
     a.positions = positions;
     a.turns = r->turns;
-    a.n_tokens = (int32_t)n_tokens;
     a.d = r->d;
     a.half = r->rot_dim / 2;
     a.eps = eps;
     a.amplitude = r->amplitude;
     const bool f16 = dtype == ISOQ_F16, halves = r->layout == ISOQ_ROPE_HALVES;
-    void *args[] = {&a};
     // the largest chunks that all rows are made of
     for (const int chunk : {f16 ? 8 : 4, 2, 1}) {
         const int cr = 2 * a.half / chunk, cz = (r->d - 2 * a.half) / chunk, pairs = (cr + 1) / 2 + (cz + 1) / 2;
@@ -237,13 +260,12 @@ isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int6
             lanes *= 2;
         const int64_t rows = 64 / lanes, most = (n_q_heads + rows - 1) / rows + (n_kv_heads + rows - 1) / rows;
         a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, kRopeWaves / n_tokens));
-        return launch_lds(rope_tile_kernel_for(f16, halves, chunk, lanes), dim3((unsigned)((n_tokens * a.parts + 3) / 4)),
-                          256, args, 0, stream);
+        return launch_rope(rope_tile_kernel_for(f16, halves, chunk, lanes), a, n_tokens, a.parts, es, stream);
     }
     int steps = 0;
     while ((64 << steps) < r->d)
         steps++;
-    return launch_lds(rope_kernel(f16, halves, steps), dim3((unsigned)((n_tokens * heads + 3) / 4)), 256, args, 0, stream);
+    return launch_rope(rope_kernel(f16, halves, steps), a, n_tokens, heads, es, stream);
 }
 
 }  // extern "C"
