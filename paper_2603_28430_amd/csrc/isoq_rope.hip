@@ -214,8 +214,10 @@ __global__ __launch_bounds__(256) void rope_tile_kernel(const RopeArgs a)
                 float sum = 0.f;
                 if (there) {
 #pragma unroll
-                    for (int i = 0; i < CH; i++)
-                        sum = fmaf(both ? xb[i] : 0.f, xb[i], fmaf(xa[i], xa[i], sum));
+                    for (int i = 0; i < CH; i++) {
+                        const float other = both ? xb[i] : 0.f;   // (in both factors: 0 times an infinity is no number)
+                        sum = fmaf(other, other, fmaf(xa[i], xa[i], sum));
+                    }
                 }
                 const float scale = 1.f / sqrtf(row_sum<L>(sum) / (float)a.d + a.eps);
 #pragma unroll
