@@ -511,9 +511,11 @@ def isoq_kv_attn(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, block_ta
     are not written (see include/isoquant.h).  workspace: a uint8 tensor of at
     least isoq_kv_attn_workspace(...) bytes.  What is not passed (out, lse,
     workspace) is allocated from torch's pool for `stream`, by default the
-    current one.  causal=False is isoq_kv_attn_cross; prefix, the arguments of
-    isoq_kv_attn_prefix."""
+    current one.  causal=False is isoq_kv_attn_cross; prefix is what
+    isoq_kv_attn_prefix, to be called instead, makes of its arguments."""
     torch = _torch()
+    if prefix is not None and not causal:
+        raise ValueError("attention behind a prefix is causal")
     shape, cache, table = q.shape, k_idx.shape, block_table.shape
     if len(shape) != 3 or len(cache) != 4 or len(table) != 2:
         raise ValueError("q [n_tokens, n_q_heads, d], k_idx [n_blocks, n_kv_heads, block_size, R], "
