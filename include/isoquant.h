@@ -459,6 +459,8 @@ isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int
  *
  *   block_table, seq_lens, max_len  the sequences' own positions (their new tokens
  *               are the last of those).
+ *               Rotary positions count the prefix's too: what isoq_kv_plan gives, which
+ *               counts from 0 here, and prefix_lens[p].
  *   prefix_start  device, int32 [n_prefixes + 1], ascending: prefix p is shared by
  *               the sequences prefix_start[p] .. prefix_start[p + 1] - 1, which stand
  *               side by side.  Sequences of none have only their own positions.
@@ -572,7 +574,9 @@ isoq_status isoq_kv_compact(const isoq_params *pk, const isoq_sketch *sk, const 
  *   q_start     device, int32 [n_seqs + 1]: sequence s has the tokens q_start[s] ..
  *               q_start[s + 1] - 1, those of refused sequences among them.
  *   slot_mapping, positions  device, int64 and int32 [n_tokens]: each token's slot
- *               (-1 for none: isoq_kv_append skips it) and position.  n_tokens may
+ *               (-1 for none: isoq_kv_append skips it) and position in its sequence
+ *               (behind a prefix, isoq_kv_attn_prefix, its rotary position is that and
+ *               the prefix's length).  n_tokens may
  *               be more than there are (a captured step of a fixed size): tokens
  *               past the last have slot -1 and position 0.  If it is fewer, those
  *               past n_tokens are left out, though lengths and blocks count them.

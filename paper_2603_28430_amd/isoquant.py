@@ -624,6 +624,7 @@ def isoq_kv_attn_prefix(pk: Params, q, k_idx, k_rho, pv: Params, v_idx, v_rho, b
     same cache once, and prefix p is what the sequences prefix_start[p] ..
     prefix_start[p + 1] - 1 (int32 [n_prefixes + 1]; None: one prefix, of all) begin
     with; block_table and seq_lens are the sequences' own positions after it.
+    Rows are to be rotated by positions that count the prefix's (isoq_kv_plan's do not).
     max_prefix_tokens: tokens of one prefix's sequences at most (by default all
     there are); max_prefix_len: positions of the longest prefix at most.  Other
     arguments and results as isoq_kv_attn, workspace of at least
@@ -833,8 +834,11 @@ def isoq_kv_plan(lens, new_lens, block_table, block_size: int, free_blocks, n_fr
     have (by default as many as slot_mapping holds).  Returns (seq_lens int32
     [n_seqs], q_start int32 [n_seqs + 1], slot_mapping int64 [n_tokens], positions
     int32 [n_tokens], n_free_out int32 [1]): seq_lens may be lens, n_free_out
-    n_free.  See include/isoquant.h for sequences that are refused.  What is not
-    passed is allocated from torch's pool for `stream`."""
+    n_free.  positions count from 0 in a sequence's own table: behind a prefix
+    (isoq_kv_attn_prefix) add its length before isoq_qk_norm_rope.  See
+    include/isoquant.h for sequences that are refused.  What is not passed is
+    allocated from torch's pool for `stream`; where none of the int32 results is
+    passed they are parts of one allocation, which any of them keeps."""
     torch = _torch()
     table = block_table.shape
     if len(table) != 2 or free_blocks.dim() != 1:
