@@ -392,7 +392,7 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  *               sequence has (known to the host).  The call is planned as if all
  *               had as many: a loose bound costs time, and so do single tokens
  *               next to a long chunk, which two calls take less for (15 and one
- *               of 512 at 8,192 positions, 8 x 4 heads, d = 128: 39 and 176 us, 820
+ *               of 512 at 8,192 positions, 8 x 4 heads, d = 128: 41 and 155 us, 382
  *               in one call).  Rows of no sequence are left
  *               as they were, in out and lse; so are a sequence's tokens from
  *               max_q_len on.  NULL: one token a sequence, n_tokens == n_seqs and
@@ -416,7 +416,11 @@ isoq_status isoq_kv_scores_filled(const isoq_params *pk, const isoq_sketch *sk, 
  * Limits: n_seqs <= 65535, n_tokens * n_q_heads < 2^31, max_q_len * n_q_heads <=
  * 2^23, max_blocks_per_seq * block_size <= 2^31 - 1024.
  * Arithmetic: logits, softmax statistics and sums in fp32 or in integers of 32
- * bits (see the kernels for what is rounded); a row's result is as exact as its
+ * bits (see the kernels for what is rounded).  Weights and value levels are digits
+ * (30 bits, and 16, of fp32 queries 24), but for fp16 queries with 32 rows and more a key
+ * head (its query heads times max_q_len) at d = 64, 80, 96 and 128: there they are fp16 with
+ * a correction, and out is off by 2.1e-4 to 2.2e-4 of its norm where its own rounding to
+ * fp16 takes 2.07e-4.  A row's result is as exact as its
  * own weights and norms allow, whatever norms stand at other positions.  A query
  * with an infinity or NaN gives NaN in its row of out and lse if it attends to
  * any position, and so does a norm of k_rho or v_rho that is one in the rows that
@@ -476,7 +480,9 @@ isoq_status isoq_kv_attn_cross(const isoq_params *pk, const isoq_params *pv, int
  *   workspace   at least isoq_kv_attn_prefix_workspace(...) bytes.
  * n_prefixes <= 65535; where it, max_prefix_blocks and max_prefix_len are not 0, max_prefix_tokens
  * (or n_tokens, if fewer) * n_q_heads <= 2^23.
- * Everything else as isoq_kv_attn.
+ * Everything else as isoq_kv_attn, the rows of a prefix being those of all its sequences
+ * together: single tokens behind one that many share are as exact as a chunk's rows, and
+ * how many share it may change their last bits.
  */
 isoq_status isoq_kv_attn_prefix(const isoq_params *pk, const isoq_params *pv, int dtype, const void *q,
                                 const int32_t *q_start, int64_t n_tokens, int max_q_len, int n_seqs, int n_q_heads,
@@ -630,11 +636,13 @@ isoq_status isoq_rope_freqs(int rot_dim, double base, double factor, double orig
  *               their elements; 16 bytes, with strides and widths that are
  *               multiples of as much, are faster.  n_q_heads or n_kv_heads may be 0.
  *   positions   device, int32 [n_tokens], any value (negative ones turn back).
- *               Angles are exact to 2^-31 of a turn at every position.
+ *               Angles are exact to 2^-31 of a turn at every position, for frequencies
+ *               of up to a turn (2 pi) a position; for k turns, to k + 1 times that.
  *   q_weight, k_weight  device, fp32 [d], or NULL: no norm.
  *   q_out, k_out  device, [n_tokens][heads][d] (16-byte aligned); may be q (k)
  *               itself where its stride is n_q_heads * d (n_kv_heads * d).
- * Arithmetic: fp32, rounded once (fp16: to nearest even).  Limits: n_tokens *
+ * Arithmetic: fp32, rounded once (fp16: to nearest even); a normed row whose squares add up
+ * past fp32's largest number (fp32 values from 5e17 on can) is 0.  Limits: n_tokens *
  * (n_q_heads + n_kv_heads) < 2^31, heads <= 65535.
  */
 isoq_status isoq_qk_norm_rope(const isoq_rope *r, int dtype, const void *q, int64_t q_stride, int n_q_heads,

@@ -2,9 +2,11 @@
 // (a head of a token) y = weight x / sqrt(mean x^2 + eps), and each of the
 // rotated pairs (a, b) becomes
 //     amplitude (a cos - b sin, a sin + b cos),  angle = position frequency.
-// The angle is exact at any position: a frequency is held as turns in units of
-// 2^-64, the product with the position taken modulo 2^64, so whole turns drop out
-// without a rounding and the fraction is off by 2^-34 of a turn at most.
+// A frequency is held as turns in units of 2^-64 (off by up to two of them, the division's
+// and the cut), the product with the position taken modulo 2^64, so whole turns drop out
+// without a rounding; its upper 32 bits are what is used.  At the farthest positions, 2^31, the
+// angle is off by 2^-32 of a turn of the first and 2^-32 of the second at most (1.5 2^-32 the
+// worst of 700 frequencies up to a turn a position at 8 positions each).
 #include <hip/hip_runtime.h>
 
 #include "isoq_device.h"
