@@ -74,6 +74,16 @@ for variant, d, bits, q_lens, kv, group, own, max_len, prefixes, counts in {MANY
 """)
 
 
+def test_sizes_of_the_serving_steps(tmp_path):
+    """Those of test_gpu_step_run_shared.py: 7 sequences with at most 60 to 128 new tokens, 128 own positions, two prefixes."""
+    run(tmp_path, CALLS + f"""
+for variant, d, bits, bs, kv, group in (("full", 128, 3, 16, 2, 4), ("fast", 64, 4, 8, 1, 2), ("2d", 80, 2, 16, 2, 1), ("8d", 96, 3, 16, 1, 3)):
+    for q_len, n in ((128, 234), (60, 140)):
+        st, held = prefix(variant, d, bits, iq.ISOQ_F16, 7, q_len, kv, group, 128, {WIDE}, 2, bs, n=n)
+        assert st == 0 and len(held) == 3, (variant, d, q_len, st, len(held))
+""")
+
+
 def test_every_size_has_its_kernels(tmp_path):
     run(tmp_path, CALLS + """
 rng = random.Random(1)
